@@ -23,3 +23,21 @@ from .api import (  # noqa: F401
     tile_attn_plan,
     tile_attn_plan_cache_stats,
 )
+from .blocks import (  # noqa: F401
+    BLOCK_TOKENS,
+    block_attn,
+    block_attn_bwd,
+    block_attn_bwd_workspace,
+    block_attn_fwd,
+    block_attn_fwd_workspace,
+    block_attn_grad,
+    block_attn_lists,
+    block_attn_means,
+    block_lists,
+    block_means,
+    cache_attn,
+    cache_attn_fwd,
+    cache_attn_fwd_workspace,
+    cache_attn_write,
+    cache_write,
+)

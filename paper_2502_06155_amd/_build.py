@@ -11,7 +11,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_NAME = "libtileattn.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = [os.path.join(CSRC, f) for f in ("tile_attn_host.cpp", "tile_attn_kernels.hip", "tile_attn_bwd.hip",
-                                               "tile_attn_noalloc.hip")]
+                                               "tile_attn_noalloc.hip", "block_host.cpp", "block_lists.hip",
+                                               "block_fwd.hip", "block_bwd.hip", "cache_attn.hip")]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950",

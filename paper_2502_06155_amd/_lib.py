@@ -24,6 +24,15 @@ EXPORTS = (
     "tile_attn_plan_cache_stats",
     "tile_attn_status_string",
     "tile_attn_last_error",
+    "block_attn_means",
+    "block_attn_lists",
+    "block_attn_fwd_workspace",
+    "block_attn_fwd",
+    "block_attn_bwd_workspace",
+    "block_attn_bwd",
+    "cache_attn_write",
+    "cache_attn_fwd_workspace",
+    "cache_attn_fwd",
 )
 
 
@@ -78,6 +87,20 @@ def _load() -> ctypes.CDLL:
     lib.tile_attn_status_string.restype = ctypes.c_char_p
     lib.tile_attn_last_error.argtypes = []
     lib.tile_attn_last_error.restype = ctypes.c_char_p
+    cz, pz = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+    for name, args in {
+        "block_attn_means": [vp] * 2 + [ci] * 4 + [vp] * 2,
+        "block_attn_lists": [vp] * 3 + [ci] * 10 + [vp] * 2,
+        "block_attn_fwd_workspace": [ci] * 7 + [pz],
+        "block_attn_fwd": [vp] * 6 + [ci] * 8 + [vp, cf, vp, cz, vp],
+        "block_attn_bwd_workspace": [ci] * 7 + [pz],
+        "block_attn_bwd": [vp] * 10 + [ci] * 8 + [vp, cf, vp, cz, vp],
+        "cache_attn_write": [vp] * 9 + [ci] * 6 + [vp],
+        "cache_attn_fwd_workspace": [ci] * 6 + [pz],
+        "cache_attn_fwd": [vp] * 7 + [ci] + [vp] * 2 + [ci] * 7 + [cf, vp, cz, vp],
+    }.items():
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, ci
     return lib
 
 
