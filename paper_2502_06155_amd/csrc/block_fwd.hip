@@ -135,11 +135,14 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_fwd_kernel(const BlockFwdA
     wait_tile_loads();
     __syncthreads();
 
-    // The weights of a block count once no lane's sum of them is above 2^10; otherwise the
-    // references are raised to the block's maximum, what is there is rescaled, and they form anew.
+    // The weights of a block count once neither of a row's two lanes has a sum above 2^10; otherwise
+    // the row's reference is raised to the block's maximum, what is there is rescaled, and the
+    // weights form anew. Rows that need not move keep their reference: a row's bits do not depend
+    // on the rows beside it.
     auto settle = [&](const f32x16& s, bf16x8(&p)[2], float sum) {
       if (__builtin_amdgcn_ballot_w64(!(sum <= lazy)) != 0) {
-        const float m_new = fmaxf(m, pair_max(lane_max(s)) * c);
+        const bool moves = pair_max(sum <= lazy ? 0.f : 1.f) > 0.f;
+        const float m_new = moves ? fmaxf(m, pair_max(lane_max(s)) * c) : m;
         const float alpha = fast_exp2(m - m_new);
         l *= alpha;
 #pragma unroll

@@ -1,0 +1,376 @@
+"""Block means, lists, attention over lists and its gradients against the float64 reference.
+
+Tolerances count roundings (half a step of bf16 is 2^-8 of the value): weights and dS are rounded to
+bf16 once before their second product and results once more; scores are fp32 sums of up to 128
+exact products, whose error (below 128 * 2^-24 of the sum of their magnitudes, about 1e-4 in the
+exponent at these sizes, twice that where the log-sum-exp enters as well) changes weights by less
+than 5e-4."""
+import numpy as np
+import pytest
+
+import workloads
+from oracle import blocks as ob
+from tests.gpu_helpers import from_dev, to_dev, widen
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2502_06155_amd as ta  # noqa: E402
+
+HALF = 2.0 ** -8
+FP32 = 5e-4
+NAN = 0x7FC1
+
+
+def bits(rng, *shape, scale=1.0):
+    return workloads.f32_to_bf16_bits((scale * rng.standard_normal(shape)).astype(np.float32))
+
+
+def i32(x):
+    return None if x is None else torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def within(got, ref, bound, what):
+    off = np.abs(got - ref) - bound
+    assert np.isfinite(got).all(), what
+    worst = np.unravel_index(np.argmax(off), off.shape)
+    print(f"[parity] {what}: error {np.abs(got - ref).max():.2e}, at the worst {got[worst]:.5g} for {ref[worst]:.5g}, "
+          f"bound {bound[worst]:.2e}", flush=True)
+    assert off[worst] <= 0, what
+
+
+def some_lists(rng, B, Hkv, Sq, Skv, n, kind="random"):
+    """Lists in any order, with gaps, repeats and entries that name no block; "near": every query
+    block's own block among them; "empty": none at all for every second query block."""
+    nq, nb = -(-Sq // 128), -(-Skv // 128)
+    x = rng.integers(0, nb, (B, Hkv, nq, n)).astype(np.int32)
+    x[rng.random(x.shape) < 0.2] = -1
+    x[rng.random(x.shape) < 0.05] = nb + 3
+    x[rng.random(x.shape) < 0.03] = 2 ** 31 - 1
+    x[rng.random(x.shape) < 0.03] = -2 ** 31
+    if kind == "near":
+        x[..., n // 2] = (Skv - Sq + 128 * np.arange(nq)) // 128
+    if kind == "empty":
+        x[:, :, ::2] = -1
+    return x
+
+
+# B, H, Hkv, Sq, Skv, d, n, causal, lens, kind
+CASES = [
+    (1, 1, 1, 1, 1, 64, 1, True, None, "near"),
+    (1, 2, 1, 127, 127, 96, 1, False, None, "near"),
+    (1, 2, 2, 128, 128, 128, 2, True, None, "near"),
+    (2, 2, 1, 129, 129, 64, 3, True, [129, 128], "near"),
+    (2, 4, 2, 300, 300, 96, 3, True, [300, 0], "near"),
+    (1, 3, 1, 333, 333, 128, 2, False, None, "empty"),
+    (3, 2, 2, 257, 257, 64, 4, False, [257, 1, 200], "random"),
+    (1, 4, 1, 200, 777, 128, 5, True, None, "random"),
+    (2, 6, 2, 1, 700, 96, 6, True, [700, 650], "random"),
+    (2, 8, 1, 3, 900, 64, 9, False, None, "random"),
+    (1, 2, 2, 150, 650, 96, 4, True, [600], "near"),
+    (1, 5, 1, 40, 300, 128, 3, True, None, "random"),
+    (1, 1, 1, 640, 640, 64, 40, True, None, "random"),
+]
+IDS = ["-".join(str(x) for x in c[:7]) + ("-causal" if c[7] else "") + ("-" + c[9]) for c in CASES]
+
+
+def make(case, seed=0):
+    B, H, Hkv, Sq, Skv, d, n, causal, lens, kind = case
+    rng = np.random.default_rng(1000 + seed + sum(case[:7]))
+    q, k, v, go = bits(rng, B, H, Sq, d), bits(rng, B, Hkv, Skv, d), bits(rng, B, Hkv, Skv, d), bits(rng, B, H, Sq, d)
+    if lens is not None:  # what lies behind the end counts for nobody
+        for b, ln in enumerate(lens):
+            k[b, :, ln:] = NAN
+            v[b, :, ln:] = NAN
+            q[b, :, max(0, ln - (Skv - Sq)):] = NAN
+            go[b, :, max(0, ln - (Skv - Sq)):] = NAN
+    return q, k, v, go, some_lists(rng, B, Hkv, Sq, Skv, n, kind)
+
+
+def zero_nan(x):
+    return np.where(x == NAN, np.uint16(0), x)
+
+
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+@pytest.mark.parametrize("scale", [None, -0.3, 0.0])
+def test_forward_and_gradients(case, scale):
+    B, H, Hkv, Sq, Skv, d, n, causal, lens, kind = case
+    q, k, v, go, lists = make(case)
+    qd, kd, vd, gd = (to_dev(x) for x in (q, k, v, go))
+    out = torch.full_like(qd, float("nan"))
+    got, lse = ta.block_attn(qd, kd, vd, i32(lists), causal, scale, i32(lens), out, return_lse=True)
+    assert got is out
+    plain = [zero_nan(x) for x in (q, k, v, go)]
+    ref, rlse, mag = ob.attention(*plain[:3], lists, causal, lens, scale)
+    within(widen(from_dev(got)), ref, HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30, "out")
+    some = np.isfinite(rlse)
+    lse_h = lse.cpu().numpy().astype(np.float64)
+    assert np.array_equal(lse_h[~some], rlse[~some])
+    assert np.abs(lse_h[some] - rlse[some]).max(initial=0) <= 2e-4
+    assert not from_dev(got)[~some].any()
+
+    grads = ta.block_attn_grad(qd, kd, vd, i32(lists), got, gd, lse, causal, scale, i32(lens))
+    dq, dk, dv = ob.attention_backward(*plain, lists, causal, lens, scale)
+    for name, g, r in zip(("dq", "dk"), grads, (dq, dk)):
+        bound = HALF * np.abs(r[0]) + HALF * r[1] + FP32 * r[2] + r[3] + 1e-30
+        within(widen(from_dev(g)), r[0], bound, name)
+    within(widen(from_dev(grads[2])), dv[0], HALF * np.abs(dv[0]) + (HALF + FP32) * dv[1] + 1e-30, "dv")
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_enough_units_for_whole_lists_and_cut_columns(d, causal):
+    """As many units as the device holds (lists are not cut), grouped heads, a block that every
+    query block keeps and an odd length; rows of some heads against the reference, gradients of one
+    group."""
+    B, H, Hkv, S, n = 2, 32, 8, 1300, 5
+    assert ta.block_attn_fwd_workspace(B, H, Hkv, S, S, d, n) == 0
+    rng = np.random.default_rng(d + causal)
+    q, k, v, go = (bits(rng, B, h, S, d) for h in (H, Hkv, Hkv, H))
+    lists = some_lists(rng, B, Hkv, S, S, n, "near")
+    lists[..., 0] = 0
+    qd, kd, vd, gd = (to_dev(x) for x in (q, k, v, go))
+    out, lse = ta.block_attn(qd, kd, vd, i32(lists), causal, return_lse=True)
+    grads = ta.block_attn_grad(qd, kd, vd, i32(lists), out, gd, lse, causal)
+    for b, g in ((0, 0), (1, Hkv - 1), (1, 3)):
+        hs = slice(4 * g, 4 * g + 4)
+        part = (q[b:b + 1, hs], k[b:b + 1, g:g + 1], v[b:b + 1, g:g + 1])
+        ref, rlse, mag = ob.attention(*part, lists[b:b + 1, g:g + 1], causal)
+        within(widen(from_dev(out[b:b + 1, hs])), ref, HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30, f"out {b} {g}")
+        some = np.isfinite(rlse)
+        got = lse[b:b + 1, hs].cpu().numpy()
+        assert np.abs(got[some] - rlse[some]).max() <= 2e-4 and np.array_equal(got[~some], rlse[~some].astype(np.float32))
+        dq, dk, dv = ob.attention_backward(*part, go[b:b + 1, hs], lists[b:b + 1, g:g + 1], causal)
+        for name, x, r in (("dq", grads[0][b:b + 1, hs], dq), ("dk", grads[1][b:b + 1, g:g + 1], dk)):
+            bound = HALF * np.abs(r[0]) + HALF * r[1] + FP32 * r[2] + r[3] + 1e-30
+            within(widen(from_dev(x)), r[0], bound, f"{name} {b} {g}")
+        within(widen(from_dev(grads[2][b:b + 1, g:g + 1])), dv[0], HALF * np.abs(dv[0]) + (HALF + FP32) * dv[1] + 1e-30,
+               f"dv {b} {g}")
+
+
+def test_order_and_repeats_of_a_list_change_no_bit():
+    case = (2, 4, 2, 700, 700, 64, 6, True, [700, 555], "near")
+    q, k, v, go, lists = make(case)
+    q, k, v, go = (zero_nan(x) for x in (q, k, v, go))
+    args = [to_dev(x) for x in (q, k, v)]
+    lens = i32(case[8])
+    rng = np.random.default_rng(5)
+    longer = np.concatenate([lists, lists[..., ::-1], lists[..., :2]], -1)
+    ref = None
+    for x in (lists, rng.permuted(lists, axis=-1), longer):
+        out, lse = ta.block_attn(*args, i32(x), True, lens=lens, return_lse=True)
+        grads = ta.block_attn_grad(*args, i32(x), out, to_dev(go), lse, True, lens=lens)
+        if x is not longer:
+            got = [out, lse, *grads]
+            if ref is not None:
+                assert all(torch.equal(a, b) for a, b in zip(got, ref))
+            ref = got
+        else:  # a longer list may be cut into other pieces
+            right, _, mag = ob.attention(q, k, v, lists, True, case[8])
+            within(widen(from_dev(out)), right, HALF * np.abs(right) + (HALF + FP32) * mag + 1e-30, "repeats")
+
+
+def test_blocks_outside_the_lists_and_later_keys_are_never_used():
+    """NaN keys and values in unlisted blocks, and NaN keys behind a row, change nothing."""
+    rng = np.random.default_rng(8)
+    q, k, v, go = (bits(rng, 1, h, 512, 96) for h in (2, 1, 1, 2))
+    lists = np.array([[[[0, -1], [1, 0], [0, 2], [3, 0]]]], np.int32)
+    kn, vn = k.copy(), v.copy()
+    lists[0, 0, 3] = [0, -1]  # nobody keeps block 3
+    kn[:, :, 384:] = NAN
+    vn[:, :, 384:] = NAN
+    q2 = q.copy()
+    out = [ta.block_attn(to_dev(q2), to_dev(a), to_dev(b), i32(lists), True, return_lse=True) for a, b in ((k, v), (kn, vn))]
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    grads = [ta.block_attn_grad(to_dev(q2), to_dev(a), to_dev(b), i32(lists), *o[:1], to_dev(go), o[1], True)
+             for (a, b), o in zip(((k, v), (kn, vn)), out)]
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+    assert not from_dev(grads[0][1])[:, :, 384:].any() and not from_dev(grads[0][2])[:, :, 384:].any()
+    late = k.copy()
+    late[:, :, 120:] = NAN  # rows before 120 of the first block mask them
+    first = ta.block_attn(to_dev(q2), to_dev(late), to_dev(v), i32(lists), True)
+    assert torch.equal(first[:, :, :120], out[0][0][:, :, :120])
+
+
+def test_large_logits():
+    rng = np.random.default_rng(9)
+    q, k, v = bits(rng, 1, 2, 300, 64, scale=8.0), bits(rng, 1, 2, 300, 64, scale=8.0), bits(rng, 1, 2, 300, 64)
+    lists = np.array([[[[2, 0], [1, 2], [0, 1]]] * 2], np.int32)
+    out, lse = ta.block_attn(*(to_dev(x) for x in (q, k, v)), i32(lists), return_lse=True)
+    ref, rlse, mag = ob.attention(q, k, v, lists)
+    # scores up to some 300: fp32 sums of 64 products and the base-2 logarithm's scaling are off by
+    # at most 66 * 2^-24 of the products' magnitudes (about 400 here), 1.6e-3, in the exponent
+    within(widen(from_dev(out)), ref, HALF * np.abs(ref) + (HALF + 4e-3) * mag + 1e-30, "out")
+    assert np.abs(lse.cpu().numpy() - rlse).max() <= 2e-3
+
+
+@pytest.mark.parametrize("B,H,S,d,lens", [(1, 1, 1, 64, None), (2, 3, 129, 96, [129, 7]), (1, 2, 1000, 128, None),
+                                          (3, 1, 384, 64, [0, 384, 257])])
+def test_means(B, H, S, d, lens):
+    rng = np.random.default_rng(S)
+    x = bits(rng, B, H, S, d)
+    if lens:
+        for b, ln in enumerate(lens):
+            x[b, :, ln:] = NAN
+    got = ta.block_means(to_dev(x), i32(lens))
+    assert np.array_equal(from_dev(got), ob.block_means(zero_nan(x), lens))
+
+
+@pytest.mark.parametrize("B,H,Hkv,Sq,Skv,d,n,causal,sink,local,lens", [
+    (1, 1, 1, 1, 1, 64, 1, False, 0, 0, None),
+    (2, 4, 2, 300, 300, 64, 2, True, 0, 1, [300, 200]),
+    (1, 6, 2, 1500, 1500, 96, 4, False, 1, 1, None),
+    (1, 2, 1, 1500, 1500, 128, 6, False, 1, 2, None),
+    (2, 2, 2, 1, 5000, 128, 9, True, 1, 2, [5000, 4990]),
+    (1, 2, 2, 700, 1000, 64, 5, True, 1, 2, None),
+    (1, 2, 2, 600, 1000, 64, 50, False, 0, 0, [900]),
+    (1, 1, 1, 90, 128 * 1100, 64, 33, True, 0, 1, None),
+    (1, 1, 1, 130, 128 * 4500, 64, 200, False, 2, 1, None),
+    (1, 1, 1, 1, 128 * 16384, 64, 64, True, 0, 0, None),
+])
+def test_lists(B, H, Hkv, Sq, Skv, d, n, causal, sink, local, lens):
+    rng = np.random.default_rng(Sq + Skv)
+    nb = -(-Skv // 128)
+    q, km = bits(rng, B, H, Sq, d), bits(rng, B, Hkv, nb, d)
+    if lens:
+        for b, ln in enumerate(lens):
+            q[b, :, max(0, ln - (Skv - Sq)):] = NAN
+    out = torch.full((B, Hkv, -(-Sq // 128), n), 77, dtype=torch.int32, device="cuda")
+    got = ta.block_lists(to_dev(q), to_dev(km), Skv, n, causal, sink, local, i32(lens), out)
+    assert got is out
+    ref = ob.block_lists(zero_nan(q), km, Skv, n, causal, sink, local, lens)
+    assert np.array_equal(got.cpu().numpy(), ref)
+
+
+def test_lists_with_equal_scores_take_the_lower_index_and_nan_last():
+    d, nb = 64, 300
+    means = np.zeros((1, 1, nb, d))
+    means[..., 0] = np.arange(nb) % 7  # many equal scores
+    means[0, 0, 5] = -0.0
+    kb = ob.to_bf16(means)
+    q = ob.to_bf16(np.eye(1, d)[None, None].repeat(1, 2))
+    for n in (1, 42, 43, 44, 150, 299, 300):
+        got = ta.block_lists(to_dev(q), to_dev(kb), 128 * nb, n, local=0).cpu().numpy()
+        assert np.array_equal(got, ob.block_lists(q, kb, 128 * nb, n, local=0)), n
+    kb[0, 0, 6, 0] = NAN  # the best score of the first seven
+    got = ta.block_lists(to_dev(q), to_dev(kb), 128 * nb, 1, local=0).cpu().numpy()
+    assert got.ravel().tolist() == [13]
+    every = ta.block_lists(to_dev(q), to_dev(kb), 128 * nb, nb, local=0).cpu().numpy()
+    assert every.ravel().tolist() == list(range(nb))
+    most = ta.block_lists(to_dev(q), to_dev(kb), 128 * nb, nb - 1, local=0).cpu().numpy()
+    assert 6 not in most.ravel().tolist() and most.ravel().tolist()[-1] == nb - 1
+
+
+def _step(x, lens):
+    """Lists from the data, forward, gradients: a sparse layer's training step."""
+    q, k, v, go = x
+    lists = ta.block_lists(q, ta.block_means(k, lens), k.shape[2], 3, True, 1, 1, lens)
+    out, lse = ta.block_attn(q, k, v, lists, True, lens=lens, return_lse=True)
+    return [lists, out, lse, *ta.block_attn_grad(q, k, v, lists, out, go, lse, True, lens=lens)]
+
+
+def _inputs(seed, S=900):
+    rng = np.random.default_rng(seed)
+    return [to_dev(bits(rng, 2, h, S, 64)) for h in (4, 2, 2, 4)]
+
+
+def test_a_training_step_of_all_operators_together():
+    x, lens = _inputs(1), [900, 700]
+    lists, out, lse, dq, dk, dv = _step(x, i32(lens))
+    qb, kb, vb, gb = (from_dev(t) for t in x)
+    chosen = ob.block_lists(qb, ob.block_means(kb, lens), 900, 3, True, 1, 1, lens)
+    assert np.array_equal(lists.cpu().numpy(), chosen)
+    ref, rlse, mag = ob.attention(qb, kb, vb, chosen, True, lens)
+    within(widen(from_dev(out)), ref, HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30, "out")
+    rq, rk, rv = ob.attention_backward(qb, kb, vb, gb, chosen, True, lens)
+    for name, g, r in (("dq", dq, rq), ("dk", dk, rk)):
+        within(widen(from_dev(g)), r[0], HALF * np.abs(r[0]) + HALF * r[1] + FP32 * r[2] + r[3] + 1e-30, name)
+    within(widen(from_dev(dv)), rv[0], HALF * np.abs(rv[0]) + (HALF + FP32) * rv[1] + 1e-30, "dv")
+
+
+def test_two_captured_steps_replayed_with_eager_work_between():
+    """Two graphs of whole steps, captured one after the other on one stream, replayed in turns on
+    two streams: each has its own workspaces, and the results are the eager ones' bits."""
+    lens = i32([900, 700])
+    sets = [_inputs(20 + i) for i in range(4)]
+    eager = [[t.clone() for t in _step(x, lens)] for x in sets]
+    graphs, inputs, results = [], [], []
+    for g in range(2):
+        static = [t.clone() for t in sets[g]]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(_step(static, lens))
+        graphs.append(graph)
+        inputs.append(static)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(4):
+        for g in range(2):
+            for a, b in zip(inputs[g], sets[(turn + 2 * g) % 4]):
+                a.copy_(b)
+        torch.cuda.synchronize()
+        for g in range(2):
+            with torch.cuda.stream(streams[g]):
+                graphs[g].replay()
+        again = _step(sets[turn], lens)  # the program's own work meanwhile
+        torch.cuda.synchronize()
+        for g in range(2):
+            for a, b in zip(results[g], eager[(turn + 2 * g) % 4]):
+                assert torch.equal(a, b), (turn, g)
+        assert all(torch.equal(a, b) for a, b in zip(again, eager[turn]))
+
+
+def test_another_stream_and_repeated_calls_give_the_same_bits():
+    lens = i32([900, 700])
+    x = _inputs(30)
+    ref = _step(x, lens)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = [_step(x, lens) for _ in range(3)]
+    s.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, ref))
+
+
+def test_workspace_contents_do_not_matter():
+    B, H, Hkv, S, d, n = 1, 4, 2, 900, 96, 6
+    rng = np.random.default_rng(3)
+    q, k, v, go = (to_dev(bits(rng, B, h, S, d)) for h in (H, Hkv, Hkv, H))
+    lists = some_lists(rng, B, Hkv, S, S, n, "near")
+    lists[..., 1] = 0
+    lists = i32(lists)
+    got = []
+    for fill in (0, 255, 127):
+        out, lse = torch.empty_like(q), torch.empty((B, H, S), device="cuda")
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        nf, nb = (f(B, H, Hkv, S, S, d, n) for f in (ta.block_attn_fwd_workspace, ta.block_attn_bwd_workspace))
+        assert nf > 0
+        wf, wb = (torch.full((x + 64,), fill, dtype=torch.uint8, device="cuda") for x in (nf, nb))
+        stream = torch.cuda.current_stream()
+        ta.block_attn_fwd(q, k, v, lists, out, lse, B, H, Hkv, S, S, d, n, True, None, 0.1, wf, nf, stream)
+        ta.block_attn_bwd(q, k, v, lists, out, go, lse, *grads, B, H, Hkv, S, S, d, n, True, None, 0.1, wb, nb, stream)
+        got.append([out, lse, *grads])
+        assert (wf[nf:] == fill).all() and (wb[nb:] == fill).all()
+    for g in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(g, got[0]))
+
+
+def test_wrappers_refuse():
+    q, k = torch.zeros(1, 4, 300, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 2, 300, 64, dtype=torch.bfloat16, device="cuda")
+    lists = torch.zeros(1, 2, 3, 2, dtype=torch.int32, device="cuda")
+    for bad in ((q.half(), k, k, lists), (q, k, k[:, :1], lists), (q, k, k, lists.long()), (q, k, k, lists[:, :, :2]),
+                (q, k.transpose(1, 2).contiguous().transpose(1, 2), k, lists), (q, k, k.cpu(), lists)):
+        with pytest.raises(ValueError):
+            ta.block_attn(*bad)
+    with pytest.raises(ValueError, match="lens"):
+        ta.block_attn(q, k, k, lists, lens=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ta.TileAttnError, match="multiple"):
+        ta.block_attn(q[:, :3].contiguous(), k, k, lists)
+    with pytest.raises(ta.TileAttnError, match="overlap"):
+        ta.block_attn(k, k, k, lists, out=k)
+    with pytest.raises(ta.TileAttnError, match="forced"):
+        ta.block_lists(q, torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16, device="cuda"), 300, 1, sink=1)
+    with pytest.raises(ValueError, match="blocks"):
+        ta.block_lists(q, torch.zeros(1, 2, 4, 64, dtype=torch.bfloat16, device="cuda"), 300, 2)

@@ -1,0 +1,332 @@
+"""The 8-bit cache: writing it (codes and scales to the bit) and attention over it, against the
+float64 reference. Tolerances as for attention over lists: codes are exact numbers, weights times
+the page's scale are rounded to bf16 once, results once (2^-8 of the value each)."""
+import numpy as np
+import pytest
+
+import workloads
+from oracle import blocks as ob
+from tests.gpu_helpers import from_dev, to_dev, widen
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2502_06155_amd as ta  # noqa: E402
+
+HALF = 2.0 ** -8
+FP32 = 5e-4
+
+
+def i32(x):
+    return None if x is None else torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def bits(rng, *shape):
+    return workloads.f32_to_bf16_bits(rng.standard_normal(shape).astype(np.float32))
+
+
+def new_pages(rng, n, Hkv, d):
+    """Pages of any codes, NaN among them, with power-of-two scales: what a cache holds where nobody
+    has written."""
+    k, v = (rng.integers(0, 256, s).astype(np.uint8) for s in ((n, Hkv, 128, d), (n, Hkv, d, 128)))
+    return [k, v, *(2.0 ** rng.integers(-9, -5, (n, Hkv)).astype(np.float32) for _ in range(2))]
+
+
+def to_gpu(cache):
+    codes = [torch.from_numpy(x.copy()).cuda().view(torch.float8_e4m3fn) for x in cache[:2]]
+    return codes + [torch.from_numpy(x.copy()).cuda() for x in cache[2:]]
+
+
+def same(gpu, cache):
+    for name, a, b in zip(("k codes", "v codes", "k scales", "v scales"), gpu, cache):
+        got = a.view(torch.uint8).cpu().numpy() if a.dtype == torch.float8_e4m3fn else a.cpu().numpy()
+        assert np.array_equal(got, b), (name, np.argwhere(got != b)[:4])
+
+
+def write_both(k, v, cache, gpu, table, lens, n_new=None):
+    ob.cache_write(k, v, *cache, np.asarray(table), lens, n_new)
+    ta.cache_write(to_dev(k), to_dev(v), *gpu, i32(table), i32(lens), i32(n_new))
+
+
+@pytest.mark.parametrize("B,Hkv,N,d,lens,n_new", [
+    (1, 1, 1, 64, [0], None),
+    (2, 2, 1, 128, [127, 128], None),
+    (3, 1, 5, 96, [0, 126, 300], [5, 3, 0]),
+    (2, 3, 300, 64, [100, 511], None),
+    (2, 2, 129, 96, [0, 127], [129, 128]),
+    (1, 2, 400, 128, [5], [1000]),
+    (2, 1, 3, 64, [-4, 640], None),      # a length below 0 is 0; 640: past the table's pages
+    (1, 1, 200, 64, [600], [-1]),
+])
+def test_write(B, Hkv, N, d, lens, n_new):
+    rng = np.random.default_rng(N + d)
+    cache = new_pages(rng, 5 * B + 2, Hkv, d)
+    for x in cache[:2]:
+        x[(x & 127) == 127] = 0  # held tokens are numbers
+    gpu = to_gpu(cache)
+    table = rng.permutation(5 * B + 2)[:5 * B].reshape(B, 5).astype(np.int32)
+    write_both(bits(rng, B, Hkv, N, d), bits(rng, B, Hkv, N, d), cache, gpu, table, lens, n_new)
+    same(gpu, cache)
+
+
+def test_every_finite_bf16_value_and_the_others():
+    """All 2^16 bit patterns as tokens of pages of their own magnitude: codes to the bit, scales at
+    both ends of their range, infinities at the largest code, NaN kept."""
+    b = np.arange(1 << 16, dtype=np.uint32).astype(np.uint16)
+    order = np.argsort(b & 0x7FFF, kind="stable")
+    k = b[order].reshape(1, 1, 1024, 64)
+    cache = new_pages(np.random.default_rng(0), 8, 1, 64)
+    gpu = to_gpu(cache)
+    table = np.arange(8, dtype=np.int32)[None]
+    write_both(k, k[:, :, ::-1].copy(), cache, gpu, table, [0])
+    codes = gpu[0].view(torch.uint8).cpu().numpy()
+    nan = (codes & 127) == 127
+    assert np.array_equal(nan, (cache[0] & 127) == 127)
+    assert np.array_equal(np.where(nan, 0, codes), np.where(nan, 0, cache[0]))
+    assert np.array_equal(gpu[2].cpu().numpy(), cache[2]) and np.array_equal(gpu[3].cpu().numpy(), cache[3])
+    assert cache[2].min() == 2.0 ** -100 and cache[2].max() == 2.0 ** 120
+
+
+def test_tokens_one_by_one_raise_the_scale_of_their_page():
+    """Magnitudes that grow and shrink: old codes move with the scale, down to subnormal ones."""
+    rng = np.random.default_rng(2)
+    cache = new_pages(rng, 4, 2, 96)
+    gpu = to_gpu(cache)
+    table = np.array([[2, 0, 1]], np.int32)
+    for t in range(140):
+        k, v = (workloads.f32_to_bf16_bits((rng.standard_normal((1, 2, 1, 96)) * 2.0 ** rng.integers(-9, 9)).astype(np.float32))
+                for _ in range(2))
+        write_both(k, v, cache, gpu, table, [t])
+    same(gpu, cache)
+
+
+def test_pages_that_are_none_and_a_written_prefix_at_once():
+    rng = np.random.default_rng(3)
+    cache = new_pages(rng, 3, 1, 64)
+    gpu = to_gpu(cache)
+    table = np.array([[0, -1, 2], [3, 1, -2 ** 31]], np.int32)
+    write_both(bits(rng, 2, 1, 384, 64), bits(rng, 2, 1, 384, 64), cache, gpu, table, [0, 0])
+    same(gpu, cache)
+
+
+def check(out, lse, q, cache, table, lens, scale=None):
+    ref, rlse, mag = ob.cache_attention(q, *cache, np.asarray(table), np.asarray(lens), scale)
+    got = widen(from_dev(out))
+    assert np.isfinite(got).all()
+    off = np.abs(got - ref) - (HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30)
+    assert off.max() <= 0, np.unravel_index(np.argmax(off), off.shape)
+    some = np.isfinite(rlse)
+    l = lse.cpu().numpy().astype(np.float64)
+    assert np.array_equal(l[~some], rlse[~some]) and not from_dev(out)[~some].any()
+    assert np.abs(l[some] - rlse[some]).max(initial=0) <= 2e-4
+
+
+def held(rng, B, Hkv, d, lens, width=None, spare=2):
+    """A cache whose sequences hold lens tokens; everything behind them is any code."""
+    need = [-(-x // 128) for x in lens]
+    width = max(1, max(need)) if width is None else width
+    cache = new_pages(rng, sum(need) + spare, Hkv, d)
+    perm = rng.permutation(sum(need) + spare)
+    table = np.full((B, width), -1, np.int32)
+    at = 0
+    for b in range(B):
+        table[b, :need[b]] = perm[at:at + need[b]]
+        at += need[b]
+        for i in range(need[b]):
+            n = min(128, lens[b] - 128 * i)
+            p = table[b, i]
+            for x in (cache[0][p, :, :n], cache[1][p, :, :, :n]):
+                x[(x & 127) == 127] = 5
+    return cache, table
+
+
+@pytest.mark.parametrize("B,H,Hkv,N,d,lens", [
+    (1, 1, 1, 1, 64, [1]),
+    (2, 2, 1, 1, 96, [0, 63]),
+    (3, 4, 2, 1, 128, [64, 65, 127]),
+    (3, 8, 1, 1, 64, [128, 129, 1000]),
+    (2, 3, 3, 4, 96, [2, 700]),       # fewer tokens than rows: some rows see none
+    (2, 16, 2, 2, 128, [193, 3000]),
+    (2, 20, 1, 1, 64, [500, 77]),     # more than 16 rows
+    (1, 16, 1, 5, 96, [900]),         # 80 rows: three passes
+    (2, 34, 2, 3, 128, [130, 257]),
+    (20, 6, 3, 1, 64, [0, 5, 0, 0, 300, 128, 0, 1, 640, 2, 0, 256, 7, 0, 90, 0, 0, 1280, 3, 0]),
+])
+@pytest.mark.parametrize("scale", [None, -0.2, 0.0])
+def test_attention(B, H, Hkv, N, d, lens, scale):
+    rng = np.random.default_rng(sum(lens) + d)
+    cache, table = held(rng, B, Hkv, d, lens)
+    q = bits(rng, B, H, N, d)
+    out = torch.full((B, H, N, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    got, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), scale, out, return_lse=True)
+    assert got is out
+    check(got, lse, q, cache, table, lens, scale)
+
+
+def test_many_short_sequences_and_one_long():
+    """More segments than a wave scans at once, and one that most workgroups share."""
+    rng = np.random.default_rng(5)
+    lens = [int(x) for x in rng.integers(0, 200, 150)]
+    lens[77] = 20000
+    cache, table = held(rng, 150, 2, 64, lens)
+    q = bits(rng, 150, 4, 1, 64)
+    out, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), return_lse=True)
+    check(out, lse, q, cache, table, lens)
+
+
+def test_lengths_past_the_table_and_pages_that_are_none():
+    rng = np.random.default_rng(6)
+    cache, table = held(rng, 2, 2, 96, [512, 512])
+    table[0, 1], table[1, 3], table[1, 0] = -1, 99, -2 ** 31
+    q, lens = bits(rng, 2, 4, 1, 96), [2 ** 31 - 1, 512]
+    out, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), return_lse=True)
+    check(out, lse, q, cache, table, lens)
+    none = np.full_like(table, -1)
+    out, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(none), i32([512, 3]), return_lse=True)
+    assert not from_dev(out).any() and torch.isneginf(lse).all()
+
+
+def test_scales_of_any_kind():
+    rng = np.random.default_rng(7)
+    cache, table = held(rng, 1, 1, 64, [400])
+    cache[2] = rng.uniform(-0.01, 0.01, cache[2].shape).astype(np.float32)
+    cache[3] = rng.uniform(-2, 2, cache[3].shape).astype(np.float32)
+    q = bits(rng, 1, 2, 1, 64)
+    out, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32([400]), return_lse=True)
+    check(out, lse, q, cache, table, [400])
+
+
+def _generate(B, H, Hkv, d, prompt, steps, seed, sink=1, local=1, n=3):
+    """A program that generates: the prompt into the cache, then token after token: its keys and
+    values written, the pages of the best blocks chosen for each key head, attention over those."""
+    rng = np.random.default_rng(seed)
+    total = max(prompt) + steps
+    width = -(-total // 128)
+    k, v, q = (bits(rng, B, x, total, d) for x in (Hkv, Hkv, H))
+    cache = new_pages(rng, B * width, Hkv, d)
+    table = rng.permutation(B * width).reshape(B, width).astype(np.int32)
+    return dict(k=k, v=v, q=q, cache=cache, table=table, prompt=prompt, steps=steps, n=n, sink=sink, local=local)
+
+
+def test_generating_with_chosen_pages():
+    B, H, Hkv, d, prompt = 2, 4, 2, 64, [700, 513]
+    g = _generate(B, H, Hkv, d, prompt, 3, 11)
+    gpu, table = to_gpu(g["cache"]), i32(g["table"])
+    lens = i32([0, 0])
+    first = max(prompt)
+    ta.cache_write(to_dev(g["k"][:, :, :first]), to_dev(g["v"][:, :, :first]), *gpu, table, lens, i32(prompt))
+    ob.cache_write(g["k"][:, :, :first], g["v"][:, :, :first], *g["cache"], g["table"], [0, 0], prompt)
+    same(gpu, g["cache"])
+    keys = np.zeros((B, Hkv, first + 3, d), np.uint16)  # what the program keeps block means of
+    for b in range(B):
+        keys[b, :, :prompt[b]] = g["k"][b, :, :prompt[b]]
+    for step in range(3):
+        held_now = [p + step for p in prompt]
+        now = [g[x][np.arange(B), :, held_now][:, :, None].copy() for x in "kvq"]
+        ta.cache_write(to_dev(now[0]), to_dev(now[1]), *gpu, table, i32(held_now))
+        ob.cache_write(now[0], now[1], *g["cache"], g["table"], held_now)
+        same(gpu, g["cache"])
+        pages = np.full((B, Hkv, 3), -1, np.int32)
+        lens_h = np.zeros((B, Hkv), np.int32)
+        for b in range(B):  # one sequence a call: their positions differ
+            keys[b, :, held_now[b]] = now[0][b, :, 0]
+            S = held_now[b] + 1
+            kb = keys[b:b + 1, :, :S].copy()
+            lists = ta.block_lists(to_dev(now[2][b:b + 1]), ta.block_means(to_dev(kb)), S, 3, True, 1, 1).cpu().numpy()
+            assert np.array_equal(lists, ob.block_lists(now[2][b:b + 1], ob.block_means(kb), S, 3, True, 1, 1))
+            for h in range(Hkv):
+                chosen = [j for j in lists[0, h, 0] if j >= 0]
+                pages[b, h, :len(chosen)] = g["table"][b][chosen]
+                lens_h[b, h] = 128 * (len(chosen) - 1) + S - 128 * chosen[-1]
+        out, lse = ta.cache_attn(to_dev(now[2]), *gpu, i32(pages), i32(lens_h), return_lse=True)
+        check(out, lse, now[2], g["cache"], pages, lens_h)
+        # attention over the lists on the cache's numbers says the same
+        values = ob.e4m3_values()
+        whole, wl = ta.cache_attn(to_dev(now[2]), *gpu, table, i32([x + 1 for x in held_now]), return_lse=True)
+        check(whole, wl, now[2], g["cache"], g["table"], [x + 1 for x in held_now])
+        assert not np.isnan(values[g["cache"][0][g["table"][0, 0]]]).any()
+
+
+def test_captured_write_and_attention_replayed():
+    """Writing and reading in one graph, lengths moved on between the replays by the program."""
+    rng = np.random.default_rng(12)
+    B, H, Hkv, d = 3, 6, 2, 128
+    start = [126, 5, 400]
+    cache, table = held(rng, B, Hkv, d, start, width=5, spare=12)
+    free = [p for p in range(len(cache[0])) if p not in table]
+    for b in range(B):
+        for i in range(5):
+            if table[b, i] < 0 and free:
+                table[b, i] = free.pop()
+    gpu, t = to_gpu(cache), i32(table)
+    lens = i32(start)
+    k, v, q = (torch.zeros(B, x, 1, d, dtype=torch.bfloat16, device="cuda") for x in (Hkv, Hkv, H))
+
+    def step():
+        ta.cache_write(k, v, *gpu, t, lens)
+        after = lens + 1
+        return ta.cache_attn(q, *gpu, t, after, return_lse=True)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out, lse = step()
+    for i in range(5):
+        x = [bits(rng, B, h, 1, d) for h in (Hkv, Hkv, H)]
+        for a, b in zip((k, v, q), x):
+            a.copy_(to_dev(b))
+        at = [s + i for s in start]
+        lens.copy_(i32(at))
+        graph.replay()
+        ob.cache_write(x[0], x[1], *cache, table, at)
+        torch.cuda.synchronize()
+        same(gpu, cache)
+        check(out, lse, x[2], cache, table, [y + 1 for y in at])
+        eager = ta.cache_attn(q, *gpu, t, lens + 1, return_lse=True)
+        assert torch.equal(eager[0], out) and torch.equal(eager[1], lse)
+
+
+def test_offsets_past_32_bits():
+    """A cache of more than 2^32 bytes a tensor: pages at its far end."""
+    d, Hkv = 128, 8
+    n = 2 ** 32 // (Hkv * 128 * d) + 40
+    kp = torch.zeros((n, Hkv, 128, d), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    vp = torch.zeros((n, Hkv, d, 128), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    ks, vs = torch.ones((n, Hkv), device="cuda"), torch.ones((n, Hkv), device="cuda")
+    rng = np.random.default_rng(13)
+    k, v, q = bits(rng, 1, Hkv, 300, d), bits(rng, 1, Hkv, 300, d), bits(rng, 1, Hkv, 1, d)
+    table = np.array([[n - 1, 3, n - 7]], np.int32)
+    ta.cache_write(to_dev(k), to_dev(v), kp, vp, ks, vs, i32(table), i32([0]))
+    out, lse = ta.cache_attn(to_dev(q), kp, vp, ks, vs, i32(table), i32([300]), return_lse=True)
+    small = [np.zeros((3, Hkv, 128, d), np.uint8), np.zeros((3, Hkv, d, 128), np.uint8),
+             np.ones((3, Hkv), np.float32), np.ones((3, Hkv), np.float32)]
+    near = np.array([[0, 1, 2]], np.int32)
+    ob.cache_write(k, v, *small, near, [0])
+    for i, page in enumerate(table[0]):
+        assert np.array_equal(kp[page].view(torch.uint8).cpu().numpy(), small[0][i])
+        assert np.array_equal(vp[page].view(torch.uint8).cpu().numpy(), small[1][i])
+    check(out, lse, q, small, near, [300])
+
+
+def test_wrappers_refuse():
+    rng = np.random.default_rng(1)
+    cache, table = held(rng, 1, 2, 64, [200])
+    gpu, t, lens = to_gpu(cache), i32(table), i32([200])
+    q = torch.zeros(1, 4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="k_pages"):
+        ta.cache_attn(q, gpu[0].view(torch.uint8), *gpu[1:], t, lens)
+    with pytest.raises(ValueError, match="v_pages"):
+        ta.cache_attn(q, gpu[0], gpu[0], *gpu[2:], t, lens)
+    with pytest.raises(ValueError, match="lens"):
+        ta.cache_attn(q, *gpu, t[:, None].expand(1, 2, 2).contiguous(), lens)
+    with pytest.raises(ValueError, match="table"):
+        ta.cache_attn(q, *gpu, t.long(), lens)
+    with pytest.raises(ValueError, match="k must"):
+        ta.cache_write(k[:, :1], k, *gpu, t, lens)
+    with pytest.raises(ta.TileAttnError, match="overlap"):
+        ta.cache_attn(q[:, :, :, :], *gpu, t, lens, out=q)
