@@ -5,12 +5,11 @@
 // dv = sum P dout, the last two over the query rows of all G heads of the group.
 //
 // Passes, on the caller's stream:
-//   prep     base-2 lse (+inf for rows without tokens: their P is 0) and -delta per row; clears the
-//            columns.
-//   columns  the lists turned round: for every key block a bitmap of the query blocks that list it
-//            (one atomic OR per entry: the result does not depend on their order).
-//   plan     counts a column's query blocks and cuts long ones (a block that every query keeps)
-//            into pieces of at most `entries` query blocks.
+//   prep     base-2 lse (+inf for rows without tokens: their P is 0) and -delta per row; in the same
+//            launch the lists turned round: for every key block a bitmap (its column) of the query
+//            blocks that list it, 32 of them a workgroup.
+//   plan     counts a column's query blocks, cuts long ones (a block that every query keeps) into
+//            pieces of at most `entries` query blocks, and orders the pieces longest first.
 //   dq       one workgroup per unit of 128 query rows, over its list's key tiles:
 //            S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T; a lane owns one query.
 //   dk, dv   one workgroup per piece of a key block (128 keys, 4 waves of 32), over the 64-row
@@ -35,15 +34,41 @@ namespace {
 
 constexpr int kPrepRowsB = 64;
 
+__device__ __forceinline__ int query_words(const BlockGeo& g) { return (g.nq + 31) / 32; }
+
+// One word of every column of a (batch, key head): the lists of 32 query blocks. Entries that name
+// no block, or one that no row of the query block may attend to, are left out as in the forward.
+__device__ __forceinline__ void column_words(const BlockBwdArgs& a, uint32_t work, uint32_t* col) {
+  const BlockGeo& g = a.g;
+  const int words = query_words(g);
+  const int w = (int)(work % words);
+  const uint32_t bh = work / words;
+  const int len = seq_len(g, (int)(bh / g.Hkv));
+  for (int j = threadIdx.x; j < g.nb; j += kThreadsB) col[j] = 0;
+  __syncthreads();
+  const int i0 = 32 * w, n = min(32, g.nq - i0) * g.n_list;
+  const int32_t* lists = a.lists + ((size_t)bh * g.nq + i0) * g.n_list;
+  for (int x = threadIdx.x; x < n; x += kThreadsB) {
+    const int bit = x / g.n_list, i = i0 + bit, j = lists[x];
+    const int first = g.off + i * kBlock, last = min(first + min(kBlock, g.Sq - i * kBlock), len) - 1;
+    const int end = last < first ? 0 : min(g.nb, (g.causal ? last : len - 1) / kBlock + 1);
+    if (j >= 0 && j < end) atomicOr(&col[j], 1u << bit);
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < g.nb; j += kThreadsB) a.cols[((size_t)bh * g.nb + j) * words + w] = col[j];
+}
+
 template <int D>
-__global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArgs a, int64_t n_rows, int64_t n_words) {
+__global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArgs a, int64_t n_rows, uint32_t prep_wgs) {
   constexpr int kPieces = D / 8, kPer = kPrepRowsB * kPieces / kThreadsB;
   static_assert(kPrepRowsB * kPieces == kThreadsB * kPer, "whole pieces per thread");
-  __shared__ float part[kPrepRowsB * kPieces];
-  for (int64_t x = (int64_t)blockIdx.x * kThreadsB + threadIdx.x; x < n_words; x += (int64_t)gridDim.x * kThreadsB)
-    a.cols[x] = 0;
+  extern __shared__ float part[];  // the rows' pieces, or the columns' words
+  if (blockIdx.x >= prep_wgs) {
+    column_words(a, blockIdx.x - prep_wgs, reinterpret_cast<uint32_t*>(part));
+    return;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.counts[8] = 0;
   const int64_t row0 = (int64_t)blockIdx.x * kPrepRowsB;
-  if (row0 >= n_rows) return;
   const int n = (int)min(n_rows - row0, (int64_t)kPrepRowsB);
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
@@ -71,38 +96,55 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
 }
 
 // ---------------------------------------------------------------------------------------------
-// columns and plan
+// plan
 
-__device__ __forceinline__ int query_words(const BlockGeo& g) { return (g.nq + 31) / 32; }
+// One workgroup per XCD cuts the columns of its share into pieces and lists the pieces longest first
+// (by 64 sizes): popular blocks' pieces start the launch, and those of blocks that hardly anybody
+// lists even out its end. plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first
+// slot; items[xcd * cap + i] = {column, piece}; counts[xcd] = items of the share. Slots come from a
+// counter and items of one size in any order: where a piece's sums lie and when it runs may differ
+// from call to call, what it adds up and in which order does not.
+constexpr int kPlanThreads = 1024, kSizes = 64;
 
-__global__ __launch_bounds__(kThreadsB) void block_columns_kernel(const BlockBwdArgs a, int64_t n_entries) {
-  const BlockGeo& g = a.g;
-  const int words = query_words(g);
-  for (int64_t x = (int64_t)blockIdx.x * kThreadsB + threadIdx.x; x < n_entries; x += (int64_t)gridDim.x * kThreadsB) {
-    const uint32_t list = (uint32_t)(x / g.n_list);
-    const int j = a.lists[x];
-    const int i = (int)(list % g.nq);
-    const uint32_t bh = list / g.nq;
-    const int len = seq_len(g, (int)(bh / g.Hkv));
-    const int first = g.off + i * kBlock, last = min(first + min(kBlock, g.Sq - i * kBlock), len) - 1;
-    const int end = last < first ? 0 : min(g.nb, (g.causal ? last : len - 1) / kBlock + 1);
-    if (j >= 0 && j < end) atomicOr(&a.cols[((size_t)bh * g.nb + j) * words + (i >> 5)], 1u << (i & 31));
-  }
-}
-
-// plan[4 x] = query blocks of column x, [4 x + 1] = its pieces, [4 x + 2] = its first slot. Slots
-// are handed out by a counter: which ones a column gets may differ from call to call, what it sums
-// up and in which order does not.
-__global__ __launch_bounds__(kThreadsB) void block_plan_kernel(const BlockBwdArgs a, int64_t n_cols) {
+__global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwdArgs a, uint32_t cols, uint32_t per) {
+  __shared__ int hist[kSizes];
   const int words = query_words(a.g);
-  const int64_t x = (int64_t)blockIdx.x * kThreadsB + threadIdx.x;
-  if (x >= n_cols) return;
-  int n = 0;
-  for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[x * words + w]);
-  const int pieces = max(1, (n + a.entries - 1) / a.entries);
-  a.plan[4 * x] = n;
-  a.plan[4 * x + 1] = pieces;
-  if (pieces > 1) a.plan[4 * x + 2] = atomicAdd(reinterpret_cast<int*>(a.cols + n_cols * words), pieces);
+  const uint32_t x0 = blockIdx.x * per, x1 = min(cols, x0 + per);
+  const int tid = threadIdx.x;
+  if (tid < kSizes) hist[tid] = 0;
+  __syncthreads();
+  // Entries of pieces of one column differ by at most one: one size stands for all.
+  auto size_of = [&](int n, int pieces) {
+    return kSizes - 1 - min(kSizes - 1, (int)((int64_t)((n + pieces - 1) / pieces) * kSizes / (a.entries + 1)));
+  };
+  for (uint32_t x = x0 + tid; x < x1; x += kPlanThreads) {
+    int n = 0;
+    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
+    const int pieces = max(1, (n + a.entries - 1) / a.entries);
+    a.plan[4 * (size_t)x] = n;
+    a.plan[4 * (size_t)x + 1] = pieces;
+    a.plan[4 * (size_t)x + 2] = pieces > 1 ? atomicAdd(&a.counts[8], pieces) : 0;
+    atomicAdd(&hist[size_of(n, pieces)], pieces);
+  }
+  __syncthreads();
+  if (tid < kSizes) {  // one wave: where each size starts
+    const int own = hist[tid];
+    int upto = own;
+#pragma unroll
+    for (int s = 1; s < kSizes; s <<= 1) {
+      const int y = __shfl_up(upto, s);
+      if (tid >= s) upto += y;
+    }
+    hist[tid] = upto - own;
+    if (tid == kSizes - 1) a.counts[blockIdx.x] = upto;
+  }
+  __syncthreads();
+  int2* items = reinterpret_cast<int2*>(a.items) + (size_t)blockIdx.x * per * a.pieces_k;
+  for (uint32_t x = x0 + tid; x < x1; x += kPlanThreads) {
+    const int n = a.plan[4 * (size_t)x], pieces = a.plan[4 * (size_t)x + 1];
+    const int at = atomicAdd(&hist[size_of(n, pieces)], pieces);
+    for (int p = 0; p < pieces; ++p) items[at + p] = int2{(int)x, p};
+  }
 }
 
 // P = exp2(c s - lse2) clamped to [0, 1] (the exponent is <= 0 up to rounding for kept pairs; the
@@ -125,14 +167,14 @@ __device__ __forceinline__ void score_grads(const f32x16& s, const f32x16& dp, f
   }
 }
 
+// The query-side pass of one unit; `id` as a workgroup id.
 template <int D>
-__global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdArgs a) {
+__device__ __forceinline__ void dq_unit(const BlockBwdArgs& a, uint32_t id, uint16_t (&sK)[2][BlockShape<D>::kTileElems],
+                                        uint16_t (&sV)[2][BlockShape<D>::kTileElems], uint32_t (&bits)[kBlockWords]) {
   using Sh = BlockShape<D>;
-  __shared__ uint16_t sK[2][Sh::kTileElems], sV[2][Sh::kTileElems];
-  __shared__ uint32_t bits[kBlockWords];
   const BlockGeo& g = a.g;
   const uint32_t lists = (uint32_t)g.B * g.Hkv * g.nq;
-  const uint32_t work = xcd_unit(blockIdx.x, lists * a.units * a.pieces_q);
+  const uint32_t work = xcd_unit(id, lists * a.units * a.pieces_q);
   if (work >= lists * a.units * a.pieces_q) return;
   const int piece = (int)(work % a.pieces_q);
   const uint32_t lu = work / a.pieces_q, list = lu / a.units;
@@ -259,28 +301,6 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdAr
   }
 }
 
-// Adds the pieces of dq units, in order; a thread takes 4 consecutive d of a row.
-template <int D>
-__global__ __launch_bounds__(kThreadsB) void block_dq_sum_kernel(const BlockBwdArgs a) {
-  const BlockGeo& g = a.g;
-  const uint32_t lu = blockIdx.x, list = lu / a.units;
-  const int unit = (int)(lu % a.units), i = (int)(list % g.nq);
-  const int bh = (int)(list / g.nq), b = bh / g.Hkv, h = bh - b * g.Hkv;
-  const ListRows rows(g, b, h, i);
-  const int n_rows = g.G * rows.tokens;
-  const float* part = a.part_q + (size_t)lu * a.pieces_q * kUnitRows * D;
-  for (int x = threadIdx.x; x < kUnitRows * (D / 4); x += kThreadsB) {
-    const int rr = x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
-    if (r >= n_rows) return;
-    int pos;
-    const size_t row = rows.global(r, pos);
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < a.pieces_q; ++p)
-      y += *reinterpret_cast<const f32x4*>(part + ((size_t)p * kUnitRows + rr) * D + d0);
-    *reinterpret_cast<u32x2*>(a.dq + row * D + d0) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
-  }
-}
-
 // ---------------------------------------------------------------------------------------------
 // dk, dv
 
@@ -311,23 +331,19 @@ struct QueryTiles {
   }
 };
 
-template <int D>
-constexpr int dkdv_wgs() { return D == 128 ? 1 : 2; }
-
+// The key-side pass of one piece of a key block; `id` as a workgroup id: every XCD runs the items of
+// its share in the plan's order.
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kThreadsB, dkdv_wgs<D>()) void block_dkdv_kernel(const BlockBwdArgs a) {
+__device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, uint16_t (&sQ)[2][BlockShape<D>::kTileElems],
+                                          uint16_t (&sG)[2][BlockShape<D>::kTileElems], float (&sL)[2][kBlockK],
+                                          float (&sD)[2][kBlockK], uint32_t (&bits)[kBlockWords]) {
   using Sh = BlockShape<D>;
-  __shared__ uint16_t sQ[2][Sh::kTileElems], sG[2][Sh::kTileElems];
-  __shared__ float sL[2][kBlockK], sD[2][kBlockK];
-  __shared__ uint32_t bits[kBlockWords];
   const BlockGeo& g = a.g;
-  const uint32_t cols = (uint32_t)g.B * g.Hkv * g.nb;
-  const uint32_t work = xcd_unit(blockIdx.x, cols * a.pieces_k);
-  if (work >= cols * a.pieces_k) return;
-  const int piece = (int)(work % a.pieces_k);
-  const uint32_t col = work / a.pieces_k;
-  const int pieces = a.plan[4 * (size_t)col + 1];
-  if (piece >= pieces) return;
+  const uint32_t cap = ((uint32_t)g.B * g.Hkv * g.nb + 7) / 8 * (uint32_t)a.pieces_k;
+  if (id / 8 >= (uint32_t)a.counts[id % 8]) return;
+  const int2 item = reinterpret_cast<const int2*>(a.items)[(size_t)(id % 8) * cap + id / 8];
+  const uint32_t col = (uint32_t)item.x;
+  const int piece = item.y, pieces = a.plan[4 * (size_t)col + 1];
   const int all = a.plan[4 * (size_t)col];
   const int j = (int)(col % g.nb);
   const int bh = (int)(col / g.nb), b = bh / g.Hkv, h = bh - b * g.Hkv;
@@ -385,25 +401,22 @@ __global__ __launch_bounds__(kThreadsB, dkdv_wgs<D>()) void block_dkdv_kernel(co
       }
     };
     load_tile(nxt, 0);
-    int first = nxt.first();
+    [[maybe_unused]] int first = nxt.first(), block = nxt.walk.at;
     nxt.next();
     wait_tile_loads();
     __syncthreads();
 
     // One tile as a stream of MFMAs, each in a fenced packet with its share of the vector work and
     // its operand read from LDS two packets ahead: S and dP of half 0, S and dP of half 1 with half
-    // 0's P and dS forming, the updates of half 0 with half 1's, the updates of half 1. MASK: rows
-    // before this lane's key (lim of the tile's rows) get P = 0.
-    auto stream = [&](auto bufc, auto maskc, int lim) {
+    // 0's P and dS forming, the updates of half 0 with half 1's, the updates of half 1.
+    auto stream = [&](auto bufc) {
       constexpr int buf = decltype(bufc)::value;
-      constexpr bool kMask = decltype(maskc)::value;
       constexpr int kC = Sh::kChunks, kMb = Sh::kDBlocks, kAhead = 2;
       constexpr int kHalf = 2 * kC, kAcc = 4 * kMb, kN = 2 * kHalf + 2 * kAcc, kPerC2 = kAcc / 2;
       f32x16 sc[2], dp[2];
       bf16x8 pb[2][2], db[2][2];
       f32x4 l4[2][4];
       float t0, t1, y0, y1;
-      const int low = lim - 4 * hf;
       auto dp_start = [&](int qc, f32x16& x) {
 #pragma unroll
         for (int c2 = 0; c2 < 2; ++c2)
@@ -454,15 +467,8 @@ __global__ __launch_bounds__(kThreadsB, dkdv_wgs<D>()) void block_dkdv_kernel(co
           for (int m = k * 80 / kPk; m < (k + 1) * 80 / kPk; ++m) {
             // Step m % 10 of pair m / 10: entries e, e + 1 are tile rows 32 hh + 16 c2 + 8 u + 4 hf + j.
             const int op = m % 10, e = 2 * (m / 10), c2 = e / 8, u = (e % 8) / 4, jj = e % 4;
-            const int rr = 32 * hh + 16 * c2 + 8 * u + jj;
-            if (op == 0) {
-              t0 = __builtin_fmaf(sc[hh][e], a.c, -l4[hh][2 * c2 + u][jj]);
-              if (kMask && rr < low) t0 = -INFINITY;
-            }
-            if (op == 1) {
-              t1 = __builtin_fmaf(sc[hh][e + 1], a.c, -l4[hh][2 * c2 + u][jj + 1]);
-              if (kMask && rr + 1 < low) t1 = -INFINITY;
-            }
+            if (op == 0) t0 = __builtin_fmaf(sc[hh][e], a.c, -l4[hh][2 * c2 + u][jj]);
+            if (op == 1) t1 = __builtin_fmaf(sc[hh][e + 1], a.c, -l4[hh][2 * c2 + u][jj + 1]);
             if (op == 2) t0 = __builtin_amdgcn_fmed3f(fast_exp2(t0), 0.f, 1.f);
             if (op == 4) t1 = __builtin_amdgcn_fmed3f(fast_exp2(t1), 0.f, 1.f);
             if (op == 6) y0 = t0 * dp[hh][e];
@@ -492,27 +498,75 @@ __global__ __launch_bounds__(kThreadsB, dkdv_wgs<D>()) void block_dkdv_kernel(co
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    auto tile_step = [&](auto bufc, bool more) {
-      if (more) load_tile(nxt, decltype(bufc)::value ^ 1);
-      if (wave_active) {
-        const int lim = CAUSAL ? key - first : 0;  // the tile's first row that attends to this key
-        if (CAUSAL && __builtin_amdgcn_ballot_w64(lim > 0) != 0) stream(bufc, std::true_type{}, lim);
-        else stream(bufc, std::false_type{}, 0);
+    // A tile in which some rows may come before the keys (`lim`: the first row that attends to this
+    // lane's key), half after half. The column's query blocks come in ascending order, so such tiles
+    // come first, in a loop of their own: beside the stream, in one loop, this would cost the stream
+    // its registers (374 bytes of scratch at d = 96).
+    [[maybe_unused]] auto masked = [&](const uint16_t* tq, const uint16_t* tg, const float* tl, const float* td, int lim) {
+#pragma unroll 1
+      for (int hh = 0; hh < 2; ++hh) {
+        f32x16 s = f32x16{}, dp;
+        f32x4 l4[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(td + 32 * hh + 8 * u + 4 * hf);
+          l4[u] = *reinterpret_cast<const f32x4*>(tl + 32 * hh + 8 * u + 4 * hf);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * u + e] = d4[e];
+        }
+#pragma unroll
+        for (int cc = 0; cc < Sh::kChunks; ++cc) {
+          s = mfma32(rows_frag<D>(tq, ra, hh, cc), kf[cc], s);
+          dp = mfma32(rows_frag<D>(tg, ra, hh, cc), vf[cc], dp);
+        }
+        bf16x8 pb[2], db[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int rr = 32 * hh + 8 * (e / 4) + 4 * hf + e % 4;
+          const float p = rr < lim ? 0.f : prob(s[e], a.c, l4[e / 4][e % 4]);
+          pb[e / 8][e % 8] = (__bf16)p;
+          db[e / 8][e % 8] = (__bf16)(p * dp[e]);
+        }
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+          for (int mb = 0; mb < Sh::kDBlocks; ++mb) {
+            dv[mb] = mfma32(cols_frag<D>(tg, ca, mb, 2 * hh + c2), pb[c2], dv[mb]);
+            dk[mb] = mfma32(cols_frag<D>(tq, ca, mb, 2 * hh + c2), db[c2], dk[mb]);
+          }
       }
-      if (more) {
-        first = nxt.first();
-        nxt.next();
+    };
+    bool more = true;  // a tile is loaded
+    if constexpr (CAUSAL) {
+      int buf = 0;
+      const int own_last = j * kBlock + kBlock - 1;
+      while (more && (g.off + block * kBlock < own_last || buf)) {
+        more = !nxt.done();
+        if (more) load_tile(nxt, buf ^ 1);
+        if (wave_active) masked(sQ[buf], sG[buf], sL[buf], sD[buf], key - first);
+        if (more) {
+          first = nxt.first();
+          block = nxt.walk.at;
+          nxt.next();
+        }
+        wait_tile_loads();
+        __syncthreads();
+        buf ^= 1;
       }
+    }
+    auto tile_step = [&](auto bufc) {
+      constexpr int buf = decltype(bufc)::value;
+      more = !nxt.done();
+      if (more) load_tile(nxt, buf ^ 1);
+      if (wave_active) stream(bufc);
+      if (more) nxt.next();
       wait_tile_loads();
       __syncthreads();
     };
-    for (;;) {
-      bool more = !nxt.done();
-      tile_step(std::integral_constant<int, 0>{}, more);
+    while (more) {
+      tile_step(std::integral_constant<int, 0>{});
       if (!more) break;
-      more = !nxt.done();
-      tile_step(std::integral_constant<int, 1>{}, more);
-      if (!more) break;
+      tile_step(std::integral_constant<int, 1>{});
     }
   }
 
@@ -538,11 +592,59 @@ __global__ __launch_bounds__(kThreadsB, dkdv_wgs<D>()) void block_dkdv_kernel(co
   }
 }
 
-// Adds the pieces of cut key blocks, in order; dk by blockIdx.y = 0, dv by 1.
+// Both passes in one launch (two workgroups a compute unit): the key side's items first, they are
+// the longer ones, then the query side's units, which fill the places as they fall free.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(kThreadsB, 2) void block_grad_kernel(const BlockBwdArgs a, uint32_t key_wgs) {
+  __shared__ uint16_t s0[2][BlockShape<D>::kTileElems], s1[2][BlockShape<D>::kTileElems];
+  __shared__ float sL[2][kBlockK], sD[2][kBlockK];
+  __shared__ uint32_t bits[kBlockWords];
+  if (blockIdx.x < key_wgs) dkdv_unit<D, CAUSAL>(a, blockIdx.x, s0, s1, sL, sD, bits);
+  else dq_unit<D>(a, blockIdx.x - key_wgs, s0, s1, bits);
+}
+
+// d = 128: the key side's accumulators and operands take 256 registers by themselves, so it runs one
+// workgroup a compute unit, and each pass has a launch of its own.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(kThreadsB, 1) void block_dkdv_kernel(const BlockBwdArgs a) {
+  __shared__ uint16_t s0[2][BlockShape<D>::kTileElems], s1[2][BlockShape<D>::kTileElems];
+  __shared__ float sL[2][kBlockK], sD[2][kBlockK];
+  __shared__ uint32_t bits[kBlockWords];
+  dkdv_unit<D, CAUSAL>(a, blockIdx.x, s0, s1, sL, sD, bits);
+}
 template <int D>
-__global__ __launch_bounds__(kThreadsB) void block_dkdv_sum_kernel(const BlockBwdArgs a) {
+__global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdArgs a) {
+  __shared__ uint16_t s0[2][BlockShape<D>::kTileElems], s1[2][BlockShape<D>::kTileElems];
+  __shared__ uint32_t bits[kBlockWords];
+  dq_unit<D>(a, blockIdx.x, s0, s1, bits);
+}
+
+// Adds the pieces of a dq unit, in order; a thread takes 4 consecutive d of a row.
+template <int D>
+__device__ __forceinline__ void sum_dq(const BlockBwdArgs& a, uint32_t lu) {
   const BlockGeo& g = a.g;
-  const uint32_t col = blockIdx.x;
+  const uint32_t list = lu / a.units;
+  const int unit = (int)(lu % a.units), i = (int)(list % g.nq);
+  const int bh = (int)(list / g.nq), b = bh / g.Hkv, h = bh - b * g.Hkv;
+  const ListRows rows(g, b, h, i);
+  const int n_rows = g.G * rows.tokens;
+  const float* part = a.part_q + (size_t)lu * a.pieces_q * kUnitRows * D;
+  for (int x = threadIdx.x; x < kUnitRows * (D / 4); x += kThreadsB) {
+    const int rr = x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
+    if (r >= n_rows) return;
+    int pos;
+    const size_t row = rows.global(r, pos);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.pieces_q; ++p)
+      y += *reinterpret_cast<const f32x4*>(part + ((size_t)p * kUnitRows + rr) * D + d0);
+    *reinterpret_cast<u32x2*>(a.dq + row * D + d0) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+  }
+}
+
+// Adds the pieces of a cut key block, in order: dk, or dv.
+template <int D>
+__device__ __forceinline__ void sum_dkdv(const BlockBwdArgs& a, uint32_t col, int which) {
+  const BlockGeo& g = a.g;
   const int pieces = a.plan[4 * (size_t)col + 1];
   if (pieces == 1) return;
   const int slot = a.plan[4 * (size_t)col + 2];
@@ -550,8 +652,8 @@ __global__ __launch_bounds__(kThreadsB) void block_dkdv_sum_kernel(const BlockBw
   const int j = (int)(col % g.nb);
   const size_t row0 = (size_t)(col / g.nb) * g.Skv + (size_t)j * kBlock;
   const int n_rows = min(kBlock, g.Skv - j * kBlock);
-  const float* part = a.part_k + ((size_t)slot * 2 + blockIdx.y) * kBlock * D;
-  uint16_t* out = blockIdx.y ? a.dv : a.dk;
+  const float* part = a.part_k + ((size_t)slot * 2 + which) * kBlock * D;
+  uint16_t* out = which ? a.dv : a.dk;
   for (int x = threadIdx.x; x < n_rows * (D / 4); x += kThreadsB) {
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < pieces; ++p) y += *reinterpret_cast<const f32x4*>(part + (size_t)p * 2 * kBlock * D + 4 * x);
@@ -560,21 +662,33 @@ __global__ __launch_bounds__(kThreadsB) void block_dkdv_sum_kernel(const BlockBw
 }
 
 template <int D>
+__global__ __launch_bounds__(kThreadsB) void block_sum_kernel(const BlockBwdArgs a, uint32_t dq_wgs) {
+  if (blockIdx.x < dq_wgs) sum_dq<D>(a, blockIdx.x);
+  else sum_dkdv<D>(a, (blockIdx.x - dq_wgs) / 2, (blockIdx.x - dq_wgs) % 2);
+}
+
+template <int D>
 hipError_t block_bwd_for(const BlockBwdArgs& a, hipStream_t s) {
   const BlockGeo& g = a.g;
-  const int64_t rows = (int64_t)g.B * g.H * g.Sq, cols = (int64_t)g.B * g.Hkv * g.nb;
-  const int64_t words = cols * ((g.nq + 31) / 32) + 1;  // the slot counter behind them
-  const int64_t lists = (int64_t)g.B * g.Hkv * g.nq, entries = lists * g.n_list;
-  block_prep_kernel<D><<<(unsigned)((rows + kPrepRowsB - 1) / kPrepRowsB), kThreadsB, 0, s>>>(a, rows, words);
-  block_columns_kernel<<<(unsigned)std::min<int64_t>((entries + kThreadsB - 1) / kThreadsB, 4096), kThreadsB, 0, s>>>(
-      a, entries);
-  block_plan_kernel<<<(unsigned)((cols + kThreadsB - 1) / kThreadsB), kThreadsB, 0, s>>>(a, cols);
-  block_dq_kernel<D><<<xcd_grid((uint32_t)(lists * a.units * a.pieces_q)), kThreadsB, 0, s>>>(a);
-  if (a.pieces_q > 1) block_dq_sum_kernel<D><<<(unsigned)(lists * a.units), kThreadsB, 0, s>>>(a);
-  const unsigned grid_k = xcd_grid((uint32_t)(cols * a.pieces_k));
-  if (g.causal) block_dkdv_kernel<D, true><<<grid_k, kThreadsB, 0, s>>>(a);
-  else block_dkdv_kernel<D, false><<<grid_k, kThreadsB, 0, s>>>(a);
-  if (a.pieces_k > 1) block_dkdv_sum_kernel<D><<<dim3((unsigned)cols, 2), kThreadsB, 0, s>>>(a);
+  const int64_t rows = (int64_t)g.B * g.H * g.Sq;
+  const uint32_t cols = (uint32_t)((int64_t)g.B * g.Hkv * g.nb), per = (cols + 7) / 8;
+  const uint32_t lists = (uint32_t)((int64_t)g.B * g.Hkv * g.nq);
+  const uint32_t prep = (uint32_t)((rows + kPrepRowsB - 1) / kPrepRowsB);
+  const uint32_t words = (uint32_t)((int64_t)g.B * g.Hkv * ((g.nq + 31) / 32));
+  const size_t lds = std::max((size_t)kPrepRowsB * (D / 8), (size_t)g.nb) * 4;
+  block_prep_kernel<D><<<prep + words, kThreadsB, lds, s>>>(a, rows, prep);
+  block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols, per);
+  const uint32_t keys = 8 * per * (uint32_t)a.pieces_k, queries = xcd_grid(lists * a.units * a.pieces_q);
+  if constexpr (D == 128) {
+    if (g.causal) block_dkdv_kernel<D, true><<<keys, kThreadsB, 0, s>>>(a);
+    else block_dkdv_kernel<D, false><<<keys, kThreadsB, 0, s>>>(a);
+    block_dq_kernel<D><<<queries, kThreadsB, 0, s>>>(a);
+  } else {
+    if (g.causal) block_grad_kernel<D, true><<<keys + queries, kThreadsB, 0, s>>>(a, keys);
+    else block_grad_kernel<D, false><<<keys + queries, kThreadsB, 0, s>>>(a, keys);
+  }
+  const uint32_t sum_q = a.pieces_q > 1 ? lists * a.units : 0, sum_k = a.pieces_k > 1 ? 2 * cols : 0;
+  if (sum_q + sum_k) block_sum_kernel<D><<<sum_q + sum_k, kThreadsB, 0, s>>>(a, sum_q);
   return hipGetLastError();
 }
 

@@ -103,7 +103,7 @@ size_t fwd_bytes(const BlockGeo& g) {
 struct BwdPlan {
   int entries, pieces_q, pieces_k;
   int64_t slots;
-  size_t off_ndelta, off_cols, off_plan, off_q, off_k, bytes;
+  size_t off_ndelta, off_cols, off_plan, off_counts, off_items, off_q, off_k, bytes;
 };
 BwdPlan plan_bwd(const BlockGeo& g) {
   BwdPlan p;
@@ -126,9 +126,13 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   p.off_ndelta = at;
   at += up(rows * 4);
   p.off_cols = at;
-  at += up(((size_t)cols * ((g.nq + 31) / 32) + 1) * 4);
+  at += up((size_t)cols * ((g.nq + 31) / 32) * 4);
   p.off_plan = at;
   at += up((size_t)cols * 16);
+  p.off_counts = at;
+  at += up(9 * 4);
+  p.off_items = at;
+  at += up((size_t)((cols + 7) / 8 * 8) * p.pieces_k * 8);
   p.off_q = at;
   at += p.pieces_q == 1 ? 0 : up((size_t)(lists_of(g) * units_of(g)) * p.pieces_q * kBlock * g.d * 4);
   p.off_k = at;
@@ -322,10 +326,12 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
   a.ndelta = reinterpret_cast<float*>(ws + p.off_ndelta);
   a.cols = reinterpret_cast<uint32_t*>(ws + p.off_cols);
   a.plan = reinterpret_cast<int32_t*>(ws + p.off_plan);
+  a.counts = reinterpret_cast<int32_t*>(ws + p.off_counts);
+  a.items = reinterpret_cast<int32_t*>(ws + p.off_items);
   a.part_q = reinterpret_cast<float*>(ws + p.off_q);
   a.part_k = reinterpret_cast<float*>(ws + p.off_k);
-  if (int st = check_grid(std::max((double)lists_of(a.g) * a.units * a.pieces_q, (double)cols * a.pieces_k))) return st;
-  if (int st = check_grid((double)rows / 64)) return st;
+  if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces_q + (double)cols * a.pieces_k + 2.0 * cols)) return st;
+  if (int st = check_grid((double)rows / 64 + (double)lists_of(a.g))) return st;
   return launched(launch_block_bwd(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -69,7 +69,9 @@ struct BlockBwdArgs {
   float* lse2;       // [B, H, Sq]: base-2 lse, +inf for rows without tokens
   float* ndelta;     // [B, H, Sq]: -<dout, out>
   uint32_t* cols;    // [B, Hkv, nb][nq / 32 words]: the query blocks that list a key block
-  int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot; then the slot counter
+  int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot
+  int32_t* counts;   // [9]: items of each XCD's share; the slot counter
+  int32_t* items;    // [8][columns of a share * pieces_k][2]: column, piece
   float* part_q;     // pieces_q > 1: fp32 [list][unit][piece][128][d]
   float* part_k;     // fp32 [slot][2][128][d]: dk, dv
 };
