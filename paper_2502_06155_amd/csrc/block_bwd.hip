@@ -8,8 +8,8 @@
 //   prep     base-2 lse (+inf for rows without tokens: their P is 0) and -delta per row; in the same
 //            launch the lists turned round: for every key block a bitmap (its column) of the query
 //            blocks that list it, 32 of them a workgroup.
-//   plan     counts a column's query blocks, cuts long ones (a block that every query keeps) into
-//            pieces of at most `entries` query blocks, and orders the pieces longest first.
+//   plan     deals the columns out to the XCDs by work, cuts long ones (a block that every query
+//            keeps) into pieces of at most `entries` query blocks, and orders the pieces longest first.
 //   dq       one workgroup per unit of 128 query rows, over its list's key tiles:
 //            S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T; a lane owns one query.
 //   dk, dv   one workgroup per piece of a key block (128 keys, 4 waves of 32), over the 64-row
@@ -98,53 +98,90 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
 // ---------------------------------------------------------------------------------------------
 // plan
 
-// One workgroup per XCD cuts the columns of its share into pieces and lists the pieces longest first
-// (by 64 sizes): popular blocks' pieces start the launch, and those of blocks that hardly anybody
-// lists even out its end. plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first
-// slot; items[xcd * cap + i] = {column, piece}; counts[xcd] = items of the share. Slots come from a
-// counter and items of one size in any order: where a piece's sums lie and when it runs may differ
-// from call to call, what it adds up and in which order does not.
+// One workgroup per XCD. The columns, in order, are dealt out to the XCDs as contiguous shares of
+// equal work (a column's query blocks, and a quarter of the mean for its start and end): in causal
+// order early blocks have many more query blocks than late ones, and shares of equal count left
+// half of the XCDs idle (4 key heads of 128 blocks: 986 us). Each workgroup cuts the columns of its
+// share into pieces and lists the pieces longest first (by 64 sizes): popular blocks' pieces start
+// the launch, those of blocks that hardly anybody lists even out its end.
+// plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first slot; items[xcd * cap
+// + i] = {column, piece}; counts[xcd] = items of the share. Slots come from a counter and items of
+// one size in any order: where a piece's sums lie and when it runs may differ from call to call,
+// what it adds up and in which order does not.
 constexpr int kPlanThreads = 1024, kSizes = 64;
 
-__global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwdArgs a, uint32_t cols, uint32_t per) {
+__global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwdArgs a, uint32_t cols) {
   __shared__ int hist[kSizes];
+  __shared__ int64_t wave_sums[kPlanThreads / 64];
   const int words = query_words(a.g);
-  const uint32_t x0 = blockIdx.x * per, x1 = min(cols, x0 + per);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const uint32_t each = (cols + kPlanThreads - 1) / kPlanThreads;
+  const uint32_t x0 = min(cols, tid * each), x1 = min(cols, x0 + each);
+  auto blocks_of = [&](uint32_t x) {
+    int n = 0;
+#pragma unroll 4
+    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
+    return n;
+  };
   if (tid < kSizes) hist[tid] = 0;
+  int64_t own = 0;
+  for (uint32_t x = x0; x < x1; ++x) own += blocks_of(x);
+  int64_t upto = own;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t y = __shfl_up((long long)upto, s);
+    if (lane >= s) upto += y;
+  }
+  if (lane == 63) wave_sums[wave] = upto;
   __syncthreads();
+  int64_t total = 0, before = upto - own;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) before += wave_sums[w];
+    total += wave_sums[w];
+  }
+  const int64_t start = max((int64_t)1, (total + 4 * (int64_t)cols - 1) / (4 * (int64_t)cols));
+  const int64_t work = total + start * cols;
+  before += start * x0;
   // Entries of pieces of one column differ by at most one: one size stands for all.
   auto size_of = [&](int n, int pieces) {
     return kSizes - 1 - min(kSizes - 1, (int)((int64_t)((n + pieces - 1) / pieces) * kSizes / (a.entries + 1)));
   };
-  for (uint32_t x = x0 + tid; x < x1; x += kPlanThreads) {
-    int n = 0;
-    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
-    const int pieces = max(1, (n + a.entries - 1) / a.entries);
+  auto mine = [&](auto&& fn) {
+    int64_t at = before;
+    for (uint32_t x = x0; x < x1; ++x) {
+      const int xcd = (int)(at * 8 / work);
+      if (xcd > (int)blockIdx.x) break;
+      const int n = blocks_of(x);
+      at += n + start;
+      if (xcd == (int)blockIdx.x) fn(x, n, max(1, (n + a.entries - 1) / a.entries));
+    }
+  };
+  mine([&](uint32_t x, int n, int pieces) {
     a.plan[4 * (size_t)x] = n;
     a.plan[4 * (size_t)x + 1] = pieces;
     a.plan[4 * (size_t)x + 2] = pieces > 1 ? atomicAdd(&a.counts[8], pieces) : 0;
     atomicAdd(&hist[size_of(n, pieces)], pieces);
-  }
+  });
   __syncthreads();
   if (tid < kSizes) {  // one wave: where each size starts
-    const int own = hist[tid];
-    int upto = own;
+    const int mine_n = hist[tid];
+    int sum = mine_n;
 #pragma unroll
     for (int s = 1; s < kSizes; s <<= 1) {
-      const int y = __shfl_up(upto, s);
-      if (tid >= s) upto += y;
+      const int y = __shfl_up(sum, s);
+      if (tid >= s) sum += y;
     }
-    hist[tid] = upto - own;
-    if (tid == kSizes - 1) a.counts[blockIdx.x] = upto;
+    hist[tid] = sum - mine_n;
+    if (tid == kSizes - 1) a.counts[blockIdx.x] = min(sum, a.items_cap);
   }
   __syncthreads();
-  int2* items = reinterpret_cast<int2*>(a.items) + (size_t)blockIdx.x * per * a.pieces_k;
-  for (uint32_t x = x0 + tid; x < x1; x += kPlanThreads) {
-    const int n = a.plan[4 * (size_t)x], pieces = a.plan[4 * (size_t)x + 1];
+  int2* items = reinterpret_cast<int2*>(a.items) + (size_t)blockIdx.x * a.items_cap;
+  mine([&](uint32_t x, int n, int pieces) {
     const int at = atomicAdd(&hist[size_of(n, pieces)], pieces);
-    for (int p = 0; p < pieces; ++p) items[at + p] = int2{(int)x, p};
-  }
+    for (int p = 0; p < pieces; ++p)
+      if (at + p < a.items_cap) items[at + p] = int2{(int)x, p};
+  });
 }
 
 // P = exp2(c s - lse2) clamped to [0, 1] (the exponent is <= 0 up to rounding for kept pairs; the
@@ -173,14 +210,10 @@ __device__ __forceinline__ void dq_unit(const BlockBwdArgs& a, uint32_t id, uint
                                         uint16_t (&sV)[2][BlockShape<D>::kTileElems], uint32_t (&bits)[kBlockWords]) {
   using Sh = BlockShape<D>;
   const BlockGeo& g = a.g;
-  const uint32_t lists = (uint32_t)g.B * g.Hkv * g.nq;
-  const uint32_t work = xcd_unit(id, lists * a.units * a.pieces_q);
-  if (work >= lists * a.units * a.pieces_q) return;
-  const int piece = (int)(work % a.pieces_q);
-  const uint32_t lu = work / a.pieces_q, list = lu / a.units;
-  const int unit = (int)(lu % a.units);
-  const int i = (int)(list % g.nq);
-  const int bh = (int)(list / g.nq), b = bh / g.Hkv, h = bh - b * g.Hkv;
+  UnitPlace u;
+  if (!u.find(g, id, a.units, a.pieces_q)) return;
+  const uint32_t list = u.list, lu = list * a.units + u.unit;
+  const int piece = u.piece, unit = u.unit, i = u.i, b = u.b, h = u.h, bh = u.b * g.Hkv + u.h;
   const ListRows rows(g, b, h, i);
   const int n_rows = g.G * rows.tokens;
   if (unit * kUnitRows >= n_rows) return;
@@ -308,6 +341,15 @@ __device__ __forceinline__ void dq_unit(const BlockBwdArgs& a, uint32_t id, uint
 struct QueryTiles {
   BitWalk walk;
   int head, half, G, off, Sq, len;
+  // The column's query blocks [e0, e1).
+  __device__ __forceinline__ void start(const BlockGeo& g, int length, const uint32_t* bits, int words, int e0, int e1) {
+    head = half = 0;
+    G = g.G;
+    off = g.off;
+    Sq = g.Sq;
+    len = length;
+    walk.start(bits, words, e0, e1 - e0);
+  }
   __device__ __forceinline__ bool done() const { return walk.at < 0; }
   __device__ __forceinline__ int first() const { return off + walk.at * kBlock + half * kBlockK; }  // position
   // Valid rows from the tile's first on (rows past the tile's 64 among them).
@@ -331,40 +373,133 @@ struct QueryTiles {
   }
 };
 
-// The key-side pass of one piece of a key block; `id` as a workgroup id: every XCD runs the items of
-// its share in the plan's order.
+// dK, dV += a 64-row tile in which some rows may come before the keys (`lim`: the first row that
+// attends to this lane's key), half after half. The columns' query blocks come in ascending order, so
+// such tiles come first, in a loop of their own: beside the unmasked stream, in one loop, this
+// would cost the stream its registers (374 bytes of scratch at d = 96).
+template <int D>
+__device__ __forceinline__ void masked_tile(const uint16_t* tq, const uint16_t* tg, const float* tl, const float* td,
+                                            int lim, float c, int hf, const RowsAt<D>& ra, const ColsAt<D>& ca,
+                                            const bf16x8 (&kf)[D / 16], const bf16x8 (&vf)[D / 16],
+                                            f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32]) {
+#pragma unroll 1
+  for (int hh = 0; hh < 2; ++hh) {
+    f32x16 s = f32x16{}, dp;
+    f32x4 l4[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const f32x4 d4 = *reinterpret_cast<const f32x4*>(td + 32 * hh + 8 * u + 4 * hf);
+      l4[u] = *reinterpret_cast<const f32x4*>(tl + 32 * hh + 8 * u + 4 * hf);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[4 * u + e] = d4[e];
+    }
+#pragma unroll
+    for (int cc = 0; cc < D / 16; ++cc) {
+      s = mfma32(rows_frag<D>(tq, ra, hh, cc), kf[cc], s);
+      dp = mfma32(rows_frag<D>(tg, ra, hh, cc), vf[cc], dp);
+    }
+    bf16x8 pb[2], db[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int rr = 32 * hh + 8 * (e / 4) + 4 * hf + e % 4;
+      const float p = rr < lim ? 0.f : prob(s[e], c, l4[e / 4][e % 4]);
+      pb[e / 8][e % 8] = (__bf16)p;
+      db[e / 8][e % 8] = (__bf16)(p * dp[e]);
+    }
+#pragma unroll
+    for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) {
+        dv[mb] = mfma32(cols_frag<D>(tg, ca, mb, 2 * hh + c2), pb[c2], dv[mb]);
+        dk[mb] = mfma32(cols_frag<D>(tq, ca, mb, 2 * hh + c2), db[c2], dk[mb]);
+      }
+  }
+}
+
+// A piece of a column as one workgroup finds it.
+struct KeyPiece {
+  uint32_t col;
+  int piece, pieces, all;  // all: query blocks of the column
+  int j, bh, b, h, len;
+  size_t group_row;        // row of the group's first head in [B, H, Sq]
+  // Every XCD runs the items of its share in the plan's order; false past their end.
+  __device__ __forceinline__ bool find(const BlockBwdArgs& a, uint32_t id) {
+    const BlockGeo& g = a.g;
+    if (id / 8 >= (uint32_t)a.counts[id % 8]) return false;
+    const int2 item = reinterpret_cast<const int2*>(a.items)[(size_t)(id % 8) * a.items_cap + id / 8];
+    // The same in every lane; in scalar registers the tiles' addresses are scalar work.
+    col = (uint32_t)__builtin_amdgcn_readfirstlane(item.x);
+    piece = __builtin_amdgcn_readfirstlane(item.y);
+    all = __builtin_amdgcn_readfirstlane(a.plan[4 * (size_t)col]);
+    pieces = __builtin_amdgcn_readfirstlane(a.plan[4 * (size_t)col + 1]);
+    j = (int)(col % g.nb);
+    bh = (int)(col / g.nb);
+    b = bh / g.Hkv;
+    h = bh - b * g.Hkv;
+    len = seq_len(g, b);
+    group_row = ((size_t)b * g.H + (size_t)h * g.G) * g.Sq;
+    return true;
+  }
+  __device__ __forceinline__ int begin() const { return (int)((int64_t)all * piece / pieces); }
+  __device__ __forceinline__ int end() const { return (int)((int64_t)all * (piece + 1) / pieces); }
+  __device__ __forceinline__ void load_bits(const BlockBwdArgs& a, uint32_t* bits, int words) const {
+    for (int x = threadIdx.x; x < words; x += kThreadsB) bits[x] = a.cols[(size_t)col * words + x];
+    __syncthreads();
+  }
+};
+
+// Stores this lane's key row of dK and dV, or the piece's part of it. Rows of padding are zeros:
+// what formed for their zero K and V rows counts for nobody.
+template <int D>
+__device__ __forceinline__ void store_key(const BlockBwdArgs& a, const KeyPiece& kp, int row, int hf, f32x16 (&dk)[D / 32],
+                                          f32x16 (&dv)[D / 32]) {
+  const int key = kp.j * kBlock + row;
+  if (key >= kp.len) {
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb) {
+      dk[mb] = f32x16{};
+      dv[mb] = f32x16{};
+    }
+  }
+  if (kp.pieces == 1) {
+    if (key < a.g.Skv) {
+      const size_t kr = (size_t)kp.bh * a.g.Skv + key;
+      store_bf16<D>(a.dk + kr * D, dk, a.scale, hf);
+      store_bf16<D>(a.dv + kr * D, dv, 1.f, hf);
+    }
+  } else {
+    const int slot = a.plan[4 * (size_t)kp.col + 2] + kp.piece;
+    if (slot < a.slots) {
+      float* part = a.part_k + ((size_t)slot * 2 * kBlock + row) * D;
+      store_f32<D>(part, dk, a.scale, hf);
+      store_f32<D>(part + (size_t)kBlock * D, dv, 1.f, hf);
+    }
+  }
+}
+
+// The key-side pass of one piece of a key block (d = 64 and 96); `id` as a workgroup id.
 template <int D, bool CAUSAL>
 __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, uint16_t (&sQ)[2][BlockShape<D>::kTileElems],
                                           uint16_t (&sG)[2][BlockShape<D>::kTileElems], float (&sL)[2][kBlockK],
                                           float (&sD)[2][kBlockK], uint32_t (&bits)[kBlockWords]) {
   using Sh = BlockShape<D>;
   const BlockGeo& g = a.g;
-  const uint32_t cap = ((uint32_t)g.B * g.Hkv * g.nb + 7) / 8 * (uint32_t)a.pieces_k;
-  if (id / 8 >= (uint32_t)a.counts[id % 8]) return;
-  const int2 item = reinterpret_cast<const int2*>(a.items)[(size_t)(id % 8) * cap + id / 8];
-  const uint32_t col = (uint32_t)item.x;
-  const int piece = item.y, pieces = a.plan[4 * (size_t)col + 1];
-  const int all = a.plan[4 * (size_t)col];
-  const int j = (int)(col % g.nb);
-  const int bh = (int)(col / g.nb), b = bh / g.Hkv, h = bh - b * g.Hkv;
-  const int len = seq_len(g, b);
-  const size_t group_row = ((size_t)b * g.H + (size_t)h * g.G) * g.Sq;
-
+  KeyPiece kp;
+  if (!kp.find(a, id)) return;
+  const size_t group_row = kp.group_row;
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 31, hf = lane >> 5;
   const int words = query_words(g);
-  for (int x = tid; x < words; x += kThreadsB) bits[x] = a.cols[(size_t)col * words + x];
-  __syncthreads();
+  kp.load_bits(a, bits, words);
 
   // This lane's key as the B operand of S = Q K^T and dP = dO V^T.
-  const int key = j * kBlock + wave * 32 + n;
-  const bool valid = key < len;
-  const bool wave_active = j * kBlock + wave * 32 < len;
-  const size_t kr = (size_t)bh * g.Skv + key;
+  const int key = kp.j * kBlock + wave * 32 + n;
+  const bool wave_active = kp.j * kBlock + wave * 32 < kp.len;
+  const size_t kr = (size_t)kp.bh * g.Skv + key;
   bf16x8 kf[Sh::kChunks], vf[Sh::kChunks];
-  lane_row<D>(a.k + kr * D, valid, a.keep, a.flip, hf, kf);
-  lane_row<D>(a.v + kr * D, valid, ~0u, 0u, hf, vf);
+  lane_row<D>(a.k + kr * D, key < kp.len, a.keep, a.flip, hf, kf);
+  lane_row<D>(a.v + kr * D, key < kp.len, ~0u, 0u, hf, vf);
   f32x16 dk[Sh::kDBlocks], dv[Sh::kDBlocks];
 #pragma unroll
   for (int mb = 0; mb < Sh::kDBlocks; ++mb) {
@@ -373,14 +508,7 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
   }
 
   QueryTiles nxt;
-  nxt.head = 0;
-  nxt.half = 0;
-  nxt.G = g.G;
-  nxt.off = g.off;
-  nxt.Sq = g.Sq;
-  nxt.len = len;
-  const int e0 = (int)((int64_t)all * piece / pieces), e1 = (int)((int64_t)all * (piece + 1) / pieces);
-  nxt.walk.start(bits, words, e0, e1 - e0);
+  nxt.start(g, kp.len, bits, words, kp.begin(), kp.end());
   if (!nxt.done()) {
     TileLoads<D> ld;
     ld.init(wave, lane);
@@ -498,52 +626,15 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    // A tile in which some rows may come before the keys (`lim`: the first row that attends to this
-    // lane's key), half after half. The column's query blocks come in ascending order, so such tiles
-    // come first, in a loop of their own: beside the stream, in one loop, this would cost the stream
-    // its registers (374 bytes of scratch at d = 96).
-    [[maybe_unused]] auto masked = [&](const uint16_t* tq, const uint16_t* tg, const float* tl, const float* td, int lim) {
-#pragma unroll 1
-      for (int hh = 0; hh < 2; ++hh) {
-        f32x16 s = f32x16{}, dp;
-        f32x4 l4[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const f32x4 d4 = *reinterpret_cast<const f32x4*>(td + 32 * hh + 8 * u + 4 * hf);
-          l4[u] = *reinterpret_cast<const f32x4*>(tl + 32 * hh + 8 * u + 4 * hf);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dp[4 * u + e] = d4[e];
-        }
-#pragma unroll
-        for (int cc = 0; cc < Sh::kChunks; ++cc) {
-          s = mfma32(rows_frag<D>(tq, ra, hh, cc), kf[cc], s);
-          dp = mfma32(rows_frag<D>(tg, ra, hh, cc), vf[cc], dp);
-        }
-        bf16x8 pb[2], db[2];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int rr = 32 * hh + 8 * (e / 4) + 4 * hf + e % 4;
-          const float p = rr < lim ? 0.f : prob(s[e], a.c, l4[e / 4][e % 4]);
-          pb[e / 8][e % 8] = (__bf16)p;
-          db[e / 8][e % 8] = (__bf16)(p * dp[e]);
-        }
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-          for (int mb = 0; mb < Sh::kDBlocks; ++mb) {
-            dv[mb] = mfma32(cols_frag<D>(tg, ca, mb, 2 * hh + c2), pb[c2], dv[mb]);
-            dk[mb] = mfma32(cols_frag<D>(tq, ca, mb, 2 * hh + c2), db[c2], dk[mb]);
-          }
-      }
-    };
     bool more = true;  // a tile is loaded
     if constexpr (CAUSAL) {
       int buf = 0;
-      const int own_last = j * kBlock + kBlock - 1;
+      const int own_last = kp.j * kBlock + kBlock - 1;
       while (more && (g.off + block * kBlock < own_last || buf)) {
         more = !nxt.done();
         if (more) load_tile(nxt, buf ^ 1);
-        if (wave_active) masked(sQ[buf], sG[buf], sL[buf], sD[buf], key - first);
+        if (wave_active)
+          masked_tile<D>(sQ[buf], sG[buf], sL[buf], sD[buf], key - first, a.c, hf, ra, ca, kf, vf, dk, dv);
         if (more) {
           first = nxt.first();
           block = nxt.walk.at;
@@ -570,26 +661,325 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
     }
   }
 
-  if (!valid) {  // padding: its K and V rows were zeros, what formed for them counts for nobody
+  store_key<D>(a, kp, wave * 32 + n, hf, dk, dv);
+}
+
+// ---------------------------------------------------------------------------------------------
+// dk, dv at d = 128, one wave per SIMD
+//
+// The accumulators (128 registers), the K and V operands (64) and the scores do not fit 256
+// registers, so one 4-wave workgroup runs per compute unit with 512 registers a wave: accumulators in
+// AGPRs, what the vector ALU touches in VGPRs. Nothing else on the SIMD hides a stall, so each wave
+// runs one unbroken stream of matrix instructions over 32-row query blocks h:
+//   S, dP of block h            | P, dS of block h - 1, second half of its rows
+//   dV, dK update of h - 1      | P, dS of block h, first half
+// with the vector work dealt out a few instructions per MFMA, operands read kAhead packets ahead
+// across the phases, and the blocks in a ring of LDS slots, five loaded ahead, so that a barrier every
+// two blocks never waits for the block it is about to use. Causal tiles that need a mask come first,
+// in the plain form, through the same LDS.
+
+// A lane id the compiler cannot hoist: rows derived from it hold no register across the stream.
+__device__ __forceinline__ int fresh_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
+// acc += a b with the accumulator in AGPRs. The compiler does not track an asm MFMA's hazards; none
+// arise: a comes from LDS (its wait counts asm operands), b was written by the vector ALU at least
+// one MFMA earlier, and acc is read by nothing but these MFMAs, the next on the same accumulator 7
+// others later, until the drain after the loop.
+__device__ __forceinline__ void mfma_acc(bf16x8 a, bf16x8 b, f32x16& acc) {
+  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+
+constexpr int kRing = 8;
+constexpr int kRingBlock = 32 * 128;                  // elements of a 32-row block of one tensor
+constexpr int kRingSlot = 2 * kRingBlock + 256;       // Q and dO rows, then lse2 and -delta (64 floats each)
+
+template <bool CAUSAL>
+__device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, uint32_t id, uint16_t* ring, uint32_t* bits) {
+  constexpr int D = 128, kC = D / 16, kMb = D / 32;
+  constexpr int kLd = kRingBlock * 2 / 2048;          // loads per wave and block (two waves per tensor)
+  constexpr int kAhead = 3;
+  const BlockGeo& g = a.g;
+  KeyPiece kp;
+  if (!kp.find(a, id)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int words = query_words(g);
+  kp.load_bits(a, bits, words);
+
+  bf16x8 kf[kC], vf[kC];
+  f32x16 dk[kMb], dv[kMb];
+  {
+    const int lane = fresh_lane(), key = kp.j * kBlock + wave * 32 + (lane & 31);
+    const size_t kr = (size_t)kp.bh * g.Skv + key;
+    lane_row<D>(a.k + kr * D, key < kp.len, a.keep, a.flip, lane >> 5, kf);
+    lane_row<D>(a.v + kr * D, key < kp.len, ~0u, 0u, lane >> 5, vf);
+  }
 #pragma unroll
-    for (int mb = 0; mb < Sh::kDBlocks; ++mb) {
-      dk[mb] = f32x16{};
-      dv[mb] = f32x16{};
+  for (int mb = 0; mb < kMb; ++mb) dk[mb] = dv[mb] = f32x16{};
+
+  QueryTiles tiles;
+  tiles.start(g, kp.len, bits, words, kp.begin(), kp.end());
+  if constexpr (CAUSAL) {
+    // The column's first blocks, up to where every row comes after every key of the block.
+    const int own_last = kp.j * kBlock + kBlock - 1;
+    if (!tiles.done() && g.off + tiles.walk.at * kBlock < own_last) {
+      const int lane = fresh_lane(), hf = lane >> 5, key = kp.j * kBlock + wave * 32 + (lane & 31);
+      constexpr int kTileE = kBlockK * D;
+      TileLoads<D> ld;
+      ld.init(wave, lane);
+      RowsAt<D> ra;
+      ra.init(lane & 31, hf);
+      ColsAt<D> ca;
+      ca.init(lane);
+      auto at = [&](int bi) { return ring + bi * (2 * kTileE + 256); };
+      auto load_tile = [&](int bi) {
+        const size_t row0 = tiles.row0(kp.group_row);
+        const int nv = tiles.valid();
+        ld.load(a.q + row0 * D, nv, at(bi), wave);
+        ld.load(a.dout + row0 * D, nv, at(bi) + kTileE, wave);
+        if (wave == 0) {
+          load_dword_to_lds(buffer_words(a.lse2 + row0, (uint32_t)(nv * 4)), lds_addr(at(bi) + 2 * kTileE), 4 * lane);
+          load_dword_to_lds(buffer_words(a.ndelta + row0, (uint32_t)(nv * 4)), lds_addr(at(bi) + 2 * kTileE + 128),
+                            4 * lane);
+        }
+      };
+      auto more = [&]() { return !tiles.done() && g.off + tiles.walk.at * kBlock < own_last; };
+      load_tile(0);
+      int buf = 0;
+      for (bool go = true; go; buf ^= 1) {
+        const int first = tiles.first();
+        tiles.next();
+        wait_tile_loads();
+        __syncthreads();
+        go = more();
+        if (go) load_tile(buf ^ 1);  // the buffer that the tile before the barrier used
+        const float* rows = reinterpret_cast<const float*>(at(buf) + 2 * kTileE);
+        masked_tile<D>(at(buf), at(buf) + kTileE, rows, rows + 64, key - first, a.c, hf, ra, ca, kf, vf, dk, dv);
+      }
+      __syncthreads();  // the ring takes the buffers over
     }
   }
-  if (pieces == 1) {
-    if (key < g.Skv) {
-      store_bf16<D>(a.dk + kr * D, dk, a.scale, hf);
-      store_bf16<D>(a.dv + kr * D, dv, 1.f, hf);
-    }
-  } else {
-    const int slot = a.plan[4 * (size_t)col + 2] + piece;
-    if (slot < a.slots) {
-      float* part = a.part_k + ((size_t)slot * 2 * kBlock + wave * 32 + n) * D;
-      store_f32<D>(part, dk, a.scale, hf);
-      store_f32<D>(part + (size_t)kBlock * D, dv, 1.f, hf);
-    }
+  // 32-row blocks left: four for every query block and head, fewer for a short last one (the
+  // highest bit a column can have).
+  int nb = 0;
+  if (!tiles.done()) {
+    const int rows = min(g.Sq, kp.len - g.off), last = (rows - 1) / kBlock, short_rows = rows - last * kBlock;
+    nb = tiles.walk.left * 4;
+    if (kp.end() == kp.all && (bits[last >> 5] >> (last & 31)) & 1) nb -= 4 - (short_rows + 31) / 32;
+    nb = __builtin_amdgcn_readfirstlane(nb * g.G);
   }
+  if (nb > 0) {
+    const int lane = fresh_lane();
+    const int hf = lane >> 5;
+    RowsAt<D> ra;
+    ra.init(lane & 31, hf);
+    ColsAt<D> ca;
+    ca.init(lane);
+    // Waves 0 and 1 load the Q blocks (half a block each) and lse2, waves 2 and 3 dO and -delta;
+    // every wave has the same number of loads in flight.
+    const bool second = wave >= 2;
+    const uint16_t* const src_all = second ? a.dout : a.q;
+    const float* const lsrc_all = second ? a.ndelta : a.lse2;
+    int off[kLd];
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      const int q = 64 * ((wave & 1) * kLd + x) + lane;
+      const int r = q / (D / 8), ps = q % (D / 8);
+      off[x] = (r * D + 8 * (ps ^ swizzle<D>(r))) * 2;
+    }
+    const uint32_t lds_dst = lds_addr(ring) + (second ? kRingBlock * 2 : 0) + (wave & 1) * kLd * 1024;
+    const uint32_t lds_row_dst = lds_addr(ring) + 4 * kRingBlock + (second ? 256 : 0);
+    // The block to load next: its rows start at src / lsrc, `left` valid rows remain of its query
+    // block and head (0 past the last block: those loads write zeros), at ring byte offset ld_off.
+    const uint16_t* src;
+    const float* lsrc;
+    int left;
+    uint32_t ld_off = 0;
+    auto at_head = [&]() {
+      const size_t row0 = tiles.row0(kp.group_row);
+      src = src_all + row0 * D;
+      lsrc = lsrc_all + row0;
+      left = tiles.valid();
+    };
+    at_head();
+    auto rsrc = [](const void* p, uint32_t bytes) {  // buffer_words of what is scalar already
+      const uint64_t x = reinterpret_cast<uint64_t>(p);
+      return i32x4{(int)(uint32_t)x, (int)(uint32_t)(x >> 32), (int)bytes, 0x00020000};
+    };
+    auto load_part = [&](int x) {
+      load_to_lds(rsrc(src, (uint32_t)(min(left, 32) * D * 2)), lds_dst + ld_off + 1024u * x, off[x]);
+    };
+    auto load_rows = [&]() {
+      load_dword_to_lds(rsrc(lsrc, (uint32_t)(min(left, 32) * 4)), lds_row_dst + ld_off, 4 * lane);
+    };
+    auto load_advance = [&]() {
+      ld_off = ld_off == (kRing - 1) * kRingSlot * 2 ? 0 : ld_off + kRingSlot * 2;
+      src += 32 * D;
+      lsrc += 32;
+      left -= 32;
+      if (left <= 0) {
+        left = 0;
+        if (!tiles.done()) {
+          if (++tiles.head == tiles.G) {
+            tiles.head = 0;
+            tiles.walk.next();
+          }
+          if (!tiles.done()) at_head();
+        }
+      }
+    };
+    // Zeros in the last slot: the block that the body before block 0's update runs over. (Weights
+    // of zero times block 0's own rows would turn an infinite dO into NaN.) Then blocks 0 .. 4 in
+    // flight, the zeros and block 0 visible.
+    const int left0 = left;
+    left = 0;
+    ld_off = (kRing - 1) * kRingSlot * 2;
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) load_part(x);
+    load_rows();
+    left = left0;
+    ld_off = 0;
+#pragma unroll
+    for (int y = 0; y < 5; ++y) {
+      if (y > 0) load_advance();
+#pragma unroll
+      for (int x = 0; x < kLd; ++x) load_part(x);
+      load_rows();
+    }
+    wait_loads<4 * (kLd + 1)>();
+    __syncthreads();
+
+    // By block parity: S and dP - delta, P and dS of the first 16 row entries (rows
+    // 16 c2 + 8 u + 4 hf + j are entries 8 c2 + 4 u + j); p1, d1 of the second.
+    f32x16 sc[2], dp[2];
+    bf16x8 p0[2], d0[2], p1, d1;
+    auto row_values = [&](const uint16_t* at, int first, f32x4& lo, f32x4& hi) {
+      const float* L = reinterpret_cast<const float*>(at + 2 * kRingBlock) + first + 4 * hf;
+      lo = *reinterpret_cast<const f32x4*>(L);
+      hi = *reinterpret_cast<const f32x4*>(L + 8);
+    };
+    // P and dS of entries 8 c2 .. 8 c2 + 7 as 10 steps per pair of entries (an exponential counts
+    // two), dealt out evenly to n packets; packet i's share.
+    float t0, t1, y0, y1;
+    auto vec_share = [&](auto parc, auto c2c, auto ic, auto nc, const f32x4(&l4)[2]) {
+      constexpr int par = decltype(parc)::value, c2 = decltype(c2c)::value, i = decltype(ic)::value,
+                    n = decltype(nc)::value;
+      if constexpr (i >= 0) {
+#pragma unroll
+        for (int m = i * 40 / n; m < (i + 1) * 40 / n; ++m) {
+          const int op = m % 10, e = 8 * c2 + 2 * (m / 10), w = (e % 8) / 2;
+          if (op == 0) t0 = __builtin_fmaf(sc[par][e], a.c, -l4[(e % 8) / 4][e % 4]);
+          if (op == 1) t1 = __builtin_fmaf(sc[par][e + 1], a.c, -l4[(e % 8) / 4][e % 4 + 1]);
+          if (op == 2) t0 = __builtin_amdgcn_fmed3f(fast_exp2(t0), 0.f, 1.f);
+          if (op == 4) t1 = __builtin_amdgcn_fmed3f(fast_exp2(t1), 0.f, 1.f);
+          if (op == 6) y0 = t0 * dp[par][e];
+          if (op == 7) y1 = t1 * dp[par][e + 1];
+          if (op >= 8) {
+            const f32x2 v = op == 8 ? f32x2{t0, t1} : f32x2{y0, y1};
+            bf16x8& dst = op == 8 ? (c2 ? p1 : p0[par]) : (c2 ? d1 : d0[par]);
+            u32x4 x = __builtin_bit_cast(u32x4, dst);
+            x[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+            dst = __builtin_bit_cast(bf16x8, x);
+          }
+        }
+      }
+    };
+    constexpr int kNA = 2 * kC, kNU = 4 * kMb;  // MFMAs of the two phases
+    auto frag_a = [&](const uint16_t* at, auto ic) -> bf16x8 {
+      constexpr int i = decltype(ic)::value;
+      return as_bf16x8(load16(at + (i < kC ? ra.get(i) : kRingBlock + ra.get(i - kC))));
+    };
+    auto frag_u = [&](const uint16_t* at, auto ic) -> bf16x8 {
+      constexpr int i = decltype(ic)::value, c2 = i / (2 * kMb), q = i % (2 * kMb);
+      return cols_frag<D>(at + (q % 2 ? 0 : kRingBlock), ca, q / 2, c2);
+    };
+    bf16x8 pf[kAhead];  // the first fragments of the next phase
+    uint32_t at_c = 0, at_p = (kRing - 1) * kRingSlot;  // ring offsets (elements) of blocks h and h - 1
+    auto body = [&](auto parc) {
+      constexpr int par = decltype(parc)::value;
+      const uint32_t at_n = at_c == (kRing - 1) * kRingSlot ? 0 : at_c + kRingSlot;
+      const uint16_t *tc = ring + at_c, *tp = ring + at_p, *tn = ring + at_n;
+      f32x4 l4[2];
+      bf16x8 fr[kAhead + 1];
+      using ParC = std::integral_constant<int, par>;
+      using ParP = std::integral_constant<int, par ^ 1>;
+      row_values(tp, 16, l4[0], l4[1]);
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) fr[x] = pf[x];
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kNA>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i + kAhead < kNA) fr[(i + kAhead) % (kAhead + 1)] = frag_a(tc, std::integral_constant<int, i + kAhead>{});
+        else pf[i + kAhead - kNA] = frag_u(tp, std::integral_constant<int, i + kAhead - kNA>{});
+        if constexpr (i == kC - 2) {  // dP starts at the rows' -delta
+          f32x4 d4[4];
+          row_values(tc, 64, d4[0], d4[1]);
+          row_values(tc, 80, d4[2], d4[3]);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dp[par][e] = d4[e / 4][e % 4];
+        }
+        const bf16x8& f = fr[i % (kAhead + 1)];
+        if constexpr (i < kC) sc[par] = mfma32(f, kf[i], i == 0 ? f32x16{} : sc[par]);
+        else dp[par] = mfma32(f, vf[i - kC], dp[par]);
+        vec_share(ParP{}, std::integral_constant<int, 1>{}, std::integral_constant<int, i - 1>{},
+                  std::integral_constant<int, kNA - 1>{}, l4);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      // Keeps the compiler from sinking the packets' vector work past the branch in load_advance.
+      asm volatile("" : "+v"(p1), "+v"(d1));
+      load_advance();
+      if constexpr (par == 0) {
+        // Blocks h + 1 and h + 2 have landed (those of h + 3 and h + 4 may be in flight), for every
+        // wave once all are here; every wave is also done with block h - 2, so the slots of blocks
+        // h - 3 and h - 2 can take blocks h + 5 and h + 6.
+        wait_loads<2 * (kLd + 1)>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      row_values(tc, 0, l4[0], l4[1]);
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) fr[x] = pf[x];
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kNU>([&](auto ic) {
+        constexpr int i = decltype(ic)::value, c2 = i / (2 * kMb), q = i % (2 * kMb), mb = q / 2;
+        if constexpr (i + kAhead < kNU) fr[(i + kAhead) % (kAhead + 1)] = frag_u(tp, std::integral_constant<int, i + kAhead>{});
+        else pf[i + kAhead - kNU] = frag_a(tn, std::integral_constant<int, i + kAhead - kNU>{});
+        if constexpr (i >= 1 && i <= kLd) load_part(i - 1);
+        if constexpr (i == kLd + 1) load_rows();
+        const bf16x8& f = fr[i % (kAhead + 1)];
+        if constexpr (q % 2) mfma_acc(f, c2 ? d1 : d0[par ^ 1], dk[mb]);
+        else mfma_acc(f, c2 ? p1 : p0[par ^ 1], dv[mb]);
+        vec_share(ParC{}, std::integral_constant<int, 0>{}, std::integral_constant<int, i - 2>{},
+                  std::integral_constant<int, kNU - 2>{}, l4);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      asm volatile("" : "+v"(p0[par]), "+v"(d0[par]));
+      at_p = at_c;
+      at_c = at_n;
+    };
+    // Before block 0 there is nothing to update: P, dS (exp2(-inf)) and rows are zero. Blocks nb and
+    // nb + 1 are zeros, so the bodies past the last block add exactly nothing.
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      sc[1][e] = -INFINITY;
+      dp[1][e] = 0.f;
+    }
+    p0[1] = d0[1] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
+    static_for<kAhead>([&](auto jc) { pf[decltype(jc)::value] = frag_a(ring, jc); });
+    for (int h = 0; h <= nb; h += 2) {
+      body(std::integral_constant<int, 0>{});
+      body(std::integral_constant<int, 1>{});
+    }
+    wait_tile_loads();
+  }
+  // The last MFMAs are done before the accumulators are read (16 passes at most).
+#pragma unroll
+  for (int mb = 0; mb < kMb; ++mb) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(dk[mb]), "+a"(dv[mb]));
+  const int lane = fresh_lane();
+  store_key<D>(a, kp, wave * 32 + (lane & 31), lane >> 5, dk, dv);
 }
 
 // Both passes in one launch (two workgroups a compute unit): the key side's items first, they are
@@ -603,14 +993,12 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_grad_kernel(const BlockBwd
   else dq_unit<D>(a, blockIdx.x - key_wgs, s0, s1, bits);
 }
 
-// d = 128: the key side's accumulators and operands take 256 registers by themselves, so it runs one
-// workgroup a compute unit, and each pass has a launch of its own.
-template <int D, bool CAUSAL>
+// d = 128: each pass has a launch of its own, the key side one workgroup a compute unit.
+template <bool CAUSAL>
 __global__ __launch_bounds__(kThreadsB, 1) void block_dkdv_kernel(const BlockBwdArgs a) {
-  __shared__ uint16_t s0[2][BlockShape<D>::kTileElems], s1[2][BlockShape<D>::kTileElems];
-  __shared__ float sL[2][kBlockK], sD[2][kBlockK];
+  __shared__ __attribute__((aligned(1024))) uint16_t ring[kRing * kRingSlot];
   __shared__ uint32_t bits[kBlockWords];
-  dkdv_unit<D, CAUSAL>(a, blockIdx.x, s0, s1, sL, sD, bits);
+  dkdv_roll_unit<CAUSAL>(a, blockIdx.x, ring, bits);
 }
 template <int D>
 __global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdArgs a) {
@@ -619,9 +1007,9 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdAr
   dq_unit<D>(a, blockIdx.x, s0, s1, bits);
 }
 
-// Adds the pieces of a dq unit, in order; a thread takes 4 consecutive d of a row.
+// Adds the pieces of 32 rows of a dq unit, in order; a thread takes 4 consecutive d of a row.
 template <int D>
-__device__ __forceinline__ void sum_dq(const BlockBwdArgs& a, uint32_t lu) {
+__device__ __forceinline__ void sum_dq(const BlockBwdArgs& a, uint32_t lu, int r0) {
   const BlockGeo& g = a.g;
   const uint32_t list = lu / a.units;
   const int unit = (int)(lu % a.units), i = (int)(list % g.nq);
@@ -629,8 +1017,8 @@ __device__ __forceinline__ void sum_dq(const BlockBwdArgs& a, uint32_t lu) {
   const ListRows rows(g, b, h, i);
   const int n_rows = g.G * rows.tokens;
   const float* part = a.part_q + (size_t)lu * a.pieces_q * kUnitRows * D;
-  for (int x = threadIdx.x; x < kUnitRows * (D / 4); x += kThreadsB) {
-    const int rr = x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
+  for (int x = threadIdx.x; x < 32 * (D / 4); x += kThreadsB) {
+    const int rr = r0 + x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
     if (r >= n_rows) return;
     int pos;
     const size_t row = rows.global(r, pos);
@@ -641,9 +1029,9 @@ __device__ __forceinline__ void sum_dq(const BlockBwdArgs& a, uint32_t lu) {
   }
 }
 
-// Adds the pieces of a cut key block, in order: dk, or dv.
+// Adds the pieces of 32 rows of a cut key block, in order: dk, or dv.
 template <int D>
-__device__ __forceinline__ void sum_dkdv(const BlockBwdArgs& a, uint32_t col, int which) {
+__device__ __forceinline__ void sum_dkdv(const BlockBwdArgs& a, uint32_t col, int which, int r0) {
   const BlockGeo& g = a.g;
   const int pieces = a.plan[4 * (size_t)col + 1];
   if (pieces == 1) return;
@@ -651,11 +1039,12 @@ __device__ __forceinline__ void sum_dkdv(const BlockBwdArgs& a, uint32_t col, in
   if (slot + pieces > a.slots) return;
   const int j = (int)(col % g.nb);
   const size_t row0 = (size_t)(col / g.nb) * g.Skv + (size_t)j * kBlock;
-  const int n_rows = min(kBlock, g.Skv - j * kBlock);
+  const int end = min(r0 + 32, min(kBlock, g.Skv - j * kBlock));
   const float* part = a.part_k + ((size_t)slot * 2 + which) * kBlock * D;
   uint16_t* out = which ? a.dv : a.dk;
-  for (int x = threadIdx.x; x < n_rows * (D / 4); x += kThreadsB) {
+  for (int x = r0 * (D / 4) + threadIdx.x; x < end * (D / 4); x += kThreadsB) {
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int p = 0; p < pieces; ++p) y += *reinterpret_cast<const f32x4*>(part + (size_t)p * 2 * kBlock * D + 4 * x);
     *reinterpret_cast<u32x2*>(out + row0 * D + 4 * x) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
   }
@@ -663,31 +1052,35 @@ __device__ __forceinline__ void sum_dkdv(const BlockBwdArgs& a, uint32_t col, in
 
 template <int D>
 __global__ __launch_bounds__(kThreadsB) void block_sum_kernel(const BlockBwdArgs a, uint32_t dq_wgs) {
-  if (blockIdx.x < dq_wgs) sum_dq<D>(a, blockIdx.x);
-  else sum_dkdv<D>(a, (blockIdx.x - dq_wgs) / 2, (blockIdx.x - dq_wgs) % 2);
+  if (blockIdx.x < dq_wgs) {
+    sum_dq<D>(a, blockIdx.x / 4, blockIdx.x % 4 * 32);
+  } else {
+    const uint32_t x = blockIdx.x - dq_wgs;
+    sum_dkdv<D>(a, x / 8, x % 2, (int)(x % 8 / 2) * 32);
+  }
 }
 
 template <int D>
 hipError_t block_bwd_for(const BlockBwdArgs& a, hipStream_t s) {
   const BlockGeo& g = a.g;
   const int64_t rows = (int64_t)g.B * g.H * g.Sq;
-  const uint32_t cols = (uint32_t)((int64_t)g.B * g.Hkv * g.nb), per = (cols + 7) / 8;
+  const uint32_t cols = (uint32_t)((int64_t)g.B * g.Hkv * g.nb);
   const uint32_t lists = (uint32_t)((int64_t)g.B * g.Hkv * g.nq);
   const uint32_t prep = (uint32_t)((rows + kPrepRowsB - 1) / kPrepRowsB);
   const uint32_t words = (uint32_t)((int64_t)g.B * g.Hkv * ((g.nq + 31) / 32));
   const size_t lds = std::max((size_t)kPrepRowsB * (D / 8), (size_t)g.nb) * 4;
   block_prep_kernel<D><<<prep + words, kThreadsB, lds, s>>>(a, rows, prep);
-  block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols, per);
-  const uint32_t keys = 8 * per * (uint32_t)a.pieces_k, queries = xcd_grid(lists * a.units * a.pieces_q);
+  block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
+  const uint32_t keys = 8 * (uint32_t)a.items_cap, queries = unit_grid(g, a.units * a.pieces_q);
   if constexpr (D == 128) {
-    if (g.causal) block_dkdv_kernel<D, true><<<keys, kThreadsB, 0, s>>>(a);
-    else block_dkdv_kernel<D, false><<<keys, kThreadsB, 0, s>>>(a);
+    if (g.causal) block_dkdv_kernel<true><<<keys, kThreadsB, 0, s>>>(a);
+    else block_dkdv_kernel<false><<<keys, kThreadsB, 0, s>>>(a);
     block_dq_kernel<D><<<queries, kThreadsB, 0, s>>>(a);
   } else {
     if (g.causal) block_grad_kernel<D, true><<<keys + queries, kThreadsB, 0, s>>>(a, keys);
     else block_grad_kernel<D, false><<<keys + queries, kThreadsB, 0, s>>>(a, keys);
   }
-  const uint32_t sum_q = a.pieces_q > 1 ? lists * a.units : 0, sum_k = a.pieces_k > 1 ? 2 * cols : 0;
+  const uint32_t sum_q = a.pieces_q > 1 ? 4 * lists * a.units : 0, sum_k = a.pieces_k > 1 ? 8 * cols : 0;
   if (sum_q + sum_k) block_sum_kernel<D><<<sum_q + sum_k, kThreadsB, 0, s>>>(a, sum_q);
   return hipGetLastError();
 }

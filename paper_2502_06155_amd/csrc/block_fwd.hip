@@ -14,8 +14,9 @@
 // entries vanish, the blocks come in ascending order whatever the list's order was, and the walk
 // over them costs a scalar bit scan per block.
 //
-// Units of one (batch, key head) run on one XCD next to each other: the lists of neighbouring query
-// blocks share blocks, and so do the heads of a group, which the XCD's L2 then holds. Where units
+// Units of one list, and of one (batch, key head) as far as the balance allows (UnitPlace), run on one
+// XCD next to each other: the lists of neighbouring query blocks share blocks, and so do the heads
+// of a group, which the XCD's L2 then holds. Where units
 // are few, each list is cut into pieces by its number of blocks and a second kernel joins the
 // pieces' results by their log-sum-exp.
 #include <hip/hip_runtime.h>
@@ -76,14 +77,10 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_fwd_kernel(const BlockFwdA
   __shared__ uint16_t sK[2][Sh::kTileElems], sV[2][Sh::kTileElems];
   __shared__ uint32_t bits[kBlockWords];
   const BlockGeo& g = a.g;
-  const uint32_t lists = (uint32_t)g.B * g.Hkv * g.nq;
-  const uint32_t work = xcd_unit(blockIdx.x, lists * a.units * a.pieces);
-  if (work >= lists * a.units * a.pieces) return;
-  const int piece = (int)(work % a.pieces);
-  const uint32_t lu = work / a.pieces, list = lu / a.units;
-  const int unit = (int)(lu % a.units);
-  const int i = (int)(list % g.nq);
-  const int bh = (int)(list / g.nq), b = bh / g.Hkv, h = bh - b * g.Hkv;
+  UnitPlace u;
+  if (!u.find(g, blockIdx.x, a.units, a.pieces)) return;
+  const uint32_t list = u.list, lu = list * a.units + u.unit;
+  const int piece = u.piece, unit = u.unit, i = u.i, b = u.b, h = u.h, bh = u.b * g.Hkv + u.h;
   const ListRows rows(g, b, h, i);
   const int n_rows = g.G * rows.tokens;
   if (unit * kUnitRows >= n_rows) return;
@@ -250,7 +247,7 @@ __global__ __launch_bounds__(kThreadsB) void block_merge_kernel(const BlockFwdAr
 template <int D>
 hipError_t block_fwd_for(const BlockFwdArgs& a, hipStream_t s) {
   const uint32_t units = (uint32_t)a.g.B * a.g.Hkv * a.g.nq * a.units;
-  block_fwd_kernel<D><<<xcd_grid(units * a.pieces), kThreadsB, 0, s>>>(a);
+  block_fwd_kernel<D><<<unit_grid(a.g, a.units * a.pieces), kThreadsB, 0, s>>>(a);
   if (a.pieces > 1) block_merge_kernel<D><<<units, kThreadsB, 0, s>>>(a);
   return hipGetLastError();
 }

@@ -102,7 +102,7 @@ size_t fwd_bytes(const BlockGeo& g) {
 // How the gradient's key side is cut, and where things lie in the workspace.
 struct BwdPlan {
   int entries, pieces_q, pieces_k;
-  int64_t slots;
+  int64_t slots, items_cap;
   size_t off_ndelta, off_cols, off_plan, off_counts, off_items, off_q, off_k, bytes;
 };
 BwdPlan plan_bwd(const BlockGeo& g) {
@@ -120,6 +120,13 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   p.pieces_k = (g.nq + p.entries - 1) / p.entries;
   // A column in ceil(n / entries) > 1 pieces has n > entries, so fewer than 2 n / entries pieces.
   p.slots = p.pieces_k == 1 ? 0 : std::min(cols * p.pieces_k, 2 * held / p.entries);
+  // An XCD's share: with T query blocks in all columns (T <= held) and s = max(1, ceil(T / 4 cols)) the
+  // plan counts W = T + s cols of work, and the columns of a share but its last one less than W / 8.
+  // So a share has at most W / 8 s <= 5 / 8 cols columns, rounded up, which hold at most
+  // W / 8 <= 5 / 32 T + cols / 8 query blocks and those of the last one, nq at most; and a column of n
+  // is cut into at most 1 + (n - 1) / entries pieces.
+  const int64_t share_blocks = (5 * held + 31) / 32 + (cols + 7) / 8 + g.nq;
+  p.items_cap = std::min(cols * p.pieces_k, (5 * cols + 7) / 8 + share_blocks / p.entries);
   const size_t rows = (size_t)g.B * g.H * g.Sq;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t at = up(rows * 4);
@@ -132,7 +139,7 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   p.off_counts = at;
   at += up(9 * 4);
   p.off_items = at;
-  at += up((size_t)((cols + 7) / 8 * 8) * p.pieces_k * 8);
+  at += up((size_t)p.items_cap * 8 * 8);
   p.off_q = at;
   at += p.pieces_q == 1 ? 0 : up((size_t)(lists_of(g) * units_of(g)) * p.pieces_q * kBlock * g.d * 4);
   p.off_k = at;
@@ -328,9 +335,11 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
   a.plan = reinterpret_cast<int32_t*>(ws + p.off_plan);
   a.counts = reinterpret_cast<int32_t*>(ws + p.off_counts);
   a.items = reinterpret_cast<int32_t*>(ws + p.off_items);
+  a.items_cap = (int)p.items_cap;
   a.part_q = reinterpret_cast<float*>(ws + p.off_q);
   a.part_k = reinterpret_cast<float*>(ws + p.off_k);
-  if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces_q + (double)cols * a.pieces_k + 2.0 * cols)) return st;
+  if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces_q + 8.0 * a.items_cap)) return st;
+  if (int st = check_grid(4.0 * lists_of(a.g) * a.units + 8.0 * cols)) return st;
   if (int st = check_grid((double)rows / 64 + (double)lists_of(a.g))) return st;
   return launched(launch_block_bwd(a, static_cast<hipStream_t>(stream)));
 }

@@ -71,7 +71,8 @@ struct BlockBwdArgs {
   uint32_t* cols;    // [B, Hkv, nb][nq / 32 words]: the query blocks that list a key block
   int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot
   int32_t* counts;   // [9]: items of each XCD's share; the slot counter
-  int32_t* items;    // [8][columns of a share * pieces_k][2]: column, piece
+  int32_t* items;    // [8][items_cap][2]: column, piece
+  int items_cap;     // items of an XCD's share, at most
   float* part_q;     // pieces_q > 1: fp32 [list][unit][piece][128][d]
   float* part_k;     // fp32 [slot][2][128][d]: dk, dv
 };

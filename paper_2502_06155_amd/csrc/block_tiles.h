@@ -147,8 +147,9 @@ __device__ __forceinline__ void store_f32(float* row, const f32x16 (&acc)[D / 32
     }
 }
 
+// Tokens of sequence b (b is the same in every lane).
 __device__ __forceinline__ int seq_len(const BlockGeo& g, int b) {
-  return g.lens ? min(max(g.lens[b], 0), g.Skv) : g.Skv;
+  return g.lens ? __builtin_amdgcn_readfirstlane(min(max(g.lens[b], 0), g.Skv)) : g.Skv;
 }
 
 // The rows of one list: the `tokens` query tokens of block i of every head of the group, head after
@@ -176,12 +177,41 @@ struct ListRows {
   __device__ __forceinline__ int last() const { return min(first + tokens, len) - 1; }
 };
 
-// Contiguous shares of the units for the 8 XCDs: workgroup id runs unit (id % 8) * per + id / 8.
-__device__ __forceinline__ uint32_t xcd_unit(uint32_t id, uint32_t total) {
-  const uint32_t per = (total + 7) / 8;
-  return id / 8 < per ? (id % 8) * per + id / 8 : total;
+// The unit that a workgroup runs: piece `piece` of the 128 rows `unit` of a list. Workgroup id goes to
+// XCD id % 8. Where all lists are alike (no causal order, no lengths) each XCD runs a contiguous
+// share of the lists, so that the heads it reads stay in its L2. Else lists differ in length, and
+// they are dealt out one by one, late query blocks (causal: the long lists) first; with a multiple
+// of 8 key heads over the batch each XCD still sees its own heads only. A list's units stay together.
+struct UnitPlace {
+  uint32_t list;
+  int unit, piece, i, b, h;
+  __device__ __forceinline__ bool find(const BlockGeo& g, uint32_t id, int units, int pieces) {
+    const uint32_t heads = (uint32_t)g.B * g.Hkv, lists = heads * g.nq, per = (lists + 7) / 8;
+    const uint32_t at = id / 8, of = (uint32_t)(units * pieces), l = at / of, rem = at - l * of;
+    unit = (int)(rem / pieces);
+    piece = (int)(rem - (uint32_t)unit * pieces);
+    uint32_t bh;
+    if (!g.causal && !g.lens) {
+      list = (id % 8) * per + l;
+      if (l >= per || list >= lists) return false;
+      bh = list / g.nq;
+      i = (int)(list - bh * g.nq);
+    } else {
+      const uint32_t x = l * 8 + id % 8;
+      if (x >= lists) return false;
+      const uint32_t late = x / heads;
+      bh = x - late * heads;
+      i = g.nq - 1 - (int)late;
+      list = bh * g.nq + i;
+    }
+    b = (int)(bh / g.Hkv);
+    h = (int)(bh - (uint32_t)b * g.Hkv);
+    return true;
+  }
+};
+inline uint32_t unit_grid(const BlockGeo& g, int of) {
+  return ((uint32_t)((int64_t)g.B * g.Hkv * g.nq) + 7) / 8 * 8 * (uint32_t)of;
 }
-inline uint32_t xcd_grid(uint32_t total) { return (total + 7) / 8 * 8; }
 
 // A list as a bitmap in LDS (all threads; ends with a barrier): entries that name no block, blocks
 // past the sequence's end and (causal) past the last row's position are left out, a block listed
