@@ -176,8 +176,9 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   const int64_t rows = (int64_t)(H / Hkv) * N;
   p.rows = cache_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
   p.passes = (int)((rows + p.rows - 1) / p.rows);
-  p.workers = (int)std::min<int64_t>(kSlots, (int64_t)B * Hkv * max_pages);
-  p.bytes = (size_t)p.passes * 2 * p.workers * p.rows * (d + 2) * sizeof(float);
+  // Two workgroups run on a compute unit in passes of 16 rows, one in passes of 32.
+  p.workers = (int)std::min<int64_t>(p.rows == 16 ? kSlots : kSlots / 2, (int64_t)B * Hkv * (max_pages + kCacheSegment));
+  p.bytes = (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
 int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
@@ -186,7 +187,9 @@ int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   if (H % Hkv) return fail(TA_ERR_BAD_SHAPE, "H must be a multiple of Hkv");
   if (max_pages > INT_MAX / TA_BLOCK) return fail(TA_ERR_BAD_SHAPE, "max_pages pages hold more than 2^31 - 1 tokens");
   // The passes over the rows and the sequences times heads are grid dimensions of their own.
-  if ((int64_t)B * Hkv > 65535 || (int64_t)(H / Hkv) * N > 16 * 65535)
+  if ((int64_t)B * Hkv * (max_pages + kCacheSegment) > INT_MAX)
+    return fail(TA_ERR_BAD_SHAPE, "B * Hkv * max_pages exceeds 2^31 - 1");
+  if ((int64_t)B * Hkv > 65535 || (int64_t)(H / Hkv) * N > 8 * 65535)
     return fail(TA_ERR_BAD_SHAPE, "B * Hkv or H / Hkv * N exceeds the grid limit");
   return check_dim(d);
 }

@@ -16,6 +16,8 @@ struct BlockGeo {
   const int32_t* lens;  // [B] or null
 };
 
+constexpr int kCacheSegment = 3;  // what a (sequence, head) costs cache attention beside its pages
+
 struct MeansArgs {
   const uint16_t* x;
   uint16_t* means;
@@ -105,7 +107,7 @@ struct CacheAttnArgs {
   float c;     // scale * log2(e)
   int workers;       // workgroups that share the pages of all sequences
   int row_blocks;    // 32-row (or 16-row) passes over the G * N rows
-  float* part;       // fp32 [row block][2 * workers][rows][d + 2]
+  float* part;       // fp32 [row block][2 * workers][rows][d + 4]: O/l, base-2 lse
 };
 
 hipError_t launch_block_means(const MeansArgs& a, hipStream_t stream);

@@ -143,13 +143,13 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 // attention
 //
 // The cache's bytes bound this: a decoding step reads every code once and does 4 G N operations a
-// byte. Tiles of 64 tokens go from memory into registers, one tile ahead, as the operands of
-// v_mfma_f32_16x16x32_bf16 (A: lane l holds row l % 16 and the k indices 8 (l / 16) .. + 7; B the
+// byte. A wave takes a page at a time, its codes from memory straight into registers, one page ahead,
+// as the operands of v_mfma_f32_16x16x32_bf16 (A: lane l holds row l % 16 and the k indices 8 (l / 16) .. + 7; B the
 // same with columns; C: column l % 16, rows 4 (l / 16) + j):
 //   S^T = K Q^T. The matrix instruction adds over k in any order, so a lane's 16 bytes of a K row,
 //   dims 64 c + 16 g .. + 15 (g = l / 16), serve two instructions, and q is laid out alike. Which
-//   token a row of A holds is free too: row r of instruction group i (of 4) is token
-//   16 (r / 4) + 4 i + r % 4, which puts tokens 16 g .. 16 g + 15 of the tile's scores into lane
+//   token a row of A holds is free too: in each half of 64 tokens row r of instruction group i (of
+//   4) is token 16 (r / 4) + 4 i + r % 4, which puts the scores of tokens 16 g .. 16 g + 15 into lane
 //   group g, in order: exactly the P^T operand of
 //   O^T += V^T P^T, whose V operand is 16 bytes of a V row (tokens 16 g .. + 15).
 // e4m3 codes become bf16 exactly (v_cvt_scalef32_pk_bf16_fp8); the page's K scale multiplies the
@@ -162,55 +162,72 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 // kernel joins them in the order of the pages.
 
 
-// The line of all segments' pages. Segment order: entry i of lens, then (where all heads share an
-// entry) the key heads. Every wave finds its place by itself, 64 entries at a time.
-struct Place {
-  int64_t total;  // pages of the line
-  int64_t start;  // of entry `entry`, pages of the line before it
-  int entry;      // the entry that holds the asked page (or the asked entry)
-};
+// A quotient of numbers that are the same in every lane, in a scalar register (the division itself runs
+// on the vector ALU; left there, it would make every address and branch behind it a lane's own).
+__device__ __forceinline__ int scalar_div(int x, int y) {
+  return __builtin_amdgcn_readfirstlane((int)((uint32_t)x / (uint32_t)y));
+}
+
+// The line of all segments, each kSegment + its pages long (below 2^31, checked by the host): what a
+// segment's start and end cost a workgroup is about kSegment pages' time (32 sequences of 4 to 512
+// pages: 208 us with 0, 188 with 3). Segment order: entry i of lens, then (where all heads share an
+// entry) the key heads. Worker w takes line / workers, the first line % workers ones one more. Every
+// wave finds its place by itself, 64 entries at a time.
+constexpr int kSegment = kCacheSegment;
+using ScalarInts = const __attribute__((address_space(4))) int32_t*;    // read with scalar loads
+using ScalarFloats = const __attribute__((address_space(4))) float*;
+
 __device__ __forceinline__ int cache_len(const CacheAttnArgs& a, int i) {
   return (int)min((int64_t)max(a.lens[i], 0), (int64_t)a.max_pages * kBlock);
 }
-__device__ __forceinline__ int pages_of(int len) { return (len + kBlock - 1) / kBlock; }
+__device__ __forceinline__ int pages_of(int len) { return (int)(((uint32_t)len + kBlock - 1) / kBlock); }
+// A segment's length on the line; one without pages has none.
+__device__ __forceinline__ int extent_of(int pages) { return pages > 0 ? kSegment + pages : 0; }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+struct Line {
+  int entries, per;  // entries of lens, segments of an entry
+  int total;         // its length
+  int each, more;    // every worker's part, workers with one more
+  __device__ __forceinline__ Line(const CacheAttnArgs& a) {
+    entries = a.per_head ? a.B * a.Hkv : a.B;
+    per = a.per_head ? 1 : a.Hkv;
+    int n = 0;
+    for (int i = threadIdx.x & 63; i < entries; i += 64) n += extent_of(pages_of(cache_len(a, i)));
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) x += __shfl_xor((long long)x, s);
-  return x;
-}
-__device__ __forceinline__ int64_t line_total(const CacheAttnArgs& a, int entries, int per) {
-  const int lane = threadIdx.x & 63;
-  int64_t n = 0;
-  for (int i = lane; i < entries; i += 64) n += pages_of(cache_len(a, i));
-  return wave_sum(n) * per;
-}
-// The entry that holds page `at` of the line (at < total), and the line's pages before it.
-__device__ __forceinline__ Place find_page(const CacheAttnArgs& a, int entries, int per, int64_t total, int64_t at) {
-  const int lane = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int i0 = 0; i0 < entries; i0 += 64) {
-    const int64_t own = i0 + lane < entries ? (int64_t)pages_of(cache_len(a, i0 + lane)) * per : 0;
-    int64_t upto = own;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int64_t y = __shfl_up((long long)upto, s);
-      if (lane >= s) upto += y;
-    }
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
-    if (past) {
-      const int src = __ffsll((unsigned long long)past) - 1;
-      return Place{total, before + __shfl((long long)(upto - own), src), i0 + src};
-    }
-    before += __shfl((long long)upto, 63);
+    for (int s = 1; s < 64; s <<= 1) n += __shfl_xor(n, s);
+    total = __builtin_amdgcn_readfirstlane(n) * per;
+    each = scalar_div(total, a.workers);
+    more = total - each * a.workers;
   }
-  return Place{total, total, entries};
-}
-// The first page of the line that worker w of W takes, and the worker that takes page x.
-__device__ __forceinline__ int64_t worker_start(int64_t total, int w, int W) { return total * w / W; }
-__device__ __forceinline__ int worker_of(int64_t total, int64_t x, int W) {
-  return (int)(((x + 1) * W + total - 1) / total) - 1;
-}
+  __device__ __forceinline__ int start(int w) const { return w * each + min(w, more); }
+  // The worker that takes place x of the line, x < total.
+  __device__ __forceinline__ int worker(int x) const {
+    const int y = x - more * (each + 1);
+    return y < 0 ? scalar_div(x, each + 1) : more + scalar_div(y, each);
+  }
+  // The entry that holds place `at` (at < total), and where it starts.
+  __device__ __forceinline__ int entry_of(const CacheAttnArgs& a, int at, int& before) const {
+    const int lane = threadIdx.x & 63;
+    before = 0;
+    for (int i0 = 0; i0 < entries; i0 += 64) {
+      const int own = i0 + lane < entries ? extent_of(pages_of(cache_len(a, i0 + lane))) * per : 0;
+      int upto = own;
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) {
+        const int y = __shfl_up(upto, s);
+        if (lane >= s) upto += y;
+      }
+      const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
+      if (past) {
+        const int src = __ffsll((unsigned long long)past) - 1;
+        before = __builtin_amdgcn_readfirstlane(before + __shfl(upto - own, src));
+        return __builtin_amdgcn_readfirstlane(i0 + src);
+      }
+      before = __builtin_amdgcn_readfirstlane(before + __shfl(upto, 63));
+    }
+    return entries;
+  }
+};
 
 // max and sum over the four lane groups that hold one query row's tokens.
 __device__ __forceinline__ float group_max(float x) {
@@ -234,42 +251,45 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-constexpr int kTile = 64;      // tokens of a wave's tile: half a page
 constexpr float kNoRef = -1e30f;  // a running maximum before the first token (base-2 logits)
 
-// One tile's codes and scales in a lane's registers; page < 0: no tile.
+// A page's codes in a lane's registers, by halves of 64 tokens. Base addresses are the same in every
+// lane (scalar registers), lanes add a 32-bit offset that no page changes. Both halves of a V row (a
+// 128-byte line) are read one after the other: with 64 tokens a wave the second half came from memory
+// again a third of the time (1.04 GB fetched for 0.88).
 template <int D>
-struct CacheTile {
-  uint32_t k[4][D / 16];
-  u32x4 v[D / 16];
-  float ks, vs;
-  int page;
-  __device__ __forceinline__ void load(const CacheAttnArgs& a, int p, int h, int half, int lane) {
-    page = p;
-    if (p < 0) return;
-    const size_t ph = (size_t)p * a.Hkv + h;
-    ks = a.k_scales[ph];
-    vs = a.v_scales[ph];
+struct KeyPage {
+  uint32_t k[8][D / 16];
+  __device__ __forceinline__ void load(const uint8_t* page, int lane) {
     const int n = lane & 15, g = lane >> 4;
-    const uint8_t* kb = a.k_pages + (ph * kBlock + half * kTile) * D + (16 * (n >> 2) + (n & 3)) * D;
+    const uint32_t at = (uint32_t)((16 * (n >> 2) + (n & 3)) * D);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint8_t* row = kb + 4 * i * D;
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t row = at + (uint32_t)((64 * (i / 4) + 4 * (i % 4)) * D);
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(row + 64 * c + 16 * g);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(page + (row + (uint32_t)(64 * c + 16 * g)));
 #pragma unroll
         for (int e = 0; e < 4; ++e) k[i][4 * c + e] = w[e];
       }
       if constexpr (D % 64 != 0) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + D / 64 * 64 + 8 * g);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(page + (row + (uint32_t)(D / 64 * 64 + 8 * g)));
         k[i][D / 16 - 2] = w[0];
         k[i][D / 16 - 1] = w[1];
       }
     }
-    const uint8_t* vb = a.v_pages + ph * kBlock * D + n * kBlock + half * kTile + 16 * g;
+  }
+};
+template <int D>
+struct ValuePage {
+  u32x4 v[D / 16][2];
+  __device__ __forceinline__ void load(const uint8_t* page, int lane) {
+    const uint32_t at = (uint32_t)((lane & 15) * kBlock + 16 * (lane >> 4));
 #pragma unroll
-    for (int mb = 0; mb < D / 16; ++mb) v[mb] = *reinterpret_cast<const u32x4*>(vb + 16 * mb * kBlock);
+    for (int mb = 0; mb < D / 16; ++mb)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        v[mb][half] = *reinterpret_cast<const u32x4*>(page + (at + (uint32_t)(16 * mb * kBlock + 64 * half)));
   }
 };
 
@@ -279,33 +299,69 @@ __device__ __forceinline__ int slice_dim(int m, int g) {
   return m < D / 64 * 2 ? 64 * (m / 2) + 16 * g + 8 * (m % 2) : D / 64 * 64 + 8 * g;
 }
 
+// Workgroups a compute unit: at 16 rows a wave holds 32 KB of codes in flight or in work, their
+// results and the queries in 256 registers, at 32 rows in 512.
+template <int RB>
+constexpr int cache_wgs() { return RB == 1 ? 2 : 1; }
+
 template <int D, int RB>
-__global__ __launch_bounds__(kThreadsC, 2) void cache_attn_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(const CacheAttnArgs a) {
   constexpr int kRows = 16 * RB, kWaves = kThreadsC / 64, kMb = D / 16, kSl = D / 32;
   __shared__ float s_o[kWaves][kRows][D + 4];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 15, g = lane >> 4;
-  const int entries = a.per_head ? a.B * a.Hkv : a.B, per = a.per_head ? 1 : a.Hkv;
   const int w = blockIdx.x, row0 = blockIdx.y * kRows, rows = a.G * a.N;
 
-  const int64_t total = line_total(a, entries, per);
-  const int64_t lo = worker_start(total, w, a.workers), hi = worker_start(total, w + 1, a.workers);
+  const Line line(a);
+  const int lo = line.start(w), hi = line.start(w + 1);
   if (lo >= hi) return;
-  const Place pl = find_page(a, entries, per, total, lo);
-  int entry = __builtin_amdgcn_readfirstlane(pl.entry);
+  int seg0;  // the line's place where the segment starts
+  int entry = line.entry_of(a, lo, seg0);
   int len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
   int pages = pages_of(len);
-  int head = (int)((lo - pl.start) / pages);
-  int64_t seg0 = pl.start + (int64_t)head * pages;  // the line's page where the segment starts
+  int head = scalar_div(lo - seg0, extent_of(pages));
+  seg0 += head * extent_of(pages);
 
-  int64_t at = lo;
-  while (at < hi) {
-    const int h = a.per_head ? entry % a.Hkv : head, b = a.per_head ? entry / a.Hkv : entry;
-    const int p0 = (int)(at - seg0), p1 = (int)min((int64_t)pages, hi - seg0);
-    const int32_t* table = a.table + (size_t)entry * a.max_pages;
+  int at = lo;
+  auto advance = [&]() {  // to the next segment with pages; false past the worker's part
+    at = seg0 + kSegment + pages;
+    if (at >= hi) return false;
+    seg0 = at;
+    if (++head == line.per) {
+      head = 0;
+      pages = 0;
+      while (pages == 0 && ++entry < line.entries) {
+        len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
+        pages = pages_of(len);
+      }
+    }
+    return true;
+  };
+  do {
+    const int b = a.per_head ? scalar_div(entry, a.Hkv) : entry, h = a.per_head ? entry - b * a.Hkv : head;
+    const int p0 = max(0, at - seg0 - kSegment), p1 = min(pages, hi - seg0 - kSegment);
+    const ScalarInts table = (ScalarInts)(a.table + (size_t)entry * a.max_pages);
+    const ScalarFloats k_scales = (ScalarFloats)a.k_scales, v_scales = (ScalarFloats)a.v_scales;
     const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N;  // rows of the group lie together
+
+    if (p1 <= p0) continue;
+    // Pages p0 + wave, + 4, ... up to p1. A page that is none is passed over: its tokens are not read.
+    auto page_of = [&](int p) {
+      if (p >= p1) return -1;
+      const int x = table[p];
+      return x < a.n_pages ? x : -1;
+    };
+    auto base_of = [&](const uint8_t* pages_at, int page) { return pages_at + ((size_t)page * a.Hkv + h) * kBlock * D; };
+    int p = p0 + wave;
+    int page = page_of(p);
+    KeyPage<D> kt;
+    ValuePage<D> vt;
+    if (page >= 0) {
+      kt.load(base_of(a.k_pages, page), lane);
+      vt.load(base_of(a.v_pages, page), lane);
+    }
 
     bf16x8 qf[RB][kSl];
     int end[RB];  // tokens this lane's row attends to
@@ -330,92 +386,100 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache_attn_kernel(const CacheAtt
       for (int mb = 0; mb < kMb; ++mb) o[rb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Tiles wave, wave + 4, ... of pages [p0, p1), those that hold a token.
-    const int t_end = min(2 * p1, (len + kTile - 1) / kTile);
-    auto page_of = [&](int t) {
-      if (t >= t_end) return -1;
-      const int p = table[t >> 1];
-      return p < a.n_pages ? p : -1;  // no page: its tokens are not read
-    };
-    auto step = [&](CacheTile<D>& cur, int t) {
-      if (cur.page < 0) return;
-      const int tok0 = t * kTile;
-      if (tok0 + kTile > len) {  // codes behind the last token may be NaN: clear them in V
+    // The next page's K loads go out as soon as this one's K is used, its V loads when V is: both
+    // have a page's time to arrive, in one set of registers.
+    for (; p < p1; p += kWaves) {
+      const int next = page_of(p + kWaves);
+      const int tok0 = p * kBlock;
+      f32x4 s[RB][8];
+      float ks = 0.f, vs = 0.f;
+      if (page >= 0) {
+        ks = k_scales[(size_t)page * a.Hkv + h];
+        vs = v_scales[(size_t)page * a.Hkv + h];
+        // Fences keep the codes of later slices from being widened early (twice the registers).
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int left = len - (tok0 + 16 * g + 4 * e);
-          const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+        for (int m = 0; m < kSl; ++m)
 #pragma unroll
-          for (int mb = 0; mb < kMb; ++mb) cur.v[mb][e] &= keep;
-        }
-      }
-      f32x4 s[RB][4];
+          for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+            for (int i = 4 * half; i < 4 * half + 4; ++i) {
+              const bf16x8 kf = widen8(kt.k[i][2 * m], kt.k[i][2 * m + 1]);
 #pragma unroll
-        for (int m = 0; m < kSl; ++m) {
-          const bf16x8 kf = widen8(cur.k[i][2 * m], cur.k[i][2 * m + 1]);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-            s[rb][i] = mfma16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i]);
-        }
-      const float c = a.c * cur.ks;
-      bf16x8 pf[RB][2];
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[rb][i] *= c;
-        if (tok0 + kTile > len - (a.N - 1)) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (tok0 + 16 * g + 4 * i + j >= end[rb]) s[rb][i][j] = -INFINITY;
-        }
-        float mx = s[rb][0][0];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
-        const float m_new = fmaxf(m_ref[rb], group_max(mx));
-        if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
-          const float alpha = fast_exp2(m_ref[rb] - m_new);
-          l_run[rb] *= alpha;
-#pragma unroll
-          for (int mb = 0; mb < kMb; ++mb) o[rb][mb] *= alpha;
-          m_ref[rb] = m_new;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p = fast_exp2(s[rb][i][j] - m_ref[rb]);
-            sum += p;
-            pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)(p * cur.vs);
+              for (int rb = 0; rb < RB; ++rb)
+                s[rb][i] = mfma16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
           }
-        l_run[rb] += sum;
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next >= 0) kt.load(base_of(a.k_pages, next), lane);
+      __builtin_amdgcn_sched_barrier(0);
+      if (page >= 0) {
+        const float c = a.c * ks;
+        bf16x8 pf[RB][4];
 #pragma unroll
-      for (int mb = 0; mb < kMb; ++mb)
+        for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) {
-          const bf16x8 vf = widen8(cur.v[mb][2 * c2], cur.v[mb][2 * c2 + 1]);
+          for (int i = 0; i < 8; ++i) s[rb][i] *= c;
+          if (tok0 + kBlock > len - (a.N - 1)) {
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) o[rb][mb] = mfma16(vf, pf[rb][c2], o[rb][mb]);
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (tok0 + 64 * (i / 4) + 16 * g + 4 * (i % 4) + j >= end[rb]) s[rb][i][j] = -INFINITY;
+          }
+          float mx = s[rb][0][0];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
+          const float m_new = fmaxf(m_ref[rb], group_max(mx));
+          if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
+            const float alpha = fast_exp2(m_ref[rb] - m_new);
+            l_run[rb] *= alpha;
+#pragma unroll
+            for (int mb = 0; mb < kMb; ++mb) o[rb][mb] *= alpha;
+            m_ref[rb] = m_new;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+              sum += x;
+              pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)(x * vs);
+            }
+          l_run[rb] += sum;
         }
-    };
-    int t = 2 * p0 + wave;
-    CacheTile<D> ta, tb;
-    ta.load(a, page_of(t), h, t & 1, lane);
-    int next = page_of(t + kWaves);
-    for (; t < t_end; t += 2 * kWaves) {
-      tb.load(a, next, h, (t + kWaves) & 1, lane);
-      next = page_of(t + 2 * kWaves);
-      step(ta, t);
-      ta.load(a, next, h, (t + 2 * kWaves) & 1, lane);
-      next = page_of(t + 3 * kWaves);
-      step(tb, t + kWaves);
+        if (tok0 + kBlock > len) {  // codes behind the last token may be NaN: clear them in V
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int left = len - (tok0 + 64 * half + 16 * g + 4 * e);
+              const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+              for (int mb = 0; mb < kMb; ++mb) vt.v[mb][half][e] &= keep;
+            }
+        }
+#pragma unroll
+        for (int mb = 0; mb < kMb; mb += 2) {
+#pragma unroll
+          for (int c2 = 0; c2 < 4; ++c2)
+#pragma unroll
+            for (int x = mb; x < mb + 2; ++x) {
+              const u32x4 w = vt.v[x][c2 / 2];
+              const bf16x8 vf = widen8(w[2 * (c2 % 2)], w[2 * (c2 % 2) + 1]);
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb) o[rb][x] = mfma16(vf, pf[rb][c2], o[rb][x]);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next >= 0) vt.load(base_of(a.v_pages, next), lane);
+      page = next;
     }
 
     // The waves' states join in LDS.
@@ -432,7 +496,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache_attn_kernel(const CacheAtt
     __syncthreads();
     const bool alone = p0 == 0 && p1 == pages;
     const int slot = 2 * w + (at == lo ? 0 : 1);
-    float* part = a.part + ((size_t)blockIdx.y * 2 * a.workers + slot) * kRows * (D + 2);
+    float* part = a.part + ((size_t)blockIdx.y * 2 * a.workers + slot) * kRows * (D + 4);
     for (int i = tid; i < kRows * (D / 4); i += kThreadsC) {
       const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
       if (row0 + r >= rows) continue;
@@ -454,87 +518,71 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache_attn_kernel(const CacheAtt
             __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
         if (a.lse && d0 == 0) a.lse[q_row + row0 + r] = lse2 * 0.69314718055994531f;
       } else {
-        float* pr = part + (size_t)r * (D + 2);
-        *reinterpret_cast<f32x2*>(pr + d0) = f32x2{y[0], y[1]};
-        *reinterpret_cast<f32x2*>(pr + d0 + 2) = f32x2{y[2], y[3]};
+        float* pr = part + (size_t)r * (D + 4);
+        *reinterpret_cast<f32x4*>(pr + d0) = y;
         if (d0 == 0) pr[D] = lse2;
       }
     }
     __syncthreads();
-
-    at = seg0 + p1;
-    if (p1 == pages) {  // the next segment with pages
-      seg0 += pages;
-      if (++head == per) {
-        head = 0;
-        pages = 0;
-        while (pages == 0 && ++entry < entries) {
-          len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
-          pages = pages_of(len);
-        }
-      }
-    }
-  }
+  } while (advance());
 }
 
 // Joins the partial results of a segment that several workers share, in the order of its pages;
-// a segment without tokens gets its zeros here.
+// a segment without tokens gets its zeros here. A workgroup per segment and 8 rows.
+constexpr int kMergeRows = 8;
 template <int D, int RB>
 __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnArgs a) {
   constexpr int kRows = 16 * RB;
-  const int entries = a.per_head ? a.B * a.Hkv : a.B, per = a.per_head ? 1 : a.Hkv;
   const int b = blockIdx.x / a.Hkv, h = blockIdx.x - b * a.Hkv;
   const int entry = a.per_head ? (int)blockIdx.x : b;
-  const int row0 = blockIdx.y * kRows, rows = a.G * a.N;
+  const int first = blockIdx.y * kMergeRows, rows = min(kMergeRows, a.G * a.N - first);
   const int lane = threadIdx.x & 63;
-  const int pages = pages_of(cache_len(a, entry));
-  const int64_t total = line_total(a, entries, per);
-  int64_t before = 0;
-  for (int i = lane; i < entry; i += 64) before += pages_of(cache_len(a, i));
-  const int64_t s0 = wave_sum(before) * per + (a.per_head ? 0 : (int64_t)h * pages);
+  const int pages = pages_of(__builtin_amdgcn_readfirstlane(cache_len(a, entry)));
+  const Line line(a);
+  int before = 0;
+  for (int i = lane; i < entry; i += 64) before += extent_of(pages_of(cache_len(a, i)));
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) before += __shfl_xor(before, s);
+  const int s0 = __builtin_amdgcn_readfirstlane(before) * line.per + (a.per_head ? 0 : h * extent_of(pages));
   int w0 = 0, w1 = -1;
   if (pages > 0) {
-    w0 = worker_of(total, s0, a.workers);
-    w1 = worker_of(total, s0 + pages - 1, a.workers);
+    w0 = line.worker(s0 + kSegment);
+    w1 = line.worker(s0 + kSegment + pages - 1);
     if (w0 == w1) return;  // that worker wrote the rows
   }
-  const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N;
-  const float* parts = a.part + (size_t)blockIdx.y * 2 * a.workers * kRows * (D + 2);
-  auto row_of = [&](int w, int r) {
-    return parts + ((size_t)(2 * w + (worker_start(total, w, a.workers) < s0 ? 1 : 0)) * kRows + r) * (D + 2);
-  };
-  auto empty = [&](int w) {
-    return worker_start(total, w, a.workers) == worker_start(total, w + 1, a.workers);
-  };
-  for (int i = threadIdx.x; i < kRows * (D / 4); i += kThreadsC) {
+  const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N + first;
+  // Worker w's part of the segment: its first one (slot 2 w), or w0's second where that began before.
+  const int early = w1 >= w0 && line.start(w0) < s0 ? 1 : 0;
+  const float* parts = a.part + (size_t)(first / kRows) * 2 * a.workers * kRows * (D + 4) + (size_t)(first % kRows) * (D + 4);
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsC) {
     const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
-    if (row0 + r >= rows) continue;
-    float m = -INFINITY;
-    for (int w = w0; w <= w1; ++w)
-      if (!empty(w)) m = fmaxf(m, row_of(w, r)[D]);
-    float l = 0.f;
+    const float* pr = parts + (size_t)r * (D + 4);
+    const size_t step = (size_t)2 * kRows * (D + 4);
+    float m = -INFINITY, l = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    if (m > -INFINITY) {
-      for (int w = w0; w <= w1; ++w) {
-        if (empty(w)) continue;
-        const float* pr = row_of(w, r);
-        const float f = fast_exp2(pr[D] - m);
-        const f32x2 u = *reinterpret_cast<const f32x2*>(pr + d0), v = *reinterpret_cast<const f32x2*>(pr + d0 + 2);
-        l += f;
-        y += f * f32x4{u[0], u[1], v[0], v[1]};
-      }
-      y *= 1.f / l;
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+      const float* pw = pr + w * step + (w == w0 ? early * (step / 2) : 0);
+      const f32x4 u = *reinterpret_cast<const f32x4*>(pw + d0);
+      const float part = pw[D], m_new = fmaxf(m, part);
+      const float f = m_new > -INFINITY ? fast_exp2(part - m_new) : 0.f;
+      const float keep = m_new > -INFINITY ? fast_exp2(m - m_new) : 0.f;
+      l = l * keep + f;
+      y = y * keep + f * u;
+      m = m_new;
     }
-    *reinterpret_cast<u32x2*>(a.out + (q_row + row0 + r) * D + d0) =
+    if (l > 0.f) y *= 1.f / l;
+    *reinterpret_cast<u32x2*>(a.out + (q_row + r) * D + d0) =
         __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
     if (a.lse && d0 == 0)
-      a.lse[q_row + row0 + r] = m > -INFINITY ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+      a.lse[q_row + r] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
   }
 }
 
 template <int D>
 hipError_t cache_attn_for(const CacheAttnArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks), segs((unsigned)(a.B * a.Hkv), (unsigned)a.row_blocks);
+  const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
+  const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
   if (cache_rows_per_pass(a.G * a.N) == 16) {
     cache_attn_kernel<D, 1><<<grid, kThreadsC, 0, s>>>(a);
     cache_merge_kernel<D, 1><<<segs, kThreadsC, 0, s>>>(a);
