@@ -8,12 +8,20 @@ stream of the tensors' device.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 
 from ._lib import lib
 from .api import _check, _ptr, _stream
 
+try:
+    import torch
+except ImportError:  # the functions of the C ABI take addresses and do without
+    torch = None
+
 BLOCK_TOKENS = 128
+_HERE = contextlib.nullcontext()
 
 
 def block_attn_means(x, means, B: int, H: int, S: int, d: int, lens=None, stream=None) -> None:
@@ -34,6 +42,7 @@ def _bytes_of(fn, name: str, *sizes: int) -> int:
     return n.value
 
 
+@functools.lru_cache(maxsize=1024)
 def block_attn_fwd_workspace(B: int, H: int, Hkv: int, Sq: int, Skv: int, d: int, n_list: int) -> int:
     """Bytes of workspace that block_attn_fwd needs for these sizes."""
     return _bytes_of(lib.block_attn_fwd_workspace, "block_attn_fwd_workspace", B, H, Hkv, Sq, Skv, d, n_list)
@@ -47,6 +56,7 @@ def block_attn_fwd(q, k, v, lists, out, lse, B: int, H: int, Hkv: int, Sq: int, 
                               _stream(stream)), "block_attn_fwd")
 
 
+@functools.lru_cache(maxsize=1024)
 def block_attn_bwd_workspace(B: int, H: int, Hkv: int, Sq: int, Skv: int, d: int, n_list: int) -> int:
     """Bytes of workspace that block_attn_bwd needs for these sizes."""
     return _bytes_of(lib.block_attn_bwd_workspace, "block_attn_bwd_workspace", B, H, Hkv, Sq, Skv, d, n_list)
@@ -69,6 +79,7 @@ def cache_attn_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_
                                 _stream(stream)), "cache_attn_write")
 
 
+@functools.lru_cache(maxsize=1024)
 def cache_attn_fwd_workspace(B: int, H: int, Hkv: int, N: int, d: int, max_pages: int) -> int:
     """Bytes of workspace that cache_attn_fwd needs for these sizes."""
     return _bytes_of(lib.cache_attn_fwd_workspace, "cache_attn_fwd_workspace", B, H, Hkv, N, d, max_pages)
@@ -90,14 +101,24 @@ def cache_attn_fwd(q, k_pages, v_pages, k_scales, v_scales, table, lens, per_hea
 def _want(t, name: str, shape, dtype, device) -> None:
     """t is a contiguous tensor of this shape and type on this GPU: checked before anything is
     launched, since the kernels read and write that many elements."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_cuda or t.device != device:
+    if t.device != device or not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU {device}, got {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+def _on(device):
+    """The context in which `device` is the current one."""
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _current(device) -> int:
+    """The handle of the device's current stream."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _heads(q, k):
@@ -111,8 +132,6 @@ def _heads(q, k):
 
 
 def _lens(lens, shape, device) -> None:
-    import torch
-
     if lens is not None:
         _want(lens, "lens", shape, torch.int32, device)
 
@@ -120,27 +139,23 @@ def _lens(lens, shape, device) -> None:
 def _workspace(n: int, device):
     """Scratch of n bytes from torch's allocator, which hands it on in stream order and gives calls
     that are captured into a graph memory of that graph's own."""
-    import torch
-
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
 def block_means(x, lens=None, out=None):
     """Means of every block of 128 tokens: x [B, H, S, d] bf16 -> [B, H, ceil(S / 128), d] bf16; lens
     (int32 [B]) leaves out the tokens behind a sequence's end."""
-    import torch
-
     if x.dim() != 4:
         raise ValueError("expected a [B, H, S, d] tensor")
     B, H, S, d = x.shape
     _want(x, "x", x.shape, torch.bfloat16, x.device)
     shape = (B, H, -(-S // BLOCK_TOKENS), d)
-    with torch.cuda.device(x.device):
+    with _on(x.device):
         if out is None:
             out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
         _want(out, "out", shape, torch.bfloat16, x.device)
         _lens(lens, (B,), x.device)
-        block_attn_means(x, out, B, H, S, d, lens, torch.cuda.current_stream())
+        block_attn_means(x, out, B, H, S, d, lens, _current(x.device))
     return out
 
 
@@ -149,27 +164,23 @@ def block_lists(q, kmeans, Skv: int, n_list: int, causal=False, sink: int = 0, l
     block means: q [B, H, Sq, d], kmeans [B, Hkv, ceil(Skv / 128), d] (block_means of the keys) ->
     int32 [B, Hkv, ceil(Sq / 128), n_list], ascending, -1 behind the end. The first `sink` blocks
     and the rows' own (with local - 1 more beside them; local = 0: none) are always chosen."""
-    import torch
-
     B, H, Hkv, Sq, nb, d = _heads(q, kmeans)
     if nb != -(-Skv // BLOCK_TOKENS):
         raise ValueError(f"kmeans must hold {-(-Skv // BLOCK_TOKENS)} blocks for Skv = {Skv}, got {nb}")
     _want(q, "q", q.shape, torch.bfloat16, q.device)
     _want(kmeans, "kmeans", (B, Hkv, nb, d), torch.bfloat16, q.device)
     shape = (B, Hkv, -(-Sq // BLOCK_TOKENS), n_list)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         if out is None:
             out = torch.empty(shape, dtype=torch.int32, device=q.device)
         _want(out, "out", shape, torch.int32, q.device)
         _lens(lens, (B,), q.device)
         block_attn_lists(q, kmeans, out, B, H, Hkv, Sq, Skv, d, n_list, sink, local, causal, lens,
-                         torch.cuda.current_stream())
+                         _current(q.device))
     return out
 
 
 def _check_qkv(q, k, v, lists):
-    import torch
-
     B, H, Hkv, Sq, Skv, d = _heads(q, k)
     _want(q, "q", q.shape, torch.bfloat16, q.device)
     _want(k, "k", (B, Hkv, Skv, d), torch.bfloat16, q.device)
@@ -183,11 +194,9 @@ def _check_qkv(q, k, v, lists):
 def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=None, out=None, return_lse=False):
     """Attention over the listed blocks: q [B, H, Sq, d], k and v [B, Hkv, Skv, d], lists as
     block_lists gives them. The rows are the last Sq of Skv positions. Returns out, or (out, lse)."""
-    import torch
-
     sizes = _check_qkv(q, k, v, lists)
     B, H, _, Sq, _, d, _ = sizes
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         if out is None:
             out = torch.empty_like(q)
         _want(out, "out", q.shape, torch.bfloat16, q.device)
@@ -195,33 +204,29 @@ def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=No
         lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device) if return_lse else None
         n = block_attn_fwd_workspace(*sizes)
         block_attn_fwd(q, k, v, lists, out, lse, *sizes, causal, lens, d ** -0.5 if scale is None else scale,
-                       _workspace(n, q.device), n, torch.cuda.current_stream())
+                       _workspace(n, q.device), n, _current(q.device))
     return (out, lse) if return_lse else out
 
 
 def block_attn_grad(q, k, v, lists, out, dout, lse, causal=False, scale: float | None = None, lens=None):
     """(dq, dk, dv) of block_attn: out and lse are what it returned for the same arguments, dout is
     the gradient of out."""
-    import torch
-
     sizes = _check_qkv(q, k, v, lists)
     B, H, _, Sq, _, d, _ = sizes
     _want(out, "out", q.shape, torch.bfloat16, q.device)
     _want(dout, "dout", q.shape, torch.bfloat16, q.device)
     _want(lse, "lse", (B, H, Sq), torch.float32, q.device)
     _lens(lens, (B,), q.device)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
         n = block_attn_bwd_workspace(*sizes)
         block_attn_bwd(q, k, v, lists, out, dout, lse, dq, dk, dv, *sizes, causal, lens,
-                       d ** -0.5 if scale is None else scale, _workspace(n, q.device), n, torch.cuda.current_stream())
+                       d ** -0.5 if scale is None else scale, _workspace(n, q.device), n, _current(q.device))
     return dq, dk, dv
 
 
 def _check_cache(k_pages, v_pages, k_scales, v_scales, device):
     """(pages, key heads, d) of the cache's tensors."""
-    import torch
-
     if k_pages.dim() != 4:
         raise ValueError("k_pages must be [n_pages, Hkv, 128, d]")
     pages, Hkv, _, d = k_pages.shape
@@ -237,8 +242,6 @@ def cache_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new=N
     k_pages [n_pages, Hkv, 128, d] and v_pages [n_pages, Hkv, d, 128] float8_e4m3fn, scales fp32
     [n_pages, Hkv], table int32 [B, max_pages], lens int32 [B] (left as it is). n_new (int32 [B]):
     how many of the N tokens each sequence takes."""
-    import torch
-
     if k.dim() != 4 or not k.is_cuda:
         raise ValueError("k must be a [B, Hkv, N, d] tensor on a GPU")
     pages, Hkv, d = _check_cache(k_pages, v_pages, k_scales, v_scales, k.device)
@@ -251,9 +254,9 @@ def cache_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new=N
     _want(lens, "lens", (B,), torch.int32, k.device)
     if n_new is not None:
         _want(n_new, "n_new", (B,), torch.int32, k.device)
-    with torch.cuda.device(k.device):
+    with _on(k.device):
         cache_attn_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new, B, Hkv, N, d,
-                         table.shape[1], pages, torch.cuda.current_stream())
+                         table.shape[1], pages, _current(k.device))
 
 
 def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: float | None = None, out=None,
@@ -261,8 +264,6 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
     """Attention of q [B, H, N, d], the last N tokens of each sequence, over the cache; lens counts
     them. table [B, max_pages] with lens [B], or, for pages chosen per key head, [B, Hkv, max_pages]
     with [B, Hkv]. Returns out, or (out, lse)."""
-    import torch
-
     if q.dim() != 4 or not q.is_cuda:
         raise ValueError("q must be a [B, H, N, d] tensor on a GPU")
     pages, Hkv, d = _check_cache(k_pages, v_pages, k_scales, v_scales, q.device)
@@ -275,7 +276,7 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
     width = table.shape[-1]
     _want(table, "table", (*lead, width), torch.int32, q.device)
     _want(lens, "lens", lead, torch.int32, q.device)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         if out is None:
             out = torch.empty_like(q)
         _want(out, "out", q.shape, torch.bfloat16, q.device)
@@ -283,5 +284,5 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
         n = cache_attn_fwd_workspace(B, H, Hkv, N, d, width)
         cache_attn_fwd(q, k_pages, v_pages, k_scales, v_scales, table, lens, per_head, out, lse, B, H, Hkv, N, d,
                        width, pages, d ** -0.5 if scale is None else scale, _workspace(n, q.device), n,
-                       torch.cuda.current_stream())
+                       _current(q.device))
     return (out, lse) if return_lse else out

@@ -209,7 +209,9 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_fwd_kernel(const BlockFwdA
   }
 }
 
-// Joins the pieces of a unit's rows, in order; a thread takes 4 consecutive d of a row.
+// Joins the pieces of 16 of a unit's rows, in order; a thread takes 4 consecutive d of a row.
+constexpr int kMergeRowsF = 16;
+
 template <int D>
 __global__ __launch_bounds__(kThreadsB) void block_merge_kernel(const BlockFwdArgs a) {
   const BlockGeo& g = a.g;
@@ -219,28 +221,28 @@ __global__ __launch_bounds__(kThreadsB) void block_merge_kernel(const BlockFwdAr
   const ListRows rows(g, b, h, i);
   const int n_rows = g.G * rows.tokens;
   const float* part = a.part + (size_t)lu * a.pieces * kUnitRows * (D + 4);
-  for (int x = threadIdx.x; x < kUnitRows * (D / 4); x += kThreadsB) {
-    const int rr = x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
+  constexpr size_t kStep = (size_t)kUnitRows * (D + 4);
+  for (int x = threadIdx.x; x < kMergeRowsF * (D / 4); x += kThreadsB) {
+    const int rr = blockIdx.y * kMergeRowsF + x / (D / 4), d0 = 4 * (x % (D / 4)), r = unit * kUnitRows + rr;
     if (r >= n_rows) return;
     int pos;
     const size_t row = rows.global(r, pos);
     const float* p = part + (size_t)rr * (D + 4);
-    float m = -INFINITY;
-    for (int y = 0; y < a.pieces; ++y) m = fmaxf(m, p[(size_t)y * kUnitRows * (D + 4) + D]);
-    float l = 0.f;
+    float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (m > -INFINITY) {
-      for (int y = 0; y < a.pieces; ++y) {
-        const float* py = p + (size_t)y * kUnitRows * (D + 4);
-        const float f = fast_exp2(py[D] - m);
-        l += f;
-        o += f * *reinterpret_cast<const f32x4*>(py + d0);
-      }
-      o *= 1.f / l;
+#pragma unroll 4
+    for (int y = 0; y < a.pieces; ++y) {
+      const f32x4 u = *reinterpret_cast<const f32x4*>(p + y * kStep + d0);
+      const float lse2 = p[y * kStep + D], m_new = fmaxf(m, lse2);
+      const float f = m_new > -INFINITY ? fast_exp2(lse2 - m_new) : 0.f;
+      const float keep = m_new > -INFINITY ? fast_exp2(m - m_new) : 0.f;
+      l = l * keep + f;
+      o = o * keep + f * u;
+      m = m_new;
     }
+    if (l > 0.f) o *= 1.f / l;
     *reinterpret_cast<u32x2*>(a.out + row * D + d0) = __builtin_bit_cast(u32x2, __builtin_convertvector(o, bf16x4));
-    if (a.lse && d0 == 0)
-      a.lse[row] = m > -INFINITY ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+    if (a.lse && d0 == 0) a.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
   }
 }
 
@@ -248,7 +250,11 @@ template <int D>
 hipError_t block_fwd_for(const BlockFwdArgs& a, hipStream_t s) {
   const uint32_t units = (uint32_t)a.g.B * a.g.Hkv * a.g.nq * a.units;
   block_fwd_kernel<D><<<unit_grid(a.g, a.units * a.pieces), kThreadsB, 0, s>>>(a);
-  if (a.pieces > 1) block_merge_kernel<D><<<units, kThreadsB, 0, s>>>(a);
+  if (a.pieces > 1) {
+    // Where every unit has few rows (single tokens) only the first of them.
+    const int rows = a.g.nq == 1 ? (int)std::min<int64_t>(kUnitRows, (int64_t)a.g.G * a.g.Sq) : kUnitRows;
+    block_merge_kernel<D><<<dim3(units, (rows + kMergeRowsF - 1) / kMergeRowsF), kThreadsB, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
