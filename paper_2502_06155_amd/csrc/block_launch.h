@@ -31,6 +31,7 @@ struct ListsArgs {
   const uint16_t* kmeans;
   int32_t* lists;
   int sink, local;
+  int rows;  // query blocks of a workgroup (set by the launch)
 };
 
 struct BlockFwdArgs {
@@ -111,14 +112,12 @@ struct CacheAttnArgs {
 };
 
 hipError_t launch_block_means(const MeansArgs& a, hipStream_t stream);
-hipError_t launch_block_lists(const ListsArgs& a, hipStream_t stream);
+hipError_t launch_block_lists(ListsArgs a, hipStream_t stream);
 hipError_t launch_block_fwd(const BlockFwdArgs& a, hipStream_t stream);
 hipError_t launch_block_bwd(const BlockBwdArgs& a, hipStream_t stream);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t stream);
 
-// Query blocks whose lists one workgroup of the list kernel forms.
-int lists_per_workgroup(int nb);
 // Rows of a pass of cache attention over a sequence's G * N rows.
 int cache_rows_per_pass(int rows);
 

@@ -374,3 +374,31 @@ def test_wrappers_refuse():
         ta.block_lists(q, torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16, device="cuda"), 300, 1, sink=1)
     with pytest.raises(ValueError, match="blocks"):
         ta.block_lists(q, torch.zeros(1, 2, 4, 64, dtype=torch.bfloat16, device="cuda"), 300, 2)
+
+
+@pytest.mark.parametrize("kind", ["zeros", "equal", "near", "huge", "infinite"])
+def test_lists_where_scores_are_hard_to_tell_apart(kind):
+    """Scores that 32 bits cannot order: all equal, equal but for the last bits, sums that cancel, and
+    infinities: the choice is the one that 64 bits make."""
+    rng = np.random.default_rng(17)
+    B, H, S, d, nb, n = 1, 2, 300, 96, 700, 33
+    q, km = bits(rng, B, H, S, d), bits(rng, B, H, nb, d)
+    if kind == "zeros":
+        km[:] = 0
+    elif kind == "equal":
+        km[:] = km[:, :, :1]
+    elif kind == "near":  # one step of bf16 in one small value apart
+        km[:] = km[:, :, :1]
+        km[..., 3] = 0x2000 + rng.integers(0, 64, (B, H, nb))
+    elif kind == "huge":  # pairs that cancel
+        x = ob.widen(km) * 2.0 ** 30
+        x[..., 1::2] = -x[..., 0::2]
+        x[..., 5] += 2.0 ** 22
+        km = ob.to_bf16(x)
+        q[..., 1::2] = q[..., 0::2]
+    else:
+        km[0, 0, 5, 7], km[0, 1, 600, 2] = 0x7F80, 0xFF80
+    got = ta.block_lists(to_dev(q), to_dev(km), 128 * nb, n, local=1).cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        ref = ob.block_lists(q, km, 128 * nb, n, local=1)
+    assert np.array_equal(got, ref)
