@@ -35,27 +35,33 @@ __device__ __forceinline__ int scale_exponent(uint32_t bits) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// e4m3 code of x: nearest, ties to even; infinities become +-448, NaN stays NaN.
-__device__ __forceinline__ uint32_t code_of(float x) {
-  const float y = __builtin_amdgcn_fmed3f(x, -kMaxCode, kMaxCode);
-  const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xffu;
-  return x != x ? 0x7fu : c;
+// e4m3 codes of two numbers in the low (or high) half of a word: nearest, ties to even; infinities become
+// +-448, NaN stays NaN.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t code_pair(float x, float y, uint32_t word) {
+  const float a = __builtin_amdgcn_fmed3f(x, -kMaxCode, kMaxCode), b = __builtin_amdgcn_fmed3f(y, -kMaxCode, kMaxCode);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x != x ? x : a, y != y ? y : b, (int)word, HIGH);
 }
-__device__ __forceinline__ float value_of(uint32_t code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
+__device__ __forceinline__ float bf16_at(u32x4 w, int e) {
+  return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+}
 
-// One workgroup writes K (blockIdx.z = 0) or V (1) of one (sequence, key head, touched page).
+// One workgroup writes K (blockIdx.z = 0) or V (1) of one (sequence, key head, touched page). A thread
+// holds 16-byte pieces (8 dims) of four tokens in a row, read once: the page's maximum needs them all
+// before the first can be rounded. K codes go out as they lie, V's through LDS.
 template <int D>
 __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWriteArgs a) {
-  constexpr int kPieces = D / 8;  // 16-byte pieces of a token's bf16 row
+  constexpr int kPieces = D / 8, kPer = (kBlock / 4 * kPieces + kThreadsC - 1) / kThreadsC;
+  constexpr int kRow = kBlock + 16;  // bytes of a V row in LDS: rows of 16-byte pieces, on different banks
   __shared__ uint32_t s_max[kThreadsC / 64];
-  __shared__ uint8_t s_codes[D * (kBlock + 4)];  // V: codes [d][token], rows padded against bank conflicts
+  __shared__ __attribute__((aligned(16))) uint8_t s_codes[D * kRow];
   const int b = blockIdx.y / a.Hkv, h = blockIdx.y - b * a.Hkv;
   const bool is_v = blockIdx.z != 0;
   const int64_t len = max(a.lens[b], 0);
   const int n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
   const int64_t slot = len / kBlock + blockIdx.x;
   if (slot >= a.max_pages) return;
-  // Page positions [t0, t1) receive new tokens, the first of them token `src`.
+  // Page positions [t0, t1) receive new tokens, the first of them token pos0 + t0 - len of the call.
   const int64_t pos0 = slot * kBlock;
   const int t0 = (int)max(len - pos0, (int64_t)0);
   const int t1 = (int)min(len + n - pos0, (int64_t)kBlock);
@@ -67,72 +73,103 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
   uint8_t* codes = (is_v ? a.v_pages : a.k_pages) + ph * kBlock * D;
   float* scale = (is_v ? a.v_scales : a.k_scales) + ph;
   const int tid = threadIdx.x;
-  const int n_pieces = (t1 - t0) * kPieces;
+  const int g0 = t0 / 4 * kPieces, g1 = (t1 + 3) / 4 * kPieces;  // items that hold new tokens
 
   // The largest finite magnitude of the new tokens: bf16 bits without the sign order as integers.
+  const float s_old = *scale;
+  u32x4 w[kPer][4];
   uint32_t most = 0;
-  for (int p = tid; p < n_pieces; p += kThreadsC) {
-    const u32x4 w = load16(x + 8 * (size_t)p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t lo = w[e] & 0x7fffu, hi = (w[e] >> 16) & 0x7fffu;
-      most = max(most, lo < 0x7f80u ? lo : 0u);
-      most = max(most, hi < 0x7f80u ? hi : 0u);
+  for (int i = 0; i < kPer; ++i) {
+    const int item = g0 + tid + kThreadsC * i, t = item / kPieces * 4, d0 = item % kPieces * 8;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      w[i][y] = u32x4{0u, 0u, 0u, 0u};
+      if (item < g1 && t + y >= t0 && t + y < t1) w[i][y] = load16(x + (size_t)(t + y - t0) * D + d0);
     }
   }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = w[i][y][e] & 0x7fffu, hi = (w[i][y][e] >> 16) & 0x7fffu;
+        most = max(most, lo < 0x7f80u ? lo : 0u);
+        most = max(most, hi < 0x7f80u ? hi : 0u);
+      }
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, s));
   if ((tid & 63) == 0) s_max[tid >> 6] = most;
-  const float s_old = *scale;
   __syncthreads();
   most = 0;
 #pragma unroll
-  for (int w = 0; w < kThreadsC / 64; ++w) most = max(most, s_max[w]);
+  for (int y = 0; y < kThreadsC / 64; ++y) most = max(most, s_max[y]);
   float s_new = pow2(scale_exponent(most << 16));
   if (t0 > 0) s_new = fmaxf(s_old, s_new);
-  const float inv = 1.f / s_new;  // exact: a power of two, unless the page's own scale was none
+  const float inv = 1.f / s_new;  // exact: a power of two
 
   if (t0 > 0 && s_new != s_old) {
-    // The page's old tokens under the larger scale.
+    // The page's old tokens under the larger scale, 16 codes at a time: of K the first t0 rows, of V the
+    // first t0 of every row (the codes behind them stay as they are).
     const float ratio = s_old * inv;
-    for (int p = tid; p < t0 * D; p += kThreadsC) {
-      uint8_t* c = is_v ? codes + (size_t)(p / t0) * kBlock + p % t0 : codes + p;
-      *c = (uint8_t)code_of(value_of(*c) * ratio);
+    constexpr int kVecs = kBlock / 16;
+    const int vecs = is_v ? D * kVecs : t0 * (D / 16);
+    for (int p = tid; p < vecs; p += kThreadsC) {
+      const int old = is_v ? min(max(t0 - p % kVecs * 16, 0), 16) : 16;  // codes of these 16 to move
+      if (old == 0) continue;
+      u32x4 c = *reinterpret_cast<const u32x4*>(codes + 16 * (size_t)p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = (int)c[e];
+        uint32_t y = code_pair<false>(__builtin_amdgcn_cvt_f32_fp8(v, 0) * ratio,
+                                      __builtin_amdgcn_cvt_f32_fp8(v, 1) * ratio, 0u);
+        y = code_pair<true>(__builtin_amdgcn_cvt_f32_fp8(v, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8(v, 3) * ratio, y);
+        const int left = old - 4 * e;
+        const uint32_t keep = left >= 4 ? 0u : left <= 0 ? ~0u : ~0u << (8 * left);
+        c[e] = (y & ~keep) | (c[e] & keep);
+      }
+      *reinterpret_cast<u32x4*>(codes + 16 * (size_t)p) = c;
+    }
+    if (is_v) __syncthreads();  // new tokens may share 16 codes with old ones
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int item = g0 + tid + kThreadsC * i, t = item / kPieces * 4, d0 = item % kPieces * 8;
+    if (item >= g1) continue;
+    if (!is_v) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (t + y < t0 || t + y >= t1) continue;
+        u32x2 c = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          c[e] = code_pair<false>(bf16_at(w[i][y], 4 * e) * inv, bf16_at(w[i][y], 4 * e + 1) * inv, 0u);
+          c[e] = code_pair<true>(bf16_at(w[i][y], 4 * e + 2) * inv, bf16_at(w[i][y], 4 * e + 3) * inv, c[e]);
+        }
+        *reinterpret_cast<u32x2*>(codes + (size_t)(t + y) * D + d0) = c;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t c = code_pair<false>(bf16_at(w[i][0], e) * inv, bf16_at(w[i][1], e) * inv, 0u);
+        c = code_pair<true>(bf16_at(w[i][2], e) * inv, bf16_at(w[i][3], e) * inv, c);
+        *reinterpret_cast<uint32_t*>(s_codes + (d0 + e) * kRow + t) = c;
+      }
     }
   }
-  if (!is_v) {
-    for (int p = tid; p < n_pieces; p += kThreadsC) {
-      const u32x4 w = load16(x + 8 * (size_t)p);
-      u32x2 c = {0u, 0u};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[e / 2] |= code_of(__uint_as_float(w[e] << 16) * inv) << (16 * (e % 2));
-        c[e / 2] |= code_of(__uint_as_float(w[e] & 0xffff0000u) * inv) << (16 * (e % 2) + 8);
-      }
-      *reinterpret_cast<u32x2*>(codes + (size_t)t0 * D + 8 * (size_t)p) = c;
-    }
-  } else {
-    constexpr int kRow = kBlock + 4;
-    for (int p = tid; p < n_pieces; p += kThreadsC) {
-      const u32x4 w = load16(x + 8 * (size_t)p);
-      const int t = t0 + p / kPieces, d0 = 8 * (p % kPieces);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s_codes[(d0 + 2 * e) * kRow + t] = (uint8_t)code_of(__uint_as_float(w[e] << 16) * inv);
-        s_codes[(d0 + 2 * e + 1) * kRow + t] = (uint8_t)code_of(__uint_as_float(w[e] & 0xffff0000u) * inv);
-      }
-    }
+  if (is_v) {
     __syncthreads();
-    // Whole dwords of four tokens where all four are new, single bytes at the ends.
-    for (int p = tid; p < D * (kBlock / 4); p += kThreadsC) {
-      const int d0 = p / (kBlock / 4), t = 4 * (p % (kBlock / 4));
-      if (t >= t1 || t + 4 <= t0) continue;
+    // 16 codes at a time where all are new, single ones at the ends.
+    const int v0 = t0 / 16, nv = (t1 + 15) / 16 - v0;
+    for (int p = tid; p < D * nv; p += kThreadsC) {
+      const int d0 = p / nv, t = 16 * (v0 + p - d0 * nv);
       uint8_t* dst = codes + (size_t)d0 * kBlock + t;
       const uint8_t* from = s_codes + d0 * kRow + t;
-      if (t >= t0 && t + 4 <= t1) {
-        *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(from);
+      if (t >= t0 && t + 16 <= t1) {
+        *reinterpret_cast<u32x4*>(dst) = *reinterpret_cast<const u32x4*>(from);
       } else {
-        for (int y = max(t0 - t, 0); y < min(t1 - t, 4); ++y) dst[y] = from[y];
+        for (int y = max(t0 - t, 0); y < min(t1 - t, 16); ++y) dst[y] = from[y];
       }
     }
   }
