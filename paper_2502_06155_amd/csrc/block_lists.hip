@@ -116,8 +116,6 @@ __device__ __forceinline__ float key_score(uint32_t key) {
 }
 __device__ __forceinline__ int leading_zeros(uint32_t x) { return __clz((int)x); }
 __device__ __forceinline__ int leading_zeros(uint64_t x) { return __clzll((long long)x); }
-__device__ __forceinline__ uint32_t from_lane(uint32_t x, int m) { return (uint32_t)__shfl_xor((int)x, m); }
-__device__ __forceinline__ uint64_t from_lane(uint64_t x, int m) { return (uint64_t)__shfl_xor((long long)x, m); }
 template <typename Key>
 __device__ __forceinline__ Key lesser(Key a, Key b) { return a < b ? a : b; }
 template <typename Key>
@@ -175,20 +173,59 @@ __device__ __forceinline__ void wave_sums(const uint16_t* x, int rows, int G, si
   }
 }
 
-// <q, k> of two bf16 rows in 64 bits.
+// <q, k> of two bf16 rows in 64 bits, 64 dims of k read ahead at a time (q lies in LDS).
 template <int D>
 __device__ __forceinline__ double score64(const uint16_t* k, const uint16_t* q) {
   double s = 0.0;
-#pragma unroll 2
-  for (int p = 0; p < D / 8; ++p) {
-    const u32x4 x = load16(k + 8 * p), y = load16(q + 8 * p);
+#pragma unroll 1
+  for (int c = 0; c < D; c += 64) {
+    u32x4 x[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s = __builtin_fma((double)bf16_lo(x[e]), (double)bf16_lo(y[e]), s);
-      s = __builtin_fma((double)bf16_hi(x[e]), (double)bf16_hi(y[e]), s);
+    for (int p = 0; p < 8; ++p) x[p] = load16(k + min(c + 8 * p, D - 8));
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      if (D % 64 != 0 && c + 8 * p >= D) break;
+      const u32x4 y = load16(q + c + 8 * p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s = __builtin_fma((double)bf16_lo(x[p][e]), (double)bf16_lo(y[e]), s);
+        s = __builtin_fma((double)bf16_hi(x[p][e]), (double)bf16_hi(y[e]), s);
+      }
     }
   }
   return s;
+}
+
+// Inclusive scan over the wave's lanes in ascending order by the vector ALU's lane shifts: within rows
+// of 16, then the rows' last lanes handed on. `none` is the operation's identity.
+template <typename Op>
+__device__ __forceinline__ uint32_t lane_scan(uint32_t x, uint32_t none, Op&& op) {
+#define TA_STEP(ctrl, rows) x = op(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, ctrl, rows, 0xf, false))
+  TA_STEP(0x111, 0xf);  // row_shr:1
+  TA_STEP(0x112, 0xf);
+  TA_STEP(0x114, 0xf);
+  TA_STEP(0x118, 0xf);
+  TA_STEP(0x142, 0xa);  // row_bcast:15
+  TA_STEP(0x143, 0xc);  // row_bcast:31
+#undef TA_STEP
+  return x;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ __forceinline__ uint32_t least_of(uint32_t x) {
+  return last_lane(lane_scan(x, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); }));
+}
+__device__ __forceinline__ uint32_t most_of(uint32_t x) {
+  return last_lane(lane_scan(x, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }));
+}
+__device__ __forceinline__ uint64_t least_of(uint64_t x) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) x = lesser(x, (uint64_t)__shfl_xor((long long)x, s));
+  return x;
+}
+__device__ __forceinline__ uint64_t most_of(uint64_t x) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) x = greater(x, (uint64_t)__shfl_xor((long long)x, s));
+  return x;
 }
 
 // A list's keys in LDS, padded with 0 to whole sweeps; fn(j, key) for every key, lane by lane in
@@ -255,11 +292,8 @@ __device__ __forceinline__ bool find_bar(const Keys& kr, int stride, int n, uint
     ties = need < 0 ? n : 0;
     return false;
   }
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    low = lesser(low, from_lane(low, s));
-    high = greater(high, from_lane(high, s));
-  }
+  low = least_of(low);
+  high = most_of(high);
   Key width = high - low;  // the bar lies in [low, low + width]
   int shift = max(0, (int)(8 * sizeof(Key) - 8) - leading_zeros((Key)(width | 1)));
   for (;;) {
@@ -270,31 +304,25 @@ __device__ __forceinline__ bool find_bar(const Keys& kr, int stride, int n, uint
       if (key >= low && key - low <= width) atomicAdd(&hist[(uint32_t)((key - low) >> shift)], 1u);
     });
     wave_sync();
-    // Lane l holds bins 4 l .. 4 l + 3; above = keys in the bins past its own.
+    // Lane l holds bins 255 - 4 l downwards; above = keys in the bins past its own.
     uint32_t in[4], own = 0;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) own += in[x] = hist[4 * lane + x];
-    uint32_t upto = own;  // bins of lanes >= this one
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const uint32_t y = __shfl_down(upto, s);
-      if (lane + s < 64) upto += y;
-    }
-    uint32_t above = upto - own;
+    for (int x = 0; x < 4; ++x) own += in[x] = hist[255 - 4 * lane - x];
+    uint32_t above = lane_scan(own, 0u, [](uint32_t a, uint32_t b) { return a + b; }) - own;
     int bin = -1, in_bin = 0, left = 0;
 #pragma unroll
-    for (int x = 3; x >= 0; --x) {
+    for (int x = 0; x < 4; ++x) {
       if (above < (uint32_t)need && above + in[x] >= (uint32_t)need) {
-        bin = 4 * lane + x;
+        bin = 255 - 4 * lane - x;
         in_bin = (int)in[x];
         left = need - (int)above;
       }
       above += in[x];
     }
     const int src = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(bin >= 0)) - 1;
-    bin = __shfl(bin, src);
-    in_bin = __shfl(in_bin, src);
-    need = __shfl(left, src);
+    bin = __builtin_amdgcn_readlane(bin, src);
+    in_bin = __builtin_amdgcn_readlane(in_bin, src);
+    need = __builtin_amdgcn_readlane(left, src);
     bar = low + ((Key)bin << shift);
     if (in_bin == need) return true;  // the whole bin is chosen
     if (shift == 0) {                 // equal keys
@@ -335,6 +363,14 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
     return Gate{end, lo - a.local + 1, g.causal ? hi + 1 : hi + a.local};
   };
 
+  // The key means of a wave's first 16 blocks are on their way while the queries' form.
+  const uint16_t* km = a.kmeans + (size_t)bh * g.nb * D;
+  u32x4 next[kC];
+  auto load = [&](int j) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) next[c] = load16(km + (size_t)min(j, g.nb - 1) * D + 32 * c + 8 * (lane >> 4));
+  };
+  load(16 * wave + (lane & 15));
   {
     // 8 / R waves a list (a power of two), each with a part of every head's rows; their sums meet in LDS.
     double* part = reinterpret_cast<double*>(hists);  // [8][D]
@@ -360,7 +396,6 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
     __syncthreads();
   }
 
-  const uint16_t* km = a.kmeans + (size_t)bh * g.nb * D;
   {
     const int n = lane & 15, k = lane >> 4;
     bf16x8 qa[kC];
@@ -370,12 +405,6 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
 #pragma unroll
     for (int x = 0; x < 4; ++x) gates[x] = gate_of(i0 + 4 * k + x);
     uint32_t most = 0;  // the largest magnitude of a key mean, as bf16 bits in the upper half
-    u32x4 next[kC];
-    auto load = [&](int j) {
-#pragma unroll
-      for (int c = 0; c < kC; ++c) next[c] = load16(km + (size_t)min(j, g.nb - 1) * D + 32 * c + 8 * k);
-    };
-    load(16 * wave + n);
     for (int j0 = 16 * wave; j0 < stride; j0 += 16 * kWavesM) {
       const int j = j0 + n;
       u32x4 w[kC];
@@ -396,8 +425,7 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
           keys[(size_t)r * stride + j] = j >= gates[x].end ? 0u : gates[x].forced(j, a.sink) ? kForced<uint32_t> : score_key(s[x]);
       }
     }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, x));
+    most = most_of(most);
     if (lane == 0) hists[wave] = most;
   }
   __syncthreads();
@@ -438,11 +466,9 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
       sweep(kr, stride, lane, [&](int, uint32_t key) { least = lesser(least, key >= bar ? key : kForced<uint32_t>); });
       float l1 = 0.f;
       for (int x = lane; x < D; x += 64) l1 += fabsf(bf16_lo(qm[r * D + x]));
+      least = least_of(least);
 #pragma unroll
-      for (int x = 1; x < 64; x <<= 1) {
-        least = lesser(least, from_lane(least, x));
-        l1 += __shfl_xor(l1, x);
-      }
+      for (int x = 1; x < 64; x <<= 1) l1 += __shfl_xor(l1, x);
       // 1.01: the bound's own rounding.
       const float t = key_score(least), off = 1.01f * (2.f * D * 0x1p-22f * l1 * __uint_as_float(most) + 1e-30f);
       const float over = t + off * 1.01f + fabsf(t) * 0x1p-22f, under = t - off * 1.01f - fabsf(t) * 0x1p-22f;
