@@ -21,7 +21,7 @@
  *     on are padding: their keys count for nobody, whatever they hold, and their query rows give
  *     zeros, a log-sum-exp of -inf and zero gradients. Values are taken into 0..Skv.
  *   - causal: nonzero lets a row attend only to positions up to its own.
- *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], the blocks a query block's rows (of all G heads)
+ *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], 1 <= n_list <= TA_MAX_BLOCKS, the blocks a query block's rows (of all G heads)
  *     attend to, in any order. Entries outside 0..NB-1 are skipped (-1 fills up), and a block
  *     that is listed twice counts once.
  *   - Nothing is allocated and nothing is kept between calls. What a call needs beside its tensors

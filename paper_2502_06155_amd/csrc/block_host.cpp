@@ -53,6 +53,9 @@ int launched(hipError_t e) {
   return TA_OK;
 }
 
+int check_grid(double workgroups) {
+  return workgroups <= (double)kMaxGrid ? TA_OK : fail(TA_ERR_BAD_SHAPE, "the call exceeds the grid limit");
+}
 int check_dim(int d) {
   return d == 64 || d == 96 || d == 128 ? TA_OK : fail(TA_ERR_HEAD_DIM, "d must be 64, 96 or 128");
 }
@@ -61,7 +64,7 @@ int make_geo(BlockGeo& g, int B, int H, int Hkv, int Sq, int Skv, int d, int n_l
   if (B < 1 || H < 1 || Hkv < 1 || Sq < 1 || Skv < 1) return fail(TA_ERR_BAD_SHAPE, "B, H, Hkv, Sq and Skv must be >= 1");
   if (H % Hkv) return fail(TA_ERR_BAD_SHAPE, "H must be a multiple of Hkv");
   if (Sq > Skv) return fail(TA_ERR_BAD_SHAPE, "the query rows are the last Sq of Skv positions: Sq <= Skv");
-  if (n_list < 1) return fail(TA_ERR_BAD_SHAPE, "n_list must be >= 1");
+  if (n_list < 1 || n_list > TA_MAX_BLOCKS) return fail(TA_ERR_BAD_SHAPE, "n_list must be in 1..TA_MAX_BLOCKS");
   if (Skv > TA_MAX_BLOCKS * TA_BLOCK) return fail(TA_ERR_BAD_SHAPE, "Skv exceeds TA_MAX_BLOCKS blocks");
   if (int st = check_dim(d)) return st;
   g.B = B;
@@ -77,11 +80,8 @@ int make_geo(BlockGeo& g, int B, int H, int Hkv, int Sq, int Skv, int d, int n_l
   g.n_list = n_list;
   g.causal = causal != 0;
   g.lens = lens;
-  const double rows = (double)B * H * Sq, lists = (double)B * Hkv * g.nq;
-  if (rows * d > 1e15 || lists * n_list > 1e15 || (double)B * H * g.nq > (double)kMaxGrid / 64 ||
-      (double)B * Hkv * g.nb > (double)kMaxGrid / 64)
-    return fail(TA_ERR_BAD_SHAPE, "the call exceeds the grid limit");
-  return TA_OK;
+  // A workgroup for every query block of a head and for every key block of a key head, at least.
+  return check_grid(std::max((double)B * H * g.nq, (double)B * Hkv * g.nb));
 }
 
 int64_t lists_of(const BlockGeo& g) { return (int64_t)g.B * g.Hkv * g.nq; }
@@ -160,10 +160,6 @@ int check_workspace(const void* ws, size_t have, size_t need) {
   if (have < need || (need && !ws))
     return fail(TA_ERR_BAD_SHAPE, "the workspace is smaller than the call needs (" + std::to_string(need) + " bytes)");
   return check_aligned({ws}, 16, "the workspace must be 16-byte aligned");
-}
-
-int check_grid(double workgroups) {
-  return workgroups <= (double)kMaxGrid ? TA_OK : fail(TA_ERR_BAD_SHAPE, "the call exceeds the grid limit");
 }
 
 // The workgroups that share a cache attention's pages, and the passes over its rows.

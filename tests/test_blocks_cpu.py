@@ -78,7 +78,7 @@ def test_null_pointers(call, pointers):
 @pytest.mark.parametrize("call", [_lists, _fwd, _bwd])
 def test_shapes_of_block_calls(call):
     for kw in (dict(B=0), dict(H=0), dict(Hkv=0), dict(Hkv=3), dict(Sq=0), dict(Skv=-1), dict(Sq=301), dict(n_list=0),
-               dict(Skv=128 * 16384 + 1), dict(B=1 << 20, H=1 << 10, Hkv=1 << 10)):
+               dict(Skv=128 * 16384 + 1), dict(n_list=16385), dict(B=1 << 20, H=1 << 10, Hkv=1 << 10)):
         assert call(**kw) == SHAPE, kw
     for d in (0, 32, 80, 256):
         assert call(d=d) == DIM
@@ -171,6 +171,37 @@ def test_reserved_pieces_hold_the_worst_lists(sizes):
     n = ta.block_attn_bwd_workspace(*sizes[:5], 64, sizes[5])
     rows = sizes[0] * sizes[1] * sizes[3]
     assert n >= rows * 8 + slots * 2 * 128 * 64 * 4
+
+
+def _share_items(counts, entries):
+    """Items per XCD as the gradient's plan deals them out: contiguous shares of equal work, a column
+    counting its query blocks and s, pieces of at most `entries` query blocks."""
+    total, cols = int(counts.sum()), len(counts)
+    s = max(1, -(-total // (4 * cols)))
+    before = np.concatenate([[0], np.cumsum(counts + s)[:-1]])
+    xcd = before * 8 // (total + s * cols)
+    assert xcd.max() <= 7
+    return np.bincount(xcd, np.maximum(1, -(-counts // entries)), 8).astype(int)
+
+
+@pytest.mark.parametrize("sizes", [(1, 4, 4, 1000, 1000, 3), (2, 8, 2, 5000, 5000, 40), (1, 1, 1, 128 * 300, 128 * 300, 2),
+                                   (1, 16, 1, 40000, 40000, 24), (3, 2, 2, 777, 3000, 9), (1, 24, 24, 28800, 28800, 32),
+                                   (1, 2, 2, 100, 128 * 2000, 5)])
+def test_no_share_of_the_key_side_holds_more_items_than_there_is_room_for(sizes):
+    nq, nb, held, cols, entries, slots = _piece_bound(*sizes)
+    pieces = -(-nq // entries)
+    cap = min(cols * pieces, (5 * cols + 7) // 8 + ((5 * held + 31) // 32 + (cols + 7) // 8 + nq) // entries)
+    rng = np.random.default_rng(cols)
+    for trial in range(60):
+        counts = np.zeros(cols, np.int64)
+        left = held if trial % 3 else int(rng.integers(0, held + 1))
+        order = {0: np.arange(cols), 1: np.arange(cols)[::-1], 2: rng.permutation(cols)}[trial % 3]
+        for c in order:  # few full columns, or many at a piece's edge, or anything
+            most = [nq, min(nq, entries + 1), int(rng.integers(0, nq + 1)), 1][trial % 4]
+            counts[c] = min(left, most)
+            left -= counts[c]
+        assert _share_items(counts, entries).max() <= cap, (trial, cap)
+        assert (np.where(counts > entries, -(-counts // entries), 0)).sum() <= max(slots, 0)
 
 
 def test_wrappers_check_tensors_before_any_launch():

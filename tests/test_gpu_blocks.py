@@ -402,3 +402,48 @@ def test_lists_where_scores_are_hard_to_tell_apart(kind):
     with np.errstate(invalid="ignore"):
         ref = ob.block_lists(q, km, 128 * nb, n, local=1)
     assert np.array_equal(got, ref)
+
+
+def test_the_longest_sequences():
+    """TA_MAX_BLOCKS key blocks: the listed ones (the last among them) give what the same blocks give
+    side by side in a short sequence, gradients too, and the rest get zeros."""
+    d, nb, Sq, n = 64, 16384, 130, 3
+    rng = np.random.default_rng(23)
+    k, v = (torch.randn(1, 1, 128 * nb - 5, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q, go = to_dev(bits(rng, 1, 2, Sq, d)), to_dev(bits(rng, 1, 2, Sq, d))
+    far = np.array([[[[nb - 1, 5, 9000], [nb - 1, 12345, -1]]]], np.int32)
+    blocks = [5, 9000, 12345, nb - 1]
+    near = np.array([[[[3, 0, 1], [3, 2, -1]]]], np.int32)
+    ks, vs = (torch.cat([x[:, :, 128 * j:128 * (j + 1)] for j in blocks], 2).contiguous() for x in (k, v))
+    out, lse = ta.block_attn(q, k, v, i32(far), return_lse=True)
+    ref, rlse = ta.block_attn(q, ks, vs, i32(near), return_lse=True)
+    assert torch.equal(out, ref) and torch.equal(lse, rlse)
+    grads = ta.block_attn_grad(q, k, v, i32(far), out, go, lse)
+    refs = ta.block_attn_grad(q, ks, vs, i32(near), ref, go, rlse)
+    assert torch.equal(grads[0], refs[0])
+    for g, r in zip(grads[1:], refs[1:]):
+        assert torch.equal(torch.cat([g[:, :, 128 * j:128 * (j + 1)] for j in blocks], 2), r)
+        assert g.count_nonzero() == r.count_nonzero()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_against_differences(d):
+    """Along a direction: the change of sum(out * dout) between two points, computed in float64 from the
+    reference's formula, against the kernels' gradients."""
+    rng = np.random.default_rng(31)
+    grid = lambda *s: np.round(rng.uniform(-0.5, 0.5, s) * 64) / 64  # noqa: E731
+    S, H, lists = 260, 2, np.array([[[[0, -1], [1, 0], [2, 1]]]], np.int32)
+    q, k, v, go = grid(1, H, S, d), grid(1, 1, S, d), grid(1, 1, S, d), grid(1, H, S, d)
+    dev = [to_dev(ob.to_bf16(x)) for x in (q, k, v, go)]
+    out, lse = ta.block_attn(*dev[:3], i32(lists), True, return_lse=True)
+    grads = ta.block_attn_grad(*dev[:3], i32(lists), out, dev[3], lse, True)
+    for i, x in enumerate((q, k, v)):
+        step = rng.integers(-1, 2, x.shape) * 2.0 ** -8
+        at = [[ob.to_bf16(y + s * step if j == i else y) for j, y in enumerate((q, k, v))] for s in (1, -1)]
+        plus, minus = (float((ob.attention(*z, lists, True)[0] * go).sum()) for z in at)
+        got = widen(from_dev(grads[i]))
+        # the kernels' own bound, and the differences' (their step is 2^-8)
+        r = ob.attention_backward(*(ob.to_bf16(y) for y in (q, k, v, go)), lists, True)[i]
+        slack = HALF * np.abs(r[0]) + (HALF + FP32) * r[1] + (FP32 * r[2] + r[3] if i < 2 else 0)
+        bound = float((slack * np.abs(step)).sum()) + 1e-3 * float((np.abs(r[0]) * np.abs(step)).sum())
+        assert abs((plus - minus) / 2 - float((got * step).sum())) <= bound, i
