@@ -162,9 +162,19 @@ int check_workspace(const void* ws, size_t have, size_t need) {
   return check_aligned({ws}, 16, "the workspace must be 16-byte aligned");
 }
 
+// Short tables run a workgroup per (sequence, key head), four pages at a time, and need no second
+// launch to join parts: up to 8 pages at d = 128 (16 at d = 64), and up to 16 where the segments alone
+// fill half of the device. Measured, whole and split: 12 segments of 12 pages at d = 64 8.3 and 9.8 us;
+// 8 of 8 at d = 128 12.5 and 10.8 with one launch (3 us of the host's time) less, 8 of 16 19.4 and 11.9;
+// 256 of 16 27.5 and 35.1.
+bool whole_segments(int64_t segments, int d, int max_pages) {
+  return (int64_t)max_pages * d <= 1024 || (max_pages <= 16 && segments >= kSlots / 2);
+}
+
 // The workgroups that share a cache attention's pages, and the passes over its rows.
 struct CachePlan {
   int workers, passes, rows;
+  bool whole;
   size_t bytes;
 };
 CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
@@ -174,7 +184,9 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.passes = (int)((rows + p.rows - 1) / p.rows);
   // Two workgroups run on a compute unit in passes of 16 rows, one in passes of 32.
   p.workers = (int)std::min<int64_t>(p.rows == 16 ? kSlots : kSlots / 2, (int64_t)B * Hkv * (max_pages + kCacheSegment));
-  p.bytes = (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
+  p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
+  if (p.whole) p.workers = B * Hkv;
+  p.bytes = p.whole ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
 int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
@@ -423,6 +435,7 @@ int cache_attn_fwd(const void* q, const void* k_pages, const void* v_pages, cons
   a.max_pages = max_pages;
   a.n_pages = n_pages;
   a.c = scale * 1.4426950408889634f;
+  a.whole = p.whole;
   a.workers = p.workers;
   a.row_blocks = p.passes;
   a.part = static_cast<float*>(workspace);

@@ -106,6 +106,7 @@ struct CacheAttnArgs {
   float* lse;  // or null
   int B, H, Hkv, G, N, d, max_pages, n_pages;
   float c;     // scale * log2(e)
+  int whole;         // a workgroup per (sequence, head) instead of an even share of all pages
   int workers;       // workgroups that share the pages of all sequences
   int row_blocks;    // 32-row (or 16-row) passes over the G * N rows
   float* part;       // fp32 [row block][2 * workers][rows][d + 4]: O/l, base-2 lse

@@ -225,9 +225,11 @@ struct Line {
   int entries, per;  // entries of lens, segments of an entry
   int total;         // its length
   int each, more;    // every worker's part, workers with one more
-  __device__ __forceinline__ Line(const CacheAttnArgs& a) {
+  __device__ __forceinline__ Line(const CacheAttnArgs& a, bool measure = true) {
     entries = a.per_head ? a.B * a.Hkv : a.B;
     per = a.per_head ? 1 : a.Hkv;
+    total = each = more = 0;
+    if (!measure) return;
     int n = 0;
     for (int i = threadIdx.x & 63; i < entries; i += 64) n += extent_of(pages_of(cache_len(a, i)));
 #pragma unroll
@@ -351,18 +353,28 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
   const int n = lane & 15, g = lane >> 4;
   const int w = blockIdx.x, row0 = blockIdx.y * kRows, rows = a.G * a.N;
 
-  const Line line(a);
-  const int lo = line.start(w), hi = line.start(w + 1);
-  if (lo >= hi) return;
-  int seg0;  // the line's place where the segment starts
-  int entry = line.entry_of(a, lo, seg0);
-  int len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
-  int pages = pages_of(len);
-  int head = scalar_div(lo - seg0, extent_of(pages));
-  seg0 += head * extent_of(pages);
+  // Short tables: a workgroup per segment, and nothing to join (a.whole).
+  const Line line(a, !a.whole);
+  int lo = 0, hi = INT32_MAX, seg0 = 0, entry, head, len, pages;  // seg0: the line's place where the segment starts
+  if (a.whole) {
+    entry = scalar_div(w, line.per);
+    head = w - entry * line.per;
+    len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
+    pages = pages_of(len);
+  } else {
+    lo = line.start(w);
+    hi = line.start(w + 1);
+    if (lo >= hi) return;
+    entry = line.entry_of(a, lo, seg0);
+    len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
+    pages = pages_of(len);
+    head = scalar_div(lo - seg0, extent_of(pages));
+    seg0 += head * extent_of(pages);
+  }
 
   int at = lo;
   auto advance = [&]() {  // to the next segment with pages; false past the worker's part
+    if (a.whole) return false;
     at = seg0 + kSegment + pages;
     if (at >= hi) return false;
     seg0 = at;
@@ -383,7 +395,7 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
     const ScalarFloats k_scales = (ScalarFloats)a.k_scales, v_scales = (ScalarFloats)a.v_scales;
     const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N;  // rows of the group lie together
 
-    if (p1 <= p0) continue;
+    if (p1 <= p0 && !a.whole) continue;  // (alone, a segment without tokens gets its zeros)
     // Pages p0 + wave, + 4, ... up to p1. A page that is none is passed over: its tokens are not read.
     auto page_of = [&](int p) {
       if (p >= p1) return -1;
@@ -622,10 +634,10 @@ hipError_t cache_attn_for(const CacheAttnArgs& a, hipStream_t s) {
   const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
   if (cache_rows_per_pass(a.G * a.N) == 16) {
     cache_attn_kernel<D, 1><<<grid, kThreadsC, 0, s>>>(a);
-    cache_merge_kernel<D, 1><<<segs, kThreadsC, 0, s>>>(a);
+    if (!a.whole) cache_merge_kernel<D, 1><<<segs, kThreadsC, 0, s>>>(a);
   } else {
     cache_attn_kernel<D, 2><<<grid, kThreadsC, 0, s>>>(a);
-    cache_merge_kernel<D, 2><<<segs, kThreadsC, 0, s>>>(a);
+    if (!a.whole) cache_merge_kernel<D, 2><<<segs, kThreadsC, 0, s>>>(a);
   }
   return hipGetLastError();
 }

@@ -61,7 +61,7 @@ def _write(**kw):
 
 def _cache(**kw):
     a = dict(q=M, kp=2 * M, vp=3 * M, ks=4 * M, vs=5 * M, table=6 * M, lens=7 * M, per_head=0, out=8 * M, lse=9 * M, B=2,
-             H=4, Hkv=2, N=3, d=64, max_pages=4, n_pages=8, scale=0.1, ws=16 * M, bytes=1 << 30)
+             H=4, Hkv=2, N=3, d=64, max_pages=40, n_pages=8, scale=0.1, ws=16 * M, bytes=1 << 30)
     a.update(kw)
     return lib.cache_attn_fwd(*a.values(), None)
 

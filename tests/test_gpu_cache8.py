@@ -155,10 +155,12 @@ def held(rng, B, Hkv, d, lens, width=None, spare=2):
     (2, 34, 2, 3, 128, [130, 257]),
     (20, 6, 3, 1, 64, [0, 5, 0, 0, 300, 128, 0, 1, 640, 2, 0, 256, 7, 0, 90, 0, 0, 1280, 3, 0]),
 ])
-@pytest.mark.parametrize("scale", [None, -0.2, 0.0])
-def test_attention(B, H, Hkv, N, d, lens, scale):
+@pytest.mark.parametrize("scale,width", [(None, None), (None, 40), (-0.2, 40), (0.0, None)])
+def test_attention(B, H, Hkv, N, d, lens, scale, width):
+    """Tables as short as the sequences (a workgroup a segment, where they are short enough) and tables
+    of 40 pages (work shared evenly and joined)."""
     rng = np.random.default_rng(sum(lens) + d)
-    cache, table = held(rng, B, Hkv, d, lens)
+    cache, table = held(rng, B, Hkv, d, lens, width)
     q = bits(rng, B, H, N, d)
     out = torch.full((B, H, N, d), float("nan"), dtype=torch.bfloat16, device="cuda")
     got, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), scale, out, return_lse=True)
