@@ -116,12 +116,14 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   // Query blocks that all columns hold together, at most, and what a column holds on average. A
   // piece takes up to twice that, or an eighth of a resident workgroup's share of all work where
   // that is more (long launches even out by themselves); in launches of few columns less, so that
-  // about two pieces per resident workgroup form, but not below four units of 128 rows.
+  // about one piece per resident workgroup forms, but not below four units of 128 rows. 16 heads of
+  // 8192 positions, 16 blocks each: 485 us so, 519 at two pieces per workgroup, 648 at four; 4 heads of
+  // 16384, four query heads each, 24 blocks, causal: 1280 (half a piece 1312, two 1290, four 1433).
   const int64_t held = lists_of(g) * std::min(g.n_list, g.nb), cols = (int64_t)g.B * g.Hkv * g.nb;
   const int64_t mean = (held + cols - 1) / cols;
   const int64_t most = std::max(2 * mean, held / (8 * kSlots));
   const int64_t least = std::min<int64_t>(most, (3 + g.G) / g.G);
-  p.entries = (int)std::min<int64_t>(INT_MAX, std::min(most, std::max(least, (held + 2 * kSlots - 1) / (2 * kSlots))));
+  p.entries = (int)std::min<int64_t>(INT_MAX, std::min(most, std::max(least, (held + kSlots - 1) / kSlots)));
   p.pieces_k = (g.nq + p.entries - 1) / p.entries;
   // A column in ceil(n / entries) > 1 pieces has n > entries, so fewer than 2 n / entries pieces.
   p.slots = p.pieces_k == 1 ? 0 : std::min(cols * p.pieces_k, 2 * held / p.entries);
@@ -354,7 +356,7 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
   a.items_cap = (int)p.items_cap;
   a.part_q = reinterpret_cast<float*>(ws + p.off_q);
   a.part_k = reinterpret_cast<float*>(ws + p.off_k);
-  if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces_q + 8.0 * a.items_cap)) return st;
+  if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces_q + 8.0 * p.items_cap)) return st;
   if (int st = check_grid(4.0 * lists_of(a.g) * a.units + 8.0 * cols)) return st;
   if (int st = check_grid((double)rows / 64 + (double)lists_of(a.g))) return st;
   return launched(launch_block_bwd(a, static_cast<hipStream_t>(stream)));
