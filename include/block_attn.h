@@ -21,8 +21,12 @@
  *     on are padding: their keys count for nobody, whatever they hold, and their query rows give
  *     zeros, a log-sum-exp of -inf and zero gradients. Values are taken into 0..Skv.
  *   - causal: nonzero lets a row attend only to positions up to its own.
- *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], 1 <= n_list <= TA_MAX_BLOCKS, the blocks a query block's rows (of all G heads)
- *     attend to, in any order. Entries outside 0..NB-1 are skipped (-1 fills up), and a block
+ *   - A row's result depends on the tokens it attends to alone: infinities and NaN elsewhere, in
+ *     later tokens too, do not reach it. A row that meets a NaN has NaN for its log-sum-exp. For
+ *     gradients this holds between query blocks only: a key or value that is no number may reach
+ *     the gradients of all rows of a query block that lists it.
+ *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], 1 <= n_list <= TA_MAX_BLOCKS, the blocks a query
+ *     block's rows (of all G heads) attend to, in any order. Entries outside 0..NB-1 are skipped (-1 fills up), and a block
  *     that is listed twice counts once.
  *   - Nothing is allocated and nothing is kept between calls. What a call needs beside its tensors
  *     the caller hands in: workspace, DEVICE memory of at least the bytes that the entry's

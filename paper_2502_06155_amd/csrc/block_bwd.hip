@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
     for (int c = 0; c < kPieces; ++c) acc += part[threadIdx.x * kPieces + c];
     const int64_t r = row0 + threadIdx.x;
     const float l = a.lse[r];
-    const bool some = l > -INFINITY;
+    const bool some = l != -INFINITY;  // NaN, of a row of NaN, passes into its gradients
     a.lse2[r] = some ? l * 1.4426950408889634f : INFINITY;
     a.ndelta[r] = some ? -acc : 0.f;
   }

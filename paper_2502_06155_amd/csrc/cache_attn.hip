@@ -12,6 +12,8 @@
 #include <algorithm>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "block_launch.h"
 #include "tile_common.h"
 
@@ -286,6 +288,12 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// A one in the lowest bit of every byte that is a NaN code (0x7f, 0xff).
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u; }
+// The bytes of a word that come before byte `left`.
+__device__ __forceinline__ uint32_t bytes_before(int left) {
+  return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+}
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -403,132 +411,176 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
       return x < a.n_pages ? x : -1;
     };
     auto base_of = [&](const uint8_t* pages_at, int page) { return pages_at + ((size_t)page * a.Hkv + h) * kBlock * D; };
-    int p = p0 + wave;
-    int page = page_of(p);
-    KeyPage<D> kt;
-    ValuePage<D> vt;
-    if (page >= 0) {
-      kt.load(base_of(a.k_pages, page), lane);
-      vt.load(base_of(a.v_pages, page), lane);
-    }
-
-    bf16x8 qf[RB][kSl];
     int end[RB];  // tokens this lane's row attends to
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = row0 + 16 * rb + n;
-      end[rb] = r < rows ? len - (a.N - 1) + r % a.N : 0;
-#pragma unroll
-      for (int m = 0; m < kSl; ++m) {
-        u32x4 x = {0u, 0u, 0u, 0u};
-        if (r < rows) x = load16(a.q + (q_row + r) * D + slice_dim<D>(m, g));
-        qf[rb][m] = as_bf16x8(x);
-      }
-    }
     f32x4 o[RB][kMb];
     float m_ref[RB], l_run[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      m_ref[rb] = kNoRef;
-      l_run[rb] = 0.f;
-#pragma unroll
-      for (int mb = 0; mb < kMb; ++mb) o[rb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // The next page's K loads go out as soon as this one's K is used, its V loads when V is: both
-    // have a page's time to arrive, in one set of registers.
-    for (; p < p1; p += kWaves) {
-      const int next = page_of(p + kWaves);
-      const int tok0 = p * kBlock;
-      f32x4 s[RB][8];
-      float ks = 0.f, vs = 0.f;
+    // All of it; `apart`: NaN codes among the last tokens, which some rows do not see, apart.
+    auto attend = [&](auto apart) {
+      int p = p0 + wave;
+      int page = page_of(p);
+      KeyPage<D> kt;
+      ValuePage<D> vt;
       if (page >= 0) {
-        ks = k_scales[(size_t)page * a.Hkv + h];
-        vs = v_scales[(size_t)page * a.Hkv + h];
-        // Fences keep the codes of later slices from being widened early (twice the registers).
-#pragma unroll
-        for (int m = 0; m < kSl; ++m)
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int i = 4 * half; i < 4 * half + 4; ++i) {
-              const bf16x8 kf = widen8(kt.k[i][2 * m], kt.k[i][2 * m + 1]);
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb)
-                s[rb][i] = mfma16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
+        kt.load(base_of(a.k_pages, page), lane);
+        vt.load(base_of(a.v_pages, page), lane);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) kt.load(base_of(a.k_pages, next), lane);
-      __builtin_amdgcn_sched_barrier(0);
-      if (page >= 0) {
-        const float c = a.c * ks;
-        bf16x8 pf[RB][4];
+
+      bf16x8 qf[RB][kSl];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
+      for (int rb = 0; rb < RB; ++rb) {
+        const int r = row0 + 16 * rb + n;
+        end[rb] = r < rows ? len - (a.N - 1) + r % a.N : 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[rb][i] *= c;
-          if (tok0 + kBlock > len - (a.N - 1)) {
+        for (int m = 0; m < kSl; ++m) {
+          u32x4 x = {0u, 0u, 0u, 0u};
+          if (r < rows) x = load16(a.q + (q_row + r) * D + slice_dim<D>(m, g));
+          qf[rb][m] = as_bf16x8(x);
+        }
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        m_ref[rb] = kNoRef;
+        l_run[rb] = 0.f;
+#pragma unroll
+        for (int mb = 0; mb < kMb; ++mb) o[rb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+
+      // The next page's K loads go out as soon as this one's K is used, its V loads when V is: both
+      // have a page's time to arrive, in one set of registers.
+      for (; p < p1; p += kWaves) {
+        const int next = page_of(p + kWaves);
+        const int tok0 = p * kBlock;
+        f32x4 s[RB][8];
+        float ks = 0.f, vs = 0.f;
+        if (page >= 0) {
+          ks = k_scales[(size_t)page * a.Hkv + h];
+          vs = v_scales[(size_t)page * a.Hkv + h];
+          // Fences keep the codes of later slices from being widened early (twice the registers).
+#pragma unroll
+          for (int m = 0; m < kSl; ++m)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+              for (int i = 4 * half; i < 4 * half + 4; ++i) {
+                const bf16x8 kf = widen8(kt.k[i][2 * m], kt.k[i][2 * m + 1]);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                  s[rb][i] = mfma16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i]);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (next >= 0) kt.load(base_of(a.k_pages, next), lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if (page >= 0) {
+          const float c = a.c * ks;
+          bf16x8 pf[RB][4];
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[rb][i] *= c;
+            if (tok0 + kBlock > len - (a.N - 1)) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (tok0 + 64 * (i / 4) + 16 * g + 4 * (i % 4) + j >= end[rb]) s[rb][i][j] = -INFINITY;
+            }
+            float mx = s[rb][0][0];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (tok0 + 64 * (i / 4) + 16 * g + 4 * (i % 4) + j >= end[rb]) s[rb][i][j] = -INFINITY;
+              for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
+            const float m_new = fmaxf(m_ref[rb], group_max(mx));
+            if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
+              const float alpha = fast_exp2(m_ref[rb] - m_new);
+              l_run[rb] *= alpha;
+#pragma unroll
+              for (int mb = 0; mb < kMb; ++mb) o[rb][mb] *= alpha;
+              m_ref[rb] = m_new;
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+                sum += x;
+                pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)(x * vs);
+              }
+            l_run[rb] += sum;
           }
-          float mx = s[rb][0][0];
+          if (tok0 + kBlock > len) {  // codes behind the last token may be NaN: clear them in V
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
-          const float m_new = fmaxf(m_ref[rb], group_max(mx));
-          if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
-            const float alpha = fast_exp2(m_ref[rb] - m_new);
-            l_run[rb] *= alpha;
+              for (int e = 0; e < 4; ++e) {
+                const int left = len - (tok0 + 64 * half + 16 * g + 4 * e);
 #pragma unroll
-            for (int mb = 0; mb < kMb; ++mb) o[rb][mb] *= alpha;
-            m_ref[rb] = m_new;
+                for (int mb = 0; mb < kMb; ++mb) vt.v[mb][half][e] &= bytes_before(left);
+              }
           }
-          float sum = 0.f;
+          if (decltype(apart)::value && tok0 + kBlock > len - (a.N - 1)) {
+            // NaN codes (as ones, 0x38) times the tokens that a row sees: it becomes NaN where that sums to
+            // something. Only numbers are added below.
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+            for (int mb = 0; mb < kMb; ++mb) {
+              f32x4 sum[RB];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
-              sum += x;
-              pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)(x * vs);
+              for (int c2 = 0; c2 < 4; ++c2) {
+                const int t = tok0 + 64 * (c2 / 2) + 8 * (c2 % 2) + 16 * g;
+                uint32_t nan[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  nan[e] = nan_codes(vt.v[mb][c2 / 2][2 * (c2 % 2) + e]);
+                  vt.v[mb][c2 / 2][2 * (c2 % 2) + e] &= ~(nan[e] * 0xffu);
+                }
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                  const bf16x8 sees = widen8(bytes_before(end[rb] - t) & 0x38383838u, bytes_before(end[rb] - t - 4) & 0x38383838u);
+                  sum[rb] = mfma16(widen8(nan[0] * 0x38u, nan[1] * 0x38u), sees, c2 == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[rb]);
+                }
+              }
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (sum[rb][j] > 0.f) o[rb][mb][j] = __builtin_nanf("");
+              __builtin_amdgcn_sched_barrier(0);
             }
-          l_run[rb] += sum;
+          }
+#pragma unroll
+          for (int mb = 0; mb < kMb; mb += 2) {
+#pragma unroll
+            for (int c2 = 0; c2 < 4; ++c2)
+#pragma unroll
+              for (int x = mb; x < mb + 2; ++x) {
+                const u32x4 w = vt.v[x][c2 / 2];
+                const bf16x8 vf = widen8(w[2 * (c2 % 2)], w[2 * (c2 % 2) + 1]);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) o[rb][x] = mfma16(vf, pf[rb][c2], o[rb][x]);
+              }
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-        if (tok0 + kBlock > len) {  // codes behind the last token may be NaN: clear them in V
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int left = len - (tok0 + 64 * half + 16 * g + 4 * e);
-              const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-#pragma unroll
-              for (int mb = 0; mb < kMb; ++mb) vt.v[mb][half][e] &= keep;
-            }
-        }
-#pragma unroll
-        for (int mb = 0; mb < kMb; mb += 2) {
-#pragma unroll
-          for (int c2 = 0; c2 < 4; ++c2)
-#pragma unroll
-            for (int x = mb; x < mb + 2; ++x) {
-              const u32x4 w = vt.v[x][c2 / 2];
-              const bf16x8 vf = widen8(w[2 * (c2 % 2)], w[2 * (c2 % 2) + 1]);
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) o[rb][x] = mfma16(vf, pf[rb][c2], o[rb][x]);
-            }
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (next >= 0) vt.load(base_of(a.v_pages, next), lane);
+        page = next;
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) vt.load(base_of(a.v_pages, next), lane);
-      page = next;
+    };
+    attend(std::false_type{});
+    // The matrix cores add 0 times a NaN to rows that mask its token: where rows see different tokens, a
+    // wave that finds a NaN does its pages again with those apart. (In the loop above this took 8%.)
+    if (a.N > 1) {
+      float worst = 0.f;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) worst += 0.f * o[rb][mb][j];
+      if (__builtin_amdgcn_ballot_w64(worst != worst)) attend(std::true_type{});
     }
 
     // The waves' states join in LDS.
@@ -561,7 +613,7 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
         y += f * *reinterpret_cast<const f32x4*>(&s_o[x][r][d0]);
       }
       y *= l > 0.f ? 1.f / l : 0.f;
-      const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) : -INFINITY;
+      const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // NaN for a row of NaN
       if (alone) {
         *reinterpret_cast<u32x2*>(a.out + (q_row + row0 + r) * D + d0) =
             __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
@@ -614,8 +666,8 @@ __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnA
       const float* pw = pr + w * step + (w == w0 ? early * (step / 2) : 0);
       const f32x4 u = *reinterpret_cast<const f32x4*>(pw + d0);
       const float part = pw[D], m_new = fmaxf(m, part);
-      const float f = m_new > -INFINITY ? fast_exp2(part - m_new) : 0.f;
-      const float keep = m_new > -INFINITY ? fast_exp2(m - m_new) : 0.f;
+      const float f = part == -INFINITY ? 0.f : fast_exp2(part - m_new);  // a NaN stays one
+      const float keep = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
       l = l * keep + f;
       y = y * keep + f * u;
       m = m_new;
@@ -624,22 +676,21 @@ __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnA
     *reinterpret_cast<u32x2*>(a.out + (q_row + r) * D + d0) =
         __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
     if (a.lse && d0 == 0)
-      a.lse[q_row + r] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+      a.lse[q_row + r] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
   }
 }
 
-template <int D>
-hipError_t cache_attn_for(const CacheAttnArgs& a, hipStream_t s) {
+template <int D, int RB>
+hipError_t cache_attn_rows(const CacheAttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
   const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
-  if (cache_rows_per_pass(a.G * a.N) == 16) {
-    cache_attn_kernel<D, 1><<<grid, kThreadsC, 0, s>>>(a);
-    if (!a.whole) cache_merge_kernel<D, 1><<<segs, kThreadsC, 0, s>>>(a);
-  } else {
-    cache_attn_kernel<D, 2><<<grid, kThreadsC, 0, s>>>(a);
-    if (!a.whole) cache_merge_kernel<D, 2><<<segs, kThreadsC, 0, s>>>(a);
-  }
+  cache_attn_kernel<D, RB><<<grid, kThreadsC, 0, s>>>(a);
+  if (!a.whole) cache_merge_kernel<D, RB><<<segs, kThreadsC, 0, s>>>(a);
   return hipGetLastError();
+}
+template <int D>
+hipError_t cache_attn_for(const CacheAttnArgs& a, hipStream_t s) {
+  return cache_rows_per_pass(a.G * a.N) == 16 ? cache_attn_rows<D, 1>(a, s) : cache_attn_rows<D, 2>(a, s);
 }
 
 }  // namespace

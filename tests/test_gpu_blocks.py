@@ -447,3 +447,55 @@ def test_gradients_against_differences(d):
         slack = HALF * np.abs(r[0]) + (HALF + FP32) * r[1] + (FP32 * r[2] + r[3] if i < 2 else 0)
         bound = float((slack * np.abs(step)).sum()) + 1e-3 * float((np.abs(r[0]) * np.abs(step)).sum())
         assert abs((plus - minus) / 2 - float((got * step).sum())) <= bound, i
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("Sq,Skv,n,ends", [(300, 300, 3, 300), (300, 300, 3, 270), (40, 2000, 16, 2000)],
+                         ids=["whole", "padded", "pieces"])
+def test_values_that_are_no_numbers_reach_only_the_rows_that_see_them(d, Sq, Skv, n, ends):
+    """NaN and infinities among the values, in causal order: earlier rows and padded ones keep their
+    bits, later ones get what the sum gives, in these dims only."""
+    rng = np.random.default_rng(d + Skv)
+    q, k, v = (bits(rng, 1, h, s, d) for h, s in ((4, Sq), (2, Skv), (2, Skv)))
+    lists = np.broadcast_to(np.arange(n, dtype=np.int32), (1, 2, -(-Sq // 128), n)).copy()
+    lens = [ends]
+    assert (ta.block_attn_fwd_workspace(1, 4, 2, Sq, Skv, d, n) > 0) == (n == 16)
+    t0 = Skv - 100 if n < 16 else Skv - 20
+    t1 = t0 + 10
+    bad = v.copy()
+    bad[:, :, t0, [3, 5, 40]] = [NAN, 0x7F80, 0xFF80]  # dim 5: +inf, then inf - inf; dim 40: -inf
+    bad[:, :, t1, [5, 7]] = [0xFF80, 0x7F80]
+    zeroed = v.copy()
+    zeroed[:, :, t0, [3, 5, 40]] = 0
+    zeroed[:, :, t1, [5, 7]] = 0
+    run = lambda x: ta.block_attn(to_dev(q), to_dev(k), to_dev(x), i32(lists), True, None, i32(lens), return_lse=True)  # noqa: E731
+    (got, lse), (ref, rlse) = run(bad), run(zeroed)
+    assert torch.equal(lse, rlse)
+    want, got = ref.float().cpu().numpy(), got.float().cpu().numpy()
+    pos = Skv - Sq + np.arange(Sq)
+    sees0, sees1 = (pos >= t0) & (pos < ends), (pos >= t1) & (pos < ends)
+    assert sees0.any() and sees1.any() and not sees0.all()
+    want[:, :, sees0, 3] = np.nan
+    want[:, :, sees0, 5] = np.inf
+    want[:, :, sees0, 40] = -np.inf
+    want[:, :, sees1, 5] = np.nan
+    want[:, :, sees1, 7] = np.inf
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("Sq,Skv,n", [(200, 400, 3), (6, 2000, 16)])
+def test_a_query_that_is_no_number_shows_in_its_row_and_gradients(Sq, Skv, n):
+    rng = np.random.default_rng(Skv)
+    q, k, v, go = (bits(rng, 1, h, s, 64) for h, s in ((2, Sq), (1, Skv), (1, Skv), (2, Sq)))
+    lists = np.broadcast_to(np.arange(n, dtype=np.int32), (1, 1, -(-Sq // 128), n)).copy()
+    bad = q.copy()
+    bad[0, 1, 4, 9] = NAN
+    (out, lse), (ref, rlse) = (ta.block_attn(to_dev(x), to_dev(k), to_dev(v), i32(lists), return_lse=True) for x in (bad, q))
+    assert out[0, 1, 4].isnan().all() and lse[0, 1, 4].isnan()
+    other = torch.ones((2, Sq), dtype=torch.bool, device="cuda")
+    other[1, 4] = False
+    assert torch.equal(out[0, other], ref[0, other]) and torch.equal(lse[0, other], rlse[0, other])
+    dq, dk, _ = ta.block_attn_grad(to_dev(bad), to_dev(k), to_dev(v), i32(lists), out, to_dev(go), lse)
+    clean = ta.block_attn_grad(to_dev(q), to_dev(k), to_dev(v), i32(lists), ref, to_dev(go), rlse)
+    assert dq[0, 1, 4].isnan().all() and torch.equal(dq[0, other], clean[0][0, other])
+    assert dk[0, 0, : 128 * n].isnan().all()

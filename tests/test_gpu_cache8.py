@@ -332,3 +332,28 @@ def test_wrappers_refuse():
         ta.cache_write(k[:, :1], k, *gpu, t, lens)
     with pytest.raises(ta.TileAttnError, match="overlap"):
         ta.cache_attn(q[:, :, :, :], *gpu, t, lens, out=q)
+
+
+@pytest.mark.parametrize("width", [3, 40])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_a_later_token_that_is_no_number_leaves_earlier_rows(d, width):
+    """NaN keys and values in the last two of five new tokens: the three rows before keep their bits,
+    the others are NaN in the dims of the values."""
+    rng = np.random.default_rng(d + width)
+    cache, table = held(rng, 1, 2, d, [300], width)
+    q = bits(rng, 1, 6, 5, d)
+    p, at = table[0, 2], 298 - 256
+    clean = [x.copy() for x in cache]
+    clean[1][p, :, 9, at:at + 2] = 0
+    cache[1][p, 0, 9, at], cache[1][p, 0, 9, at + 1] = 127, 255
+    cache[1][p, 1, 9, at] = 255
+    run = lambda c: ta.cache_attn(to_dev(q), *to_gpu(c), i32(table), i32([300]), return_lse=True)  # noqa: E731
+    (got, lse), (ref, rlse) = run(cache), run(clean)
+    assert torch.equal(lse, rlse)
+    want = ref.clone()
+    want[:, :, 3:, 9] = float("nan")
+    assert np.array_equal(got.float().cpu().numpy(), want.float().cpu().numpy(), equal_nan=True)
+    cache[0][p, :, at, 4] = 127  # now a key: the rows that see it are NaN, and so is their sum
+    got, lse = run(cache)
+    assert torch.equal(got[:, :, :3], ref[:, :, :3]) and torch.equal(lse[:, :, :3], rlse[:, :, :3])
+    assert got[:, :, 3:].isnan().all() and lse[:, :, 3:].isnan().all()
