@@ -101,14 +101,23 @@ def cache_attn_fwd(q, k_pages, v_pages, k_scales, v_scales, table, lens, per_hea
 def _want(t, name: str, shape, dtype, device) -> None:
     """t is a contiguous tensor of this shape and type on this GPU: checked before anything is
     launched, since the kernels read and write that many elements."""
+    if t.shape == shape and t.dtype is dtype and t.device == device and t.is_contiguous():
+        return
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.device != device or not t.is_cuda:
+    if t.device != device:
         raise ValueError(f"{name} must be on the GPU {device}, got {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _out(out, shape, dtype, device):
+    """The output that the caller gave, or a new one."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _want(out, "out", shape, dtype, device)
+    return out
 
 
 def _on(device):
@@ -145,15 +154,13 @@ def _workspace(n: int, device):
 def block_means(x, lens=None, out=None):
     """Means of every block of 128 tokens: x [B, H, S, d] bf16 -> [B, H, ceil(S / 128), d] bf16; lens
     (int32 [B]) leaves out the tokens behind a sequence's end."""
-    if x.dim() != 4:
-        raise ValueError("expected a [B, H, S, d] tensor")
+    if x.dim() != 4 or not x.is_cuda:
+        raise ValueError("x must be a [B, H, S, d] tensor on a GPU")
     B, H, S, d = x.shape
     _want(x, "x", x.shape, torch.bfloat16, x.device)
     shape = (B, H, -(-S // BLOCK_TOKENS), d)
     with _on(x.device):
-        if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
-        _want(out, "out", shape, torch.bfloat16, x.device)
+        out = _out(out, shape, torch.bfloat16, x.device)
         _lens(lens, (B,), x.device)
         block_attn_means(x, out, B, H, S, d, lens, _current(x.device))
     return out
@@ -171,9 +178,7 @@ def block_lists(q, kmeans, Skv: int, n_list: int, causal=False, sink: int = 0, l
     _want(kmeans, "kmeans", (B, Hkv, nb, d), torch.bfloat16, q.device)
     shape = (B, Hkv, -(-Sq // BLOCK_TOKENS), n_list)
     with _on(q.device):
-        if out is None:
-            out = torch.empty(shape, dtype=torch.int32, device=q.device)
-        _want(out, "out", shape, torch.int32, q.device)
+        out = _out(out, shape, torch.int32, q.device)
         _lens(lens, (B,), q.device)
         block_attn_lists(q, kmeans, out, B, H, Hkv, Sq, Skv, d, n_list, sink, local, causal, lens,
                          _current(q.device))
@@ -199,7 +204,8 @@ def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=No
     with _on(q.device):
         if out is None:
             out = torch.empty_like(q)
-        _want(out, "out", q.shape, torch.bfloat16, q.device)
+        else:
+            _want(out, "out", q.shape, torch.bfloat16, q.device)
         _lens(lens, (B,), q.device)
         lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device) if return_lse else None
         n = block_attn_fwd_workspace(*sizes)
@@ -279,7 +285,8 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
     with _on(q.device):
         if out is None:
             out = torch.empty_like(q)
-        _want(out, "out", q.shape, torch.bfloat16, q.device)
+        else:
+            _want(out, "out", q.shape, torch.bfloat16, q.device)
         lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device) if return_lse else None
         n = cache_attn_fwd_workspace(B, H, Hkv, N, d, width)
         cache_attn_fwd(q, k_pages, v_pages, k_scales, v_scales, table, lens, per_head, out, lse, B, H, Hkv, N, d,
