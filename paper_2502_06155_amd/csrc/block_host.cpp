@@ -122,7 +122,12 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   const int64_t held = lists_of(g) * std::min(g.n_list, g.nb), cols = (int64_t)g.B * g.Hkv * g.nb;
   const int64_t mean = (held + cols - 1) / cols;
   const int64_t most = std::max(2 * mean, held / (8 * kSlots));
-  const int64_t least = std::min<int64_t>(most, (3 + g.G) / g.G);
+  // Where the columns themselves occupy two fifths of the resident workgroups (one a compute unit at
+  // d = 128), the average column stays whole. Whole and cut: 216 columns of 6, d = 64 50 and 53 us; 378 of
+  // 12, d = 96 118 and 129; 160 of 8, d = 128 82 and 90; below the bound 188 of 20 (six query heads
+  // each), d = 64 327 and 272; 144 of 9 41.5 and 38.5.
+  const bool enough = 5 * cols >= (g.d == 128 ? kSlots : 2 * kSlots);
+  const int64_t least = std::min(most, std::max<int64_t>((3 + g.G) / g.G, enough ? mean : 0));
   p.entries = (int)std::min<int64_t>(INT_MAX, std::min(most, std::max(least, (held + kSlots - 1) / kSlots)));
   p.pieces_k = (g.nq + p.entries - 1) / p.entries;
   // A column in ceil(n / entries) > 1 pieces has n > entries, so fewer than 2 n / entries pieces.

@@ -150,7 +150,8 @@ def _piece_bound(B, H, Hkv, Sq, Skv, n_list):
     nq, nb = -(-Sq // 128), -(-Skv // 128)
     held, cols, G = B * Hkv * nq * min(n_list, nb), B * Hkv * nb, H // Hkv
     most = max(2 * -(-held // cols), held // 4096)
-    entries = min(most, max(min(most, (3 + G) // G), -(-held // 512)))
+    least = max((3 + G) // G, -(-held // cols) if 5 * cols >= 1024 else 0)  # at d = 64
+    entries = min(most, max(min(most, least), -(-held // 512)))
     pieces = -(-nq // entries)
     return nq, nb, held, cols, entries, 0 if pieces == 1 else min(cols * pieces, 2 * held // entries)
 
