@@ -48,6 +48,9 @@ __device__ __forceinline__ float bf16_at(u32x4 w, int e) {
   return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
 }
 
+// Bound by the bytes, and for single tokens by the latency of its loads: table and length, scale and
+// token, then the codes. Two prompts of 8191 tokens, 8 heads of 128: 23.4 us for 101 MB (4.3 TB/s; a large
+// copy 5.0); one token of 32 sequences: 5.3 us.
 // One workgroup writes K (blockIdx.z = 0) or V (1) of one (sequence, key head, touched page). A thread
 // holds 16-byte pieces (8 dims) of four tokens in a row, read once: the page's maximum needs them all
 // before the first can be rounded. K codes go out as they lie, V's through LDS.
@@ -182,7 +185,8 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 // attention
 //
 // The cache's bytes bound this: a decoding step reads every code once and does 4 G N operations a
-// byte. A wave takes a page at a time, its codes from memory straight into registers, one page ahead,
+// byte (32 sequences of 512 to 65536 tokens, 8 key heads of 128: 185 to 188 us for 0.9 GB, 4.9 TB/s; a
+// large copy reaches 5.0). A wave takes a page at a time, its codes from memory straight into registers, one page ahead,
 // as the operands of v_mfma_f32_16x16x32_bf16 (A: lane l holds row l % 16 and the k indices 8 (l / 16) .. + 7; B the
 // same with columns; C: column l % 16, rows 4 (l / 16) + j):
 //   S^T = K Q^T. The matrix instruction adds over k in any order, so a lane's 16 bytes of a K row,
