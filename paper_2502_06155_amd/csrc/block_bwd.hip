@@ -9,7 +9,8 @@
 //            launch the lists turned round: for every key block a bitmap (its column) of the query
 //            blocks that list it, 32 of them a workgroup.
 //   plan     deals the columns out to the XCDs by work, cuts long ones (a block that every query
-//            keeps) into pieces of at most `entries` query blocks, and orders the pieces longest first.
+//            keeps) into pieces of at most `entries` query blocks, and orders the pieces longest first;
+//            at d = 128 (and enough work) instead one line of all columns, cut into even stretches.
 //   dq       one workgroup per unit of 128 query rows, over its list's key tiles:
 //            S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T; a lane owns one query.
 //   dk, dv   one workgroup per piece of a key block (128 keys, 4 waves of 32), over the 64-row
@@ -18,8 +19,8 @@
 //   sum      adds the pieces of cut units, in order.
 // Measured: 24 heads of 28800 tokens, 32 of 225 blocks each, d = 96: 3455 us, 787 TFLOP/s as five products
 // and 1100 as the seven that run (a library product of 16384^3: 1312; vector issue beside the matrix
-// cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1276 us, of it dk, dv 760,
-// dq 490, prep 22, sum 19, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 35 for both
+// cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1200 us, of it dk, dv 660,
+// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 35 for both
 // passes, whose columns and units are few, and three short launches around them.
 // S and dP are formed in both passes: adding dq up from the key side would take fp32 atomics, whose
 // order changes results, and more L2 traffic than the matrix cores' time it saves.
@@ -187,6 +188,80 @@ __global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwd
     for (int p = 0; p < pieces; ++p)
       if (at + p < a.items_cap) items[at + p] = int2{(int)x, p};
   });
+}
+
+// The plan at d = 128, where the key side runs one workgroup a compute unit and an item of the plan above
+// was a third of what a unit had to do (units were busy 75% of the launch, so 92%; 16 heads on 4, 16384
+// tokens, causal: 1270 us and 1210 in all): all columns form one line, a
+// column of n query blocks col_start + 4 n long (col_start: what its start and end, and in causal order
+// the masked tiles of its first block, take in quarters of a query block), and `workers` workgroups take
+// even stretches of it. A column that several share leaves one partial sum each.
+// plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first slot, + 3 = its first
+// worker; items[w] = {column, place in it} where worker w starts; counts[0] = workers.
+struct KeyLine {
+  int64_t each, more;  // every worker's part; workers with one more
+  __device__ __forceinline__ KeyLine(int64_t total, int workers) : each(total / workers), more(total % workers) {}
+  __device__ __forceinline__ int64_t start(int w) const { return w * each + min((int64_t)w, more); }
+  __device__ __forceinline__ int worker(int64_t x) const {
+    const int64_t y = x - more * (each + 1);
+    return (int)(y < 0 ? x / (each + 1) : more + y / each);
+  }
+};
+// The first of a column's n query blocks that lies at `at` or behind it.
+__device__ __forceinline__ int line_entry(int at, int col_start, int n) { return min(max((at - col_start + 3) >> 2, 0), n); }
+
+__global__ __launch_bounds__(kPlanThreads) void block_line_kernel(const BlockBwdArgs a, uint32_t cols) {
+  __shared__ int64_t wave_sums[kPlanThreads / 64];
+  const int words = query_words(a.g);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const uint32_t each = (cols + kPlanThreads - 1) / kPlanThreads;
+  const uint32_t x0 = min(cols, tid * each), x1 = min(cols, x0 + each);
+  auto blocks_of = [&](uint32_t x) {
+    int n = 0;
+#pragma unroll 4
+    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
+    return n;
+  };
+  int64_t own = 0;
+  for (uint32_t x = x0; x < x1; ++x) own += blocks_of(x);
+  int64_t upto = own;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t y = __shfl_up((long long)upto, s);
+    if (lane >= s) upto += y;
+  }
+  if (lane == 63) wave_sums[wave] = upto;
+  __syncthreads();
+  int64_t total = 0, before = upto - own;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) before += wave_sums[w];
+    total += wave_sums[w];
+  }
+  total = 4 * total + (int64_t)a.col_start * cols;
+  const int workers = (int)max((int64_t)1, min((int64_t)kLineWorkers, total / (4 * a.entries)));
+  const KeyLine line(total, workers);
+  int2* starts = reinterpret_cast<int2*>(a.items);
+  if (blockIdx.x == 0 && tid == 0) {
+    a.counts[0] = workers;
+    starts[workers] = int2{(int)cols, 0};
+  }
+  int64_t at = 4 * before + (int64_t)a.col_start * x0;
+  for (uint32_t x = x0; x < x1; ++x) {
+    const int n = blocks_of(x), length = a.col_start + 4 * n;
+    if (x % gridDim.x == blockIdx.x) {
+      const int first = line.worker(at + (n ? a.col_start : 0)), last = n ? line.worker(at + length - 4) : first;
+      const int pieces = last - first + 1;
+      a.plan[4 * (size_t)x] = n;
+      a.plan[4 * (size_t)x + 1] = pieces;
+      a.plan[4 * (size_t)x + 2] = pieces > 1 ? atomicAdd(&a.counts[8], pieces) : 0;
+      a.plan[4 * (size_t)x + 3] = first;
+      int w = line.worker(at);
+      if (line.start(w) < at) ++w;
+      for (; w < workers && line.start(w) < at + length; ++w) starts[w] = int2{(int)x, (int)(line.start(w) - at)};
+    }
+    at += length;
+  }
 }
 
 // P = exp2(c s - lse2) clamped to [0, 1] (the exponent is <= 0 up to rounding for kept pairs; the
@@ -427,14 +502,21 @@ struct KeyPiece {
   int piece, pieces, all;  // all: query blocks of the column
   int j, bh, b, h, len;
   size_t group_row;        // row of the group's first head in [B, H, Sq]
+  int e0, e1;              // the piece's query blocks: these of the column's, in order
   // Every XCD runs the items of its share in the plan's order; false past their end.
   __device__ __forceinline__ bool find(const BlockBwdArgs& a, uint32_t id) {
-    const BlockGeo& g = a.g;
     if (id / 8 >= (uint32_t)a.counts[id % 8]) return false;
     const int2 item = reinterpret_cast<const int2*>(a.items)[(size_t)(id % 8) * a.items_cap + id / 8];
     // The same in every lane; in scalar registers the tiles' addresses are scalar work.
-    col = (uint32_t)__builtin_amdgcn_readfirstlane(item.x);
+    place(a, (uint32_t)__builtin_amdgcn_readfirstlane(item.x));
     piece = __builtin_amdgcn_readfirstlane(item.y);
+    e0 = (int)((int64_t)all * piece / pieces);
+    e1 = (int)((int64_t)all * (piece + 1) / pieces);
+    return true;
+  }
+  __device__ __forceinline__ void place(const BlockBwdArgs& a, uint32_t column) {
+    const BlockGeo& g = a.g;
+    col = column;
     all = __builtin_amdgcn_readfirstlane(a.plan[4 * (size_t)col]);
     pieces = __builtin_amdgcn_readfirstlane(a.plan[4 * (size_t)col + 1]);
     j = (int)(col % g.nb);
@@ -443,10 +525,7 @@ struct KeyPiece {
     h = bh - b * g.Hkv;
     len = seq_len(g, b);
     group_row = ((size_t)b * g.H + (size_t)h * g.G) * g.Sq;
-    return true;
   }
-  __device__ __forceinline__ int begin() const { return (int)((int64_t)all * piece / pieces); }
-  __device__ __forceinline__ int end() const { return (int)((int64_t)all * (piece + 1) / pieces); }
   __device__ __forceinline__ void load_bits(const BlockBwdArgs& a, uint32_t* bits, int words) const {
     for (int x = threadIdx.x; x < words; x += kThreadsB) bits[x] = a.cols[(size_t)col * words + x];
     __syncthreads();
@@ -513,7 +592,7 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
   }
 
   QueryTiles nxt;
-  nxt.start(g, kp.len, bits, words, kp.begin(), kp.end());
+  nxt.start(g, kp.len, bits, words, kp.e0, kp.e1);
   if (!nxt.done()) {
     TileLoads<D> ld;
     ld.init(wave, lane);
@@ -703,13 +782,11 @@ constexpr int kRingBlock = 32 * 128;                  // elements of a 32-row bl
 constexpr int kRingSlot = 2 * kRingBlock + 256;       // Q and dO rows, then lse2 and -delta (64 floats each)
 
 template <bool CAUSAL>
-__device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, uint32_t id, uint16_t* ring, uint32_t* bits) {
+__device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, const KeyPiece& kp, uint16_t* ring, uint32_t* bits) {
   constexpr int D = 128, kC = D / 16, kMb = D / 32;
   constexpr int kLd = kRingBlock * 2 / 2048;          // loads per wave and block (two waves per tensor)
   constexpr int kAhead = 3;
   const BlockGeo& g = a.g;
-  KeyPiece kp;
-  if (!kp.find(a, id)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int words = query_words(g);
   kp.load_bits(a, bits, words);
@@ -726,7 +803,7 @@ __device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, uint32_t i
   for (int mb = 0; mb < kMb; ++mb) dk[mb] = dv[mb] = f32x16{};
 
   QueryTiles tiles;
-  tiles.start(g, kp.len, bits, words, kp.begin(), kp.end());
+  tiles.start(g, kp.len, bits, words, kp.e0, kp.e1);
   if constexpr (CAUSAL) {
     // The column's first blocks, up to where every row comes after every key of the block.
     const int own_last = kp.j * kBlock + kBlock - 1;
@@ -773,7 +850,7 @@ __device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, uint32_t i
   if (!tiles.done()) {
     const int rows = min(g.Sq, kp.len - g.off), last = (rows - 1) / kBlock, short_rows = rows - last * kBlock;
     nb = tiles.walk.left * 4;
-    if (kp.end() == kp.all && (bits[last >> 5] >> (last & 31)) & 1) nb -= 4 - (short_rows + 31) / 32;
+    if (kp.e1 == kp.all && (bits[last >> 5] >> (last & 31)) & 1) nb -= 4 - (short_rows + 31) / 32;
     nb = __builtin_amdgcn_readfirstlane(nb * g.G);
   }
   if (nb > 0) {
@@ -998,12 +1075,43 @@ __global__ __launch_bounds__(kThreadsB, 2) void block_grad_kernel(const BlockBwd
   else dq_unit<D>(a, blockIdx.x - key_wgs, s0, s1, bits);
 }
 
-// d = 128: each pass has a launch of its own, the key side one workgroup a compute unit.
+// d = 128: each pass has a launch of its own, the key side one workgroup a compute unit, each with an item
+// of the plan or (a.line) with its stretch of the line of all columns; an XCD's workgroups take
+// neighbouring ones.
 template <bool CAUSAL>
-__global__ __launch_bounds__(kThreadsB, 1) void block_dkdv_kernel(const BlockBwdArgs a) {
+__global__ __launch_bounds__(kThreadsB, 1) void block_dkdv_kernel(const BlockBwdArgs a, int cols) {
   __shared__ __attribute__((aligned(1024))) uint16_t ring[kRing * kRingSlot];
   __shared__ uint32_t bits[kBlockWords];
-  dkdv_roll_unit<CAUSAL>(a, blockIdx.x, ring, bits);
+  KeyPiece kp;
+  int w = 0, first, first_at = 0, last, last_at = 0;
+  if (a.line) {
+    const int workers = a.counts[0], id = (int)blockIdx.x;
+    w = workers == kLineWorkers ? id % 8 * (kLineWorkers / 8) + id / 8 : id;
+    if (w >= workers) return;
+    const int2* starts = reinterpret_cast<const int2*>(a.items);
+    const int2 from = starts[w], to = starts[w + 1];
+    first = __builtin_amdgcn_readfirstlane(from.x);
+    first_at = __builtin_amdgcn_readfirstlane(from.y);
+    last = __builtin_amdgcn_readfirstlane(to.x);
+    last_at = __builtin_amdgcn_readfirstlane(to.y);
+  } else {
+    if (!kp.find(a, blockIdx.x)) return;
+    first = last = (int)kp.col;
+  }
+#pragma unroll 1
+  for (int col = first; col <= last && col < cols; ++col) {
+    if (a.line) {
+      kp.place(a, (uint32_t)col);
+      const int at = col == first ? first_at : 0;
+      kp.e0 = line_entry(at, a.col_start, kp.all);
+      kp.e1 = col == last ? line_entry(last_at, a.col_start, kp.all) : kp.all;
+      // A column without query blocks gets its zeros from the workgroup whose stretch holds its start.
+      if (kp.all == 0 ? at != 0 || (col == last && last_at == 0) : kp.e0 >= kp.e1) continue;
+      kp.piece = w - __builtin_amdgcn_readfirstlane(a.plan[4 * (size_t)col + 3]);
+    }
+    dkdv_roll_unit<CAUSAL>(a, kp, ring, bits);
+    __syncthreads();  // the next column's loads overwrite what slower waves still read
+  }
 }
 template <int D>
 __global__ __launch_bounds__(kThreadsB, 2) void block_dq_kernel(const BlockBwdArgs a) {
@@ -1075,11 +1183,12 @@ hipError_t block_bwd_for(const BlockBwdArgs& a, hipStream_t s) {
   const uint32_t words = (uint32_t)((int64_t)g.B * g.Hkv * ((g.nq + 31) / 32));
   const size_t lds = std::max((size_t)kPrepRowsB * (D / 8), (size_t)g.nb) * 4;
   block_prep_kernel<D><<<prep + words, kThreadsB, lds, s>>>(a, rows, prep);
-  block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
-  const uint32_t keys = 8 * (uint32_t)a.items_cap, queries = unit_grid(g, a.units * a.pieces_q);
+  if (a.line) block_line_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
+  else block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
+  const uint32_t keys = a.line ? kLineWorkers : 8 * (uint32_t)a.items_cap, queries = unit_grid(g, a.units * a.pieces_q);
   if constexpr (D == 128) {
-    if (g.causal) block_dkdv_kernel<true><<<keys, kThreadsB, 0, s>>>(a);
-    else block_dkdv_kernel<false><<<keys, kThreadsB, 0, s>>>(a);
+    if (g.causal) block_dkdv_kernel<true><<<keys, kThreadsB, 0, s>>>(a, (int)cols);
+    else block_dkdv_kernel<false><<<keys, kThreadsB, 0, s>>>(a, (int)cols);
     block_dq_kernel<D><<<queries, kThreadsB, 0, s>>>(a);
   } else {
     if (g.causal) block_grad_kernel<D, true><<<keys + queries, kThreadsB, 0, s>>>(a, keys);

@@ -107,6 +107,7 @@ size_t fwd_bytes(const BlockGeo& g) {
 // How the gradient's key side is cut, and where things lie in the workspace.
 struct BwdPlan {
   int entries, pieces_q, pieces_k;
+  bool line;
   int64_t slots, items_cap;
   size_t off_ndelta, off_cols, off_plan, off_counts, off_items, off_q, off_k, bytes;
 };
@@ -139,6 +140,18 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   // is cut into at most 1 + (n - 1) / entries pieces.
   const int64_t share_blocks = (5 * held + 31) / 32 + (cols + 7) / 8 + g.nq;
   p.items_cap = std::min(cols * p.pieces_k, (5 * cols + 7) / 8 + share_blocks / p.entries);
+  // At d = 128 one line of all columns, cut into kLineWorkers stretches at most, of four units of 128 rows
+  // at least. Each end of a stretch adds a piece to one column and makes it one of several pieces. (Line
+  // and items: 4 key heads of 16384, 24 blocks, causal 1240 and 1335 us; 1 of 7000, 20 blocks 108 and
+  // 128. From 6 units a workgroup on: 6 heads of 8000 are 18, 174 and 185; 8 of 2500 are 5, 87 and 86; 16
+  // of 1100 are 2, 71 and 65.)
+  p.line = g.d == 128 && held * g.G >= 6 * kLineWorkers;
+  if (p.line) {
+    p.entries = (3 + g.G) / g.G;
+    p.pieces_k = g.nq > 1 ? 2 : 1;
+    p.slots = g.nq > 1 ? 2 * (kLineWorkers - 1) : 0;
+    p.items_cap = kLineWorkers / 8 + 1;
+  }
   const size_t rows = (size_t)g.B * g.H * g.Sq;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t at = up(rows * 4);
@@ -351,6 +364,10 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
   a.entries = p.entries;
   a.pieces_k = p.pieces_k;
   a.slots = (int)p.slots;
+  // A column's start and end take about four units' time, and the masked tiles of its own query block
+  // another block's.
+  a.line = p.line;
+  a.col_start = (16 + a.g.G - 1) / a.g.G + (causal ? 4 : 0);
   char* ws = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(ws);
   a.ndelta = reinterpret_cast<float*>(ws + p.off_ndelta);

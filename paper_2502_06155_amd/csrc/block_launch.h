@@ -16,6 +16,7 @@ struct BlockGeo {
   const int32_t* lens;  // [B] or null
 };
 
+constexpr int kLineWorkers = 256;  // workgroups of the gradients' key side at d = 128
 constexpr int kCacheSegment = 3;  // what a (sequence, head) costs cache attention beside its pages
 
 struct MeansArgs {
@@ -66,15 +67,17 @@ struct BlockBwdArgs {
   uint32_t flip, keep;
   int units;
   int pieces_q;      // pieces of a query unit's list
-  int entries;       // query blocks per piece of a key block's column, at most
+  int line;          // the key side takes stretches of the line of all columns, not the plan's items
+  int entries;       // query blocks per piece of a key block's column, at most (line: of a stretch, at least)
+  int col_start;     // line: what a column costs beside its query blocks, in quarters of one
   int pieces_k;      // pieces of a key block at most
   int slots;         // partial dk, dv blocks there is room for
   float* lse2;       // [B, H, Sq]: base-2 lse, +inf for rows without tokens
   float* ndelta;     // [B, H, Sq]: -<dout, out>
   uint32_t* cols;    // [B, Hkv, nb][nq / 32 words]: the query blocks that list a key block
-  int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot
-  int32_t* counts;   // [9]: items of each XCD's share; the slot counter
-  int32_t* items;    // [8][items_cap][2]: column, piece
+  int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot, first worker (line)
+  int32_t* counts;   // [9]: items of each XCD's share (line: workers); the slot counter
+  int32_t* items;    // [8][items_cap][2]: column, piece; line: where each worker starts
   int items_cap;     // items of an XCD's share, at most
   float* part_q;     // pieces_q > 1: fp32 [list][unit][piece][128][d]
   float* part_k;     // fp32 [slot][2][128][d]: dk, dv

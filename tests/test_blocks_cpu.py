@@ -229,3 +229,43 @@ def test_header_names_the_limits():
         hdr = f.read()
     assert "#define TA_BLOCK 128" in hdr and ta.BLOCK_TOKENS == 128
     assert np.log2(128 * 16384) == 21 and "#define TA_MAX_BLOCKS 16384" in hdr
+
+
+@pytest.mark.parametrize("cols,nq,G,causal", [(1, 1, 1, 0), (3, 2, 4, 1), (8, 300, 1, 0), (128, 32, 4, 1), (512, 128, 4, 1),
+                                              (5000, 40, 2, 0), (40, 16384, 1, 1)])
+def test_the_line_of_columns_gives_every_query_block_to_one_worker(cols, nq, G, causal):
+    """The cut of the gradients' key side at d = 128: even stretches of the line of all columns, pieces
+    of a column numbered by their workers, partial sums within the reserved 510."""
+    start, least = -(-16 // G) + 4 * causal, 4 * ((3 + G) // G)
+    entry = lambda at, n: int(min(max((at - start + 3) >> 2, 0), n))  # noqa: E731
+    rng = np.random.default_rng(cols + nq)
+    for trial in range(20):
+        counts = rng.integers(0, nq + 1, cols) * (rng.random(cols) < [1, 0.5, 0.02, 0][trial % 4])
+        total = int(4 * counts.sum() + start * cols)
+        workers = max(1, min(256, total // least))
+        each, more = divmod(total, workers)
+        begin = lambda w: w * each + min(w, more)  # noqa: E731
+        worker = lambda x: x // (each + 1) if x < more * (each + 1) else more + (x - more * (each + 1)) // each  # noqa: E731
+        at = np.concatenate([[0], np.cumsum(start + 4 * counts)])
+        slots, pieces = 0, []
+        for c, n in enumerate(counts):
+            first = worker(int(at[c]) + (start if n else 0))
+            last = worker(int(at[c + 1]) - 4) if n else first
+            pieces.append((first, last - first + 1))
+            slots += last - first + 1 if last > first else 0
+        assert slots <= 510
+        seen = [[] for _ in range(cols)]
+        starts = [(int(np.searchsorted(at, begin(w), "right")) - 1, 0) for w in range(workers)] + [(cols, 0)]
+        starts = [(c, begin(w) - int(at[c])) for w, (c, _) in enumerate(starts[:-1])] + [(cols, 0)]
+        for w in range(workers):
+            (c0, a0), (c1, a1) = starts[w], starts[w + 1]
+            for c in range(c0, min(c1, cols - 1) + 1):
+                n, a = int(counts[c]), a0 if c == c0 else 0
+                e0, e1 = entry(a, n), entry(a1, n) if c == c1 else n
+                if (a != 0 or (c == c1 and a1 == 0)) if n == 0 else e0 >= e1:
+                    continue
+                assert w - pieces[c][0] == len(seen[c])
+                seen[c].append((e0, e1))
+        for c, n in enumerate(counts):
+            assert len(seen[c]) == pieces[c][1]
+            assert seen[c][0][0] == 0 and seen[c][-1][1] == n and all(x[1] == y[0] for x, y in zip(seen[c], seen[c][1:]))

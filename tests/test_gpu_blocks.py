@@ -73,6 +73,9 @@ CASES = [
     (1, 2, 2, 150, 650, 96, 4, True, [600], "near"),
     (1, 5, 1, 40, 300, 128, 3, True, None, "random"),
     (1, 1, 1, 640, 640, 64, 40, True, None, "random"),
+    (1, 48, 2, 700, 700, 128, 6, True, [650], "near"),  # the key side by stretches of a line, columns cut often
+    (2, 26, 1, 900, 900, 128, 8, False, [900, 300], "empty"),
+    (1, 36, 1, 300, 1500, 128, 20, True, None, "random"),
 ]
 IDS = ["-".join(str(x) for x in c[:7]) + ("-causal" if c[7] else "") + ("-" + c[9]) for c in CASES]
 
