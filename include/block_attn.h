@@ -115,7 +115,8 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
  * most 448; a page that holds tokens already keeps the larger of its scale and that, and its old
  * codes are rounded again where the scale grew. Rounding is to nearest, ties to even; infinities
  * become the largest code, NaN stays NaN. Tokens behind the last one are left as they were.
- * k, v: bf16 [B, Hkv, N, d]. Pages that are written belong to one sequence.
+ * k, v: bf16 [B, Hkv, N, d]. A page that is written belongs to one sequence and stands once in its
+ * row of the table.
  */
 int cache_attn_write(const void* k, const void* v, void* k_pages, void* v_pages, float* k_scales,
                      float* v_scales, const int32_t* table, const int32_t* lens, const int32_t* n_new,

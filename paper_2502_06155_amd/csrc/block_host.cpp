@@ -117,9 +117,9 @@ BwdPlan plan_bwd(const BlockGeo& g) {
   // Query blocks that all columns hold together, at most, and what a column holds on average. A
   // piece takes up to twice that, or an eighth of a resident workgroup's share of all work where
   // that is more (long launches even out by themselves); in launches of few columns less, so that
-  // about one piece per resident workgroup forms, but not below four units of 128 rows. 16 heads of
-  // 8192 positions, 16 blocks each: 485 us so, 519 at two pieces per workgroup, 648 at four; 4 heads of
-  // 16384, four query heads each, 24 blocks, causal: 1280 (half a piece 1312, two 1290, four 1433).
+  // about one piece per resident workgroup forms, but not below four units of 128 rows. 8 heads of
+  // 16384 positions, 24 blocks each, causal, d = 96: 458 us so, 454 at half a piece per workgroup, 472 at
+  // two, 517 at four; 6 heads of 8000, 12 blocks, with average columns cut 129, whole (below) 118.
   const int64_t held = lists_of(g) * std::min(g.n_list, g.nb), cols = (int64_t)g.B * g.Hkv * g.nb;
   const int64_t mean = (held + cols - 1) / cols;
   const int64_t most = std::max(2 * mean, held / (8 * kSlots));
