@@ -88,19 +88,19 @@ int64_t lists_of(const BlockGeo& g) { return (int64_t)g.B * g.Hkv * g.nq; }
 // 128-row units per list: one per head of full query blocks; a single short block packs its heads.
 int units_of(const BlockGeo& g) { return g.nq > 1 ? g.G : (int)(((int64_t)g.G * g.Sq + kBlock - 1) / kBlock); }
 // Pieces of every unit's list: enough workgroups for the device, two blocks each at least, where that
-// takes `worth` blocks off a workgroup's way. Forward: 4 (about 2 us a block at most; joining costs 4 us
-// and a launch: 4 blocks in halves 13.7 us, whole 11.6; 6 in halves 25.3 and 18.8). Gradients: any, the
-// sums of the key side are launched all the same.
-int pieces_of(const BlockGeo& g, int worth) {
+// takes four blocks off a workgroup's way (about 2 us a block at most; joining costs 4 us and a launch.
+// Forward: 4 blocks in halves 13.7 us, whole 11.6; 6 in halves 25.3 and 18.8. Gradients of 12 heads of
+// 2251 tokens, 6 blocks: in halves 49.6, whole 48.8).
+constexpr int64_t kPieceWorth = 4;
+int pieces_of(const BlockGeo& g) {
   const int64_t units = lists_of(g) * units_of(g);
   const int64_t held = std::min(g.n_list, g.nb);
   const int64_t pieces = std::max<int64_t>(1, std::min(kSlots / units, held / 2));
-  return held - (held + pieces - 1) / pieces >= worth ? (int)pieces : 1;
+  return held - (held + pieces - 1) / pieces >= kPieceWorth ? (int)pieces : 1;
 }
-constexpr int kWorthForward = 4, kWorthGradients = 1;
 
 size_t fwd_bytes(const BlockGeo& g) {
-  const int p = pieces_of(g, kWorthForward);
+  const int p = pieces_of(g);
   return p == 1 ? 0 : (size_t)(lists_of(g) * units_of(g)) * p * kBlock * (g.d + 4) * sizeof(float);
 }
 
@@ -113,7 +113,7 @@ struct BwdPlan {
 };
 BwdPlan plan_bwd(const BlockGeo& g) {
   BwdPlan p;
-  p.pieces_q = pieces_of(g, kWorthGradients);
+  p.pieces_q = pieces_of(g);
   // Query blocks that all columns hold together, at most, and what a column holds on average. A
   // piece takes up to twice that, or an eighth of a resident workgroup's share of all work where
   // that is more (long launches even out by themselves); in launches of few columns less, so that
@@ -307,7 +307,7 @@ int block_attn_fwd(const void* q, const void* k, const void* v, const int32_t* l
   a.lse = lse;
   fold_scale(scale, a.c, a.qflip, a.qmask);
   a.units = units_of(a.g);
-  a.pieces = pieces_of(a.g, kWorthForward);
+  a.pieces = pieces_of(a.g);
   a.part = static_cast<float*>(workspace);
   if (int st = check_grid((double)lists_of(a.g) * a.units * a.pieces)) return st;
   return launched(launch_block_fwd(a, static_cast<hipStream_t>(stream)));
