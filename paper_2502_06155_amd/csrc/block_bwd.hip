@@ -22,6 +22,8 @@
 // cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1200 us, of it dk, dv 660,
 // dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 35 for both
 // passes, whose columns and units are few, and three short launches around them.
+// Roundings: P and dS to bf16 before they enter a product (the matrix cores take nothing wider at this
+// rate), and the results at the end; S, dP, delta, all sums and cut pieces' parts are fp32.
 // S and dP are formed in both passes: adding dq up from the key side would take fp32 atomics, whose
 // order changes results, and more L2 traffic than the matrix cores' time it saves.
 #include <hip/hip_runtime.h>
