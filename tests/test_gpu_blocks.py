@@ -502,3 +502,39 @@ def test_a_query_that_is_no_number_shows_in_its_row_and_gradients(Sq, Skv, n):
     clean = ta.block_attn_grad(to_dev(q), to_dev(k), to_dev(v), i32(lists), ref, to_dev(go), rlse)
     assert dq[0, 1, 4].isnan().all() and torch.equal(dq[0, other], clean[0][0, other])
     assert dk[0, 0, : 128 * n].isnan().all()
+
+
+def test_stretches_of_the_line_whatever_the_workspace_holds_and_replayed():
+    """d = 128 with work enough for the key side's line: any contents of the workspace, three streams at
+    once and replays of a captured call give the same bits."""
+    B, H, Hkv, S, d, n = 1, 48, 2, 900, 128, 6
+    rng = np.random.default_rng(31)
+    q, k, v, go = (to_dev(bits(rng, B, h, S, d)) for h in (H, Hkv, Hkv, H))
+    lists = some_lists(rng, B, Hkv, S, S, n, "near")
+    lists[..., 1] = 0
+    lists, lens = i32(lists), i32([850])
+    out, lse = ta.block_attn(q, k, v, lists, True, None, lens, return_lse=True)
+    ref = ta.block_attn_grad(q, k, v, lists, out, go, lse, True, None, lens)
+    bytes_ = ta.block_attn_bwd_workspace(B, H, Hkv, S, S, d, n)
+    streams, got, held = [torch.cuda.Stream() for _ in range(3)], [], []
+    torch.cuda.synchronize()
+    for fill, s in zip((0, 255, 127), streams):
+        with torch.cuda.stream(s):
+            ws = torch.full((bytes_ + 64,), fill, dtype=torch.uint8, device="cuda")
+            grads = [torch.empty_like(t) for t in (q, k, v)]
+            ta.block_attn_bwd(q, k, v, lists, out, go, lse, *grads, B, H, Hkv, S, S, d, n, True, lens, d ** -0.5, ws, bytes_, s)
+        got.append(grads)
+        held.append((ws, fill))
+    torch.cuda.synchronize()
+    for grads, (ws, fill) in zip(got, held):
+        assert all(torch.equal(a, b) for a, b in zip(grads, ref)) and (ws[bytes_:] == fill).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = ta.block_attn_grad(q, k, v, lists, out, go, lse, True, None, lens)
+    for _ in range(3):
+        for t in again:
+            t.fill_(1)
+        graph.replay()
+        eager = ta.block_attn_grad(q, k, v, lists, out, go, lse, True, None, lens)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(again, ref)) and all(torch.equal(a, b) for a, b in zip(eager, ref))
