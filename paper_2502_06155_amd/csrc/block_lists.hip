@@ -8,7 +8,7 @@
 //
 // Measured, 6 heads of 86400 tokens of 96, 68 of 675 blocks each: means 16.5 us for 100 MB (6 TB/s), lists
 // 40 (reading q takes 20 at the rate of a copy; the rest is the choice). One token of 4 sequences, 16 heads
-// on 4 key heads, 32 of 256 blocks: 14 us, the latency of a chain of scores, bounds and counts.
+// on 4 key heads, 32 of 256 blocks: 10 us, the latency of a chain of means, scores, counts and bounds.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -139,34 +139,37 @@ __device__ __forceinline__ Key greater(Key a, Key b) { return a > b ? a : b; }
 // took 55 us by themselves.)
 constexpr int kThreadsM = 512, kWavesM = kThreadsM / 64, kMaxRows = 16;
 
-// The column sums of `rows` rows of each of G heads (head_step rows apart), one wave: lane l takes piece
-// l % P of rows l / P, + 64 / P, ...; the row groups' sums meet by shuffles. Lanes below P end with 8
-// columns each.
+// The column sums of rows [f0, f1) of all heads' rows (`rows` of each head, head_step apart, head after
+// head), one wave: lane l takes piece l % P of rows l / P, + 64 / P, ...; the row groups' sums meet by
+// shuffles. Lanes below P end with 8 columns each.
 template <int D>
-__device__ __forceinline__ void wave_sums(const uint16_t* x, int rows, int G, size_t head_step, int lane,
-                                          double (&sum)[8]) {
+__device__ __forceinline__ void wave_sums(const uint16_t* x, int rows, int64_t f0, int64_t f1, size_t head_step,
+                                          int lane, double (&sum)[8]) {
   constexpr int P = D / 8, kGroups = 64 / P, kUnroll = D == 96 ? 13 : 16;  // a block's rows in one or two goes
   const int piece = lane % P, group = lane / P;
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
-  for (int u = 0; u < G; ++u) {
+  for (int u = (int)(f0 / rows); u * (int64_t)rows < f1; ++u) {
     const uint16_t* head = x + (size_t)u * head_step * D + 8 * piece;
-    for (int r0 = 0; r0 < rows; r0 += kGroups * kUnroll) {
+    const int begin = (int)max(f0 - u * (int64_t)rows, (int64_t)0), end = (int)min(f1 - u * (int64_t)rows, (int64_t)rows);
+    for (int r0 = begin; r0 < end; r0 += kGroups * kUnroll) {
       u32x4 w[kUnroll];
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i) {
         const int r = r0 + i * kGroups + group;
         w[i] = u32x4{0u, 0u, 0u, 0u};
-        if (r < rows && group < kGroups) w[i] = load16(head + (size_t)r * D);
+        if (r < end && group < kGroups) w[i] = load16(head + (size_t)r * D);
       }
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i)
+      for (int i = 0; i < kUnroll; ++i) {
+        if (r0 + i * kGroups >= end) break;  // additions in 64 bits are slow: none for rows that are not there
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           acc[2 * e] += (double)bf16_lo(w[i][e]);
           acc[2 * e + 1] += (double)bf16_hi(w[i][e]);
         }
+      }
     }
   }
 #pragma unroll
@@ -376,15 +379,17 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
   };
   load(16 * wave + (lane & 15));
   {
-    // 8 / R waves a list (a power of two), each with a part of every head's rows; their sums meet in LDS.
+    // 8 / R waves a list (a power of two), each with a part of the rows of all heads; their sums meet in
+    // LDS. (A part of every head's rows left a single token's heads to one wave, one after the other, and
+    // its row's sums among zeros took 5 us.)
     double* part = reinterpret_cast<double*>(hists);  // [8][D]
     const int share = R == 1 ? 3 : R == 2 ? 2 : R <= 4 ? 1 : 0;  // log2 of a list's waves
     const int r = wave >> share, p = wave & ((1 << share) - 1), rows = r < R ? rows_of(i0 + r) : 0;
-    const int t0 = (rows * p) >> share, t1 = (rows * (p + 1)) >> share;
+    const int64_t all = (int64_t)rows * g.G, t0 = (all * p) >> share, t1 = (all * (p + 1)) >> share;
     double sum[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
     if (t1 > t0)
-      wave_sums<D>(a.q + (((size_t)b * g.H + (size_t)h * g.G) * g.Sq + (size_t)(i0 + r) * kBlock + t0) * D, t1 - t0,
-                   g.G, (size_t)g.Sq, lane, sum);
+      wave_sums<D>(a.q + (((size_t)b * g.H + (size_t)h * g.G) * g.Sq + (size_t)(i0 + r) * kBlock) * D, rows, t0, t1,
+                   (size_t)g.Sq, lane, sum);
     if (lane < D / 8) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) part[wave * D + 8 * lane + e] = sum[e];
