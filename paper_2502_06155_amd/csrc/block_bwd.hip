@@ -20,8 +20,8 @@
 // Measured: 24 heads of 28800 tokens, 32 of 225 blocks each, d = 96: 3455 us, 787 TFLOP/s as five products
 // and 1100 as the seven that run (a library product of 16384^3: 1312; vector issue beside the matrix
 // cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1200 us, of it dk, dv 660,
-// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 35 for both
-// passes, whose columns and units are few, and three short launches around them.
+// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 46 us, of it 35 for both
+// passes, whose columns and units are few, and two short launches around them.
 // Roundings: P and dS to bf16 before they enter a product (the matrix cores take nothing wider at this
 // rate), and the results at the end; S, dP, delta, all sums and cut pieces' parts are fp32.
 // S and dP are formed in both passes: adding dq up from the key side would take fp32 atomics, whose
@@ -44,6 +44,12 @@ constexpr int kPrepRowsB = 64;
 
 __device__ __forceinline__ int query_words(const BlockGeo& g) { return (g.nq + 31) / 32; }
 
+// Blocks that the rows of query block i may attend to: those below this one.
+__device__ __forceinline__ int listable(const BlockGeo& g, int len, int i) {
+  const int first = g.off + i * kBlock, last = min(first + min(kBlock, g.Sq - i * kBlock), len) - 1;
+  return last < first ? 0 : min(g.nb, (g.causal ? last : len - 1) / kBlock + 1);
+}
+
 // One word of every column of a (batch, key head): the lists of 32 query blocks. Entries that name
 // no block, or one that no row of the query block may attend to, are left out as in the forward.
 __device__ __forceinline__ void column_words(const BlockBwdArgs& a, uint32_t work, uint32_t* col) {
@@ -57,14 +63,155 @@ __device__ __forceinline__ void column_words(const BlockBwdArgs& a, uint32_t wor
   const int i0 = 32 * w, n = min(32, g.nq - i0) * g.n_list;
   const int32_t* lists = a.lists + ((size_t)bh * g.nq + i0) * g.n_list;
   for (int x = threadIdx.x; x < n; x += kThreadsB) {
-    const int bit = x / g.n_list, i = i0 + bit, j = lists[x];
-    const int first = g.off + i * kBlock, last = min(first + min(kBlock, g.Sq - i * kBlock), len) - 1;
-    const int end = last < first ? 0 : min(g.nb, (g.causal ? last : len - 1) / kBlock + 1);
-    if (j >= 0 && j < end) atomicOr(&col[j], 1u << bit);
+    const int bit = x / g.n_list, j = lists[x];
+    if (j >= 0 && j < listable(g, len, i0 + bit)) atomicOr(&col[j], 1u << bit);
   }
   __syncthreads();
   for (int j = threadIdx.x; j < g.nb; j += kThreadsB) a.cols[((size_t)bh * g.nb + j) * words + w] = col[j];
 }
+
+// ---------------------------------------------------------------------------------------------
+// plan
+
+// One workgroup per XCD. The columns, in order, are dealt out to the XCDs as contiguous shares of
+// equal work (a column's query blocks, and a quarter of the mean for its start and end): in causal
+// order early blocks have many more query blocks than late ones, and shares of equal count left
+// half of the XCDs idle (4 key heads of 128 blocks: 986 us). Each workgroup cuts the columns of its
+// share into pieces and lists the pieces longest first (by 64 sizes): popular blocks' pieces start
+// the launch, those of blocks that hardly anybody lists even out its end.
+// plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first slot; items[xcd * cap
+// + i] = {column, piece}; counts[xcd] = items of the share. Items of one size come in any order: when a
+// piece runs may differ from call to call, what it adds up and in which order does not.
+constexpr int kPlanThreads = 1024, kSizes = 64;
+
+// NT threads; blocks_of(x): the query blocks of column x.
+template <int NT, typename Fn>
+__device__ __forceinline__ void plan_share(const BlockBwdArgs& a, uint32_t cols, int xcd, Fn&& blocks_of) {
+  __shared__ int hist[kSizes];
+  __shared__ int64_t wave_sums[NT / 64];
+  __shared__ int wave_slots[NT / 64];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const uint32_t each = (cols + NT - 1) / NT;
+  const uint32_t x0 = min(cols, tid * each), x1 = min(cols, x0 + each);
+  auto pieces_of = [&](int n) { return max(1, (n + a.entries - 1) / a.entries); };
+  auto slots_of = [&](int pieces) { return pieces > 1 ? pieces : 0; };
+  if (tid < kSizes) hist[tid] = 0;
+  int64_t own = 0;
+  int own_slots = 0;
+  for (uint32_t x = x0; x < x1; ++x) {
+    const int n = blocks_of(x);
+    own += n;
+    own_slots += slots_of(pieces_of(n));
+  }
+  int64_t upto = own;
+  int upto_slots = own_slots;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t y = __shfl_up((long long)upto, s);
+    const int z = __shfl_up(upto_slots, s);
+    if (lane >= s) {
+      upto += y;
+      upto_slots += z;
+    }
+  }
+  if (lane == 63) {
+    wave_sums[wave] = upto;
+    wave_slots[wave] = upto_slots;
+  }
+  __syncthreads();
+  int64_t total = 0, before = upto - own;
+  int slots_before = upto_slots - own_slots;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) {
+      before += wave_sums[w];
+      slots_before += wave_slots[w];
+    }
+    total += wave_sums[w];
+  }
+  const int64_t start = max((int64_t)1, (total + 4 * (int64_t)cols - 1) / (4 * (int64_t)cols));
+  const int64_t work = total + start * cols;
+  before += start * x0;
+  // Entries of pieces of one column differ by at most one: one size stands for all.
+  auto size_of = [&](int n, int pieces) {
+    return kSizes - 1 - min(kSizes - 1, (int)((int64_t)((n + pieces - 1) / pieces) * kSizes / (a.entries + 1)));
+  };
+  auto mine = [&](auto&& fn) {
+    int64_t at = before;
+    int slot = slots_before;
+    for (uint32_t x = x0; x < x1; ++x) {
+      const int to = (int)(at * 8 / work);
+      if (to > xcd) break;
+      const int n = blocks_of(x), pieces = pieces_of(n);
+      at += n + start;
+      if (to == xcd) fn(x, n, pieces, slot);
+      slot += slots_of(pieces);
+    }
+  };
+  mine([&](uint32_t x, int n, int pieces, int slot) {
+    a.plan[4 * (size_t)x] = n;
+    a.plan[4 * (size_t)x + 1] = pieces;
+    a.plan[4 * (size_t)x + 2] = pieces > 1 ? slot : 0;
+    atomicAdd(&hist[size_of(n, pieces)], pieces);
+  });
+  __syncthreads();
+  if (tid < kSizes) {  // one wave: where each size starts
+    const int mine_n = hist[tid];
+    int sum = mine_n;
+#pragma unroll
+    for (int s = 1; s < kSizes; s <<= 1) {
+      const int y = __shfl_up(sum, s);
+      if (tid >= s) sum += y;
+    }
+    hist[tid] = sum - mine_n;
+    if (tid == kSizes - 1) a.counts[xcd] = min(sum, a.items_cap);
+  }
+  __syncthreads();
+  int2* items = reinterpret_cast<int2*>(a.items) + (size_t)xcd * a.items_cap;
+  mine([&](uint32_t x, int n, int pieces, int) {
+    const int at = atomicAdd(&hist[size_of(n, pieces)], pieces);
+    for (int p = 0; p < pieces; ++p)
+      if (at + p < a.items_cap) items[at + p] = int2{(int)x, p};
+  });
+}
+
+__global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwdArgs a, uint32_t cols) {
+  const int words = query_words(a.g);
+  plan_share<kPlanThreads>(a, cols, (int)blockIdx.x, [&](uint32_t x) {
+    int n = 0;
+#pragma unroll 4
+    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
+    return n;
+  });
+}
+
+// Short lists: the plan in the prep launch (2 heads of 500 tokens 21.9 us and 19.3, 12 of 2251 48.9 and
+// 47.6). Every one of the eight workgroups turns all lists round in
+// its own LDS (a.plan_in_prep: few words and entries), writes its part of the columns and plans its share.
+__device__ __forceinline__ void plan_lists(const BlockBwdArgs& a, int xcd, uint32_t* col) {
+  const BlockGeo& g = a.g;
+  const int words = query_words(g);
+  const uint32_t cols = (uint32_t)g.B * g.Hkv * g.nb, all = cols * words;
+  for (uint32_t x = threadIdx.x; x < all; x += kThreadsB) col[x] = 0;
+  __syncthreads();
+  const uint32_t entries = (uint32_t)g.B * g.Hkv * g.nq * g.n_list;
+  for (uint32_t x = threadIdx.x; x < entries; x += kThreadsB) {
+    const uint32_t list = x / g.n_list, bh = list / g.nq;
+    const int i = (int)(list - bh * g.nq), j = a.lists[x];
+    const int len = g.lens ? min(max(g.lens[bh / g.Hkv], 0), g.Skv) : g.Skv;
+    if (j >= 0 && j < listable(g, len, i)) atomicOr(&col[(bh * g.nb + j) * words + i / 32], 1u << (i % 32));
+  }
+  __syncthreads();
+  for (uint32_t x = xcd * kThreadsB + threadIdx.x; x < all; x += 8 * kThreadsB) a.cols[x] = col[x];
+  plan_share<kThreadsB>(a, cols, xcd, [&](uint32_t x) {
+    int n = 0;
+    for (int w = 0; w < words; ++w) n += __builtin_popcount(col[x * words + w]);
+    return n;
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// prep's launch, and the plan of the line
 
 template <int D>
 __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArgs a, int64_t n_rows, uint32_t prep_wgs) {
@@ -72,7 +219,8 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
   static_assert(kPrepRowsB * kPieces == kThreadsB * kPer, "whole pieces per thread");
   extern __shared__ float part[];  // the rows' pieces, or the columns' words
   if (blockIdx.x >= prep_wgs) {
-    column_words(a, blockIdx.x - prep_wgs, reinterpret_cast<uint32_t*>(part));
+    if (a.plan_in_prep) plan_lists(a, (int)(blockIdx.x - prep_wgs), reinterpret_cast<uint32_t*>(part));
+    else column_words(a, blockIdx.x - prep_wgs, reinterpret_cast<uint32_t*>(part));
     return;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) a.counts[8] = 0;
@@ -101,95 +249,6 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
     a.lse2[r] = some ? l * 1.4426950408889634f : INFINITY;
     a.ndelta[r] = some ? -acc : 0.f;
   }
-}
-
-// ---------------------------------------------------------------------------------------------
-// plan
-
-// One workgroup per XCD. The columns, in order, are dealt out to the XCDs as contiguous shares of
-// equal work (a column's query blocks, and a quarter of the mean for its start and end): in causal
-// order early blocks have many more query blocks than late ones, and shares of equal count left
-// half of the XCDs idle (4 key heads of 128 blocks: 986 us). Each workgroup cuts the columns of its
-// share into pieces and lists the pieces longest first (by 64 sizes): popular blocks' pieces start
-// the launch, those of blocks that hardly anybody lists even out its end.
-// plan[4 col] = the column's query blocks, + 1 = its pieces, + 2 = its first slot; items[xcd * cap
-// + i] = {column, piece}; counts[xcd] = items of the share. Slots come from a counter and items of
-// one size in any order: where a piece's sums lie and when it runs may differ from call to call,
-// what it adds up and in which order does not.
-constexpr int kPlanThreads = 1024, kSizes = 64;
-
-__global__ __launch_bounds__(kPlanThreads) void block_plan_kernel(const BlockBwdArgs a, uint32_t cols) {
-  __shared__ int hist[kSizes];
-  __shared__ int64_t wave_sums[kPlanThreads / 64];
-  const int words = query_words(a.g);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const uint32_t each = (cols + kPlanThreads - 1) / kPlanThreads;
-  const uint32_t x0 = min(cols, tid * each), x1 = min(cols, x0 + each);
-  auto blocks_of = [&](uint32_t x) {
-    int n = 0;
-#pragma unroll 4
-    for (int w = 0; w < words; ++w) n += __builtin_popcount(a.cols[(size_t)x * words + w]);
-    return n;
-  };
-  if (tid < kSizes) hist[tid] = 0;
-  int64_t own = 0;
-  for (uint32_t x = x0; x < x1; ++x) own += blocks_of(x);
-  int64_t upto = own;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int64_t y = __shfl_up((long long)upto, s);
-    if (lane >= s) upto += y;
-  }
-  if (lane == 63) wave_sums[wave] = upto;
-  __syncthreads();
-  int64_t total = 0, before = upto - own;
-#pragma unroll
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) before += wave_sums[w];
-    total += wave_sums[w];
-  }
-  const int64_t start = max((int64_t)1, (total + 4 * (int64_t)cols - 1) / (4 * (int64_t)cols));
-  const int64_t work = total + start * cols;
-  before += start * x0;
-  // Entries of pieces of one column differ by at most one: one size stands for all.
-  auto size_of = [&](int n, int pieces) {
-    return kSizes - 1 - min(kSizes - 1, (int)((int64_t)((n + pieces - 1) / pieces) * kSizes / (a.entries + 1)));
-  };
-  auto mine = [&](auto&& fn) {
-    int64_t at = before;
-    for (uint32_t x = x0; x < x1; ++x) {
-      const int xcd = (int)(at * 8 / work);
-      if (xcd > (int)blockIdx.x) break;
-      const int n = blocks_of(x);
-      at += n + start;
-      if (xcd == (int)blockIdx.x) fn(x, n, max(1, (n + a.entries - 1) / a.entries));
-    }
-  };
-  mine([&](uint32_t x, int n, int pieces) {
-    a.plan[4 * (size_t)x] = n;
-    a.plan[4 * (size_t)x + 1] = pieces;
-    a.plan[4 * (size_t)x + 2] = pieces > 1 ? atomicAdd(&a.counts[8], pieces) : 0;
-    atomicAdd(&hist[size_of(n, pieces)], pieces);
-  });
-  __syncthreads();
-  if (tid < kSizes) {  // one wave: where each size starts
-    const int mine_n = hist[tid];
-    int sum = mine_n;
-#pragma unroll
-    for (int s = 1; s < kSizes; s <<= 1) {
-      const int y = __shfl_up(sum, s);
-      if (tid >= s) sum += y;
-    }
-    hist[tid] = sum - mine_n;
-    if (tid == kSizes - 1) a.counts[blockIdx.x] = min(sum, a.items_cap);
-  }
-  __syncthreads();
-  int2* items = reinterpret_cast<int2*>(a.items) + (size_t)blockIdx.x * a.items_cap;
-  mine([&](uint32_t x, int n, int pieces) {
-    const int at = atomicAdd(&hist[size_of(n, pieces)], pieces);
-    for (int p = 0; p < pieces; ++p)
-      if (at + p < a.items_cap) items[at + p] = int2{(int)x, p};
-  });
 }
 
 // The plan at d = 128, where the key side runs one workgroup a compute unit and an item of the plan above
@@ -1183,10 +1242,11 @@ hipError_t block_bwd_for(const BlockBwdArgs& a, hipStream_t s) {
   const uint32_t lists = (uint32_t)((int64_t)g.B * g.Hkv * g.nq);
   const uint32_t prep = (uint32_t)((rows + kPrepRowsB - 1) / kPrepRowsB);
   const uint32_t words = (uint32_t)((int64_t)g.B * g.Hkv * ((g.nq + 31) / 32));
-  const size_t lds = std::max((size_t)kPrepRowsB * (D / 8), (size_t)g.nb) * 4;
-  block_prep_kernel<D><<<prep + words, kThreadsB, lds, s>>>(a, rows, prep);
+  const size_t column_lds = a.plan_in_prep ? (size_t)cols * ((g.nq + 31) / 32) : (size_t)g.nb;
+  const size_t lds = std::max((size_t)kPrepRowsB * (D / 8), column_lds) * 4;
+  block_prep_kernel<D><<<prep + (a.plan_in_prep ? 8 : words), kThreadsB, lds, s>>>(a, rows, prep);
   if (a.line) block_line_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
-  else block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
+  else if (!a.plan_in_prep) block_plan_kernel<<<8, kPlanThreads, 0, s>>>(a, cols);
   const uint32_t keys = a.line ? kLineWorkers : 8 * (uint32_t)a.items_cap, queries = unit_grid(g, a.units * a.pieces_q);
   if constexpr (D == 128) {
     if (g.causal) block_dkdv_kernel<true><<<keys, kThreadsB, 0, s>>>(a, (int)cols);

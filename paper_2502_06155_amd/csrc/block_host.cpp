@@ -367,6 +367,8 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
   // A column's start and end take about four units' time, and the masked tiles of its own query block
   // another block's.
   a.line = p.line;
+  // Up to 32 KB of columns and 64 entries a thread.
+  a.plan_in_prep = !p.line && cols * ((a.g.nq + 31) / 32) <= 8192 && lists_of(a.g) * n_list <= 16384;
   a.col_start = (16 + a.g.G - 1) / a.g.G + (causal ? 4 : 0);
   char* ws = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(ws);

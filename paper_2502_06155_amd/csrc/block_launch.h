@@ -67,6 +67,7 @@ struct BlockBwdArgs {
   uint32_t flip, keep;
   int units;
   int pieces_q;      // pieces of a query unit's list
+  int plan_in_prep;  // few list entries: turned round and planned beside prep, not in a launch of its own
   int line;          // the key side takes stretches of the line of all columns, not the plan's items
   int entries;       // query blocks per piece of a key block's column, at most (line: of a stretch, at least)
   int col_start;     // line: what a column costs beside its query blocks, in quarters of one
@@ -76,7 +77,7 @@ struct BlockBwdArgs {
   float* ndelta;     // [B, H, Sq]: -<dout, out>
   uint32_t* cols;    // [B, Hkv, nb][nq / 32 words]: the query blocks that list a key block
   int32_t* plan;     // [B, Hkv, nb][4]: entries, pieces, first slot, first worker (line)
-  int32_t* counts;   // [9]: items of each XCD's share (line: workers); the slot counter
+  int32_t* counts;   // [9]: items of each XCD's share (line: workers); line: the slot counter
   int32_t* items;    // [8][items_cap][2]: column, piece; line: where each worker starts
   int items_cap;     // items of an XCD's share, at most
   float* part_q;     // pieces_q > 1: fp32 [list][unit][piece][128][d]

@@ -76,6 +76,7 @@ CASES = [
     (1, 48, 2, 700, 700, 128, 6, True, [650], "near"),  # the key side by stretches of a line, columns cut often
     (2, 26, 1, 900, 900, 128, 8, False, [900, 300], "empty"),
     (1, 36, 1, 300, 1500, 128, 20, True, None, "random"),
+    (2, 2, 1, 1000, 1000, 64, 1100, True, [1000, 555], "random"),  # long lists of repeats: a launch of its own plans
 ]
 IDS = ["-".join(str(x) for x in c[:7]) + ("-causal" if c[7] else "") + ("-" + c[9]) for c in CASES]
 
