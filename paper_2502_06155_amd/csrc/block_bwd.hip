@@ -20,7 +20,7 @@
 // Measured: 24 heads of 28800 tokens, 32 of 225 blocks each, d = 96: 3455 us, 787 TFLOP/s as five products
 // and 1100 as the seven that run (a library product of 16384^3: 1312; vector issue beside the matrix
 // cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1200 us, of it dk, dv 660,
-// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 46 us, of it 35 for both
+// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 39 for both
 // passes, whose columns and units are few, and two short launches around them.
 // Roundings: P and dS to bf16 before they enter a product (the matrix cores take nothing wider at this
 // rate), and the results at the end; S, dP, delta, all sums and cut pieces' parts are fp32.
