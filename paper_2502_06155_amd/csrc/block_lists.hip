@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
       for (int c = 0; c < kC; ++c) {
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qa[c], as_bf16x8(w[c]), s, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most = max(most, max(w[c][e] << 16, w[c][e]) & 0x7fff0000u);
+        for (int e = 0; e < 4; ++e) most = max(most, max((w[c][e] << 16) & 0x7fff0000u, w[c][e] & 0x7fff0000u));
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) {

@@ -539,3 +539,20 @@ def test_stretches_of_the_line_whatever_the_workspace_holds_and_replayed():
         eager = ta.block_attn_grad(q, k, v, lists, out, go, lse, True, None, lens)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(again, ref)) and all(torch.equal(a, b) for a, b in zip(eager, ref))
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("top", [-9, -12])
+def test_lists_where_a_large_channel_lies_beside_a_small_one_of_the_other_sign(d, top):
+    """Key means with 1024 beside -2^-10, twice, cancelled by the query: the sums in 32 bits keep of the
+    small channels, which order the blocks, what is left of an ulp of 1024, and the bound on their
+    error has to come from the 1024."""
+    rng = np.random.default_rng(d - top)
+    nb, n = 300, 33
+    km, q = np.zeros((1, 1, nb, d)), np.zeros((1, 1, 1, d))
+    km[..., [0, 32]], km[..., [1, 33]] = 1024, -2.0 ** -10
+    km[..., [2, 34]] = -rng.uniform(0, 2.0 ** top, (nb, 2))
+    q[..., [0, 2, 34]], q[..., 32] = 1, -1
+    kb, qb = ob.to_bf16(km), ob.to_bf16(q)
+    got = ta.block_lists(to_dev(qb), to_dev(kb), 128 * nb, n, local=0).cpu().numpy()
+    assert np.array_equal(got, ob.block_lists(qb, kb, 128 * nb, n, local=0))
