@@ -337,7 +337,7 @@ __device__ __forceinline__ bool find_bar(const Keys& kr, int stride, int n, uint
       return true;
     }
     low = bar;
-    width = ((Key)1 << shift) - 1;
+    width = lesser((Key)(((Key)1 << shift) - 1), (Key)(high - low));  // past `high` lie the forced blocks' keys
     shift = max(0, shift - 8);
   }
 }

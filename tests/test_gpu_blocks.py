@@ -556,3 +556,19 @@ def test_lists_where_a_large_channel_lies_beside_a_small_one_of_the_other_sign(d
     kb, qb = ob.to_bf16(km), ob.to_bf16(q)
     got = ta.block_lists(to_dev(qb), to_dev(kb), 128 * nb, n, local=0).cpu().numpy()
     assert np.array_equal(got, ob.block_lists(qb, kb, 128 * nb, n, local=0))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nb,infinite,n", [(80, 4, 5), (300, 8, 6), (700, 40, 30), (90, 3, 88), (60, 5, 5)])
+def test_lists_with_more_infinite_scores_than_places(d, nb, infinite, n):
+    """Forced blocks, then key means of +inf, of which only the first find a place: the last bin of
+    the search ends with them, not with the forced blocks behind."""
+    rng = np.random.default_rng(nb + n)
+    q, km = bits(rng, 1, 2, 200, d), bits(rng, 1, 1, nb, d)
+    q[..., 5] = 0x3F80
+    where = rng.permutation(nb)[:infinite]
+    km[0, 0, where, 5] = 0x7F80
+    got = ta.block_lists(to_dev(q), to_dev(km), 128 * nb, n, sink=2, local=1).cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        ref = ob.block_lists(q, km, 128 * nb, n, sink=2, local=1)
+    assert np.array_equal(got, ref)
