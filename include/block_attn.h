@@ -24,7 +24,9 @@
  *   - A row's result depends on the tokens it attends to alone: infinities and NaN elsewhere, in
  *     later tokens too, do not reach it. A row that meets a NaN has NaN for its log-sum-exp. For
  *     gradients this holds between query blocks only: a key or value that is no number may reach
- *     the gradients of all rows of a query block that lists it.
+ *     its own gradients and those of all rows of a query block that lists it, and a row that is no
+ *     number those of all keys of the blocks it lists. A row whose log-sum-exp is NaN gives NaN to
+ *     dv of the keys it attends to, and to no other dv.
  *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], 1 <= n_list <= TA_MAX_BLOCKS, the blocks a query
  *     block's rows (of all G heads) attend to, in any order. Entries outside 0..NB-1 are skipped (-1 fills up), and a block
  *     that is listed twice counts once.

@@ -245,9 +245,9 @@ __global__ __launch_bounds__(kThreadsB) void block_prep_kernel(const BlockBwdArg
     for (int c = 0; c < kPieces; ++c) acc += part[threadIdx.x * kPieces + c];
     const int64_t r = row0 + threadIdx.x;
     const float l = a.lse[r];
-    const bool some = l != -INFINITY;  // NaN, of a row of NaN, passes into its gradients
+    const bool some = l != -INFINITY;
     a.lse2[r] = some ? l * 1.4426950408889634f : INFINITY;
-    a.ndelta[r] = some ? -acc : 0.f;
+    a.ndelta[r] = l != l ? l : some ? -acc : 0.f;  // NaN, of a row of NaN, passes into dS (and dv: store_key)
   }
 }
 
@@ -326,7 +326,8 @@ __global__ __launch_bounds__(kPlanThreads) void block_line_kernel(const BlockBwd
 }
 
 // P = exp2(c s - lse2) clamped to [0, 1] (the exponent is <= 0 up to rounding for kept pairs; the
-// clamp keeps rows of zeros past a tile's valid range finite, which then add exactly nothing).
+// clamp keeps rows of zeros past a tile's valid range finite, which then add exactly nothing). The clamp
+// is part of the exponential's instruction and makes 0 of NaN; what a row of NaN owes dv, store_key adds.
 __device__ __forceinline__ float prob(float s, float c, float lse2) {
   return __builtin_amdgcn_fmed3f(fast_exp2(__builtin_fmaf(s, c, -lse2)), 0.f, 1.f);
 }
@@ -593,12 +594,54 @@ struct KeyPiece {
   }
 };
 
+// A lane id the compiler cannot hoist: rows derived from it hold no register across the stream.
+__device__ __forceinline__ int fresh_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
+// The last position of a row of NaN (its log-sum-exp is NaN) among the piece's query blocks, or -1.
+__device__ __forceinline__ int last_nan_row(const BlockBwdArgs& a, const KeyPiece& kp, const uint32_t* bits) {
+  const BlockGeo& g = a.g;
+  const int lane = fresh_lane();
+  int last = -1;
+  BitWalk walk;
+#pragma unroll 1
+  for (walk.start(bits, query_words(g), kp.e0, kp.e1 - kp.e0); walk.at >= 0; walk.next()) {
+    const int i0 = walk.at * kBlock, n = min(min(kBlock, g.Sq - i0), kp.len - g.off - i0);
+#pragma unroll 1
+    for (int head = 0; head < g.G; ++head)
+#pragma unroll 1
+      for (int t = lane; t < n; t += 64) {
+        const float l = a.lse2[kp.group_row + (size_t)head * g.Sq + i0 + t];
+        if (l != l) last = max(last, g.off + i0 + t);
+      }
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) last = max(last, __shfl_xor(last, s));
+  return last;
+}
+
 // Stores this lane's key row of dK and dV, or the piece's part of it. Rows of padding are zeros:
-// what formed for their zero K and V rows counts for nobody.
-template <int D>
-__device__ __forceinline__ void store_key(const BlockBwdArgs& a, const KeyPiece& kp, int row, int hf, f32x16 (&dk)[D / 32],
-                                          f32x16 (&dv)[D / 32]) {
+// what formed for their zero K and V rows counts for nobody. A row of NaN has NaN for the weights of
+// all keys it attends to, which the clamp of P took for 0: dS was NaN all the same, so where a key's
+// dK is, such rows are looked for, and dV of the keys up to the last of them (in causal order; else of
+// all) is NaN. (Without one the price is a comparison a unit; keeping NaN in P would take an
+// instruction a score.)
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void store_key(const BlockBwdArgs& a, const KeyPiece& kp, const uint32_t* bits, int row, int hf,
+                                          f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32]) {
   const int key = kp.j * kBlock + row;
+  if (__builtin_amdgcn_ballot_w64(dk[0][0] != dk[0][0]) != 0) {
+    const int last = last_nan_row(a, kp, bits);
+    if (last >= (CAUSAL ? key : 0)) {
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dv[mb][e] = __builtin_nanf("");
+    }
+  }
   if (key >= kp.len) {
 #pragma unroll
     for (int mb = 0; mb < D / 32; ++mb) {
@@ -806,7 +849,7 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
     }
   }
 
-  store_key<D>(a, kp, wave * 32 + n, hf, dk, dv);
+  store_key<D, CAUSAL>(a, kp, bits, wave * 32 + n, hf, dk, dv);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -822,13 +865,6 @@ __device__ __forceinline__ void dkdv_unit(const BlockBwdArgs& a, uint32_t id, ui
 // across the phases, and the blocks in a ring of LDS slots, five loaded ahead, so that a barrier every
 // two blocks never waits for the block it is about to use. Causal tiles that need a mask come first,
 // in the plain form, through the same LDS.
-
-// A lane id the compiler cannot hoist: rows derived from it hold no register across the stream.
-__device__ __forceinline__ int fresh_lane() {
-  int lane;
-  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
-  return lane;
-}
 
 // acc += a b with the accumulator in AGPRs. The compiler does not track an asm MFMA's hazards; none
 // arise: a comes from LDS (its wait counts asm operands), b was written by the vector ALU at least
@@ -1122,7 +1158,7 @@ __device__ __forceinline__ void dkdv_roll_unit(const BlockBwdArgs& a, const KeyP
 #pragma unroll
   for (int mb = 0; mb < kMb; ++mb) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(dk[mb]), "+a"(dv[mb]));
   const int lane = fresh_lane();
-  store_key<D>(a, kp, wave * 32 + (lane & 31), lane >> 5, dk, dv);
+  store_key<D, CAUSAL>(a, kp, bits, wave * 32 + (lane & 31), lane >> 5, dk, dv);
 }
 
 // Both passes in one launch (two workgroups a compute unit): the key side's items first, they are

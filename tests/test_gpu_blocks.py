@@ -572,3 +572,46 @@ def test_lists_with_more_infinite_scores_than_places(d, nb, infinite, n):
     with np.errstate(invalid="ignore"):
         ref = ob.block_lists(q, km, 128 * nb, n, sink=2, local=1)
     assert np.array_equal(got, ref)
+
+
+@pytest.mark.parametrize("B,H,Hkv,Sq,Skv,d,n,causal,lens", [
+    (1, 2, 1, 200, 400, 64, 3, False, None),
+    (1, 2, 1, 6, 2000, 64, 16, False, None),
+    (2, 4, 2, 500, 500, 96, 4, True, [500, 333]),
+    (1, 6, 3, 300, 555, 128, 5, True, [550]),
+    (1, 48, 2, 900, 900, 128, 6, True, [850]),  # the line of columns
+], ids=["rows", "token", "causal", "items", "line"])
+def test_rows_that_are_no_numbers_show_in_dv_of_the_keys_they_attend_to(B, H, Hkv, Sq, Skv, d, n, causal, lens):
+    """A query, and a key, that is NaN: its rows' weights are NaN, and so is dv of all keys these rows
+    attend to, as in the formula; every other dv keeps its bits."""
+    rng = np.random.default_rng(Skv + d)
+    q, k, v, go = (bits(rng, B, h, s, d) for h, s in ((H, Sq), (Hkv, Skv), (Hkv, Skv), (H, Sq)))
+    lists = some_lists(rng, B, Hkv, Sq, Skv, n, "near")
+    run = lambda *x: ta.block_attn(*(to_dev(y) for y in x), i32(lists), causal, lens=i32(lens), return_lse=True)  # noqa: E731
+    grad = lambda x, o: ta.block_attn_grad(*(to_dev(y) for y in x), i32(lists), o[0], to_dev(go), o[1], causal,  # noqa: E731
+                                           lens=i32(lens))
+    clean = grad((q, k, v), run(q, k, v))
+    off, at = Skv - Sq, 4 if Sq < 100 else 70
+    sees = [[ob.attends(lists[b, h], Sq, Skv, causal, Skv if lens is None else lens[b]) for h in range(Hkv)] for b in range(B)]
+    for what in ("query", "key"):
+        x = [y.copy() for y in (q, k, v)]
+        bad = np.zeros((B, H, Sq), bool)
+        if what == "query":
+            x[0][0, H - 1, at, 9] = NAN
+            bad[0, H - 1, at] = True
+        else:
+            t = off + at
+            x[1][0, 0, t, 5] = NAN
+            bad[0, :H // Hkv] = sees[0][0][:, t]
+        out = run(*x)
+        some = np.array([[sees[b][h * Hkv // H].any(1) for h in range(H)] for b in range(B)])
+        assert np.array_equal(np.isnan(out[1].cpu().numpy()), bad & some)
+        want = np.zeros((B, Hkv, Skv), bool)
+        for b in range(B):
+            for h in range(H):
+                want[b, h * Hkv // H] |= sees[b][h * Hkv // H][bad[b, h]].any(0)
+        assert what == "key" or want.any()
+        dv = grad(x, out)[2]
+        assert np.array_equal(np.isnan(widen(from_dev(dv))), np.broadcast_to(want[..., None], dv.shape))
+        keep = torch.from_numpy(~want).cuda()
+        assert torch.equal(dv[keep], clean[2][keep])
