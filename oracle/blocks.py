@@ -17,8 +17,13 @@ def widen(bits):
 
 
 def to_bf16(x):
-    """Nearest bf16 bit patterns of finite numbers that were rounded to float32, ties to even."""
-    u = np.asarray(x, np.float64).astype(np.float32).view(np.uint32).astype(np.uint64)
+    """Nearest bf16 bit patterns of finite numbers, ties to even. On the way through float32 what is not
+    exact goes to the neighbour with an odd last bit, which no tie of bf16 has."""
+    x = np.asarray(x, np.float64)
+    f = x.astype(np.float32)
+    u = f.view(np.uint32).astype(np.int64)
+    step = np.sign(np.abs(x) - np.abs(f.astype(np.float64))).astype(np.int64)
+    u = np.where(u % 2 == 0, u + step, u).astype(np.uint64)
     return ((u + 0x7FFF + ((u >> 16) & 1)) >> 16).astype(np.uint16)
 
 

@@ -72,9 +72,18 @@ struct ColumnSums {
   }
 };
 
-// The mean of `count` values as a bf16 (0 of none).
+// The mean of `count` values as the nearest bf16 (0 of none). On the way through fp32 what is not exact
+// goes to the neighbour with an odd last bit, which lies on the same side of every tie of bf16 as the
+// number itself: a plain conversion to fp32 could land on a tie, and whether the compiler joins the two
+// conversions into one hangs on its settings.
 __device__ __forceinline__ __bf16 mean_bf16(double sum, int count) {
-  return count > 0 ? (__bf16)(float)(sum / (double)count) : (__bf16)0.f;
+  if (count <= 0) return (__bf16)0.f;
+  const double x = sum / (double)count, ax = fabs(x);
+  const float f = (float)x;
+  const double af = fabs((double)f);
+  uint32_t u = __float_as_uint(f);
+  if ((u & 1) == 0 && (af < ax || af > ax)) u += af < ax ? 1u : ~0u;
+  return (__bf16)__uint_as_float(u);
 }
 
 template <int D>

@@ -615,3 +615,24 @@ def test_rows_that_are_no_numbers_show_in_dv_of_the_keys_they_attend_to(B, H, Hk
         assert np.array_equal(np.isnan(widen(from_dev(dv))), np.broadcast_to(want[..., None], dv.shape))
         keep = torch.from_numpy(~want).cuda()
         assert torch.equal(dv[keep], clean[2][keep])
+
+
+def test_means_are_rounded_once():
+    """Means just past and just before a tie of bf16, nearer than fp32 can tell: the side they lie on."""
+    x = np.zeros((1, 1, 512, 64))
+    x[0, 0, [0, 128, 256, 384]], x[0, 0, [1, 129, 257, 385]] = 4 * 32, 32 * 2.0 ** -6  # means 1 + 2^-8, a tie, and
+    x[0, 0, [2, 130]] = [[32 * 2.0 ** -28], [-32 * 2.0 ** -28]]                        # 2^-30 more and less
+    x[0, 0, 257] = 32 * 3 * 2.0 ** -6                                                  # 1 + 3 * 2^-8, a tie,
+    x[0, 0, 258] = -32 * 2.0 ** -28                                                    # 2^-30 less
+    xb = ob.to_bf16(x)
+    assert np.array_equal(ob.widen(xb), x)
+    want = [1 + 2.0 ** -7, 1.0, 1 + 2.0 ** -7, 1.0]
+    got = ta.block_means(to_dev(xb))
+    assert (widen(from_dev(got)) == np.array(want)[:, None]).all()
+    assert np.array_equal(from_dev(got), ob.block_means(xb))
+    # the same of a query block's mean: its score beside one of 1
+    km = ob.to_bf16(np.eye(2, 64)[None, None, ::-1])  # block 0 picks dim 1, block 1 dim 0
+    for i, best in enumerate([1, 0, 1, 0]):
+        q = x[:, :, 128 * i:128 * (i + 1)].copy()
+        q[..., 1] = 1
+        assert ta.block_lists(to_dev(ob.to_bf16(q)), to_dev(km), 256, 1, local=0).item() == best, i

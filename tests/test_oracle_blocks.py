@@ -87,3 +87,17 @@ def test_cache_write_and_attention_on_whole_numbers():
     assert ks[0, 0] == 2 and kp[0, 0, 0, 0] == ob.e4m3_codes(224.0) and vs[0, 0] == 1
     out, lse, _ = ob.cache_attention(ob.to_bf16(np.zeros((1, 1, 1, 64))), kp, vp, ks, vs, table, [130])
     assert np.allclose(out, 448 * 3 / 130) and np.allclose(lse, np.log(130))
+
+
+def test_to_bf16_takes_the_nearest_number():
+    """Every bf16 of a few binades, the ties between neighbours, and numbers 2^-40 beside those: nearer
+    to a tie than float32 can tell."""
+    bits = np.concatenate([s + np.arange(0x3F00, 0x4100) for s in (0, 0x8000)]).astype(np.uint16)
+    assert np.array_equal(ob.to_bf16(ob.widen(bits)), bits)
+    a, b = ob.widen(bits[:-1]), ob.widen(bits[1:])
+    keep = (a > 0) == (b > 0)
+    a, b, low = a[keep], b[keep], bits[:-1][keep]
+    tie = (a + b) / 2
+    assert np.array_equal(ob.to_bf16(tie), low + (low & 1))
+    up = 1 + 2.0 ** -40
+    assert np.array_equal(ob.to_bf16(tie * up), low + 1) and np.array_equal(ob.to_bf16(tie / up), low)
