@@ -196,7 +196,13 @@ bool whole_segments(int64_t segments, int d, int max_pages) {
   return (int64_t)max_pages * d <= 1024 || (max_pages <= 16 && segments >= kSlots / 2);
 }
 
-// The workgroups that share a cache attention's pages, and the passes over its rows.
+// The workgroups that share a cache attention's pages, and the passes over its rows. Every workgroup of
+// every pass may leave two partial results. Up to four passes run all the workgroups that the device
+// holds in each; more passes share kPassSlots between them, so that the workspace stays below 70 MB
+// whatever N is. One sequence of 32768 tokens, 32 heads on 8 of 128, all workgroups in every pass and
+// so: N = 64 144 and 116 us, 69 and 35 MB; 512 1094 and 511, 554 and 35; 2048 4370 and 1864, 2215 and 35.
+// A pass of one workgroup has every segment to itself and leaves nothing to join.
+constexpr int64_t kPassSlots = 2 * kSlots;
 struct CachePlan {
   int workers, passes, rows;
   bool whole;
@@ -208,10 +214,12 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.rows = cache_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
   p.passes = (int)((rows + p.rows - 1) / p.rows);
   // Two workgroups run on a compute unit in passes of 16 rows, one in passes of 32.
-  p.workers = (int)std::min<int64_t>(p.rows == 16 ? kSlots : kSlots / 2, (int64_t)B * Hkv * (max_pages + kCacheSegment));
+  p.workers = (int)std::min<int64_t>({p.rows == 16 ? kSlots : kSlots / 2,
+                                      p.passes < kPassSlots ? std::max<int64_t>(2, kPassSlots / p.passes) : 1,
+                                      (int64_t)B * Hkv * (max_pages + kCacheSegment)});
   p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
   if (p.whole) p.workers = B * Hkv;
-  p.bytes = p.whole ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
+  p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
 int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {

@@ -269,3 +269,14 @@ def test_the_line_of_columns_gives_every_query_block_to_one_worker(cols, nq, G, 
         for c, n in enumerate(counts):
             assert len(seen[c]) == pieces[c][1]
             assert seen[c][0][0] == 0 and seen[c][-1][1] == n and all(x[1] == y[0] for x, y in zip(seen[c], seen[c][1:]))
+
+
+def test_the_workspace_of_cache_attention_stays_small_however_many_tokens():
+    for d in (64, 128):
+        for G, N in ((4, 1), (4, 5), (4, 40), (1, 300), (4, 512), (4, 2048), (8, 4095), (4, 8192), (1, 32737), (4, 65536),
+                     (1, 524280)):
+            for B, Hkv in ((1, 1), (1, 8), (7, 4)):
+                for pages in (1, 40, 512, 16384):
+                    assert ta.cache_attn_fwd_workspace(B, G * Hkv, Hkv, N, d, pages) < 70e6, (G, N, B, pages)
+    assert ta.cache_attn_fwd_workspace(1, 32, 8, 1, 128, 512) == 512 * 2 * 16 * 132 * 4   # few rows: as many workgroups
+    assert ta.cache_attn_fwd_workspace(1, 32, 8, 32, 128, 512) == 4 * 256 * 2 * 32 * 132 * 4  # as the device holds

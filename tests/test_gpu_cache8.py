@@ -357,3 +357,23 @@ def test_a_later_token_that_is_no_number_leaves_earlier_rows(d, width):
     got, lse = run(cache)
     assert torch.equal(got[:, :, :3], ref[:, :, :3]) and torch.equal(lse[:, :, :3], rlse[:, :, :3])
     assert got[:, :, 3:].isnan().all() and lse[:, :, 3:].isnan().all()
+
+
+@pytest.mark.parametrize("B,H,Hkv,N,d,lens,width", [
+    (1, 8, 2, 40, 128, [3000], 40),             # five passes of 32 rows, each a share of the workgroups
+    (2, 8, 2, 300, 64, [900, 333], 40),         # as many tokens as one sequence holds, fewer than the other's
+    (1, 4, 4, 257, 96, [257], None),            # short tables: a workgroup a segment and pass
+    (3, 8, 1, 129, 128, [128, 0, 2100], 40),    # rows before a sequence's start, and none at all
+    (1, 40, 1, 500, 64, [700], 20),             # two workgroups a pass
+    (2, 32, 1, 1030, 64, [1030, 5], 20),        # more passes than workgroups: one a pass, no workspace
+])
+def test_chunks_of_a_prompt(B, H, Hkv, N, d, lens, width):
+    rng = np.random.default_rng(N + d)
+    cache, table = held(rng, B, Hkv, d, lens, width)
+    q = bits(rng, B, H, N, d)
+    out = torch.full((B, H, N, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    got, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), None, out, return_lse=True)
+    check(got, lse, q, cache, table, lens)
+    again = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens))
+    assert torch.equal(got, again)
+    assert N < 1030 or ta.cache_attn_fwd_workspace(B, H, Hkv, N, d, width) == 0
