@@ -107,8 +107,8 @@ int block_attn_bwd(const void* q, const void* k, const void* v, const int32_t* l
  * TA_BLOCK] (values transposed inside a page: the matrix cores then read them as they lie), both
  * 16-byte aligned; k_scales, v_scales: fp32 [n_pages, Hkv]; a number is code * scale.
  * table: int32 [B, max_pages], page i of a sequence holding its tokens 128 i .. 128 i + 127;
- * lens: int32 [B]. An entry outside 0..n_pages-1 names no page: its tokens are neither written
- * nor read. Sequences may share pages that no call writes.
+ * lens: int32 [B]; B * Hkv is at most 65535. An entry outside 0..n_pages-1 names no page: its
+ * tokens are neither written nor read. Sequences may share pages that no call writes.
  *
  * cache_attn_write puts N new tokens behind the lens[b] tokens a sequence holds (lens itself is
  * left as it is; tokens past max_pages pages are dropped). With n_new (int32 [B], or NULL) a
@@ -127,8 +127,9 @@ int cache_attn_write(const void* k, const void* v, void* k_pages, void* v_pages,
 /*
  * Attention of the last N tokens of each sequence over its pages; lens counts them too. Row t
  * attends to the first lens[b] - (N - 1) + t tokens; a row with none gives zeros and -inf.
- * q, out: bf16 [B, H, N, d]; lse: fp32 [B, H, N] or NULL. Lengths may be anything from 0 to
- * max_pages pages (longer ones are taken as that). Scales may be any finite numbers here.
+ * q, out: bf16 [B, H, N, d], H / Hkv * N at most 524280; lse: fp32 [B, H, N] or NULL. Lengths may
+ * be anything from 0 to max_pages pages (longer ones are taken as that). Scales may be any finite
+ * numbers here.
  * With per_head nonzero table is [B, Hkv, max_pages] and lens [B, Hkv]: every key head has pages
  * of its own choice, as the lists of a single token give them. A list that keeps the page of the
  * last token as its last entry, all others full, then needs no more than its own length.

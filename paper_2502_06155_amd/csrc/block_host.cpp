@@ -227,12 +227,16 @@ int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
     return fail(TA_ERR_BAD_SHAPE, "B, H, Hkv, N and max_pages must be >= 1");
   if (H % Hkv) return fail(TA_ERR_BAD_SHAPE, "H must be a multiple of Hkv");
   if (max_pages > INT_MAX / TA_BLOCK) return fail(TA_ERR_BAD_SHAPE, "max_pages pages hold more than 2^31 - 1 tokens");
-  // The passes over the rows and the sequences times heads are grid dimensions of their own.
+  // The sequences times heads are a grid dimension of their own.
   if ((int64_t)B * Hkv * (max_pages + kCacheSegment) > INT_MAX)
     return fail(TA_ERR_BAD_SHAPE, "B * Hkv * max_pages exceeds 2^31 - 1");
-  if ((int64_t)B * Hkv > 65535 || (int64_t)(H / Hkv) * N > 8 * 65535)
-    return fail(TA_ERR_BAD_SHAPE, "B * Hkv or H / Hkv * N exceeds the grid limit");
+  if ((int64_t)B * Hkv > 65535) return fail(TA_ERR_BAD_SHAPE, "B * Hkv exceeds the grid limit");
   return check_dim(d);
+}
+// Attention: so are the passes over its rows and the joins of 8 of them.
+int check_cache_attn(int B, int H, int Hkv, int N, int d, int max_pages) {
+  if (int st = check_cache(B, H, Hkv, N, d, max_pages)) return st;
+  return (int64_t)(H / Hkv) * N <= 8 * 65535 ? TA_OK : fail(TA_ERR_BAD_SHAPE, "H / Hkv * N exceeds the grid limit");
 }
 
 }  // namespace
@@ -422,7 +426,7 @@ int cache_attn_write(const void* k, const void* v, void* k_pages, void* v_pages,
 
 int cache_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes) {
   if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
-  if (int st = check_cache(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
   *bytes = plan_cache(B, H, Hkv, N, d, max_pages).bytes;
   clear_error();
   return TA_OK;
@@ -434,7 +438,7 @@ int cache_attn_fwd(const void* q, const void* k_pages, const void* v_pages, cons
                    void* workspace, size_t workspace_bytes, void* stream) {
   if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || !out)
     return fail(TA_ERR_NULL_PTR, "q, the pages, the scales, table, lens and out must be non-NULL");
-  if (int st = check_cache(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (!std::isfinite(scale)) return fail(TA_ERR_BAD_SCALE, "scale must be finite");
   if (int st = check_aligned({q, k_pages, v_pages, out}, 16, "q, out and the pages must be 16-byte aligned")) return st;

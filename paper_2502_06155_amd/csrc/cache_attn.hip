@@ -702,7 +702,9 @@ hipError_t cache_attn_for(const CacheAttnArgs& a, hipStream_t s) {
 int cache_rows_per_pass(int rows) { return rows <= 16 ? 16 : 32; }
 
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((kBlock - 1 + (int64_t)a.N + kBlock - 1) / kBlock), (unsigned)(a.B * a.Hkv), 2);
+  // The pages that N tokens can touch, of a table's.
+  const int64_t pages = std::min<int64_t>((kBlock - 1 + (int64_t)a.N + kBlock - 1) / kBlock, a.max_pages);
+  const dim3 grid((unsigned)pages, (unsigned)(a.B * a.Hkv), 2);
   if (a.d == 64) cache_write_kernel<64><<<grid, kThreadsC, 0, stream>>>(a);
   else if (a.d == 96) cache_write_kernel<96><<<grid, kThreadsC, 0, stream>>>(a);
   else cache_write_kernel<128><<<grid, kThreadsC, 0, stream>>>(a);

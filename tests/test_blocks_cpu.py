@@ -280,3 +280,12 @@ def test_the_workspace_of_cache_attention_stays_small_however_many_tokens():
                     assert ta.cache_attn_fwd_workspace(B, G * Hkv, Hkv, N, d, pages) < 70e6, (G, N, B, pages)
     assert ta.cache_attn_fwd_workspace(1, 32, 8, 1, 128, 512) == 512 * 2 * 16 * 132 * 4   # few rows: as many workgroups
     assert ta.cache_attn_fwd_workspace(1, 32, 8, 32, 128, 512) == 4 * 256 * 2 * 32 * 132 * 4  # as the device holds
+
+
+def test_a_prompt_of_any_length_may_be_written():
+    """Only attention has a limit on its tokens (of a key head's rows); these tensors overlap, which is
+    found behind the sizes."""
+    assert _write(N=600000, max_pages=5000) == OVERLAP and _write(N=2 ** 31 - 1, max_pages=1 << 23) == OVERLAP
+    assert _cache(N=600000, max_pages=5000) == SHAPE and "H / Hkv * N" in lib.tile_attn_last_error().decode()
+    with pytest.raises(ta.TileAttnError):
+        ta.cache_attn_fwd_workspace(1, 1, 1, 8 * 65535 + 1, 64, 5000)

@@ -377,3 +377,24 @@ def test_chunks_of_a_prompt(B, H, Hkv, N, d, lens, width):
     again = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens))
     assert torch.equal(got, again)
     assert N < 1030 or ta.cache_attn_fwd_workspace(B, H, Hkv, N, d, width) == 0
+
+
+def test_a_long_prompt_written_at_once():
+    """More tokens than attention takes rows, into a table a little too short for them: the same codes
+    as in two calls."""
+    N, d, pages = 540000, 64, 4200
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((1, 1, N, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    table = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32)[None]
+    got = []
+    for cuts in ((0, N), (0, 128 * 2000, N)):
+        cache = [torch.zeros((pages, 1, *s), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for s in ((128, d), (d, 128))]
+        cache += [torch.zeros((pages, 1), device="cuda") for _ in range(2)]
+        for a, b in zip(cuts, cuts[1:]):
+            ta.cache_write(k[:, :, a:b].contiguous(), v[:, :, a:b].contiguous(), *cache, table, i32([a]))
+        got.append([x.view(torch.uint8) for x in cache])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    last = int(table[0, -1])
+    want = k[0, 0, 128 * (pages - 1):128 * pages].float()
+    codes = got[0][0][last, 0].view(torch.float8_e4m3fn).float() * got[0][2].view(torch.float32)[last, 0]
+    assert ((codes - want).abs() <= 2.0 ** -4 * want.abs() + 2.0 ** -16).all()
