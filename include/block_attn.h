@@ -27,9 +27,12 @@
  *     its own gradients and those of all rows of a query block that lists it, and a row that is no
  *     number those of all keys of the blocks it lists. A row whose log-sum-exp is NaN gives NaN to
  *     dv of the keys it attends to, and to no other dv.
+ *   - Logits scale * <q, k> up to 2^29 in magnitude: past that the rounding of a row's maximum in
+ *     fp32 leaves the exponent's range, and rows may come out as zeros or NaN. The log-sum-exp is
+ *     fp32 too, so weights in the gradients are off by up to 2^-23 of the logit's magnitude.
  *   - lists: DEVICE int32 [B, Hkv, NQ, n_list], 1 <= n_list <= TA_MAX_BLOCKS, the blocks a query
- *     block's rows (of all G heads) attend to, in any order. Entries outside 0..NB-1 are skipped (-1 fills up), and a block
- *     that is listed twice counts once.
+ *     block's rows (of all G heads) attend to, in any order. Entries outside 0..NB-1 are skipped
+ *     (-1 fills up), and a block that is listed twice counts once.
  *   - Nothing is allocated and nothing is kept between calls. What a call needs beside its tensors
  *     the caller hands in: workspace, DEVICE memory of at least the bytes that the entry's
  *     ..._workspace function gives for the same sizes, 16-byte aligned (NULL if that is 0), used

@@ -636,3 +636,23 @@ def test_means_are_rounded_once():
         q = x[:, :, 128 * i:128 * (i + 1)].copy()
         q[..., 1] = 1
         assert ta.block_lists(to_dev(ob.to_bf16(q)), to_dev(km), 256, 1, local=0).item() == best, i
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 28])
+def test_logits_of_a_large_size(d, size):
+    """Scores of few bits, exact in fp32, up to the stated limit: the rows give the mean of the values
+    of their largest ones (the next are at least 2^15 below), and nothing overflows."""
+    rng = np.random.default_rng(d)
+    S = 300
+    q, k, v = np.zeros((1, 1, S, d)), np.zeros((1, 1, S, d)), bits(rng, 1, 1, S, d)
+    q[..., 3] = rng.choice([-1.0, 1.0], (1, 1, S))
+    k[..., 3] = rng.integers(-32, 33, (1, 1, S)) * (size / 32)
+    qb, kb = ob.to_bf16(q), ob.to_bf16(k)
+    lists = np.array([[[[0, 1, 2]] * 3]], np.int32)
+    for causal in (False, True):
+        out, lse = ta.block_attn(to_dev(qb), to_dev(kb), to_dev(v), i32(lists), causal, 1.0, return_lse=True)
+        ref, rlse, mag = ob.attention(qb, kb, v, lists, causal, None, 1.0)
+        # the weights of equal scores are equal, one rounding to bf16 each
+        within(widen(from_dev(out)), ref, HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30, "out")
+        assert (np.abs(lse.cpu().numpy() - rlse) <= 2.0 ** -22 * np.abs(rlse) + 1e-3).all()
