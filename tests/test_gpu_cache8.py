@@ -398,3 +398,75 @@ def test_a_long_prompt_written_at_once():
     want = k[0, 0, 128 * (pages - 1):128 * pages].float()
     codes = got[0][0][last, 0].view(torch.float8_e4m3fn).float() * got[0][2].view(torch.float32)[last, 0]
     assert ((codes - want).abs() <= 2.0 ** -4 * want.abs() + 2.0 ** -16).all()
+
+
+@pytest.mark.parametrize("B,H,Hkv,N,d,width,most", [
+    (1, 4, 4, 1, 64, 40, 40),
+    (3, 8, 2, 1, 128, 40, 23),
+    (2, 12, 3, 4, 96, 33, 33),
+    (2, 40, 2, 2, 128, 20, 20),    # 40 rows a key head: two passes
+    (40, 6, 3, 1, 64, 20, 20),     # more segments than a wave scans at once
+    (1, 8, 2, 70, 64, 40, 30),     # nine passes that share the workgroups
+])
+def test_a_page_table_for_each_key_head_on_the_shared_line(B, H, Hkv, N, d, width, most):
+    """Tables longer than a workgroup takes alone, with lengths of every kind per key head: none, within
+    the first page, full pages, past the table; some entries name no page."""
+    rng = np.random.default_rng(width + H)
+    n_pages = 4 * width
+    cache = new_pages(rng, n_pages, Hkv, d)
+    for x in cache[:2]:
+        x[(x & 127) == 127] = 3
+    table = np.stack([rng.permutation(n_pages)[:width] for _ in range(B * Hkv)]).reshape(B, Hkv, width).astype(np.int32)
+    table[rng.random(table.shape) < 0.05] = -1
+    table[rng.random(table.shape) < 0.02] = n_pages
+    lens = rng.integers(N, 128 * most + 1, (B, Hkv)).astype(np.int32)
+    lens.flat[rng.permutation(B * Hkv)[:max(1, B * Hkv // 4)]] = rng.choice([0, 1, 128, 128 * width, 2 ** 31 - 1])
+    lens.flat[0] = 128 * most
+    assert ta.cache_attn_fwd_workspace(B, H, Hkv, N, d, width) > 0
+    q = bits(rng, B, H, N, d)
+    out = torch.full((B, H, N, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    got, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), None, out, return_lse=True)
+    check(got, lse, q, cache, table, lens)
+
+
+def test_pages_chosen_for_each_key_head_of_a_long_sequence():
+    """The lists of a token as page tables of more than 16 pages, made on the device and captured with
+    the attention: replayed for other queries, the same as over the lists on the numbers the pages hold."""
+    rng = np.random.default_rng(41)
+    H, Hkv, d, S, n = 8, 2, 128, 128 * 60 - 37, 24
+    nb = -(-S // 128)
+    cache, table = held(rng, 1, Hkv, d, [S])
+    gpu, t = to_gpu(cache), i32(table)
+    values = ob.e4m3_values()
+    keys = np.zeros((1, Hkv, S, d))
+    for i in range(nb):
+        m = min(128, S - 128 * i)
+        for h in range(Hkv):
+            keys[0, h, 128 * i:128 * i + m] = values[cache[0][table[0, i], h, :m]] * cache[2][table[0, i], h]
+    kb = ob.to_bf16(keys)
+    assert np.array_equal(ob.widen(kb), keys)
+    km = ta.block_means(to_dev(kb))
+    q = to_dev(bits(rng, 1, H, 1, d))
+
+    def step():
+        lists = ta.block_lists(q, km, S, n, True, 1, 2)[:, :, 0]       # ascending, the last block last
+        pages = t[0][lists.clamp(min=0).long()].to(torch.int32)
+        lens = (torch.full_like(pages[..., 0], n * 128 - (128 * nb - S)))
+        return lists, *ta.cache_attn(q, *gpu, pages, lens, return_lse=True)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lists, out, lse = step()
+    for _ in range(3):
+        x = bits(rng, 1, H, 1, d)
+        q.copy_(to_dev(x))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ob.block_lists(x, ob.block_means(kb), S, n, True, 1, 2)
+        assert np.array_equal(lists.cpu().numpy(), want[:, :, 0])
+        check(out, lse, x, cache, table[0][want[:, :, 0]], np.full((1, Hkv), n * 128 - (128 * nb - S)))
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (lists, out, lse)))
