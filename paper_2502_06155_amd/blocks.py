@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import warnings
 
 from ._lib import lib
 from .api import _check, _ptr, _stream
@@ -112,6 +113,13 @@ def _want(t, name: str, shape, dtype, device) -> None:
     raise ValueError(f"{name} must be contiguous")
 
 
+def _unrecorded(name: str, instead: str) -> None:
+    """Called where an input requires a gradient: says that the outputs carry no graph, if autograd
+    would have recorded the call."""
+    if torch.is_grad_enabled():
+        warnings.warn(f"{name} is not recorded by autograd, its inputs get no gradient from it: {instead}", stacklevel=3)
+
+
 def _out(out, shape, dtype, device):
     """The output that the caller gave, or a new one."""
     if out is None:
@@ -198,8 +206,11 @@ def _check_qkv(q, k, v, lists):
 
 def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=None, out=None, return_lse=False):
     """Attention over the listed blocks: q [B, H, Sq, d], k and v [B, Hkv, Skv, d], lists as
-    block_lists gives them. The rows are the last Sq of Skv positions. Returns out, or (out, lse)."""
+    block_lists gives them. The rows are the last Sq of Skv positions. Autograd does not record it (it
+    warns where it would have): block_attn_grad gives the gradients. Returns out, or (out, lse)."""
     sizes = _check_qkv(q, k, v, lists)
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _unrecorded("block_attn", "block_attn_grad gives the gradients")
     B, H, _, Sq, _, d, _ = sizes
     with _on(q.device):
         if out is None:
@@ -269,9 +280,12 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
                return_lse=False):
     """Attention of q [B, H, N, d], the last N tokens of each sequence, over the cache; lens counts
     them. table [B, max_pages] with lens [B], or, for pages chosen per key head, [B, Hkv, max_pages]
-    with [B, Hkv]. Returns out, or (out, lse)."""
+    with [B, Hkv]. It has no gradient (and warns where autograd would have recorded it). Returns out,
+    or (out, lse)."""
     if q.dim() != 4 or not q.is_cuda:
         raise ValueError("q must be a [B, H, N, d] tensor on a GPU")
+    if q.requires_grad:
+        _unrecorded("cache_attn", "it has no gradient")
     pages, Hkv, d = _check_cache(k_pages, v_pages, k_scales, v_scales, q.device)
     B, H, N, _ = q.shape
     _want(q, "q", (B, H, N, d), torch.bfloat16, q.device)

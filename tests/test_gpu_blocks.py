@@ -656,3 +656,35 @@ def test_logits_of_a_large_size(d, size):
         # the weights of equal scores are equal, one rounding to bf16 each
         within(widen(from_dev(out)), ref, HALF * np.abs(ref) + (HALF + FP32) * mag + 1e-30, "out")
         assert (np.abs(lse.cpu().numpy() - rlse) <= 2.0 ** -22 * np.abs(rlse) + 1e-3).all()
+
+
+def test_calls_that_autograd_does_not_record_say_so(recwarn):
+    q, k, v, go = _inputs(3)
+    lists = ta.block_lists(q, ta.block_means(k), 900, 3)
+    ref, lse = ta.block_attn(q, k, v, lists, return_lse=True)
+    with torch.no_grad():
+        ta.block_attn(q.clone().requires_grad_(), k, v, lists)
+    assert not recwarn.list
+    for i in range(3):
+        x = [t.clone().requires_grad_() if j == i else t for j, t in enumerate((q, k, v))]
+        with pytest.warns(UserWarning, match="block_attn_grad"):
+            out = ta.block_attn(*x, lists)
+        assert torch.equal(out, ref) and not out.requires_grad
+
+    class Sparse(torch.autograd.Function):  # how a program records it
+        @staticmethod
+        def forward(ctx, q, k, v):
+            out, lse = ta.block_attn(q, k, v, lists, return_lse=True)
+            ctx.save_for_backward(q, k, v, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            q, k, v, out, lse = ctx.saved_tensors
+            return ta.block_attn_grad(q, k, v, lists, out, dout.contiguous(), lse)
+
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    Sparse.apply(*leaves).backward(go)
+    assert not recwarn.list
+    for t, g in zip(leaves, ta.block_attn_grad(q, k, v, lists, ref, go, lse)):
+        assert torch.equal(t.grad, g)

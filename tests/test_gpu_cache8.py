@@ -470,3 +470,13 @@ def test_pages_chosen_for_each_key_head_of_a_long_sequence():
         eager = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, (lists, out, lse)))
+
+
+def test_attention_that_autograd_does_not_record_says_so():
+    rng = np.random.default_rng(1)
+    cache, table = held(rng, 1, 2, 64, [200])
+    q = to_dev(bits(rng, 1, 4, 1, 64))
+    ref = ta.cache_attn(q, *to_gpu(cache), i32(table), i32([200]))
+    with pytest.warns(UserWarning, match="no gradient"):
+        out = ta.cache_attn(q.clone().requires_grad_(), *to_gpu(cache), i32(table), i32([200]))
+    assert torch.equal(out, ref) and not out.requires_grad
