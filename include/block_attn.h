@@ -16,17 +16,19 @@
  *     key head h / G with G = H / Hkv.
  *   - The Sq query rows of a sequence are its last Sq positions: row r sits at position
  *     Skv - Sq + r, 1 <= Sq <= Skv. Query blocks are cut at row 0, key blocks at position 0;
- *     NQ = ceil(Sq / TA_BLOCK), NB = ceil(Skv / TA_BLOCK) <= TA_MAX_BLOCKS.
+ *     NQ = ceil(Sq / TA_BLOCK), NB = ceil(Skv / TA_BLOCK) <= TA_MAX_BLOCKS. Skv - Sq is the same
+ *     for all sequences of a call, whatever their lens: single tokens of sequences of different
+ *     lengths take a call for each (cache_attn_fwd takes them together).
  *   - lens: DEVICE int32 [B], 4-byte aligned, or NULL for Skv everywhere. Positions from lens[b]
  *     on are padding: their keys count for nobody, whatever they hold, and their query rows give
  *     zeros, a log-sum-exp of -inf and zero gradients. Values are taken into 0..Skv.
  *   - causal: nonzero lets a row attend only to positions up to its own.
- *   - A row's result depends on the tokens it attends to alone: infinities and NaN elsewhere, in
- *     later tokens too, do not reach it. A row that meets a NaN has NaN for its log-sum-exp. For
- *     gradients this holds between query blocks only: a key or value that is no number may reach
- *     its own gradients and those of all rows of a query block that lists it, and a row that is no
- *     number those of all keys of the blocks it lists. A row whose log-sum-exp is NaN gives NaN to
- *     dv of the keys it attends to, and to no other dv.
+ *   - For given lists a row's result depends on the tokens it attends to alone: infinities and NaN
+ *     elsewhere, in later tokens too, do not reach it. A row that meets a NaN has NaN for its
+ *     log-sum-exp. For gradients this holds between query blocks only: a key or value that is no
+ *     number may reach its own gradients and those of all rows of a query block that lists it, and a
+ *     row that is no number those of all keys of the blocks it lists. A row whose log-sum-exp is NaN
+ *     gives NaN to dv of the keys it attends to, and to no other dv.
  *   - Logits scale * <q, k> up to 2^29 in magnitude: past that the rounding of a row's maximum in
  *     fp32 leaves the exponent's range, and rows may come out as zeros or NaN. The log-sum-exp is
  *     fp32 too, so weights in the gradients are off by up to 2^-23 of the logit's magnitude.
@@ -73,7 +75,10 @@ int block_attn_means(const void* x, void* means, int B, int H, int S, int d, con
  * (the first `sink` blocks, and where local >= 1 the blocks that the rows themselves lie in, with
  * local - 1 more before them and, if not causal, behind them), then those of the highest scores,
  * n_list in all, equal scores by the lower index; a score that is NaN counts as the lowest. The
- * list is ascending, -1 behind its end.
+ * list is ascending, -1 behind its end. The rows of a query block share one list, chosen by the mean
+ * of them all: with causal too, which blocks an early row attends to depends on rows up to
+ * TA_BLOCK - 1 later (no row attends to a later token). So a model trained with the lists of whole
+ * query blocks sees its choice made by later tokens, and decodes (Sq = 1) by the token's own.
  * q: bf16 [B, H, Sq, d]; kmeans: bf16 [B, Hkv, NB, d] (block_attn_means of the keys).
  * Errors: TA_ERR_BAD_SHAPE also where n_list may not hold the forced blocks.
  */

@@ -178,7 +178,11 @@ def block_lists(q, kmeans, Skv: int, n_list: int, causal=False, sink: int = 0, l
     """The key blocks that each block of 128 query rows attends to, chosen by the product of the
     block means: q [B, H, Sq, d], kmeans [B, Hkv, ceil(Skv / 128), d] (block_means of the keys) ->
     int32 [B, Hkv, ceil(Sq / 128), n_list], ascending, -1 behind the end. The first `sink` blocks
-    and the rows' own (with local - 1 more beside them; local = 0: none) are always chosen."""
+    and the rows' own (with local - 1 more beside them; local = 0: none) are always chosen. The rows
+    are the last Sq of Skv positions, the same in every sequence: with lens, a query block whose rows
+    are all padding gets an empty list. One list serves all rows of a query block, chosen by the mean
+    of them all: with causal too, which blocks a row gets depends on rows up to 127 later (Sq = 1
+    chooses by the token alone, as a program that decodes does)."""
     B, H, Hkv, Sq, nb, d = _heads(q, kmeans)
     if nb != -(-Skv // BLOCK_TOKENS):
         raise ValueError(f"kmeans must hold {-(-Skv // BLOCK_TOKENS)} blocks for Skv = {Skv}, got {nb}")
@@ -206,8 +210,10 @@ def _check_qkv(q, k, v, lists):
 
 def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=None, out=None, return_lse=False):
     """Attention over the listed blocks: q [B, H, Sq, d], k and v [B, Hkv, Skv, d], lists as
-    block_lists gives them. The rows are the last Sq of Skv positions. Autograd does not record it (it
-    warns where it would have): block_attn_grad gives the gradients. Returns out, or (out, lse)."""
+    block_lists gives them. The rows are the last Sq of Skv positions, the same in every sequence: with
+    lens, rows from lens[b] on are padding and give zeros, so decoding sequences of different lengths
+    takes a call for each (cache_attn takes them together). Autograd does not record it (it warns where
+    it would have): block_attn_grad gives the gradients. Returns out, or (out, lse)."""
     sizes = _check_qkv(q, k, v, lists)
     if q.requires_grad or k.requires_grad or v.requires_grad:
         _unrecorded("block_attn", "block_attn_grad gives the gradients")

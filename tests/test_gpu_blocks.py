@@ -688,3 +688,21 @@ def test_calls_that_autograd_does_not_record_say_so(recwarn):
     assert not recwarn.list
     for t, g in zip(leaves, ta.block_attn_grad(q, k, v, lists, ref, go, lse)):
         assert torch.equal(t.grad, g)
+
+
+def test_a_causal_list_is_chosen_by_all_rows_of_its_query_block():
+    """What the documentation says of lists: a later row of the same block moves the choice of an
+    earlier one, rows of later blocks do not; and with lens a query block of padding has none."""
+    S, d = 128 * 12, 64
+    q, k = np.zeros((1, 1, S, d)), np.zeros((1, 1, S, d))
+    for j in range(12):
+        k[0, 0, 128 * j:128 * (j + 1), j] = 1
+    q[0, 0, 128 * 8, 2], q[0, 0, 128 * 8 + 100, 5], q[0, 0, 128 * 9:, 7] = 1, 2, 9
+    means = ta.block_means(to_dev(ob.to_bf16(k)))
+    run = lambda x, lens=None: ta.block_lists(to_dev(ob.to_bf16(x)), means, S, 2, True, 0, 1, i32(lens)).cpu().numpy()[0, 0]  # noqa: E731
+    assert run(q)[8].tolist() == [5, 8]
+    q[0, 0, 128 * 8 + 100] = 0
+    assert run(q)[8].tolist() == [2, 8]
+    assert run(q, [128 * 8])[7:].tolist() == [[0, 7]] + [[-1, -1]] * 4
+    alone = ta.block_lists(to_dev(ob.to_bf16(q[:, :, 128 * 8:128 * 8 + 1])), means[:, :, :9].contiguous(), 128 * 8 + 1, 2, True)
+    assert alone.flatten().tolist() == [2, 8]
