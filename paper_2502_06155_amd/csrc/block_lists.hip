@@ -20,6 +20,8 @@
 namespace ta {
 namespace {
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kThreadsL = 256;
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -422,7 +424,7 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
     Gate gates[4];  // of this lane's four rows of the 16
 #pragma unroll
     for (int x = 0; x < 4; ++x) gates[x] = gate_of(i0 + 4 * k + x);
-    uint32_t most = 0;  // the largest magnitude of a key mean, as bf16 bits in the upper half
+    u16x2 mosts = {0, 0};  // the largest magnitudes of key means, even and odd dims apart
     for (int j0 = 16 * wave; j0 < stride; j0 += 16 * kWavesM) {
       const int j = j0 + n;
       u32x4 w[kC];
@@ -434,7 +436,8 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
       for (int c = 0; c < kC; ++c) {
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qa[c], as_bf16x8(w[c]), s, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most = max(most, max((w[c][e] << 16) & 0x7fff0000u, w[c][e] & 0x7fff0000u));
+        for (int e = 0; e < 4; ++e)
+          mosts = __builtin_elementwise_max(mosts, __builtin_bit_cast(u16x2, w[c][e] & 0x7fff7fffu));
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -443,7 +446,7 @@ __global__ __launch_bounds__(kThreadsM) void block_lists_kernel(const ListsArgs 
           keys[(size_t)r * stride + j] = j >= gates[x].end ? 0u : gates[x].forced(j, a.sink) ? kForced<uint32_t> : score_key(s[x]);
       }
     }
-    most = most_of(most);
+    const uint32_t most = most_of((uint32_t)max(mosts[0], mosts[1]) << 16);  // as the bits of an fp32
     if (lane == 0) hists[wave] = most;
   }
   __syncthreads();
