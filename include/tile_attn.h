@@ -173,7 +173,8 @@ int tile_attn_fwd_mmdit(const void* q, const void* k, const void* v, void* out,
  *   them with the same masks and scale (out bf16 [B, H, S, d], lse fp32 [B, H, S],
  *   DEVICE). dout: DEVICE bf16 [B, H, S, d], the gradient of out.
  * dq, dk, dv: DEVICE bf16 [B, H, S, d] outputs, fully written (rounded to bf16,
- *   RNE, from fp32 sums). They must not overlap each other or any input.
+ *   RNE, from fp32 sums). They must not overlap each other or any input. A row whose
+ *   lse is NaN shows in dq and dk; dv leaves it out.
  * tile_masks, n_masks: as for tile_attn_fwd_heads. All bf16 tensors 16-byte
  *   aligned, lse 4-byte aligned.
  * Workspace: B*H*S*8 bytes for the base-2 lse and delta, plus fp32 partials for

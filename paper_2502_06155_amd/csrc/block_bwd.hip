@@ -17,13 +17,15 @@
 //            tiles of its query blocks and heads: S = Q K^T, dP = dO V^T, dV^T += dO^T P,
 //            dK^T += Q^T dS; a lane owns one key.
 //   sum      adds the pieces of cut units, in order.
-// Measured: 24 heads of 28800 tokens, 32 of 225 blocks each, d = 96: 3455 us, 787 TFLOP/s as five products
-// and 1100 as the seven that run (a library product of 16384^3: 1312; vector issue beside the matrix
-// cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks, causal, d = 128: 1200 us, of it dk, dv 660,
-// dq 490, prep 22, sum 17, plan 7. 12 heads of 2251 tokens, 6 blocks, d = 64: 47 us, of it 39 for both
-// passes, whose columns and units are few, and two short launches around them.
-// Roundings: P and dS to bf16 before they enter a product (the matrix cores take nothing wider at this
-// rate), and the results at the end; S, dP, delta, all sums and cut pieces' parts are fp32.
+// Measured, a call, from card to card: 24 heads of 28800 tokens, 32 of 225 blocks each, d = 96: 3440 to 3580
+// us, 790 to 760 TFLOP/s as five products and 1105 to 1065 as the seven that run (a library product of
+// 16384^3: 1312; vector issue beside the matrix cores). 16 heads on 4 key heads, 16384 tokens, 24 blocks,
+// causal, d = 128: 1180 to 1240 us; kernel by kernel dk, dv 700, dq 520, prep 22, sum 16, plan 7. 12 heads of
+// 2251 tokens, 6 blocks, d = 64: 46 us, of it 38 for both passes, whose columns and units are few, and two
+// short launches around them.
+// Roundings: P and dS to bf16 before they enter a product (the matrix cores take fp32 at a sixteenth of
+// the rate), and the results at the end; S, dP, delta, all sums and cut pieces' parts are fp32. They
+// move the gradients' error against 64 bits, the results' own rounding in it, from 1.8e-3 to 2.4e-3.
 // S and dP are formed in both passes: adding dq up from the key side would take fp32 atomics, whose
 // order changes results, and more L2 traffic than the matrix cores' time it saves.
 #include <hip/hip_runtime.h>

@@ -8,13 +8,16 @@
 // The reference m of the exponentials moves only when a lane's sum of weights over 32 keys passes
 // 2^10 (the first block of a row always moves it): weights up to that are as exact as weights up
 // to 1, and the common path needs no row maximum. Row sums add the weights in fp32 before they are
-// rounded to bf16 for the second product, so the log-sum-exp keeps fp32 accuracy.
+// rounded to bf16 for the second product, so the log-sum-exp keeps fp32 accuracy. (The matrix cores
+// take bf16 at this rate and fp32 at a sixteenth of it; the rounding moves the error against 64 bits,
+// the results' own rounding in it, from 1.7e-3 to 1.8e-3.)
 //
 // What bounds it: vector issue beside the matrix cores, an exponential, a multiply-add, an addition and
-// half a conversion a score. 6 heads of 86400 tokens, 68 of 675 blocks each, d = 96: 1580 us = 1095
-// TFLOP/s of kept pairs, 83% of what a library product of 16384^3 reaches on the card (1312). Two column
-// blocks of 32 rows a wave, which feed two matrix instructions with every operand read (the waves split
-// the keys), took 1640: LDS is not the bound.
+// half a conversion a score, and at this size the card's power. 6 heads of 86400 tokens, 68 of 675 blocks
+// each, d = 96: 1610 to 1700 us a call from card to card = 1075 to 1020 TFLOP/s of kept pairs, 78 to 82% of
+// what a library product of 16384^3 reaches (1312); 1580 on a rested card. Two column blocks of 32 rows a
+// wave, which feed two matrix instructions with every operand read (the waves split the keys), took 1690
+// where one took 1640: LDS is not the bound.
 //
 // The list becomes a bitmap in LDS at the start (a few hundred entries): repeated and impossible
 // entries vanish, the blocks come in ascending order whatever the list's order was, and the walk

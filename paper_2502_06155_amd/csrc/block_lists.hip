@@ -7,8 +7,9 @@
 // hang on the order of the additions, and a plain program gets the same lists.
 //
 // Measured, 6 heads of 86400 tokens of 96, 68 of 675 blocks each: means 16.5 us for 100 MB (6 TB/s), lists
-// 40 (reading q takes 20 at the rate of a copy; the rest is the choice). One token of 4 sequences, 16 heads
-// on 4 key heads, 32 of 256 blocks: 10 us, the latency of a chain of means, scores, counts and bounds.
+// 40 (reading q takes 20 at the rate of a copy; the rest is the choice, during which memory idles: all
+// workgroups are resident at once and in the same phase). One token of 4 sequences, 16 heads on 4 key
+// heads, 32 of 256 blocks: 10.5 us, the latency of a chain of means, scores, counts and bounds.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 // attention
 //
 // The cache's bytes bound this: a decoding step reads every code once and does 4 G N operations a
-// byte (32 sequences of 512 to 65536 tokens, 8 key heads of 128: 185 to 188 us for 0.9 GB, 4.9 TB/s; a
+// byte (32 sequences of 512 to 65536 tokens, 8 key heads of 128: 185 to 188 us for 0.92 GB, 4.9 TB/s; a
 // large copy reaches 5.0). A wave takes a page at a time, its codes from memory straight into registers, one page ahead,
 // as the operands of v_mfma_f32_16x16x32_bf16 (A: lane l holds row l % 16 and the k indices 8 (l / 16) .. + 7; B the
 // same with columns; C: column l % 16, rows 4 (l / 16) + j):
@@ -197,7 +197,8 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 //   O^T += V^T P^T, whose V operand is 16 bytes of a V row (tokens 16 g .. + 15).
 // e4m3 codes become bf16 exactly (v_cvt_scalef32_pk_bf16_fp8); the page's K scale multiplies the
 // scores and its V scale the weights, in fp32. The row sums add the weights before they are rounded
-// to bf16 for the matrix cores.
+// to bf16, times the V scale, for the matrix cores (which take fp32 at a sixteenth of the rate): that
+// rounding moves the error against 64 bits, the results' own in it, from 1.7e-3 to 2.2e-3.
 //
 // The pages of all sequences and key heads form one line that `workers` workgroups share evenly,
 // whatever the lengths: a workgroup runs the (sequence, head) segments its stretch meets, writes
