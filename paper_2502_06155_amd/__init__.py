@@ -41,3 +41,17 @@ from .blocks import (  # noqa: F401
     cache_attn_write,
     cache_write,
 )
+from .rope import (  # noqa: F401
+    NORMS,
+    ROPE_AXES,
+    ROPE_LAYOUTS,
+    HeadRopeSpec,
+    Rows,
+    grid_positions,
+    head_rope,
+    head_rope_bwd,
+    head_rope_bwd_workspace,
+    head_rope_fwd,
+    head_rope_grad,
+    rope_freqs,
+)

@@ -33,6 +33,9 @@ EXPORTS = (
     "cache_attn_write",
     "cache_attn_fwd_workspace",
     "cache_attn_fwd",
+    "head_rope_fwd",
+    "head_rope_bwd_workspace",
+    "head_rope_bwd",
 )
 
 
@@ -98,6 +101,9 @@ def _load() -> ctypes.CDLL:
         "cache_attn_write": [vp] * 9 + [ci] * 6 + [vp],
         "cache_attn_fwd_workspace": [ci] * 6 + [pz],
         "cache_attn_fwd": [vp] * 7 + [ci] + [vp] * 2 + [ci] * 7 + [cf, vp, cz, vp],
+        "head_rope_fwd": [vp] * 8,
+        "head_rope_bwd_workspace": [vp, pz],
+        "head_rope_bwd": [vp] * 14 + [cz, vp],
     }.items():
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, ci

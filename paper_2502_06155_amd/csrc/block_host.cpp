@@ -4,11 +4,11 @@
 #include <cfloat>
 #include <climits>
 #include <cmath>
-#include <initializer_list>
 #include <string>
 
 #include "block_attn.h"
 #include "block_launch.h"
+#include "host_checks.h"
 #include "host_internal.h"
 
 namespace ta {
@@ -17,48 +17,6 @@ namespace {
 
 static_assert(kBlock == TA_BLOCK, "block size");
 static_assert(kBlockWords * 32 == TA_MAX_BLOCKS, "bitmap size");
-
-// Workgroups that the device runs at a time at two per compute unit (256 units). Work is cut by
-// this number, not by the device's own, so that workspaces have the same size everywhere.
-constexpr int64_t kSlots = 512;
-constexpr int64_t kMaxGrid = (int64_t)UINT32_MAX / 256 - 8;
-
-struct Span {
-  const void* p;
-  size_t bytes;
-};
-size_t bf16s(int64_t n) { return (size_t)n * 2; }
-
-int check_aligned(std::initializer_list<const void*> ps, unsigned align, const char* what) {
-  for (const void* p : ps)
-    if (p && reinterpret_cast<uintptr_t>(p) % align) return fail(TA_ERR_ALIGN, what);
-  return TA_OK;
-}
-// Outputs (and the workspace) must overlap neither an input nor each other.
-int check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
-  for (auto o = outs.begin(); o != outs.end(); ++o) {
-    if (!o->p || !o->bytes) continue;
-    for (const Span& x : ins)
-      if (x.p && x.bytes && ranges_overlap(o->p, o->bytes, x.p, x.bytes))
-        return fail(TA_ERR_OVERLAP, "an output or the workspace overlaps an input");
-    for (auto q = o + 1; q != outs.end(); ++q)
-      if (q->p && q->bytes && ranges_overlap(o->p, o->bytes, q->p, q->bytes))
-        return fail(TA_ERR_OVERLAP, "outputs and the workspace must not overlap each other");
-  }
-  return TA_OK;
-}
-int launched(hipError_t e) {
-  if (e != hipSuccess) return fail(TA_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
-  clear_error();
-  return TA_OK;
-}
-
-int check_grid(double workgroups) {
-  return workgroups <= (double)kMaxGrid ? TA_OK : fail(TA_ERR_BAD_SHAPE, "the call exceeds the grid limit");
-}
-int check_dim(int d) {
-  return d == 64 || d == 96 || d == 128 ? TA_OK : fail(TA_ERR_HEAD_DIM, "d must be 64, 96 or 128");
-}
 
 int make_geo(BlockGeo& g, int B, int H, int Hkv, int Sq, int Skv, int d, int n_list, int causal, const int32_t* lens) {
   if (B < 1 || H < 1 || Hkv < 1 || Sq < 1 || Skv < 1) return fail(TA_ERR_BAD_SHAPE, "B, H, Hkv, Sq and Skv must be >= 1");
@@ -179,12 +137,6 @@ void fold_scale(float scale, float& c, uint32_t& flip, uint32_t& keep) {
   c = scale == 0.f ? 1.f : std::max(std::fabs(scale) * 1.4426950408889634f, FLT_MIN);
   flip = scale < 0.f ? 0x80008000u : 0u;
   keep = scale == 0.f ? 0u : ~0u;
-}
-
-int check_workspace(const void* ws, size_t have, size_t need) {
-  if (have < need || (need && !ws))
-    return fail(TA_ERR_BAD_SHAPE, "the workspace is smaller than the call needs (" + std::to_string(need) + " bytes)");
-  return check_aligned({ws}, 16, "the workspace must be 16-byte aligned");
 }
 
 // Short tables run a workgroup per (sequence, key head), four pages at a time, and need no second

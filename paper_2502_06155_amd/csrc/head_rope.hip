@@ -1,0 +1,493 @@
+// gfx950 (MI355X, CDNA4) kernels of head norms and rotations, forward and gradients.
+//
+// A row (the d values of a head of a token) takes 8 lanes at d = 64 and 16 at 96 (12 of them at work) and
+// 128, 8 values a lane: 16-byte loads and stores, and sums over a row in four or three steps inside the lanes of
+// a DPP row. A wave holds rows of 4 (8) tokens that follow each other, of one head at a time, and goes through the
+// heads: what depends on the token alone, cosines and sines of its angles times the weights, is formed once for
+// all of them, and stores of one head are whole stretches of its [S, d] plane.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "rope_launch.h"
+#include "tile_common.h"
+
+namespace ta {
+namespace {
+
+constexpr int kNone = 0, kRms = 1, kLayer = 2;  // norms
+// How a value's partner is found: no rotation; its neighbour; 8 values that another lane holds; anywhere in
+// the row.
+constexpr int kStill = 0, kNext = 1, kWhole = 2, kAny = 3;
+
+typedef float Floats8[8];
+
+template <int D>
+struct Shape {
+  static constexpr int lanes = D == 64 ? 8 : 16;  // of a row
+  static constexpr int tokens = 64 / lanes;
+  static_assert(tokens == rope_tokens(D), "tokens of a wave");
+};
+
+// The sum over a row's lanes, in all of them: neighbours, pairs, then mirrored halves (of 8 and of 16 lanes).
+template <int CTRL>
+__device__ __forceinline__ float add_from(float x) {
+  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+template <int D>
+__device__ __forceinline__ float row_sum(float x) {
+  x = add_from<0xb1>(x);   // lanes 1 0 3 2 of each four
+  x = add_from<0x4e>(x);   // lanes 2 3 0 1
+  x = add_from<0x141>(x);  // mirrored in 8 lanes
+  if constexpr (D != 64) x = add_from<0x140>(x);  // mirrored in 16 lanes
+  return x;
+}
+
+__device__ __forceinline__ void widen(u32x4 w, Floats8& x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(w[e] << 16);
+    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+  }
+}
+// One rounding to bf16, to nearest, ties to even.
+__device__ __forceinline__ u32x4 narrow(const Floats8& x) {
+  const f32x8 y = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+  return __builtin_bit_cast(u32x4, __builtin_convertvector(y, bf16x8));
+}
+
+// What value e of a head is in the rotation: its partner, its pair (-1: it is not turned), the pair's axis,
+// and whether it is the pair's second value.
+struct Place {
+  int partner, pair, axis;
+  bool second;
+};
+__device__ __forceinline__ Place place_of(const RopeArgs& a, int e) {
+  if (e >= a.turned) return {e, -1, 0, false};
+  int axis = 0;
+  if (a.layout == 3) {  // split
+    const int h = a.turned / 2;
+    const bool second = e >= h;
+    const int pair = second ? e - h : e;
+#pragma unroll
+    for (int x = 1; x < kRopeAxes; ++x)
+      if (x < a.axes && 2 * pair >= a.start[x]) axis = x;
+    return {second ? e - h : e + h, pair, axis, second};
+  }
+  int start = 0, n = a.dims[0];
+#pragma unroll
+  for (int x = 1; x < kRopeAxes; ++x)
+    if (x < a.axes && e >= a.start[x]) {
+      axis = x;
+      start = a.start[x];
+      n = a.dims[x];
+    }
+  if (a.layout == 1) return {e ^ 1, e / 2, axis, (e & 1) != 0};  // interleaved; axes start at even values
+  const int o = e - start;
+  const bool second = o >= n / 2;
+  return {second ? e - n / 2 : e + n / 2, start / 2 + (second ? o - n / 2 : o), axis, second};
+}
+
+// The lane's 8 values in the rotation. Angles: turns = position * (frequency / 2 pi) in fp64, right to 2^-53 of the
+// angle however far the position, then the fraction alone, in fp32, for v_sin_f32 and v_cos_f32 (which take
+// turns; off by at most 1.3e-7 in [-0.5, 0.5]).
+template <int D, int ROT>
+struct Turns {
+  static constexpr int kAngles = ROT == kNext ? 4 : 8;
+  double f[ROT == kStill ? 1 : kAngles];
+  int axis[ROT == kStill ? 1 : kAngles];
+  int from[ROT == kAny ? 8 : 1];  // byte of the partner in its row, or the lane that holds all eight
+  float sign[ROT == kStill || ROT == kNext ? 1 : 8];
+
+  __device__ __forceinline__ void place(const RopeArgs& a, int l) {
+    if constexpr (ROT != kStill) {
+#pragma unroll
+      for (int i = 0; i < kAngles; ++i) {
+        const Place p = place_of(a, min(8 * l + (ROT == kNext ? 2 * i : i), D - 1));
+        f[i] = p.pair >= 0 ? a.freqs[p.pair] * 0.15915494309189533577 : 0.;
+        axis[i] = p.axis;
+        if constexpr (ROT == kAny) from[i] = 2 * p.partner;
+        if constexpr (ROT == kWhole) {
+          if (i == 0) from[0] = p.partner / 8;
+        }
+        // (A lane behind the row takes nothing from it: sums over the row's lanes add it too.)
+        if constexpr (ROT != kNext) sign[i] = 8 * l >= D ? 0.f : p.second ? 1.f : -1.f;
+      }
+    }
+  }
+  // c, s: y_e = n_e c_e + n_partner s_e.
+  __device__ __forceinline__ void at(const RopeArgs& a, int b, int t, Floats8& c, Floats8& s) const {
+    if constexpr (ROT != kStill) {
+      const int32_t* p = a.positions + b * a.positions_batch + (int64_t)t * a.axes;
+      int pos[kRopeAxes];
+#pragma unroll
+      for (int x = 0; x < kRopeAxes; ++x) pos[x] = x < a.axes ? p[x] : 0;
+#pragma unroll
+      for (int i = 0; i < kAngles; ++i) {
+        int at = pos[0];
+#pragma unroll
+        for (int x = 1; x < kRopeAxes; ++x) at = axis[i] == x ? pos[x] : at;
+        const double turns = (double)at * f[i];
+        const float part = (float)(turns - __builtin_rint(turns));
+        const float cs = __builtin_amdgcn_cosf(part), sn = __builtin_amdgcn_sinf(part);
+        if constexpr (ROT == kNext) {
+          c[2 * i] = c[2 * i + 1] = cs;
+          s[2 * i] = -sn;
+          s[2 * i + 1] = sn;
+        } else {
+          c[i] = cs;
+          s[i] = sign[i] * sn;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        c[e] = 1.f;
+        s[e] = 0.f;
+      }
+    }
+  }
+  // The partners of the lane's 8 values of a row. `row`: the 16-byte pieces of the wave's rows in LDS; only
+  // this wave writes and reads them.
+  __device__ __forceinline__ void partners(const u32x4& w, const Floats8& x, u32x4* row, int lane, Floats8& xp) const {
+    constexpr int L = Shape<D>::lanes;
+    if constexpr (ROT == kNext) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xp[e] = x[e ^ 1];
+    } else if constexpr (ROT == kWhole || ROT == kAny) {
+      row[lane] = w;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const u32x4* mine = row + lane / L * L;
+      if constexpr (ROT == kWhole) {
+        widen(mine[from[0]], xp);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          xp[e] = __uint_as_float((uint32_t) * reinterpret_cast<const uint16_t*>(reinterpret_cast<const char*>(mine) + from[e]) << 16);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xp[e] = 0.f;
+    }
+  }
+};
+
+// w[e], e = 8 l .. 8 l + 7, or `none` where there is no array. Lanes behind the row read its last values.
+template <int D>
+__device__ __forceinline__ void load8(const float* w, int l, float none, Floats8& x) {
+  const int e0 = min(8 * l, D - 8);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = w ? w[e0 + e] : none;
+}
+// The same of the values' partners.
+template <int D, int ROT>
+__device__ __forceinline__ void load_partners(const float* w, int l, float none, const Turns<D, ROT>& t, Floats8& x) {
+  if constexpr (ROT == kNext) {
+    Floats8 own;
+    load8<D>(w, l, none, own);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = own[e ^ 1];
+  } else if constexpr (ROT == kWhole) {
+    load8<D>(w, t.from[0], none, x);
+  } else if constexpr (ROT == kAny) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = w ? w[t.from[e] / 2] : none;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  }
+}
+
+// x less its mean (kLayer), and the factor that norms it. A lane behind the row holds zeros and keeps them.
+template <int D, int NORM>
+__device__ __forceinline__ float norm_factor(float eps, bool in_row, Floats8& x, float& mean) {
+  mean = 0.f;
+  if constexpr (NORM == kNone) return 1.f;
+  if constexpr (NORM == kLayer) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += x[e];
+    mean = row_sum<D>(sum) * (1.f / D);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = in_row ? x[e] - mean : 0.f;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+  return __builtin_amdgcn_rsqf(fmaf(row_sum<D>(sum), 1.f / D, eps));
+}
+
+// A lane's token.
+struct Token {
+  int b, t;
+  bool have;   // there is such a token
+  bool valid;  // and it is no padding
+  __device__ __forceinline__ Token(const RopeArgs& a, int64_t i) {
+    const int64_t total = (int64_t)a.B * a.S;
+    have = i < total;
+    const uint32_t n = (uint32_t)(have ? i : total - 1);
+    b = (int)(n / (uint32_t)a.S);
+    t = (int)(n - (uint32_t)b * (uint32_t)a.S);
+    valid = have && t < (a.lens ? a.lens[b] : a.S);
+  }
+};
+
+constexpr int kAhead = 4;  // rows of a lane that are read together
+
+template <int D, int NORM, int ROT>
+__global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeArgs a) {
+  constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
+  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAhead * 64 : 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l = lane % L;
+  const bool in_row = 8 * l < D;
+  const int64_t token0 = ((int64_t)blockIdx.x * kRopeWaves + wave) * kTokens;
+  if (token0 >= (int64_t)a.B * a.S) return;
+  const Token tok(a, token0 + lane / L);
+  const bool reads = tok.valid && in_row, writes = tok.have && in_row;
+
+  Turns<D, ROT> turns;
+  turns.place(a, l);
+  Floats8 c, s;
+  turns.at(a, tok.b, tok.t, c, s);
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * 64 : 0);
+
+  int first = blockIdx.y * a.heads_per, last = first + a.heads_per;  // of q's, k's and v's heads in a line
+#pragma unroll
+  for (int kind = 0; kind < 3; ++kind) {
+    const int h0 = max(first, 0), h1 = min(last, a.heads[kind]);
+    first -= a.heads[kind];
+    last -= a.heads[kind];
+    if (h0 >= h1) continue;
+    const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
+    uint16_t* y0 = a.y[kind] + ((int64_t)tok.b * a.heads[kind] * a.S + tok.t) * D + 8 * l;
+    const int64_t plane = (int64_t)a.S * D;
+    // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean
+    Floats8 A, Bp, C;
+    if (kind < 2) {
+      const float* weight = NORM == kNone ? nullptr : a.weight[kind % 2];
+      const float* bias = NORM == kLayer ? a.bias[kind % 2] : nullptr;
+      Floats8 w, wp, bs, bp;
+      load8<D>(weight, l, 1.f, w);
+      load_partners<D, ROT>(weight, l, 1.f, turns, wp);
+      load8<D>(bias, l, 0.f, bs);
+      load_partners<D, ROT>(bias, l, 0.f, turns, bp);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        A[e] = w[e] * c[e];
+        Bp[e] = wp[e] * s[e];
+        C[e] = NORM == kLayer ? fmaf(bs[e], c[e], bp[e] * s[e]) : 0.f;
+      }
+    }
+    for (int h = h0; h < h1; h += kAhead) {
+      u32x4 in[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        in[u] = u32x4{0u, 0u, 0u, 0u};
+        if (h + u < h1 && reads) in[u] = load16(x0 + (h + u) * a.x[kind].head);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (h + u >= h1) break;
+        u32x4 out = in[u];
+        if (kind < 2 && (NORM != kNone || ROT != kStill)) {
+          Floats8 x, xp, y;
+          widen(in[u], x);
+          turns.partners(in[u], x, rows + (ROT >= kWhole ? 64 * u : 0), lane, xp);
+          float mean;
+          const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z = ROT == kStill ? x[e] * A[e] : fmaf(x[e], A[e], (NORM == kLayer ? xp[e] - mean : xp[e]) * Bp[e]);
+            y[e] = NORM == kNone ? z : NORM == kRms ? r * z : fmaf(r, z, C[e]);
+          }
+          out = narrow(y);
+          if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
+        }
+        if (writes) *reinterpret_cast<u32x4*>(y0 + (h + u) * plane) = out;
+      }
+      if constexpr (ROT >= kWhole) {  // the rows in LDS are read before the next ones replace them
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+}
+
+// Gradients. With g the gradient of a row turned back, xhat the normed row before weights:
+//   db = sum g,  dw = sum g xhat,  u = g w,  dx = r (u - [mean u] - xhat mean(u xhat)).
+// A fixed number of workgroups deals out (tokens, heads) items among its waves, so that the sums of
+// weights and biases, kept in a lane's registers, leave few rows of partial sums; they are added in an order
+// that the sizes set.
+constexpr int kAheadGrad = 2;
+
+template <int D, int NORM, int ROT>
+__global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const RopeArgs a) {
+  constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
+  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAheadGrad * 64 : 1];
+  __shared__ float s_sum[kRopeWaves][2][D];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l = lane % L;
+  const bool in_row = 8 * l < D;
+  const int groups = (int)(((int64_t)a.B * a.S + kTokens - 1) / kTokens);
+  Turns<D, ROT> turns;
+  turns.place(a, l);
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAheadGrad * 64 : 0);
+
+#pragma unroll
+  for (int kind = 0; kind < 3; ++kind) {
+    if (a.heads[kind] == 0) continue;
+    const int parts = (a.heads[kind] + a.heads_per - 1) / a.heads_per;
+    const int64_t items = (int64_t)groups * parts, plane = (int64_t)a.S * D;
+    Floats8 w, dw, db;
+    if (kind < 2) load8<D>(NORM == kNone ? nullptr : a.weight[kind % 2], l, 1.f, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.f;
+    for (int64_t item = (int64_t)blockIdx.x * kRopeWaves + wave; item < items; item += (int64_t)a.workgroups * kRopeWaves) {
+      const int part = (int)(item / groups);
+      const Token tok(a, (item - (int64_t)part * groups) * kTokens + lane / L);
+      const bool reads = tok.valid && in_row, writes = tok.have && in_row;
+      const int h0 = part * a.heads_per, h1 = min(h0 + a.heads_per, a.heads[kind]);
+      const uint16_t* g0 = a.y[kind] + ((int64_t)tok.b * a.heads[kind] * a.S + tok.t) * D + 8 * l;
+      const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
+      uint16_t* d0 = a.dx[kind].p + tok.b * a.dx[kind].batch + tok.t * a.dx[kind].token + 8 * l;
+      Floats8 c, s;
+      if (kind < 2) turns.at(a, tok.b, tok.t, c, s);
+      for (int h = h0; h < h1; h += kAheadGrad) {
+        u32x4 in[kAheadGrad], gin[kAheadGrad];
+#pragma unroll
+        for (int u = 0; u < kAheadGrad; ++u) {
+          in[u] = gin[u] = u32x4{0u, 0u, 0u, 0u};
+          if (h + u < h1 && reads) {
+            gin[u] = load16(g0 + (h + u) * plane);
+            if (kind < 2 && NORM != kNone) in[u] = load16(x0 + (h + u) * a.x[kind].head);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kAheadGrad; ++u) {
+          if (h + u >= h1) break;
+          u32x4 out = gin[u];
+          if (kind < 2 && (NORM != kNone || ROT != kStill)) {
+            Floats8 g, gp;
+            widen(gin[u], g);
+            turns.partners(gin[u], g, rows + (ROT >= kWhole ? 64 * u : 0), lane, gp);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (ROT != kStill) g[e] = fmaf(g[e], c[e], -(gp[e] * s[e]));
+            if constexpr (NORM != kNone) {
+              Floats8 x;
+              widen(in[u], x);
+              float mean;
+              const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
+              float along = 0.f, sum = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                x[e] *= r;
+                dw[e] = fmaf(g[e], x[e], dw[e]);
+                if constexpr (NORM == kLayer) db[e] += g[e];
+                g[e] *= w[e];
+                along = fmaf(g[e], x[e], along);
+                sum += g[e];
+              }
+              along = row_sum<D>(along) * (1.f / D);
+              sum = NORM == kLayer ? row_sum<D>(sum) * (1.f / D) : 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) g[e] = r * (fmaf(-x[e], along, g[e]) - sum);
+            }
+            out = narrow(g);
+            if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
+          }
+          if (writes) *reinterpret_cast<u32x4*>(d0 + (h + u) * a.dx[kind].head) = out;
+        }
+        if constexpr (ROT >= kWhole) {
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+        }
+      }
+    }
+    if constexpr (NORM != kNone) {
+      if (kind < 2 && a.part) {
+        // Tokens of the wave, then waves, then (the second kernel) workgroups.
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+          for (int m = L; m < 64; m <<= 1) {
+            dw[e] += __shfl_xor(dw[e], m);
+            if constexpr (NORM == kLayer) db[e] += __shfl_xor(db[e], m);
+          }
+          if (lane < L && in_row) {
+            s_sum[wave][0][8 * l + e] = dw[e];
+            if constexpr (NORM == kLayer) s_sum[wave][1][8 * l + e] = db[e];
+          }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < (NORM == kLayer ? 2 : 1) * D; i += 64 * kRopeWaves) {
+          float sum = 0.f;
+#pragma unroll
+          for (int x = 0; x < kRopeWaves; ++x) sum += s_sum[x][i / D][i % D];
+          a.part[((int64_t)blockIdx.x * 4 + 2 * kind) * D + i] = sum;
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+// Adds the workgroups' partial sums: a workgroup per 16 columns of one of the four sums.
+constexpr int kSumColumns = 16, kSumThreads = 256;
+__global__ __launch_bounds__(kSumThreads) void head_rope_sum_kernel(const RopeArgs a) {
+  constexpr int kSlices = kSumThreads / kSumColumns;
+  __shared__ float s_sum[kSlices][kSumColumns];
+  float* out = a.sum[blockIdx.y];
+  if (!out || a.heads[blockIdx.y / 2] == 0) return;
+  const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
+  const int e = blockIdx.x * kSumColumns + col;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int w = slice; w < a.workgroups; w += kSlices) sum += a.part[((int64_t)w * 4 + blockIdx.y) * a.d + e];
+  s_sum[slice][col] = sum;
+  __syncthreads();
+  if (slice == 0) {
+    sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < kSlices; ++x) sum += s_sum[x][col];
+    out[e] = sum;
+  }
+}
+
+template <int D, int NORM, int ROT>
+hipError_t run(const RopeArgs& a, bool grad, hipStream_t s) {
+  if (grad) {
+    head_rope_grad_kernel<D, NORM, ROT><<<(unsigned)a.workgroups, 64 * kRopeWaves, 0, s>>>(a);
+    if (NORM != kNone && a.part) head_rope_sum_kernel<<<dim3((unsigned)(D / kSumColumns), 4), kSumThreads, 0, s>>>(a);
+  } else {
+    const int64_t waves = ((int64_t)a.B * a.S + Shape<D>::tokens - 1) / Shape<D>::tokens;
+    const int heads = a.heads[0] + a.heads[1] + a.heads[2];
+    const dim3 grid((unsigned)((waves + kRopeWaves - 1) / kRopeWaves), (unsigned)((heads + a.heads_per - 1) / a.heads_per));
+    head_rope_kernel<D, NORM, ROT><<<grid, 64 * kRopeWaves, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+template <int D, int NORM>
+hipError_t run_rot(const RopeArgs& a, bool grad, hipStream_t s) {
+  if (a.layout == 0) return run<D, NORM, kStill>(a, grad, s);
+  if (a.layout == 1) return run<D, NORM, kNext>(a, grad, s);
+  return a.whole ? run<D, NORM, kWhole>(a, grad, s) : run<D, NORM, kAny>(a, grad, s);
+}
+template <int D>
+hipError_t run_norm(const RopeArgs& a, bool grad, hipStream_t s) {
+  if (a.norm == kNone) return run_rot<D, kNone>(a, grad, s);
+  return a.norm == kRms ? run_rot<D, kRms>(a, grad, s) : run_rot<D, kLayer>(a, grad, s);
+}
+hipError_t run_all(const RopeArgs& a, bool grad, hipStream_t s) {
+  if (a.d == 64) return run_norm<64>(a, grad, s);
+  return a.d == 96 ? run_norm<96>(a, grad, s) : run_norm<128>(a, grad, s);
+}
+
+}  // namespace
+
+hipError_t launch_head_rope(const RopeArgs& a, hipStream_t stream) { return run_all(a, false, stream); }
+hipError_t launch_head_rope_grad(const RopeArgs& a, hipStream_t stream) { return run_all(a, true, stream); }
+
+}  // namespace ta
