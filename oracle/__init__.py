@@ -11,10 +11,11 @@ computes, written from the paper (Efficient-vDiT, arXiv 2502.06155):
 * ``oracle.mmdit``: the MM-DiT form, a dense text prefix before the tile-sparse video
   (Sec. 4.3, App. E).
 * ``oracle.blocks``: attention over selected blocks, its gradients, and the 8-bit cache.
+* ``oracle.cache4``: the 4-bit cache and attention over it.
 * ``oracle.heads``: norms of heads, rotation by positions, and their gradients.
 
 Only ``tests/``, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
 ``bench.py`` may import this package. The product path (the HIP library and
 its Python binding) never imports it, and it imports nothing from the product.
 """
-from . import attention, backward, blocks, heads, masks, mmdit  # noqa: F401
+from . import attention, backward, blocks, cache4, heads, masks, mmdit  # noqa: F401

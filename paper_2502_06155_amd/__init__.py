@@ -41,6 +41,17 @@ from .blocks import (  # noqa: F401
     cache_attn_write,
     cache_write,
 )
+from .cache4 import (  # noqa: F401
+    CACHE4_GROUP,
+    cache4_attn,
+    cache4_attn_fwd,
+    cache4_attn_fwd_workspace,
+    cache4_attn_read,
+    cache4_attn_write,
+    cache4_new,
+    cache4_read,
+    cache4_write,
+)
 from .rope import (  # noqa: F401
     NORMS,
     ROPE_AXES,

@@ -36,6 +36,10 @@ EXPORTS = (
     "head_rope_fwd",
     "head_rope_bwd_workspace",
     "head_rope_bwd",
+    "cache4_attn_write",
+    "cache4_attn_read",
+    "cache4_attn_fwd_workspace",
+    "cache4_attn_fwd",
 )
 
 
@@ -104,6 +108,10 @@ def _load() -> ctypes.CDLL:
         "head_rope_fwd": [vp] * 8,
         "head_rope_bwd_workspace": [vp, pz],
         "head_rope_bwd": [vp] * 14 + [cz, vp],
+        "cache4_attn_write": [vp] * 11 + [ci] * 6 + [vp],
+        "cache4_attn_read": [vp] * 8 + [ci] * 7 + [vp],
+        "cache4_attn_fwd_workspace": [ci] * 6 + [pz],
+        "cache4_attn_fwd": [vp] * 7 + [ci] + [vp] * 2 + [ci] * 7 + [cf, vp, cz, vp],
     }.items():
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, ci

@@ -1,4 +1,4 @@
-// Host side of the C ABI of attention over selected blocks and over the 8-bit cache: argument
+// Host side of the C ABI of attention over selected blocks and over the 8-bit and 4-bit caches: argument
 // checks, how work is cut, and the workspaces' sizes. Nothing is allocated and nothing is kept.
 #include <algorithm>
 #include <cfloat>
@@ -8,6 +8,7 @@
 
 #include "block_attn.h"
 #include "block_launch.h"
+#include "cache4_attn.h"
 #include "host_checks.h"
 #include "host_internal.h"
 
@@ -160,7 +161,7 @@ struct CachePlan {
   bool whole;
   size_t bytes;
 };
-CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
+CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages, int segment = kCacheSegment) {
   CachePlan p;
   const int64_t rows = (int64_t)(H / Hkv) * N;
   p.rows = cache_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
@@ -168,7 +169,7 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   // Two workgroups run on a compute unit in passes of 16 rows, one in passes of 32.
   p.workers = (int)std::min<int64_t>({p.rows == 16 ? kSlots : kSlots / 2,
                                       p.passes < kPassSlots ? std::max<int64_t>(2, kPassSlots / p.passes) : 1,
-                                      (int64_t)B * Hkv * (max_pages + kCacheSegment)});
+                                      (int64_t)B * Hkv * (max_pages + segment)});
   p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
   if (p.whole) p.workers = B * Hkv;
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
@@ -180,7 +181,7 @@ int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   if (H % Hkv) return fail(TA_ERR_BAD_SHAPE, "H must be a multiple of Hkv");
   if (max_pages > INT_MAX / TA_BLOCK) return fail(TA_ERR_BAD_SHAPE, "max_pages pages hold more than 2^31 - 1 tokens");
   // The sequences times heads are a grid dimension of their own.
-  if ((int64_t)B * Hkv * (max_pages + kCacheSegment) > INT_MAX)
+  if ((int64_t)B * Hkv * (max_pages + std::max(kCacheSegment, kCache4Segment)) > INT_MAX)
     return fail(TA_ERR_BAD_SHAPE, "B * Hkv * max_pages exceeds 2^31 - 1");
   if ((int64_t)B * Hkv > 65535) return fail(TA_ERR_BAD_SHAPE, "B * Hkv exceeds the grid limit");
   return check_dim(d);
@@ -435,6 +436,127 @@ int cache_attn_fwd(const void* q, const void* k_pages, const void* v_pages, cons
   a.row_blocks = p.passes;
   a.part = static_cast<float*>(workspace);
   return launched(launch_cache_attn(a, static_cast<hipStream_t>(stream)));
+}
+
+int cache4_attn_write(const void* k, const void* v, void* k_pages, void* v_pages, void* k_scales, void* v_scales,
+                      const int32_t* table, const int32_t* lens, const int32_t* n_new, void* k_held, void* v_held,
+                      int B, int Hkv, int N, int d, int max_pages, int n_pages, void* stream) {
+  if (!k || !v || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens)
+    return fail(TA_ERR_NULL_PTR, "k, v, the pages, the scales, table and lens must be non-NULL");
+  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages)) return st;
+  if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
+  if (int st = check_aligned({k, v, k_pages, v_pages, k_scales, v_scales, k_held, v_held}, 16,
+                             "k, v, their held values, the pages and the scales must be 16-byte aligned"))
+    return st;
+  if (int st = check_aligned({table, lens, n_new}, 4, "table, lens and n_new must be 4-byte aligned")) return st;
+  const size_t new_bytes = bf16s((int64_t)B * Hkv * N * d), pages = (size_t)n_pages * Hkv * TA_BLOCK * d / 2;
+  const size_t scales = pages / (TA_CACHE4_GROUP / 2);
+  if (int st = check_apart({{k_pages, pages}, {v_pages, pages}, {k_scales, scales}, {v_scales, scales},
+                            {k_held, new_bytes}, {v_held, new_bytes}},
+                           {{k, new_bytes},
+                            {v, new_bytes},
+                            {table, (size_t)B * max_pages * 4},
+                            {lens, (size_t)B * 4},
+                            {n_new, (size_t)B * 4}}))
+    return st;
+  const Cache4WriteArgs a{static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v),
+                          static_cast<uint8_t*>(k_pages), static_cast<uint8_t*>(v_pages),
+                          static_cast<uint8_t*>(k_scales), static_cast<uint8_t*>(v_scales), table, lens, n_new,
+                          static_cast<uint16_t*>(k_held), static_cast<uint16_t*>(v_held), B, Hkv, N, d, max_pages,
+                          n_pages};
+  return launched(launch_cache4_write(a, static_cast<hipStream_t>(stream)));
+}
+
+int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_scales, const void* v_scales,
+                     const int32_t* table, const int32_t* lens, void* k_out, void* v_out, int B, int Hkv, int N, int d,
+                     int max_pages, int n_pages, int first, void* stream) {
+  if (!k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || (!k_out && !v_out))
+    return fail(TA_ERR_NULL_PTR, "the pages, the scales, table, lens and k_out or v_out must be non-NULL");
+  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages)) return st;
+  if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
+  if (first < 0 || (int64_t)first + N > INT_MAX) return fail(TA_ERR_BAD_SHAPE, "first must be >= 0, first + N below 2^31");
+  if (int st = check_aligned({k_pages, v_pages, k_scales, v_scales, k_out, v_out}, 16,
+                             "the pages, the scales and the outputs must be 16-byte aligned"))
+    return st;
+  if (int st = check_aligned({table, lens}, 4, "table and lens must be 4-byte aligned")) return st;
+  const size_t out = bf16s((int64_t)B * Hkv * N * d), pages = (size_t)n_pages * Hkv * TA_BLOCK * d / 2;
+  const size_t scales = pages / (TA_CACHE4_GROUP / 2);
+  if (int st = check_apart({{k_out, out}, {v_out, out}},
+                           {{k_pages, pages},
+                            {v_pages, pages},
+                            {k_scales, scales},
+                            {v_scales, scales},
+                            {table, (size_t)B * max_pages * 4},
+                            {lens, (size_t)B * 4}}))
+    return st;
+  const Cache4ReadArgs a{static_cast<const uint8_t*>(k_pages), static_cast<const uint8_t*>(v_pages),
+                         static_cast<const uint8_t*>(k_scales), static_cast<const uint8_t*>(v_scales), table, lens,
+                         static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), B, Hkv, N, d, max_pages,
+                         n_pages, first};
+  return launched(launch_cache4_read(a, static_cast<hipStream_t>(stream)));
+}
+
+int cache4_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes) {
+  if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  *bytes = plan_cache(B, H, Hkv, N, d, max_pages, kCache4Segment).bytes;
+  clear_error();
+  return TA_OK;
+}
+
+int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const void* k_scales,
+                    const void* v_scales, const int32_t* table, const int32_t* lens, int per_head, void* out,
+                    float* lse, int B, int H, int Hkv, int N, int d, int max_pages, int n_pages, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || !out)
+    return fail(TA_ERR_NULL_PTR, "q, the pages, the scales, table, lens and out must be non-NULL");
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
+  if (!std::isfinite(scale)) return fail(TA_ERR_BAD_SCALE, "scale must be finite");
+  if (int st = check_aligned({q, k_pages, v_pages, k_scales, v_scales, out}, 16,
+                             "q, out, the pages and the scales must be 16-byte aligned"))
+    return st;
+  if (int st = check_aligned({table, lens, lse}, 4, "table, lens and lse must be 4-byte aligned")) return st;
+  const CachePlan p = plan_cache(B, H, Hkv, N, d, max_pages, kCache4Segment);
+  if (int st = check_workspace(workspace, workspace_bytes, p.bytes)) return st;
+  const int64_t rows = (int64_t)B * H * N, entries = per_head ? (int64_t)B * Hkv : B;
+  const size_t qb = bf16s(rows * d), pages = (size_t)n_pages * Hkv * TA_BLOCK * d / 2;
+  const size_t scales = pages / (TA_CACHE4_GROUP / 2);
+  if (int st = check_apart({{out, qb}, {lse, (size_t)rows * 4}, {workspace, p.bytes}},
+                           {{q, qb},
+                            {k_pages, pages},
+                            {v_pages, pages},
+                            {k_scales, scales},
+                            {v_scales, scales},
+                            {table, (size_t)entries * max_pages * 4},
+                            {lens, (size_t)entries * 4}}))
+    return st;
+  Cache4AttnArgs a;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_pages = static_cast<const uint8_t*>(k_pages);
+  a.v_pages = static_cast<const uint8_t*>(v_pages);
+  a.k_scales = a.v_scales = nullptr;
+  a.k_exps = static_cast<const uint8_t*>(k_scales);
+  a.v_exps = static_cast<const uint8_t*>(v_scales);
+  a.table = table;
+  a.lens = lens;
+  a.per_head = per_head != 0;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.B = B;
+  a.H = H;
+  a.Hkv = Hkv;
+  a.G = H / Hkv;
+  a.N = N;
+  a.d = d;
+  a.max_pages = max_pages;
+  a.n_pages = n_pages;
+  a.c = scale * 1.4426950408889634f;
+  a.whole = p.whole;
+  a.workers = p.workers;
+  a.row_blocks = p.passes;
+  a.part = static_cast<float*>(workspace);
+  return launched(launch_cache4_attn(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI host code and the gfx950 kernels of attention over
-// selected blocks and over the 8-bit cache.
+// selected blocks and over the 8-bit and 4-bit caches.
 #pragma once
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
@@ -18,6 +18,7 @@ struct BlockGeo {
 
 constexpr int kLineWorkers = 256;  // workgroups of the gradients' key side at d = 128
 constexpr int kCacheSegment = 3;  // what a (sequence, head) costs cache attention beside its pages
+constexpr int kCache4Segment = 3;  // the same over the 4-bit cache
 
 struct MeansArgs {
   const uint16_t* x;
@@ -116,12 +117,48 @@ struct CacheAttnArgs {
   float* part;       // fp32 [row block][2 * workers][rows][d + 4]: O/l, base-2 lse
 };
 
+struct Cache4WriteArgs {
+  const uint16_t* k;
+  const uint16_t* v;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* n_new;  // or null
+  uint16_t* k_held;      // or null
+  uint16_t* v_held;      // or null
+  int B, Hkv, N, d, max_pages, n_pages;
+};
+
+struct Cache4ReadArgs {
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const uint8_t* k_scales;
+  const uint8_t* v_scales;
+  const int32_t* table;
+  const int32_t* lens;
+  uint16_t* k_out;  // or null
+  uint16_t* v_out;  // or null
+  int B, Hkv, N, d, max_pages, n_pages, first;
+};
+
+// As over the 8-bit cache, with scales of its own (k_scales and v_scales are not looked at).
+struct Cache4AttnArgs : CacheAttnArgs {
+  const uint8_t* k_exps;
+  const uint8_t* v_exps;
+};
+
 hipError_t launch_block_means(const MeansArgs& a, hipStream_t stream);
 hipError_t launch_block_lists(ListsArgs a, hipStream_t stream);
 hipError_t launch_block_fwd(const BlockFwdArgs& a, hipStream_t stream);
 hipError_t launch_block_bwd(const BlockBwdArgs& a, hipStream_t stream);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t stream);
+hipError_t launch_cache4_write(const Cache4WriteArgs& a, hipStream_t stream);
+hipError_t launch_cache4_read(const Cache4ReadArgs& a, hipStream_t stream);
+hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream);
 
 // Rows of a pass of cache attention over a sequence's G * N rows.
 int cache_rows_per_pass(int rows);

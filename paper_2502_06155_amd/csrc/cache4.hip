@@ -1,0 +1,493 @@
+// gfx950 (MI355X, CDNA4) kernels of the 4-bit cache: writing it, reading it back, attention over it.
+//
+// Formats. A page holds 128 tokens of every key head, K and V alike: e2m1 codes [token][d / 2] (two values a byte, the
+// even one low) and for every 32 values of a token the exponent of a power of two, [d / 32][token], biased by 127: the
+// formats that v_cvt_scalef32_pk_bf16_fp4 takes as they lie, a byte shifted to a float's exponent being the scale.
+// Conversions are exact that way (the codes have 2 significant bits), and the other way round to nearest, ties to
+// the even code, 6 for what is larger. A token's scales are its own: writing it touches no other one.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <stdint.h>
+
+#include "block_launch.h"
+#include "cache_line.h"
+#include "tile_common.h"
+
+namespace ta {
+namespace {
+
+constexpr int kGroup = 32;  // values that share a scale: four lanes of 8
+constexpr int kMinExp4 = -100, kMaxExp4 = 125;
+constexpr uint32_t kNanScale = 255;
+
+// ---------------------------------------------------------------------------------------------
+// write and read: a token's row of a head takes d / 8 lanes, 8 values (4 bytes of codes) a lane.
+
+template <int D>
+struct TokenLanes {
+  static constexpr int lanes = D / 8, tokens = 64 / lanes;  // (d = 96: 5 tokens in 60 lanes)
+  static constexpr int per_pass = kThreadsC / 64 * tokens;
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_from(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
+}
+
+// bf16 halves of a word that are infinities or NaN, as a mask of the halves.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+// The biased exponent of a group's scale: the least e in [kMinExp4, kMaxExp4] with the largest magnitude at most
+// 7 * 2^e. `most`: that magnitude's bf16 bits; it is 1.m * 2^x, and 7 = 1.75 * 2^2.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
+  const int x = (int)(most >> 7) - 127;
+  const int e = (most & 0x7fu) <= 0x60u ? x - 2 : x - 1;
+  return (uint32_t)(min(max(most == 0 ? kMinExp4 : e, kMinExp4), kMaxExp4) + 127);
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// (A bit cast of a vector's element takes the first one: elements go through a copy.)
+__device__ __forceinline__ bf16x2 as_bf16x2(uint32_t w) { return __builtin_bit_cast(bf16x2, w); }
+__device__ __forceinline__ uint32_t encode8(u32x4 w, float scale) {
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, as_bf16x2(w[0]), scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, as_bf16x2(w[1]), scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, as_bf16x2(w[2]), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, as_bf16x2(w[3]), scale, 3);
+}
+__device__ __forceinline__ u32x4 decode8(uint32_t c, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3))};
+}
+
+// The page of a position, -1 if it is none.
+__device__ __forceinline__ int page_at(const int32_t* table, int max_pages, int n_pages, int64_t pos) {
+  const int64_t slot = pos / kBlock;
+  if (slot >= max_pages) return -1;
+  const int page = table[slot];
+  return page < n_pages ? page : -1;
+}
+
+constexpr int kTokensAhead = 4;  // tokens of a lane that are read together
+
+// Bound by the bytes. K and V of a token in the same lanes: a token that holds anything but finite numbers is
+// marked in K.
+template <int D>
+__global__ __launch_bounds__(kThreadsC) void cache4_write_kernel(const Cache4WriteArgs a) {
+  using Lanes = TokenLanes<D>;
+  const int b = blockIdx.y / a.Hkv, h = blockIdx.y - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int sub = lane / Lanes::lanes, l = lane - sub * Lanes::lanes;
+  if (sub >= Lanes::tokens) return;
+  const int64_t len = max(a.lens[b], 0);
+  const int n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
+  const int32_t* table = a.table + (size_t)b * a.max_pages;
+  const int t0 = (int)blockIdx.x * kTokensAhead * Lanes::per_pass + wave * Lanes::tokens + sub;
+  const size_t row0 = ((size_t)b * a.Hkv + h) * a.N;
+
+  u32x4 k[kTokensAhead], v[kTokensAhead];
+  int page[kTokensAhead];
+#pragma unroll
+  for (int i = 0; i < kTokensAhead; ++i) {
+    const int t = t0 + i * Lanes::per_pass;
+    k[i] = v[i] = u32x4{0u, 0u, 0u, 0u};
+    page[i] = -1;
+    if (t < n) {
+      k[i] = load16(a.k + (row0 + t) * D + 8 * l);
+      v[i] = load16(a.v + (row0 + t) * D + 8 * l);
+      page[i] = page_at(table, a.max_pages, a.n_pages, len + t);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTokensAhead; ++i) {
+    const int t = t0 + i * Lanes::per_pass;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= not_finite(k[i][e]) | not_finite(v[i][e]);
+    bool marked = false;
+    if (const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0)) {
+      marked = (any >> (sub * Lanes::lanes) & ((1ull << Lanes::lanes) - 1)) != 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[i][e] &= ~not_finite(k[i][e]);
+        v[i][e] &= ~not_finite(v[i][e]);
+      }
+    }
+    uint32_t most_k = 0, most_v = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      most_k = max(most_k, max(k[i][e] & 0x7fffu, k[i][e] >> 16 & 0x7fffu));
+      most_v = max(most_v, max(v[i][e] & 0x7fffu, v[i][e] >> 16 & 0x7fffu));
+    }
+    most_k = max_from<0x4e>(max_from<0xb1>(most_k));  // of four lanes
+    most_v = max_from<0x4e>(max_from<0xb1>(most_v));
+    uint32_t scale_k = scale_byte(most_k), scale_v = scale_byte(most_v);
+    const uint32_t code_k = encode8(k[i], scale_of(scale_k)), code_v = encode8(v[i], scale_of(scale_v));
+    if (marked) scale_k = kNanScale;
+    if (page[i] >= 0) {
+      const int at = (int)((len + t) % kBlock);
+      const size_t ph = (size_t)page[i] * a.Hkv + h;
+      const size_t code = (ph * kBlock + at) * (D / 2) + 4 * l, scale = (ph * (D / kGroup) + l / 4) * kBlock + at;
+      *reinterpret_cast<uint32_t*>(a.k_pages + code) = code_k;
+      *reinterpret_cast<uint32_t*>(a.v_pages + code) = code_v;
+      if (l % 4 == 0) {
+        a.k_scales[scale] = (uint8_t)scale_k;
+        a.v_scales[scale] = (uint8_t)scale_v;
+      }
+    }
+    if (t < a.N) {
+      const size_t to = (row0 + t) * D + 8 * l;
+      const u32x4 none = {0u, 0u, 0u, 0u};
+      if (a.k_held) *reinterpret_cast<u32x4*>(a.k_held + to) = page[i] < 0 ? none : decode8(code_k, scale_of(scale_k));
+      if (a.v_held) *reinterpret_cast<u32x4*>(a.v_held + to) = page[i] < 0 ? none : decode8(code_v, scale_of(scale_v));
+    }
+  }
+}
+
+// Bound by the bytes that it writes.
+template <int D>
+__global__ __launch_bounds__(kThreadsC) void cache4_read_kernel(const Cache4ReadArgs a) {
+  using Lanes = TokenLanes<D>;
+  const int b = blockIdx.y / a.Hkv, h = blockIdx.y - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int sub = lane / Lanes::lanes, l = lane - sub * Lanes::lanes;
+  if (sub >= Lanes::tokens) return;
+  const int len = a.lens[b];
+  const int32_t* table = a.table + (size_t)b * a.max_pages;
+  const int t0 = (int)blockIdx.x * kTokensAhead * Lanes::per_pass + wave * Lanes::tokens + sub;
+  const size_t row0 = ((size_t)b * a.Hkv + h) * a.N;
+
+  uint32_t k[kTokensAhead], v[kTokensAhead];
+  float ks[kTokensAhead], vs[kTokensAhead];
+#pragma unroll
+  for (int i = 0; i < kTokensAhead; ++i) {
+    const int t = t0 + i * Lanes::per_pass;
+    k[i] = v[i] = 0;
+    ks[i] = vs[i] = 1.f;
+    if (t >= a.N || a.first + t >= len) continue;
+    const int page = page_at(table, a.max_pages, a.n_pages, a.first + t);
+    if (page < 0) continue;
+    const int at = (a.first + t) % kBlock;
+    const size_t ph = (size_t)page * a.Hkv + h;
+    const size_t code = (ph * kBlock + at) * (D / 2) + 4 * l, scale = (ph * (D / kGroup) + l / 4) * kBlock + at;
+    k[i] = *reinterpret_cast<const uint32_t*>(a.k_pages + code);
+    v[i] = *reinterpret_cast<const uint32_t*>(a.v_pages + code);
+    ks[i] = scale_of(a.k_scales[scale]);
+    vs[i] = scale_of(a.v_scales[scale]);
+  }
+#pragma unroll
+  for (int i = 0; i < kTokensAhead; ++i) {
+    const int t = t0 + i * Lanes::per_pass;
+    if (t >= a.N) break;
+    const size_t to = (row0 + t) * D + 8 * l;
+    if (a.k_out) *reinterpret_cast<u32x4*>(a.k_out + to) = decode8(k[i], ks[i]);
+    if (a.v_out) *reinterpret_cast<u32x4*>(a.v_out + to) = decode8(v[i], vs[i]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention
+//
+// A wave takes a page at a time, its codes from memory straight into registers, one page ahead, as operands of
+// v_mfma_f32_16x16x32_bf16 (A: lane l holds row l % 16 and the k indices 8 (l / 16) .. + 7; B the same with
+// columns; C: column l % 16, rows 4 (l / 16) + j). With n = l % 16 and g = l / 16:
+//   S^T = K Q^T. Row n of instruction group i (of 8) is token 8 n + i. The matrix instruction adds over k in any
+//   order, so lane group g holds the d / 4 values from g d / 4 on of its token, one load, and q is laid out alike. The
+//   scores come out as: lane group g holds tokens 32 g .. 32 g + 31, s[i][j] being token 32 g + 8 j + i,
+//   which is the P^T operand of
+//   O^T += V^T P^T, step j: its V operand are, of tokens 32 g + 8 j .. + 7, the values of one channel. A lane reads of
+//   each of those tokens 4 bytes (2 at d = 64), 8 channels beside each other (4), widens them with the token's scale and
+//   swaps halves of words so that words hold two tokens of one channel: the operands of 8 (4) instructions, row n
+//   of instruction t being channel 8 n + t (4 n + t).
+// So neither K nor V is kept transposed, no scale leaves its token, and nothing goes through LDS. K codes become bf16 exactly,
+// scales among it, and so do V's.
+
+// Words of K codes a lane holds of a token, and 8-value slices of them.
+template <int D>
+struct Key4 {
+  static constexpr int kW = D / 32;
+  uint32_t k[8][kW];
+  u32x2 lo, hi;  // scales of the 8 tokens: of the lane's first group of 32 values, and of its last (d = 96)
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int lane) {
+    const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint8_t* p = codes + (uint32_t)((8 * n + i) * (D / 2) + g * (D / 8));
+      if constexpr (D == 128) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k[i][e] = w[e];
+      } else if constexpr (D == 64) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+        k[i][0] = w[0];
+        k[i][1] = w[1];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) k[i][e] = reinterpret_cast<const uint32_t*>(p)[e];
+      }
+    }
+    lo = *reinterpret_cast<const u32x2*>(scales + (uint32_t)(g * kW / 4 * kBlock + 8 * n));
+    if constexpr (D == 96) hi = *reinterpret_cast<const u32x2*>(scales + (uint32_t)((g * kW + kW - 1) / 4 * kBlock + 8 * n));
+  }
+  // Scales of slice m (of kW).
+  __device__ __forceinline__ u32x2 scales_of(int m, int g) const {
+    if constexpr (D != 96) return lo;
+    const bool last = (g * kW + m) / 4 != g * kW / 4;
+    return last ? hi : lo;
+  }
+};
+template <int D>
+struct Value4 {
+  uint32_t v[4][8];  // token 32 g + 8 c + i
+  u32x4 scales[2];   // of tokens 32 g .. + 31
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* group_scales, int lane) {
+    const int n = lane & 15, g = lane >> 4;
+    // d = 96: lanes 12 to 15 of a group have no channels and read those of lane 11.
+    const int word = D == 128 ? n : D == 96 ? min(n, 11) : n / 2, group = D == 64 ? n / 8 : word / 4;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        v[c][i] = *reinterpret_cast<const uint32_t*>(codes + (uint32_t)((32 * g + 8 * c + i) * (D / 2) + 4 * word));
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      scales[x] = *reinterpret_cast<const u32x4*>(group_scales + (uint32_t)(group * kBlock + 32 * g + 16 * x));
+  }
+};
+
+// Byte i of two words as a scale.
+__device__ __forceinline__ float scale_at(u32x2 w, int i) { return scale_of(w[i / 4] >> (8 * (i % 4)) & 0xffu); }
+
+template <int RB>
+constexpr int cache4_wgs() { return RB == 1 ? 2 : 1; }
+
+template <int D, int RB>
+__global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kernel(const Cache4AttnArgs a) {
+  constexpr int kRows = 16 * RB, kWaves = kThreadsC / 64, kSl = D / 32;
+  constexpr int kCh = D == 64 ? 4 : 8;  // channels of a lane, and O^T instructions of a step
+  __shared__ float s_o[kWaves][kRows][D + 4];
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int n = lane & 15, g = lane >> 4;
+  const int row0 = blockIdx.y * kRows, rows = a.G * a.N;
+
+  CacheWalk<kCache4Segment> walk(a, blockIdx.x);
+  if (walk.none()) return;
+  do {
+    const int len = walk.len;
+    const CacheSegment seg = walk.segment(a);
+    const int p0 = seg.p0, p1 = seg.p1;
+    if (p1 <= p0 && !a.whole) continue;  // (alone, a segment without tokens gets its zeros)
+    const ScalarInts table = (ScalarInts)(a.table + (size_t)seg.entry * a.max_pages);
+    // Pages p0 + wave, + 4, ... up to p1. A page that is none is passed over: its tokens are not read.
+    auto page_of = [&](int p) {
+      if (p >= p1) return -1;
+      const int x = table[p];
+      return x < a.n_pages ? x : -1;
+    };
+    auto load_k = [&](Key4<D>& t, int page) {
+      const size_t ph = (size_t)page * a.Hkv + seg.h;
+      t.load(a.k_pages + ph * kBlock * (D / 2), a.k_exps + ph * kBlock * (D / kGroup), lane);
+    };
+    auto load_v = [&](Value4<D>& t, int page) {
+      const size_t ph = (size_t)page * a.Hkv + seg.h;
+      t.load(a.v_pages + ph * kBlock * (D / 2), a.v_exps + ph * kBlock * (D / kGroup), lane);
+    };
+    int p = p0 + wave;
+    int page = page_of(p);
+    Key4<D> kt;
+    Value4<D> vt;
+    if (page >= 0) {
+      load_k(kt, page);
+      load_v(vt, page);
+    }
+
+    int end[RB];  // tokens this lane's row attends to
+    bf16x8 qf[RB][kSl];
+    f32x4 o[RB][kCh];
+    float m_ref[RB], l_run[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = row0 + 16 * rb + n;
+      end[rb] = r < rows ? len - (a.N - 1) + r % a.N : 0;
+#pragma unroll
+      for (int m = 0; m < kSl; ++m) {
+        u32x4 x = {0u, 0u, 0u, 0u};
+        if (r < rows) x = load16(a.q + (seg.q_row + r) * D + 8 * (g * kSl + m));
+        qf[rb][m] = as_bf16x8(x);
+      }
+      m_ref[rb] = kNoRef;
+      l_run[rb] = 0.f;
+#pragma unroll
+      for (int t = 0; t < kCh; ++t) o[rb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // The next page's K loads go out as soon as this one's K is used, its V loads when V is.
+    for (; p < p1; p += kWaves) {
+      const int next = page_of(p + kWaves);
+      const int tok0 = p * kBlock;
+      f32x4 s[RB][8];
+      if (page >= 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+          for (int m = 0; m < kSl; ++m) {
+            const bf16x8 kf = as_bf16x8(decode8(kt.k[i][m], scale_at(kt.scales_of(m, g), i)));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              s[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i], 0, 0, 0);
+          }
+          if (i % 2) __builtin_amdgcn_sched_barrier(0);  // keeps later tokens' codes from being widened early
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next >= 0) load_k(kt, next);
+      __builtin_amdgcn_sched_barrier(0);
+      if (page >= 0) {
+        bf16x8 pf[RB][4];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[rb][i] *= a.c;
+          if (tok0 + kBlock > len - (a.N - 1)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (tok0 + 32 * g + 8 * j + i >= end[rb]) s[rb][i][j] = -INFINITY;
+          }
+          float mx = s[rb][0][0];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
+          const float m_new = fmaxf(m_ref[rb], group_max(mx));
+          if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
+            const float alpha = fast_exp2(m_ref[rb] - m_new);
+            l_run[rb] *= alpha;
+#pragma unroll
+            for (int t = 0; t < kCh; ++t) o[rb][t] *= alpha;
+            m_ref[rb] = m_new;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+              sum += x;
+              pf[rb][j][i] = (__bf16)x;
+            }
+          l_run[rb] += sum;
+        }
+        if (tok0 + kBlock > len) {  // scales behind the last token may be anything: those of V become 2^-127
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vt.scales[x][e] &= bytes_before(len - (tok0 + 32 * g + 16 * x + 4 * e));
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          // vf[t]: of channel t of the lane, the step's 8 tokens.
+          u32x4 vf[kCh];
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const u32x2 sc = {vt.scales[c / 2][2 * (c % 2)], vt.scales[c / 2][2 * (c % 2) + 1]};
+            const float s0 = scale_at(sc, i), s1 = scale_at(sc, i + 1);
+            uint32_t w0 = vt.v[c][i], w1 = vt.v[c][i + 1];
+            if constexpr (D == 64) {
+              w0 >>= 16 * (n & 1);
+              w1 >>= 16 * (n & 1);
+            }
+            const u32x4 x0 = decode8(w0, s0), x1 = decode8(w1, s1);
+#pragma unroll
+            for (int y = 0; y < kCh / 2; ++y) {
+              vf[2 * y][i / 2] = __builtin_amdgcn_perm(x1[y], x0[y], 0x05040100u);
+              vf[2 * y + 1][i / 2] = __builtin_amdgcn_perm(x1[y], x0[y], 0x07060302u);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < kCh; ++t)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o[rb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[t]), pf[rb][c], o[rb][t], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next >= 0) load_v(vt, next);
+      page = next;
+    }
+
+    // The waves' states join in LDS.
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float l = group_sum(l_run[rb]);
+      if (g == 0) {
+        s_m[wave][16 * rb + n] = m_ref[rb];
+        s_l[wave][16 * rb + n] = l;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int ch = kCh * (4 * g + j);
+        if (ch >= D) continue;
+#pragma unroll
+        for (int t = 0; t < kCh; t += 4)
+          *reinterpret_cast<f32x4*>(&s_o[wave][16 * rb + n][ch + t]) =
+              f32x4{o[rb][t][j], o[rb][t + 1][j], o[rb][t + 2][j], o[rb][t + 3][j]};
+      }
+    }
+    __syncthreads();
+    join_waves<D, kRows>(a, s_o, s_m, s_l, seg.q_row, row0, rows, seg.alone, seg.slot);
+    __syncthreads();
+  } while (walk.advance(a));
+}
+
+template <int D, int RB>
+hipError_t cache4_attn_rows(const Cache4AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
+  const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
+  cache4_attn_kernel<D, RB><<<grid, kThreadsC, 0, s>>>(a);
+  if (!a.whole) cache_merge_kernel<D, RB, kCache4Segment><<<segs, kThreadsC, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t cache4_attn_for(const Cache4AttnArgs& a, hipStream_t s) {
+  return cache_rows_per_pass(a.G * a.N) == 16 ? cache4_attn_rows<D, 1>(a, s) : cache4_attn_rows<D, 2>(a, s);
+}
+
+template <int D>
+dim3 token_grid(int N, int heads) {
+  constexpr int per = kTokensAhead * TokenLanes<D>::per_pass;
+  return dim3((unsigned)((N + per - 1) / per), (unsigned)heads);
+}
+
+}  // namespace
+
+hipError_t launch_cache4_write(const Cache4WriteArgs& a, hipStream_t s) {
+  if (a.d == 64) cache4_write_kernel<64><<<token_grid<64>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  else if (a.d == 96) cache4_write_kernel<96><<<token_grid<96>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  else cache4_write_kernel<128><<<token_grid<128>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache4_read(const Cache4ReadArgs& a, hipStream_t s) {
+  if (a.d == 64) cache4_read_kernel<64><<<token_grid<64>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  else if (a.d == 96) cache4_read_kernel<96><<<token_grid<96>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  else cache4_read_kernel<128><<<token_grid<128>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream) {
+  if (a.d == 64) return cache4_attn_for<64>(a, stream);
+  if (a.d == 96) return cache4_attn_for<96>(a, stream);
+  return cache4_attn_for<128>(a, stream);
+}
+
+}  // namespace ta

@@ -15,12 +15,14 @@
 #include <type_traits>
 
 #include "block_launch.h"
+#include "cache_line.h"
 #include "tile_common.h"
 
 namespace ta {
 namespace {
 
-constexpr int kThreadsC = 256;
+constexpr int kSegment = kCacheSegment;
+using ScalarFloats = const __attribute__((address_space(4))) float*;
 constexpr float kMaxCode = 448.f;  // the largest e4m3 magnitude
 constexpr int kMinExp = -100, kMaxExp = 120;
 
@@ -206,85 +208,6 @@ __global__ __launch_bounds__(kThreadsC) void cache_write_kernel(const CacheWrite
 // kernel joins them in the order of the pages.
 
 
-// A quotient of numbers that are the same in every lane, in a scalar register (the division itself runs
-// on the vector ALU; left there, it would make every address and branch behind it a lane's own).
-__device__ __forceinline__ int scalar_div(int x, int y) {
-  return __builtin_amdgcn_readfirstlane((int)((uint32_t)x / (uint32_t)y));
-}
-
-// The line of all segments, each kSegment + its pages long (below 2^31, checked by the host): what a
-// segment's start and end cost a workgroup is about kSegment pages' time (32 sequences of 4 to 512
-// pages: 208 us with 0, 188 with 3). Segment order: entry i of lens, then (where all heads share an
-// entry) the key heads. Worker w takes line / workers, the first line % workers ones one more. Every
-// wave finds its place by itself, 64 entries at a time.
-constexpr int kSegment = kCacheSegment;
-using ScalarInts = const __attribute__((address_space(4))) int32_t*;    // read with scalar loads
-using ScalarFloats = const __attribute__((address_space(4))) float*;
-
-__device__ __forceinline__ int cache_len(const CacheAttnArgs& a, int i) {
-  return (int)min((int64_t)max(a.lens[i], 0), (int64_t)a.max_pages * kBlock);
-}
-__device__ __forceinline__ int pages_of(int len) { return (int)(((uint32_t)len + kBlock - 1) / kBlock); }
-// A segment's length on the line; one without pages has none.
-__device__ __forceinline__ int extent_of(int pages) { return pages > 0 ? kSegment + pages : 0; }
-
-struct Line {
-  int entries, per;  // entries of lens, segments of an entry
-  int total;         // its length
-  int each, more;    // every worker's part, workers with one more
-  __device__ __forceinline__ Line(const CacheAttnArgs& a, bool measure = true) {
-    entries = a.per_head ? a.B * a.Hkv : a.B;
-    per = a.per_head ? 1 : a.Hkv;
-    total = each = more = 0;
-    if (!measure) return;
-    int n = 0;
-    for (int i = threadIdx.x & 63; i < entries; i += 64) n += extent_of(pages_of(cache_len(a, i)));
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) n += __shfl_xor(n, s);
-    total = __builtin_amdgcn_readfirstlane(n) * per;
-    each = scalar_div(total, a.workers);
-    more = total - each * a.workers;
-  }
-  __device__ __forceinline__ int start(int w) const { return w * each + min(w, more); }
-  // The worker that takes place x of the line, x < total.
-  __device__ __forceinline__ int worker(int x) const {
-    const int y = x - more * (each + 1);
-    return y < 0 ? scalar_div(x, each + 1) : more + scalar_div(y, each);
-  }
-  // The entry that holds place `at` (at < total), and where it starts.
-  __device__ __forceinline__ int entry_of(const CacheAttnArgs& a, int at, int& before) const {
-    const int lane = threadIdx.x & 63;
-    before = 0;
-    for (int i0 = 0; i0 < entries; i0 += 64) {
-      const int own = i0 + lane < entries ? extent_of(pages_of(cache_len(a, i0 + lane))) * per : 0;
-      int upto = own;
-#pragma unroll
-      for (int s = 1; s < 64; s <<= 1) {
-        const int y = __shfl_up(upto, s);
-        if (lane >= s) upto += y;
-      }
-      const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
-      if (past) {
-        const int src = __ffsll((unsigned long long)past) - 1;
-        before = __builtin_amdgcn_readfirstlane(before + __shfl(upto - own, src));
-        return __builtin_amdgcn_readfirstlane(i0 + src);
-      }
-      before = __builtin_amdgcn_readfirstlane(before + __shfl(upto, 63));
-    }
-    return entries;
-  }
-};
-
-// max and sum over the four lane groups that hold one query row's tokens.
-__device__ __forceinline__ float group_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float group_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
 // Eight e4m3 codes as bf16, exactly.
 __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
@@ -295,15 +218,6 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
 }
 // A one in the lowest bit of every byte that is a NaN code (0x7f, 0xff).
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u; }
-// The bytes of a word that come before byte `left`.
-__device__ __forceinline__ uint32_t bytes_before(int left) {
-  return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-}
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-constexpr float kNoRef = -1e30f;  // a running maximum before the first token (base-2 logits)
 
 // A page's codes in a lane's registers, by halves of 64 tokens. Base addresses are the same in every
 // lane (scalar registers), lanes add a 32-bit offset that no page changes. Both halves of a V row (a
@@ -366,47 +280,15 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
   const int n = lane & 15, g = lane >> 4;
   const int w = blockIdx.x, row0 = blockIdx.y * kRows, rows = a.G * a.N;
 
-  // Short tables: a workgroup per segment, and nothing to join (a.whole).
-  const Line line(a, !a.whole);
-  int lo = 0, hi = INT32_MAX, seg0 = 0, entry, head, len, pages;  // seg0: the line's place where the segment starts
-  if (a.whole) {
-    entry = scalar_div(w, line.per);
-    head = w - entry * line.per;
-    len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
-    pages = pages_of(len);
-  } else {
-    lo = line.start(w);
-    hi = line.start(w + 1);
-    if (lo >= hi) return;
-    entry = line.entry_of(a, lo, seg0);
-    len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
-    pages = pages_of(len);
-    head = scalar_div(lo - seg0, extent_of(pages));
-    seg0 += head * extent_of(pages);
-  }
-
-  int at = lo;
-  auto advance = [&]() {  // to the next segment with pages; false past the worker's part
-    if (a.whole) return false;
-    at = seg0 + kSegment + pages;
-    if (at >= hi) return false;
-    seg0 = at;
-    if (++head == line.per) {
-      head = 0;
-      pages = 0;
-      while (pages == 0 && ++entry < line.entries) {
-        len = __builtin_amdgcn_readfirstlane(cache_len(a, entry));
-        pages = pages_of(len);
-      }
-    }
-    return true;
-  };
+  CacheWalk<kSegment> walk(a, w);
+  if (walk.none()) return;
   do {
-    const int b = a.per_head ? scalar_div(entry, a.Hkv) : entry, h = a.per_head ? entry - b * a.Hkv : head;
-    const int p0 = max(0, at - seg0 - kSegment), p1 = min(pages, hi - seg0 - kSegment);
-    const ScalarInts table = (ScalarInts)(a.table + (size_t)entry * a.max_pages);
+    const int len = walk.len;
+    const CacheSegment seg = walk.segment(a);
+    const int p0 = seg.p0, p1 = seg.p1, h = seg.h;
+    const ScalarInts table = (ScalarInts)(a.table + (size_t)seg.entry * a.max_pages);
     const ScalarFloats k_scales = (ScalarFloats)a.k_scales, v_scales = (ScalarFloats)a.v_scales;
-    const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N;  // rows of the group lie together
+    const size_t q_row = seg.q_row;
 
     if (p1 <= p0 && !a.whole) continue;  // (alone, a segment without tokens gets its zeros)
     // Pages p0 + wave, + 4, ... up to p1. A page that is none is passed over: its tokens are not read.
@@ -600,89 +482,9 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
       for (int mb = 0; mb < kMb; ++mb) *reinterpret_cast<f32x4*>(&s_o[wave][16 * rb + n][16 * mb + 4 * g]) = o[rb][mb];
     }
     __syncthreads();
-    const bool alone = p0 == 0 && p1 == pages;
-    const int slot = 2 * w + (at == lo ? 0 : 1);
-    float* part = a.part + ((size_t)blockIdx.y * 2 * a.workers + slot) * kRows * (D + 4);
-    for (int i = tid; i < kRows * (D / 4); i += kThreadsC) {
-      const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
-      if (row0 + r >= rows) continue;
-      float m = s_m[0][r];
-#pragma unroll
-      for (int x = 1; x < kWaves; ++x) m = fmaxf(m, s_m[x][r]);
-      float l = 0.f;
-      f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < kWaves; ++x) {
-        const float f = fast_exp2(s_m[x][r] - m);
-        l += f * s_l[x][r];
-        y += f * *reinterpret_cast<const f32x4*>(&s_o[x][r][d0]);
-      }
-      y *= l > 0.f ? 1.f / l : 0.f;
-      const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // NaN for a row of NaN
-      if (alone) {
-        *reinterpret_cast<u32x2*>(a.out + (q_row + row0 + r) * D + d0) =
-            __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
-        if (a.lse && d0 == 0) a.lse[q_row + row0 + r] = lse2 * 0.69314718055994531f;
-      } else {
-        float* pr = part + (size_t)r * (D + 4);
-        *reinterpret_cast<f32x4*>(pr + d0) = y;
-        if (d0 == 0) pr[D] = lse2;
-      }
-    }
+    join_waves<D, kRows>(a, s_o, s_m, s_l, q_row, row0, rows, seg.alone, seg.slot);
     __syncthreads();
-  } while (advance());
-}
-
-// Joins the partial results of a segment that several workers share, in the order of its pages;
-// a segment without tokens gets its zeros here. A workgroup per segment and 8 rows.
-constexpr int kMergeRows = 8;
-template <int D, int RB>
-__global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnArgs a) {
-  constexpr int kRows = 16 * RB;
-  const int b = blockIdx.x / a.Hkv, h = blockIdx.x - b * a.Hkv;
-  const int entry = a.per_head ? (int)blockIdx.x : b;
-  const int first = blockIdx.y * kMergeRows, rows = min(kMergeRows, a.G * a.N - first);
-  const int lane = threadIdx.x & 63;
-  const int pages = pages_of(__builtin_amdgcn_readfirstlane(cache_len(a, entry)));
-  const Line line(a);
-  int before = 0;
-  for (int i = lane; i < entry; i += 64) before += extent_of(pages_of(cache_len(a, i)));
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) before += __shfl_xor(before, s);
-  const int s0 = __builtin_amdgcn_readfirstlane(before) * line.per + (a.per_head ? 0 : h * extent_of(pages));
-  int w0 = 0, w1 = -1;
-  if (pages > 0) {
-    w0 = line.worker(s0 + kSegment);
-    w1 = line.worker(s0 + kSegment + pages - 1);
-    if (w0 == w1) return;  // that worker wrote the rows
-  }
-  const size_t q_row = ((size_t)b * a.H + (size_t)h * a.G) * a.N + first;
-  // Worker w's part of the segment: its first one (slot 2 w), or w0's second where that began before.
-  const int early = w1 >= w0 && line.start(w0) < s0 ? 1 : 0;
-  const float* parts = a.part + (size_t)(first / kRows) * 2 * a.workers * kRows * (D + 4) + (size_t)(first % kRows) * (D + 4);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsC) {
-    const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
-    const float* pr = parts + (size_t)r * (D + 4);
-    const size_t step = (size_t)2 * kRows * (D + 4);
-    float m = -INFINITY, l = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const float* pw = pr + w * step + (w == w0 ? early * (step / 2) : 0);
-      const f32x4 u = *reinterpret_cast<const f32x4*>(pw + d0);
-      const float part = pw[D], m_new = fmaxf(m, part);
-      const float f = part == -INFINITY ? 0.f : fast_exp2(part - m_new);  // a NaN stays one
-      const float keep = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
-      l = l * keep + f;
-      y = y * keep + f * u;
-      m = m_new;
-    }
-    if (l > 0.f) y *= 1.f / l;
-    *reinterpret_cast<u32x2*>(a.out + (q_row + r) * D + d0) =
-        __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
-    if (a.lse && d0 == 0)
-      a.lse[q_row + r] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-  }
+  } while (walk.advance(a));
 }
 
 template <int D, int RB>
@@ -690,7 +492,7 @@ hipError_t cache_attn_rows(const CacheAttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
   const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
   cache_attn_kernel<D, RB><<<grid, kThreadsC, 0, s>>>(a);
-  if (!a.whole) cache_merge_kernel<D, RB><<<segs, kThreadsC, 0, s>>>(a);
+  if (!a.whole) cache_merge_kernel<D, RB, kSegment><<<segs, kThreadsC, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int D>
