@@ -246,28 +246,43 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
   if (token0 >= (int64_t)a.B * a.S) return;
   const Token tok(a, token0 + lane / L);
   const bool reads = tok.valid && in_row, writes = tok.have && in_row;
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * 64 : 0);
+
+  // Heads of q, k and v in a line; this wave's are first .. last - 1. A step takes up to kAhead heads of one kind,
+  // and the next step's rows are on their way meanwhile (the first one's while the angles are formed).
+  const int k0 = a.heads[0], v0 = k0 + a.heads[1], all = v0 + a.heads[2];
+  const int first = blockIdx.y * a.heads_per, last = min(first + a.heads_per, all);
+  auto kind_of = [&](int f) { return f < k0 ? 0 : f < v0 ? 1 : 2; };
+  auto start_of = [&](int kind) { return kind == 0 ? 0 : kind == 1 ? k0 : v0; };
+  auto stop = [&](int f) { return min(min(f + kAhead, last), f < k0 ? k0 : f < v0 ? v0 : all); };
+  auto load = [&](int f, u32x4 (&in)[kAhead]) {
+    const int kind = kind_of(f), h = f - start_of(kind), n = stop(f) - f;
+    const Rows& x = a.x[kind];
+    const uint16_t* x0 = x.p + tok.b * x.batch + tok.t * x.token + 8 * l;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      in[u] = u32x4{0u, 0u, 0u, 0u};
+      if (u < n && reads) in[u] = load16(x0 + (h + u) * x.head);
+    }
+  };
+  u32x4 in[kAhead], next[kAhead];
+  load(first, in);
 
   Turns<D, ROT> turns;
   turns.place(a, l);
   Floats8 c, s;
   turns.at(a, tok.b, tok.t, c, s);
-  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * 64 : 0);
-
-  int first = blockIdx.y * a.heads_per, last = first + a.heads_per;  // of q's, k's and v's heads in a line
-#pragma unroll
-  for (int kind = 0; kind < 3; ++kind) {
-    const int h0 = max(first, 0), h1 = min(last, a.heads[kind]);
-    first -= a.heads[kind];
-    last -= a.heads[kind];
-    if (h0 >= h1) continue;
-    const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
-    uint16_t* y0 = a.y[kind] + ((int64_t)tok.b * a.heads[kind] * a.S + tok.t) * D + 8 * l;
-    const int64_t plane = (int64_t)a.S * D;
-    // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean
-    Floats8 A, Bp, C;
-    if (kind < 2) {
-      const float* weight = NORM == kNone ? nullptr : a.weight[kind % 2];
-      const float* bias = NORM == kLayer ? a.bias[kind % 2] : nullptr;
+  // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean
+  Floats8 A, Bp, C;
+  int ready = -1;  // the kind whose factors these are
+  const int64_t plane = (int64_t)a.S * D;
+  for (int f = first; f < last;) {
+    const int f1 = stop(f), kind = kind_of(f);
+    if (f1 < last) load(f1, next);
+    if (kind < 2 && kind != ready) {
+      ready = kind;
+      const float* weight = NORM == kNone ? nullptr : a.weight[kind];
+      const float* bias = NORM == kLayer ? a.bias[kind] : nullptr;
       Floats8 w, wp, bs, bp;
       load8<D>(weight, l, 1.f, w);
       load_partners<D, ROT>(weight, l, 1.f, turns, wp);
@@ -280,172 +295,169 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
         C[e] = NORM == kLayer ? fmaf(bs[e], c[e], bp[e] * s[e]) : 0.f;
       }
     }
-    for (int h = h0; h < h1; h += kAhead) {
-      u32x4 in[kAhead];
+    uint16_t* y0 = a.y[kind] + (((int64_t)tok.b * a.heads[kind] + (f - start_of(kind))) * a.S + tok.t) * D + 8 * l;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        in[u] = u32x4{0u, 0u, 0u, 0u};
-        if (h + u < h1 && reads) in[u] = load16(x0 + (h + u) * a.x[kind].head);
-      }
+    for (int u = 0; u < kAhead; ++u) {
+      if (f + u >= f1) break;
+      u32x4 out = in[u];
+      if (kind < 2 && (NORM != kNone || ROT != kStill)) {
+        Floats8 x, xp, y;
+        widen(in[u], x);
+        turns.partners(in[u], x, rows + (ROT >= kWhole ? 64 * u : 0), lane, xp);
+        float mean;
+        const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (h + u >= h1) break;
-        u32x4 out = in[u];
-        if (kind < 2 && (NORM != kNone || ROT != kStill)) {
-          Floats8 x, xp, y;
-          widen(in[u], x);
-          turns.partners(in[u], x, rows + (ROT >= kWhole ? 64 * u : 0), lane, xp);
-          float mean;
-          const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z = ROT == kStill ? x[e] * A[e] : fmaf(x[e], A[e], (NORM == kLayer ? xp[e] - mean : xp[e]) * Bp[e]);
-            y[e] = NORM == kNone ? z : NORM == kRms ? r * z : fmaf(r, z, C[e]);
-          }
-          out = narrow(y);
-          if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
+        for (int e = 0; e < 8; ++e) {
+          const float z = ROT == kStill ? x[e] * A[e] : fmaf(x[e], A[e], (NORM == kLayer ? xp[e] - mean : xp[e]) * Bp[e]);
+          y[e] = NORM == kNone ? z : NORM == kRms ? r * z : fmaf(r, z, C[e]);
         }
-        if (writes) *reinterpret_cast<u32x4*>(y0 + (h + u) * plane) = out;
+        out = narrow(y);
+        if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
       }
-      if constexpr (ROT >= kWhole) {  // the rows in LDS are read before the next ones replace them
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-      }
+      if (writes) *reinterpret_cast<u32x4*>(y0 + u * plane) = out;
     }
+    if constexpr (ROT >= kWhole) {  // the rows in LDS are read before the next ones replace them
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) in[u] = next[u];
+    f = f1;
   }
 }
 
 // Gradients. With g the gradient of a row turned back, xhat the normed row before weights:
 //   db = sum g,  dw = sum g xhat,  u = g w,  dx = r (u - [mean u] - xhat mean(u xhat)).
-// A fixed number of workgroups deals out (tokens, heads) items among its waves, so that the sums of
-// weights and biases, kept in a lane's registers, leave few rows of partial sums; they are added in an order
-// that the sizes set.
-constexpr int kAheadGrad = 2;
-
+// Workgroups first[kind] .. first[kind + 1] - 1 have the rows of q, k or v and deal out (tokens, heads) items among
+// their waves, so that the sums of weights and biases, kept in a lane's registers, leave few rows of partial
+// sums; they are added in an order that the sizes set.
 template <int D, int NORM, int ROT>
 __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const RopeArgs a) {
   constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
-  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAheadGrad * 64 : 1];
+  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * 64 : 1];
   __shared__ float s_sum[kRopeWaves][2][D];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l = lane % L;
   const bool in_row = 8 * l < D;
+  const int kind = (int)blockIdx.x < a.first[1] ? 0 : (int)blockIdx.x < a.first[2] ? 1 : 2;
+  const int waves = (a.first[kind + 1] - a.first[kind]) * kRopeWaves;
   const int groups = (int)(((int64_t)a.B * a.S + kTokens - 1) / kTokens);
-  Turns<D, ROT> turns;
-  turns.place(a, l);
-  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAheadGrad * 64 : 0);
+  const int heads = a.heads[kind], parts = (heads + a.heads_per - 1) / a.heads_per;
+  const int64_t items = (int64_t)groups * parts, plane = (int64_t)a.S * D;
+  const bool normed = NORM != kNone && kind < 2, turned = ROT != kStill && kind < 2;
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * 64 : 0);
 
+  Turns<D, ROT> turns;
+  Floats8 w, dw, db;
+  if (kind < 2) {
+    turns.place(a, l);
+    load8<D>(NORM == kNone ? nullptr : a.weight[kind], l, 1.f, w);
+  }
 #pragma unroll
-  for (int kind = 0; kind < 3; ++kind) {
-    if (a.heads[kind] == 0) continue;
-    const int parts = (a.heads[kind] + a.heads_per - 1) / a.heads_per;
-    const int64_t items = (int64_t)groups * parts, plane = (int64_t)a.S * D;
-    Floats8 w, dw, db;
-    if (kind < 2) load8<D>(NORM == kNone ? nullptr : a.weight[kind % 2], l, 1.f, w);
+  for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.f;
+  for (int64_t item = (int64_t)((int)blockIdx.x - a.first[kind]) * kRopeWaves + wave; item < items; item += waves) {
+    const int part = (int)(item / groups);
+    const Token tok(a, (item - (int64_t)part * groups) * kTokens + lane / L);
+    const bool reads = tok.valid && in_row, writes = tok.have && in_row;
+    const int h0 = part * a.heads_per, h1 = min(h0 + a.heads_per, heads);
+    const uint16_t* g0 = a.y[kind] + ((int64_t)tok.b * heads * a.S + tok.t) * D + 8 * l;
+    const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
+    uint16_t* d0 = a.dx[kind].p + tok.b * a.dx[kind].batch + tok.t * a.dx[kind].token + 8 * l;
+    u32x4 xin = {0u, 0u, 0u, 0u}, gin = {0u, 0u, 0u, 0u};
+    auto load = [&](int h, u32x4& x, u32x4& g) {
+      if (reads) {
+        g = load16(g0 + h * plane);
+        if (normed) x = load16(x0 + h * a.x[kind].head);
+      }
+    };
+    load(h0, xin, gin);
+    Floats8 c, s;
+    if (turned) turns.at(a, tok.b, tok.t, c, s);
+    for (int h = h0; h < h1; ++h) {
+      u32x4 out = gin;
+      if (normed || turned) {
+        Floats8 g;
+        widen(gin, g);
+        if (turned) {
+          Floats8 gp;
+          turns.partners(gin, g, rows, lane, gp);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.f;
-    for (int64_t item = (int64_t)blockIdx.x * kRopeWaves + wave; item < items; item += (int64_t)a.workgroups * kRopeWaves) {
-      const int part = (int)(item / groups);
-      const Token tok(a, (item - (int64_t)part * groups) * kTokens + lane / L);
-      const bool reads = tok.valid && in_row, writes = tok.have && in_row;
-      const int h0 = part * a.heads_per, h1 = min(h0 + a.heads_per, a.heads[kind]);
-      const uint16_t* g0 = a.y[kind] + ((int64_t)tok.b * a.heads[kind] * a.S + tok.t) * D + 8 * l;
-      const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
-      uint16_t* d0 = a.dx[kind].p + tok.b * a.dx[kind].batch + tok.t * a.dx[kind].token + 8 * l;
-      Floats8 c, s;
-      if (kind < 2) turns.at(a, tok.b, tok.t, c, s);
-      for (int h = h0; h < h1; h += kAheadGrad) {
-        u32x4 in[kAheadGrad], gin[kAheadGrad];
+          for (int e = 0; e < 8; ++e) gp[e] *= s[e];
 #pragma unroll
-        for (int u = 0; u < kAheadGrad; ++u) {
-          in[u] = gin[u] = u32x4{0u, 0u, 0u, 0u};
-          if (h + u < h1 && reads) {
-            gin[u] = load16(g0 + (h + u) * plane);
-            if (kind < 2 && NORM != kNone) in[u] = load16(x0 + (h + u) * a.x[kind].head);
+          for (int e = 0; e < 8; ++e) g[e] = fmaf(g[e], c[e], -gp[e]);
+          if constexpr (ROT >= kWhole) {  // the row in LDS is read before the next one replaces it
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
           }
         }
+        if constexpr (NORM != kNone) {
+          Floats8 x;
+          widen(xin, x);
+          float mean;
+          const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
+          float along = 0.f, sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < kAheadGrad; ++u) {
-          if (h + u >= h1) break;
-          u32x4 out = gin[u];
-          if (kind < 2 && (NORM != kNone || ROT != kStill)) {
-            Floats8 g, gp;
-            widen(gin[u], g);
-            turns.partners(gin[u], g, rows + (ROT >= kWhole ? 64 * u : 0), lane, gp);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (ROT != kStill) g[e] = fmaf(g[e], c[e], -(gp[e] * s[e]));
-            if constexpr (NORM != kNone) {
-              Floats8 x;
-              widen(in[u], x);
-              float mean;
-              const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
-              float along = 0.f, sum = 0.f;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                x[e] *= r;
-                dw[e] = fmaf(g[e], x[e], dw[e]);
-                if constexpr (NORM == kLayer) db[e] += g[e];
-                g[e] *= w[e];
-                along = fmaf(g[e], x[e], along);
-                sum += g[e];
-              }
-              along = row_sum<D>(along) * (1.f / D);
-              sum = NORM == kLayer ? row_sum<D>(sum) * (1.f / D) : 0.f;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) g[e] = r * (fmaf(-x[e], along, g[e]) - sum);
-            }
-            out = narrow(g);
-            if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
+          for (int e = 0; e < 8; ++e) {
+            x[e] *= r;
+            dw[e] = fmaf(g[e], x[e], dw[e]);
+            if constexpr (NORM == kLayer) db[e] += g[e];
+            g[e] *= w[e];
+            along = fmaf(g[e], x[e], along);
+            sum += g[e];
           }
-          if (writes) *reinterpret_cast<u32x4*>(d0 + (h + u) * a.dx[kind].head) = out;
+          along = row_sum<D>(along) * (1.f / D);
+          sum = NORM == kLayer ? row_sum<D>(sum) * (1.f / D) : 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[e] = r * (fmaf(-x[e], along, g[e]) - sum);
         }
-        if constexpr (ROT >= kWhole) {
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
+        out = narrow(g);
+        if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
+      }
+      if (writes) *reinterpret_cast<u32x4*>(d0 + h * a.dx[kind].head) = out;
+      if (h + 1 < h1) load(h + 1, xin, gin);
+    }
+  }
+  if constexpr (NORM != kNone) {
+    if (kind < 2 && a.part) {
+      // Tokens of the wave, then waves, then (the second kernel) workgroups.
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int m = L; m < 64; m <<= 1) {
+          dw[e] += __shfl_xor(dw[e], m);
+          if constexpr (NORM == kLayer) db[e] += __shfl_xor(db[e], m);
+        }
+        if (lane < L && in_row) {
+          s_sum[wave][0][8 * l + e] = dw[e];
+          if constexpr (NORM == kLayer) s_sum[wave][1][8 * l + e] = db[e];
         }
       }
-    }
-    if constexpr (NORM != kNone) {
-      if (kind < 2 && a.part) {
-        // Tokens of the wave, then waves, then (the second kernel) workgroups.
+      __syncthreads();
+      for (int i = threadIdx.x; i < (NORM == kLayer ? 2 : 1) * D; i += 64 * kRopeWaves) {
+        float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-          for (int m = L; m < 64; m <<= 1) {
-            dw[e] += __shfl_xor(dw[e], m);
-            if constexpr (NORM == kLayer) db[e] += __shfl_xor(db[e], m);
-          }
-          if (lane < L && in_row) {
-            s_sum[wave][0][8 * l + e] = dw[e];
-            if constexpr (NORM == kLayer) s_sum[wave][1][8 * l + e] = db[e];
-          }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < (NORM == kLayer ? 2 : 1) * D; i += 64 * kRopeWaves) {
-          float sum = 0.f;
-#pragma unroll
-          for (int x = 0; x < kRopeWaves; ++x) sum += s_sum[x][i / D][i % D];
-          a.part[((int64_t)blockIdx.x * 4 + 2 * kind) * D + i] = sum;
-        }
-        __syncthreads();
+        for (int x = 0; x < kRopeWaves; ++x) sum += s_sum[x][i / D][i % D];
+        a.part[(int64_t)blockIdx.x * 2 * D + i] = sum;
       }
     }
   }
 }
 
-// Adds the workgroups' partial sums: a workgroup per 16 columns of one of the four sums.
+// Adds the workgroups' partial sums: a workgroup per 16 columns of one of the four sums (q's weight and bias,
+// k's).
 constexpr int kSumColumns = 16, kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void head_rope_sum_kernel(const RopeArgs a) {
   constexpr int kSlices = kSumThreads / kSumColumns;
   __shared__ float s_sum[kSlices][kSumColumns];
   float* out = a.sum[blockIdx.y];
-  if (!out || a.heads[blockIdx.y / 2] == 0) return;
+  if (!out) return;
+  const int kind = blockIdx.y / 2;
   const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
   const int e = blockIdx.x * kSumColumns + col;
   float sum = 0.f;
 #pragma unroll 8
-  for (int w = slice; w < a.workgroups; w += kSlices) sum += a.part[((int64_t)w * 4 + blockIdx.y) * a.d + e];
+  for (int w = a.first[kind] + slice; w < a.first[kind + 1]; w += kSlices)
+    sum += a.part[((int64_t)w * 2 + blockIdx.y % 2) * a.d + e];
   s_sum[slice][col] = sum;
   __syncthreads();
   if (slice == 0) {
@@ -459,7 +471,7 @@ __global__ __launch_bounds__(kSumThreads) void head_rope_sum_kernel(const RopeAr
 template <int D, int NORM, int ROT>
 hipError_t run(const RopeArgs& a, bool grad, hipStream_t s) {
   if (grad) {
-    head_rope_grad_kernel<D, NORM, ROT><<<(unsigned)a.workgroups, 64 * kRopeWaves, 0, s>>>(a);
+    head_rope_grad_kernel<D, NORM, ROT><<<(unsigned)a.first[3], 64 * kRopeWaves, 0, s>>>(a);
     if (NORM != kNone && a.part) head_rope_sum_kernel<<<dim3((unsigned)(D / kSumColumns), 4), kSumThreads, 0, s>>>(a);
   } else {
     const int64_t waves = ((int64_t)a.B * a.S + Shape<D>::tokens - 1) / Shape<D>::tokens;

@@ -81,7 +81,7 @@ int from_spec(const head_rope_spec* spec, RopeArgs& a) {
     a.y[x] = nullptr;
   }
   a.heads_per = 1;
-  a.workgroups = 0;
+  for (int& x : a.first) x = 0;
   a.part = nullptr;
   for (float*& x : a.sum) x = nullptr;
   return TA_OK;
@@ -174,17 +174,30 @@ int heads_per_wave(const RopeArgs& a, int heads) {
   return (int)std::max<int64_t>(std::min(heads, 4), (heads + parts - 1) / parts);
 }
 
-// Gradients: workgroups and the heads that a wave takes at a time.
+// Gradients: the heads that a wave takes at a time, and workgroups, four a compute unit at most, as many as are
+// resident at once, shared out by the bytes of a row of q, k (read twice, written) and v (read, written).
 constexpr int64_t kGradWorkgroups = 1024;
 void plan_grad(RopeArgs& a) {
-  const int most = std::max(a.heads[0], std::max(a.heads[1], a.heads[2]));
-  const int64_t groups = groups_of(a);
-  a.heads_per = std::min(most, 4);
-  const int64_t items = groups * ((most + a.heads_per - 1) / a.heads_per);
-  a.workgroups = (int)std::min<int64_t>(kGradWorkgroups, (items + kRopeWaves - 1) / kRopeWaves);
+  const int64_t groups = groups_of(a), heads = (int64_t)a.heads[0] + a.heads[1] + a.heads[2];
+  a.heads_per = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * heads / (kGradWorkgroups * kRopeWaves)));
+  int64_t need[3], share[3], total = 0;
+  for (int x = 0; x < 3; ++x) {
+    need[x] = (groups * ((a.heads[x] + a.heads_per - 1) / a.heads_per) + kRopeWaves - 1) / kRopeWaves;
+    share[x] = (int64_t)(x < 2 && a.norm != TA_NORM_NONE ? 3 : 2) * a.heads[x];
+    total += share[x];
+  }
+  a.first[0] = 0;
+  for (int x = 0; x < 3; ++x) {
+    const int64_t n = a.heads[x] ? std::max<int64_t>(1, kGradWorkgroups * share[x] / total) : 0;
+    a.first[x + 1] = a.first[x] + (int)std::min(n, need[x]);
+  }
 }
-size_t grad_bytes(const RopeArgs& a) {
-  return a.norm == TA_NORM_NONE ? 0 : (size_t)a.workgroups * 4 * a.d * sizeof(float);
+// A row of partial sums for each workgroup of q's and k's rows: whatever of q, k and v is left out, at most
+// this many (a share is rounded down, but not to none), and no more than items of one head make.
+size_t grad_bytes(const RopeArgs& a, int H, int Hkv) {
+  if (a.norm == TA_NORM_NONE) return 0;
+  auto most = [&](int heads) { return (groups_of(a) * heads + kRopeWaves - 1) / kRopeWaves; };
+  return (size_t)std::min(kGradWorkgroups + 2, most(H) + most(Hkv)) * 2 * a.d * sizeof(float);
 }
 
 }  // namespace
@@ -233,8 +246,7 @@ int head_rope_bwd_workspace(const head_rope_spec* spec, size_t* bytes) {
   if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
   RopeArgs a;
   if (int st = from_spec(spec, a)) return st;
-  plan_grad(a);
-  *bytes = grad_bytes(a);
+  *bytes = grad_bytes(a, a.heads[0], a.heads[1]);
   clear_error();
   return TA_OK;
 }
@@ -245,8 +257,7 @@ int head_rope_bwd(const head_rope_spec* spec, const ta_rows* q, const ta_rows* k
                   size_t workspace_bytes, void* stream) {
   RopeArgs a;
   if (int st = from_spec(spec, a)) return st;
-  plan_grad(a);
-  const size_t need = grad_bytes(a);
+  const size_t need = grad_bytes(a, a.heads[0], a.heads[1]);
   const ta_rows* in[3] = {q, k, nullptr};
   const void* g[3] = {dq_out, dk_out, dv_out};
   const ta_rows* out[3] = {dq, dk, dv};
@@ -283,6 +294,7 @@ int head_rope_bwd(const head_rope_spec* spec, const ta_rows* q, const ta_rows* k
     wanted = true;
   }
   if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
+  plan_grad(a);
   a.part = wanted ? static_cast<float*>(workspace) : nullptr;
   for (int x = 0; x < 3; ++x)
     for (int y = x + 1; y < 3; ++y)

@@ -35,8 +35,8 @@ struct RopeArgs {
   int heads_per;        // heads that a wave takes of a token
   // gradients
   Rows dx[3];
-  int workgroups;
-  float* part;    // fp32 [workgroups][q, k][weight, bias][d], or null: no sums are wanted
+  int first[4];   // the first workgroup of q's, k's and v's rows, and their number
+  float* part;    // fp32 [workgroups][weight, bias][d], or null: no sums are wanted
   float* sum[4];  // gradients of q's weight and bias, k's weight and bias, or null
 };
 

@@ -8,10 +8,11 @@ stream of the tensors' device. rope_freqs and grid_positions make what they take
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from ._lib import lib
 from .api import _check, _ptr, _stream
-from .blocks import _current, _lens, _on, _unrecorded, _want, _workspace
+from .blocks import _current, _on, _unrecorded, _want, _workspace
 
 try:
     import torch
@@ -42,7 +43,8 @@ class HeadRopeSpec(ctypes.Structure):
 
 
 def _ref(x):
-    return None if x is None else ctypes.byref(x)
+    """The address of a struct: a Structure's, or bytes laid out alike."""
+    return x if x is None or type(x) is bytes else ctypes.byref(x)
 
 
 def head_rope_fwd(spec, q, k, v, q_out, k_out, v_out, stream=None) -> None:
@@ -84,7 +86,12 @@ def grid_positions(frames: int, height: int, width: int, text: int = 0, device="
     return torch.cat([torch.zeros(text, 3, dtype=torch.int32), grid]).to(device)
 
 
-def _rows(t, name: str, shape, device) -> Rows:
+# The structs as bytes, which ctypes passes by address: a third of the time that building a Structure takes.
+_PACKED_ROWS = struct.Struct("Pqqq")
+_PACKED_SPEC = struct.Struct("6if4x4P2i4i2PqP")
+
+
+def _rows(t, name: str, shape, device) -> bytes:
     """t is a bf16 tensor of this shape on this GPU whose values of a head lie together."""
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -96,47 +103,53 @@ def _rows(t, name: str, shape, device) -> Rows:
     if one != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
     # (The stride of a dimension of one place says nothing.)
-    return Rows(t.data_ptr(), batch if shape[0] > 1 else 0, token if shape[1] > 1 else 0, head if shape[2] > 1 else 0)
+    return _PACKED_ROWS.pack(t.data_ptr(), batch if shape[0] > 1 else 0, token if shape[1] > 1 else 0,
+                             head if shape[2] > 1 else 0)
 
 
 def _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias, norm, eps, lens):
-    """(spec, device, (B, S, H, Hkv, d)) of the wrappers' arguments."""
-    some = next((t for t in (q, k, v) if t is not None), None)
+    """(spec, device, B, S, H, Hkv, d) of the wrappers' arguments."""
+    some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("one of q, k and v must be given")
     if some.dim() != 4 or not some.is_cuda:
         raise ValueError("expected [B, S, heads, d] tensors on a GPU")
-    B, S, _, d = some.shape
+    B, S, H, d = some.shape
     device = some.device
-    H = q.shape[2] if q is not None and q.dim() == 4 else 1
-    heads = k if k is not None else v
-    Hkv = heads.shape[2] if heads is not None and heads.dim() == 4 else 1
+    if q is None:
+        Hkv, H = H, 1
+    else:
+        heads = k if k is not None else v
+        Hkv = heads.shape[2] if heads is not None and heads.dim() == 4 else 1
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {list(NORMS)}, got {norm!r}")
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {list(ROPE_LAYOUTS)}, got {layout!r}")
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (q_bias, "q_bias"), (k_bias, "k_bias")):
-        if t is not None:
-            _want(t, name, (d,), torch.float32, device)
-    spec = HeadRopeSpec(B=B, S=S, H=H, Hkv=Hkv, d=d, norm=NORMS[norm], eps=eps, layout=ROPE_LAYOUTS[layout],
-                        q_weight=_ptr(q_weight), k_weight=_ptr(k_weight), q_bias=_ptr(q_bias), k_bias=_ptr(k_bias))
+    w = [0, 0, 0, 0]
+    if norm is not None or q_weight is not None or k_weight is not None or q_bias is not None or k_bias is not None:
+        shape = (d,)
+        for i, t in enumerate((q_weight, k_weight, q_bias, k_bias)):
+            if t is not None:
+                _want(t, ("q_weight", "k_weight", "q_bias", "k_bias")[i], shape, torch.float32, device)
+                w[i] = t.data_ptr()
     if positions is None:
-        spec.layout = 0
+        turn = (0, 0, 0, 0, 0, 0, 0, 0, 0)
     else:
-        dims = tuple(dims) if dims is not None else (d,)
-        if not 1 <= len(dims) <= ROPE_AXES:
+        dims = (d,) if dims is None else tuple(dims)
+        n = len(dims)
+        if not 1 <= n <= ROPE_AXES:
             raise ValueError(f"dims must name 1 to {ROPE_AXES} axes")
         if freqs is None or layout is None:
             raise ValueError("positions need freqs and a layout")
         _want(freqs, "freqs", (sum(dims) // 2,), torch.float64, device)
-        shape = (S, len(dims)) if positions.dim() == 2 else (B, S, len(dims))
-        _want(positions, "positions", shape, torch.int32, device)
-        spec.axes, spec.dims = len(dims), dims + (0,) * (ROPE_AXES - len(dims))
-        spec.freqs, spec.positions = freqs.data_ptr(), positions.data_ptr()
-        spec.positions_batch = 0 if positions.dim() == 2 else S * len(dims)
-    _lens(lens, (B,), device)
-    spec.lens = _ptr(lens)
-    return spec, device, (B, S, H, Hkv, d)
+        shared = positions.dim() == 2
+        _want(positions, "positions", (S, n) if shared else (B, S, n), torch.int32, device)
+        turn = (ROPE_LAYOUTS[layout], n, *dims, *(0,) * (ROPE_AXES - n), freqs.data_ptr(), positions.data_ptr(),
+                0 if shared else S * n)
+    if lens is not None:
+        _want(lens, "lens", (B,), torch.int32, device)
+    spec = _PACKED_SPEC.pack(B, S, H, Hkv, d, NORMS[norm], eps, *w, *turn, 0 if lens is None else lens.data_ptr())
+    return spec, device, B, S, H, Hkv, d
 
 
 def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleaved", norm=None, q_weight=None,
@@ -152,24 +165,27 @@ def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleave
     values). Without positions nothing is turned. lens (int32 [B]): tokens behind a sequence's end give zeros.
     out: the three results' tensors. Autograd does not record it (it warns where it would have): head_rope_grad
     gives the gradients."""
-    spec, device, (B, S, H, Hkv, d) = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias,
-                                            k_bias, norm, eps, lens)
-    if any(t is not None and t.requires_grad for t in (q, k, v, q_weight, k_weight, q_bias, k_bias)):
-        _unrecorded("head_rope", "head_rope_grad gives the gradients")
-    rows, outs = [], []
-    for i, (t, name, heads) in enumerate(((q, "q", H), (k, "k", Hkv), (v, "v", Hkv))):
+    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias,
+                                          norm, eps, lens)
+    if torch.is_grad_enabled():
+        for t in (q, k, v, q_weight, k_weight, q_bias, k_bias):
+            if t is not None and t.requires_grad:
+                _unrecorded("head_rope", "head_rope_grad gives the gradients")
+                break
+    rows, outs, at = [None, None, None], [None, None, None], [None, None, None]
+    for i, t in enumerate((q, k, v)):
         if t is None:
-            rows.append(None)
-            outs.append(None)
             continue
-        rows.append(_rows(t, name, (B, S, heads, d), device))
+        heads = Hkv if i else H
+        rows[i] = _rows(t, "qkv"[i], (B, S, heads, d), device)
         if out is None:
-            outs.append(torch.empty((B, heads, S, d), dtype=torch.bfloat16, device=device))
+            y = t.new_empty((B, heads, S, d))
         else:
-            _want(out[i], "out", (B, heads, S, d), torch.bfloat16, device)
-            outs.append(out[i])
+            y = out[i]
+            _want(y, "out", (B, heads, S, d), torch.bfloat16, device)
+        outs[i], at[i] = y, y.data_ptr()
     with _on(device):
-        head_rope_fwd(spec, *rows, *outs, _current(device))
+        head_rope_fwd(spec, *rows, *at, _current(device))
     return tuple(outs)
 
 
@@ -180,29 +196,26 @@ def head_rope_grad(q, k, v, dq, dk, dv, positions=None, freqs=None, dims=None, l
     [B, S, heads, d], parts of one [B, S, H + 2 Hkv, d] tensor, the gradient of a projection of everything, or
     written to `out`, three tensors of any strides that keep a head's values together. What was None, or has
     no weight or bias, is None; v's own values are not read, only its shape."""
-    spec, device, (B, S, H, Hkv, d) = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias,
-                                            k_bias, norm, eps, lens)
-    given = ((q, dq, "q", H), (k, dk, "k", Hkv), (v, dv, "v", Hkv))
+    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias,
+                                          norm, eps, lens)
+    given = ((q, dq, H), (k, dk, Hkv), (v, dv, Hkv))
     if out is None:
-        heads = [n if t is not None else 0 for t, _, _, n in given]
-        whole = torch.empty((B, S, sum(heads), d), dtype=torch.bfloat16, device=device)
-        out = whole.split(heads, 2)
-    rows, grads, outs = [], [], []
-    for i, (t, g, name, n) in enumerate(given):
+        heads = [n if t is not None else 0 for t, _, n in given]
+        out = torch.empty((B, S, sum(heads), d), dtype=torch.bfloat16, device=device).split(heads, 2)
+    rows, grads, outs = [None, None, None], [None, None, None], [None, None, None]
+    for i, (t, g, n) in enumerate(given):
         if (t is None) != (g is None):
-            raise ValueError(f"{name} and d{name} go together")
+            raise ValueError(f"{'qkv'[i]} and d{'qkv'[i]} go together")
         if t is None:
-            rows.append(None)
-            grads.append(None)
-            outs.append(None)
             continue
-        rows.append(_rows(t, name, (B, S, n, d), device))
-        _want(g, "d" + name, (B, n, S, d), torch.bfloat16, device)
-        grads.append(g)
-        outs.append(_rows(out[i], "out", (B, S, n, d), device))
-    sums = [None if w is None or t is None else torch.empty(d, dtype=torch.float32, device=device)
+        shape = (B, S, n, d)
+        rows[i] = _rows(t, "qkv"[i], shape, device)
+        _want(g, ("dq", "dk", "dv")[i], (B, n, S, d), torch.bfloat16, device)
+        grads[i] = g.data_ptr()
+        outs[i] = _rows(out[i], "out", shape, device)
+    sums = [None if w is None or t is None else w.new_empty(d)
             for t, w in ((q, q_weight), (k, k_weight), (q, q_bias), (k, k_bias))]
     with _on(device):
-        n = head_rope_bwd_workspace(spec)
+        n = head_rope_bwd_workspace(spec) if norm is not None else 0
         head_rope_bwd(spec, rows[0], rows[1], *grads, *outs, *sums, _workspace(n, device), n, _current(device))
-    return (*(o if t is not None else None for o, t in zip(out, (q, k, v))), *sums)
+    return (*(None if t is None else o for o, t in zip(out, (q, k, v))), *sums)

@@ -119,6 +119,16 @@ def test_sums_need_what_they_are_of():
     assert bwd(**{**none, "kw": 9 * M}, k=None, gk=None, dk=None) == SHAPE
 
 
+def test_packed_structs_are_the_structures():
+    from paper_2502_06155_amd import rope
+
+    v = spec(dims=(2, 4, 6, 8), axes=4, positions_batch=5)
+    at = [getattr(v, n) for n, _ in v._fields_]
+    flat = [y for x in at for y in (list(x) if hasattr(x, "__len__") else [x])]
+    assert rope._PACKED_SPEC.pack(*flat) == bytes(v)
+    assert rope._PACKED_ROWS.pack(1, 2, 3, 4) == bytes(ta.Rows(1, 2, 3, 4))
+
+
 def test_workspaces():
     size = lambda **kw: ta.head_rope_bwd_workspace(spec(**kw))  # noqa: E731
     assert size(norm=0, q_weight=None, k_weight=None, q_bias=None, k_bias=None) == 0
