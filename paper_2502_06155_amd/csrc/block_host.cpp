@@ -161,7 +161,7 @@ struct CachePlan {
   bool whole;
   size_t bytes;
 };
-CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages, int segment = kCacheSegment) {
+CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   CachePlan p;
   const int64_t rows = (int64_t)(H / Hkv) * N;
   p.rows = cache_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
@@ -169,7 +169,22 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages, int seg
   // Two workgroups run on a compute unit in passes of 16 rows, one in passes of 32.
   p.workers = (int)std::min<int64_t>({p.rows == 16 ? kSlots : kSlots / 2,
                                       p.passes < kPassSlots ? std::max<int64_t>(2, kPassSlots / p.passes) : 1,
-                                      (int64_t)B * Hkv * (max_pages + segment)});
+                                      (int64_t)B * Hkv * (max_pages + kCacheSegment)});
+  p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
+  if (p.whole) p.workers = B * Hkv;
+  p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
+  return p;
+}
+// The same over the 4-bit cache, where passes of 64 and 128 rows share a page's widened codes: all passes together
+// have as many workgroups as the device holds, half that in passes of 32 rows, and at least two each, or one.
+CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
+  CachePlan p;
+  const int64_t rows = (int64_t)(H / Hkv) * N;
+  p.rows = cache4_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
+  p.passes = (int)((rows + p.rows - 1) / p.rows);
+  const int64_t slots = p.rows == 32 ? kSlots / 2 : kSlots;
+  p.workers = (int)std::min<int64_t>(p.passes < slots ? std::max<int64_t>(2, slots / p.passes) : 1,
+                                     (int64_t)B * Hkv * (max_pages + kCache4Segment));
   p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
   if (p.whole) p.workers = B * Hkv;
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
@@ -499,7 +514,7 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
 int cache4_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes) {
   if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
   if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
-  *bytes = plan_cache(B, H, Hkv, N, d, max_pages, kCache4Segment).bytes;
+  *bytes = plan_cache4(B, H, Hkv, N, d, max_pages).bytes;
   clear_error();
   return TA_OK;
 }
@@ -517,7 +532,7 @@ int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, con
                              "q, out, the pages and the scales must be 16-byte aligned"))
     return st;
   if (int st = check_aligned({table, lens, lse}, 4, "table, lens and lse must be 4-byte aligned")) return st;
-  const CachePlan p = plan_cache(B, H, Hkv, N, d, max_pages, kCache4Segment);
+  const CachePlan p = plan_cache4(B, H, Hkv, N, d, max_pages);
   if (int st = check_workspace(workspace, workspace_bytes, p.bytes)) return st;
   const int64_t rows = (int64_t)B * H * N, entries = per_head ? (int64_t)B * Hkv : B;
   const size_t qb = bf16s(rows * d), pages = (size_t)n_pages * Hkv * TA_BLOCK * d / 2;

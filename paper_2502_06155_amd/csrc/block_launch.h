@@ -162,5 +162,6 @@ hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream);
 
 // Rows of a pass of cache attention over a sequence's G * N rows.
 int cache_rows_per_pass(int rows);
+int cache4_rows_per_pass(int rows);
 
 }  // namespace ta

@@ -449,17 +449,251 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
   } while (walk.advance(a));
 }
 
+// Many rows. Above, every 32 rows of a key head widen every page again. Here the four waves of a workgroup have 16 RB
+// rows each and go through the pages together: a page's codes are widened once, by all of them, into LDS, where the
+// matrix operands of all rows come from; the next page's codes arrive in registers meanwhile.
+//   K: row 16 i + n of the tile is the token that row n of instruction group i computes, 32 (i / 2) + 8 (n / 4) + 4 (i % 2) + n % 4,
+//   so that the scores of groups 2 c and 2 c + 1 are, in lane group g, tokens 32 c + 8 g .. + 7: P^T of step c. Rows are 16
+//   bytes longer than their d values, which puts 16 rows' pieces on different banks.
+//   V^T: a row of 128 tokens for each channel, its 16-byte pieces of 8 tokens at places exchanged by the channel's
+//   number (key): both the writes (16 channels' words of the same 8 tokens) and the reads (row n of instruction t: channel 8 n + t,
+//   4 n + t at d = 64) fall on different banks.
 template <int D, int RB>
+__global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4AttnArgs a) {
+  constexpr int kWaves = kThreadsC / 64, kRows = 16 * RB * kWaves, kSl = D / 32;
+  constexpr int kCh = D == 64 ? 4 : 8;
+  constexpr int kPitch = D + 8;                       // of a K row, in values
+  constexpr int kKUnits = kBlock * (D / kGroup);      // 32 values of a token
+  constexpr int kKPer = (kKUnits + kThreadsC - 1) / kThreadsC;
+  constexpr int kWords = D / 8;                       // of a token's codes
+  constexpr int kVUnits = kBlock / 8 * kWords;        // a word of 8 tokens
+  __shared__ __attribute__((aligned(16))) uint16_t s_k[kBlock * kPitch];
+  __shared__ __attribute__((aligned(16))) uint16_t s_v[D * kBlock];
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int n = lane & 15, g = lane >> 4;
+  const int rows = a.G * a.N, row0 = blockIdx.y * kRows + 16 * RB * wave;
+  const bool works = row0 < rows;
+  const int v_word = tid % kWords, v_part = tid / kWords;  // tokens 8 v_part .. + 7
+
+  CacheWalk<kCache4Segment> walk(a, blockIdx.x);
+  if (walk.none()) return;
+  do {
+    const int len = walk.len;
+    const CacheSegment seg = walk.segment(a);
+    const int p0 = seg.p0, p1 = seg.p1;
+    if (p1 <= p0 && !a.whole) continue;  // (alone, a segment without tokens gets its zeros)
+    const ScalarInts table = (ScalarInts)(a.table + (size_t)seg.entry * a.max_pages);
+    // The next page from p on that is one; its number in `page`.
+    int page = -1;
+    auto seek = [&](int p) {
+      for (; p < p1; ++p) {
+        page = table[p];
+        if (page >= 0 && page < a.n_pages) break;
+      }
+      return p;
+    };
+    u32x4 kw[kKPer];
+    uint32_t ks[kKPer], vw[8];
+    u32x2 vs;
+    auto load = [&](int p) {
+      const size_t ph = (size_t)page * a.Hkv + seg.h;
+      const uint8_t* k = a.k_pages + ph * kBlock * (D / 2);
+      const uint8_t* ke = a.k_exps + ph * kBlock * (D / kGroup);
+      const uint8_t* v = a.v_pages + ph * kBlock * (D / 2);
+      const uint8_t* ve = a.v_exps + ph * kBlock * (D / kGroup);
+#pragma unroll
+      for (int i = 0; i < kKPer; ++i) {
+        const int u = tid + kThreadsC * i, t = u / (D / kGroup), grp = u % (D / kGroup);
+        if (u < kKUnits) {
+          kw[i] = *reinterpret_cast<const u32x4*>(k + (uint32_t)(t * (D / 2) + 16 * grp));
+          ks[i] = ke[(uint32_t)(grp * kBlock + t)];
+        }
+      }
+      if (tid < kVUnits) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          vw[i] = *reinterpret_cast<const uint32_t*>(v + (uint32_t)((8 * v_part + i) * (D / 2) + 4 * v_word));
+        vs = *reinterpret_cast<const u32x2*>(ve + (uint32_t)(v_word / 4 * kBlock + 8 * v_part));
+      }
+    };
+    auto to_lds = [&](int p) {
+#pragma unroll
+      for (int i = 0; i < kKPer; ++i) {
+        const int u = tid + kThreadsC * i, t = u / (D / kGroup), grp = u % (D / kGroup);
+        if (u < kKUnits) {
+          const int row = (t & ~31) + 16 * (t >> 2 & 1) + 4 * (t >> 3 & 3) + (t & 3);
+          const float f = scale_of(ks[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<u32x4*>(s_k + row * kPitch + 32 * grp + 8 * e) = decode8(kw[i][e], f);
+        }
+      }
+      if (tid < kVUnits) {
+        // Scales behind the last token may be anything: theirs become 2^-127.
+        const int left = len - (p * kBlock + 8 * v_part);
+        vs[0] &= bytes_before(left);
+        vs[1] &= bytes_before(left - 4);
+        u32x4 x[8];  // of the word's 8 channels
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const u32x4 x0 = decode8(vw[i], scale_at(vs, i)), x1 = decode8(vw[i + 1], scale_at(vs, i + 1));
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            x[2 * y][i / 2] = __builtin_amdgcn_perm(x1[y], x0[y], 0x05040100u);
+            x[2 * y + 1][i / 2] = __builtin_amdgcn_perm(x1[y], x0[y], 0x07060302u);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int ch = 8 * v_word + e, key = ch / kCh;
+          *reinterpret_cast<u32x4*>(s_v + ch * kBlock + 8 * (v_part ^ key)) = x[e];
+        }
+      }
+    };
+
+    int p = seek(p0);
+    if (p < p1) load(p);
+    int end[RB];  // tokens this lane's row attends to
+    bf16x8 qf[RB][kSl];
+    f32x4 o[RB][kCh];
+    float m_ref[RB], l_run[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = row0 + 16 * rb + n;
+      end[rb] = r < rows ? len - (a.N - 1) + r % a.N : 0;
+#pragma unroll
+      for (int m = 0; m < kSl; ++m) {
+        u32x4 x = {0u, 0u, 0u, 0u};
+        if (r < rows) x = load16(a.q + (seg.q_row + r) * D + 32 * m + 8 * g);
+        qf[rb][m] = as_bf16x8(x);
+      }
+      m_ref[rb] = kNoRef;
+      l_run[rb] = 0.f;
+#pragma unroll
+      for (int t = 0; t < kCh; ++t) o[rb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    while (p < p1) {
+      __syncthreads();  // the page before is done with
+      to_lds(p);
+      __syncthreads();
+      const int tok0 = p * kBlock;
+      p = seek(p + 1);
+      if (p < p1) load(p);
+      if (!works) continue;
+      // 64 tokens at a time: their scores and weights fit the registers beside sums, queries and the next page.
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        f32x4 s[RB][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int m = 0; m < kSl; ++m) {
+            const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_k + (64 * half + 16 * i + n) * kPitch + 32 * m + 8 * g));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              s[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i], 0, 0, 0);
+          }
+        bf16x8 pf[RB][2];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[rb][i] *= a.c;
+          if (tok0 + kBlock > len - (a.N - 1)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (tok0 + 64 * half + 32 * (i / 2) + 8 * g + 4 * (i % 2) + j >= end[rb]) s[rb][i][j] = -INFINITY;
+          }
+          float mx = s[rb][0][0];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
+          const float m_new = fmaxf(m_ref[rb], group_max(mx));
+          if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
+            const float alpha = fast_exp2(m_ref[rb] - m_new);
+            l_run[rb] *= alpha;
+#pragma unroll
+            for (int t = 0; t < kCh; ++t) o[rb][t] *= alpha;
+            m_ref[rb] = m_new;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+              sum += x;
+              pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)x;
+            }
+          l_run[rb] += sum;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int t = 0; t < kCh; ++t) {
+            // (d = 96: rows 12 to 15 of an instruction are no channels and read those of row 11.)
+            const int key = D == 96 ? min(n, 11) : n;
+            const bf16x8 vf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_v + (kCh * key + t) * kBlock + 8 * ((8 * half + 4 * c + g) ^ key)));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o[rb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][c], o[rb][t], 0, 0, 0);
+          }
+      }
+    }
+
+    // A wave's rows are its own: results or partial results straight from its registers.
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = row0 + 16 * rb + n;
+      const float l = group_sum(l_run[rb]);
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      // (A row of NaN stays one: its sums are NaN, and so is its quotient's product.)
+      const float lse2 = l == 0.f ? -INFINITY : m_ref[rb] + __builtin_amdgcn_logf(l);
+      if (r >= rows) continue;
+      float* pr = a.part + (((size_t)blockIdx.y * 2 * a.workers + seg.slot) * kRows + (r - blockIdx.y * kRows)) * (D + 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int ch = kCh * (4 * g + j);
+        if (ch >= D) continue;
+#pragma unroll
+        for (int t = 0; t < kCh; t += 4) {
+          const f32x4 y = f32x4{o[rb][t][j], o[rb][t + 1][j], o[rb][t + 2][j], o[rb][t + 3][j]} * inv;
+          if (seg.alone)
+            *reinterpret_cast<u32x2*>(a.out + (seg.q_row + r) * D + ch + t) =
+                __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+          else
+            *reinterpret_cast<f32x4*>(pr + ch + t) = y;
+        }
+      }
+      if (g == 0) {
+        if (!seg.alone) pr[D] = lse2;
+        else if (a.lse) a.lse[seg.q_row + r] = lse2 * 0.69314718055994531f;
+      }
+    }
+  } while (walk.advance(a));
+}
+
+template <int D, int ROWS>
 hipError_t cache4_attn_rows(const Cache4AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
   const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
-  cache4_attn_kernel<D, RB><<<grid, kThreadsC, 0, s>>>(a);
-  if (!a.whole) cache_merge_kernel<D, RB, kCache4Segment><<<segs, kThreadsC, 0, s>>>(a);
+  if constexpr (ROWS <= 32) cache4_attn_kernel<D, ROWS / 16><<<grid, kThreadsC, 0, s>>>(a);
+  else cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsC, 0, s>>>(a);
+  if (!a.whole) cache_merge_kernel<D, ROWS / 16, kCache4Segment><<<segs, kThreadsC, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int D>
 hipError_t cache4_attn_for(const Cache4AttnArgs& a, hipStream_t s) {
-  return cache_rows_per_pass(a.G * a.N) == 16 ? cache4_attn_rows<D, 1>(a, s) : cache4_attn_rows<D, 2>(a, s);
+  switch (cache4_rows_per_pass(a.G * a.N)) {
+    case 16: return cache4_attn_rows<D, 16>(a, s);
+    case 32: return cache4_attn_rows<D, 32>(a, s);
+    case 64: return cache4_attn_rows<D, 64>(a, s);
+    default: return cache4_attn_rows<D, 128>(a, s);
+  }
 }
 
 template <int D>
@@ -469,6 +703,8 @@ dim3 token_grid(int N, int heads) {
 }
 
 }  // namespace
+
+int cache4_rows_per_pass(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 hipError_t launch_cache4_write(const Cache4WriteArgs& a, hipStream_t s) {
   if (a.d == 64) cache4_write_kernel<64><<<token_grid<64>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
