@@ -566,7 +566,7 @@ int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, con
   a.d = d;
   a.max_pages = max_pages;
   a.n_pages = n_pages;
-  a.c = scale * 1.4426950408889634f;
+  fold_scale(scale, a.c, a.q_flip, a.q_keep);
   a.whole = p.whole;
   a.workers = p.workers;
   a.row_blocks = p.passes;

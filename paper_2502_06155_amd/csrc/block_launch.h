@@ -145,9 +145,11 @@ struct Cache4ReadArgs {
 };
 
 // As over the 8-bit cache, with scales of its own (k_scales and v_scales are not looked at).
+// c is positive: a scale's sign and its being 0 are in q_flip and q_keep, as in BlockFwdArgs.
 struct Cache4AttnArgs : CacheAttnArgs {
   const uint8_t* k_exps;
   const uint8_t* v_exps;
+  uint32_t q_flip, q_keep;
 };
 
 hipError_t launch_block_means(const MeansArgs& a, hipStream_t stream);

@@ -320,7 +320,7 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
       for (int m = 0; m < kSl; ++m) {
         u32x4 x = {0u, 0u, 0u, 0u};
         if (r < rows) x = load16(a.q + (seg.q_row + r) * D + 8 * (g * kSl + m));
-        qf[rb][m] = as_bf16x8(x);
+        qf[rb][m] = as_bf16x8((x ^ a.q_flip) & a.q_keep);
       }
       m_ref[rb] = kNoRef;
       l_run[rb] = 0.f;
@@ -353,8 +353,6 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
         bf16x8 pf[RB][4];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[rb][i] *= a.c;
           if (tok0 + kBlock > len - (a.N - 1)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -367,7 +365,7 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
           for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
-          const float m_new = fmaxf(m_ref[rb], group_max(mx));
+          const float m_new = fmaxf(m_ref[rb], group_max(mx) * a.c);
           if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
             const float alpha = fast_exp2(m_ref[rb] - m_new);
             l_run[rb] *= alpha;
@@ -380,7 +378,7 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
           for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+              const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
               sum += x;
               pf[rb][j][i] = (__bf16)x;
             }
@@ -566,7 +564,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
       for (int m = 0; m < kSl; ++m) {
         u32x4 x = {0u, 0u, 0u, 0u};
         if (r < rows) x = load16(a.q + (seg.q_row + r) * D + 32 * m + 8 * g);
-        qf[rb][m] = as_bf16x8(x);
+        qf[rb][m] = as_bf16x8((x ^ a.q_flip) & a.q_keep);
       }
       m_ref[rb] = kNoRef;
       l_run[rb] = 0.f;
@@ -598,8 +596,6 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
         bf16x8 pf[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[rb][i] *= a.c;
           if (tok0 + kBlock > len - (a.N - 1)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -612,7 +608,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
-          const float m_new = fmaxf(m_ref[rb], group_max(mx));
+          const float m_new = fmaxf(m_ref[rb], group_max(mx) * a.c);
           if (__builtin_amdgcn_ballot_w64(m_new > m_ref[rb])) {
             const float alpha = fast_exp2(m_ref[rb] - m_new);
             l_run[rb] *= alpha;
@@ -625,7 +621,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(s[rb][i][j] - m_ref[rb]);
+              const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
               sum += x;
               pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)x;
             }
@@ -677,13 +673,19 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
   } while (walk.advance(a));
 }
 
+constexpr int kMergeSlices = 8;
 template <int D, int ROWS>
 hipError_t cache4_attn_rows(const Cache4AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
-  const dim3 segs((unsigned)(a.B * a.Hkv), (unsigned)((a.G * a.N + kMergeRows - 1) / kMergeRows));
   if constexpr (ROWS <= 32) cache4_attn_kernel<D, ROWS / 16><<<grid, kThreadsC, 0, s>>>(a);
   else cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsC, 0, s>>>(a);
-  if (!a.whole) cache_merge_kernel<D, ROWS / 16, kCache4Segment><<<segs, kThreadsC, 0, s>>>(a);
+  if (a.whole) return hipGetLastError();
+  const int segments = a.B * a.Hkv, rows = a.G * a.N;
+  auto segs = [&](int per) { return dim3((unsigned)segments, (unsigned)((rows + per - 1) / per)); };
+  if (a.workers > 4 * segments)
+    cache_merge_kernel<D, ROWS / 16, kCache4Segment, kMergeSlices><<<segs(merge_rows<D, kMergeSlices>()), kThreadsC, 0, s>>>(a);
+  else
+    cache_merge_kernel<D, ROWS / 16, kCache4Segment><<<segs(kMergeRows), kThreadsC, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int D>

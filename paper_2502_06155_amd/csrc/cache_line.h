@@ -203,14 +203,19 @@ __device__ __forceinline__ void join_waves(const CacheAttnArgs& a, const float (
 }
 
 // Joins the partial results of a segment that several workers share, in the order of its pages;
-// a segment without tokens gets its zeros here. A workgroup per segment and 8 rows.
+// a segment without tokens gets its zeros here. A workgroup per segment and 8 rows; or, where many workers
+// share a segment, its threads share a row's parts in SLICES slices (part w is slice w % SLICES'), joined in LDS.
 constexpr int kMergeRows = 8;
-template <int D, int RB, int SEGMENT>
+template <int D, int SLICES>
+constexpr int merge_rows() { return SLICES == 1 ? kMergeRows : kThreadsC / (SLICES * (D / 4)); }
+template <int D, int RB, int SEGMENT, int SLICES = 1>
 __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnArgs a) {
-  constexpr int kRows = 16 * RB;
+  constexpr int kRows = 16 * RB, kPer = merge_rows<D, SLICES>();
+  static_assert(kRows % kPer == 0, "a workgroup's rows are of one pass");
+  __shared__ float s_y[SLICES > 1 ? SLICES * kPer : 1][D + 4];  // a slice's sum, weight and maximum
   const int b = blockIdx.x / a.Hkv, h = blockIdx.x - b * a.Hkv;
   const int entry = a.per_head ? (int)blockIdx.x : b;
-  const int first = blockIdx.y * kMergeRows, rows = min(kMergeRows, a.G * a.N - first);
+  const int first = blockIdx.y * kPer, rows = min(kPer, a.G * a.N - first);
   const int lane = threadIdx.x & 63;
   const int pages = pages_of(__builtin_amdgcn_readfirstlane(cache_len(a, entry)));
   const CacheLine<SEGMENT> line(a);
@@ -229,28 +234,61 @@ __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnA
   // Worker w's part of the segment: its first one (slot 2 w), or w0's second where that began before.
   const int early = w1 >= w0 && line.start(w0) < s0 ? 1 : 0;
   const float* parts = a.part + (size_t)(first / kRows) * 2 * a.workers * kRows * (D + 4) + (size_t)(first % kRows) * (D + 4);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsC) {
-    const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
-    const float* pr = parts + (size_t)r * (D + 4);
-    const size_t step = (size_t)2 * kRows * (D + 4);
-    float m = -INFINITY, l = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const float* pw = pr + w * step + (w == w0 ? early * (step / 2) : 0);
-      const f32x4 u = *reinterpret_cast<const f32x4*>(pw + d0);
-      const float part = pw[D], m_new = fmaxf(m, part);
-      const float f = part == -INFINITY ? 0.f : fast_exp2(part - m_new);  // a NaN stays one
-      const float keep = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
-      l = l * keep + f;
-      y = y * keep + f * u;
-      m = m_new;
-    }
+  const size_t step = (size_t)2 * kRows * (D + 4);
+  // Adds a partial result, of log-sum-exp `part` and with weight `weight` in it, to a running one.
+  auto add = [](float part, float weight, f32x4 u, float& m, float& l, f32x4& y) {
+    const float m_new = fmaxf(m, part);
+    const float f = part == -INFINITY ? 0.f : fast_exp2(part - m_new) * weight;  // a NaN stays one
+    const float keep = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
+    l = l * keep + f;
+    y = y * keep + f * u;
+    m = m_new;
+  };
+  auto write = [&](int r, int d0, float m, float l, f32x4 y) {
     if (l > 0.f) y *= 1.f / l;
     *reinterpret_cast<u32x2*>(a.out + (q_row + r) * D + d0) =
         __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
     if (a.lse && d0 == 0)
       a.lse[q_row + r] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  };
+  const int items = rows * (D / 4) * SLICES;
+  for (int i = threadIdx.x; i < items; i += kThreadsC) {
+    const int slice = SLICES == 1 ? 0 : i / (D / 4) % SLICES, r = i / (D / 4 * SLICES), d0 = 4 * (i % (D / 4));
+    const float* pr = parts + (size_t)r * (D + 4);
+    float m = -INFINITY, l = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int w = w0 + slice; w <= w1; w += SLICES) {
+      const float* pw = pr + w * step + (w == w0 ? early * (step / 2) : 0);
+      add(pw[D], 1.f, *reinterpret_cast<const f32x4*>(pw + d0), m, l, y);
+    }
+    if constexpr (SLICES == 1) {
+      write(r, d0, m, l, y);
+    } else {
+      float* to = s_y[r * SLICES + slice];
+      *reinterpret_cast<f32x4*>(to + d0) = l > 0.f ? y * (1.f / l) : y;  // (a NaN stays one)
+      if (d0 == 0) {
+        to[D] = l;
+        to[D + 1] = m;
+      }
+    }
+  }
+  if constexpr (SLICES > 1) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsC) {
+      const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
+      float m = -INFINITY, l = 0.f;
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < SLICES; ++x) {
+        const float* from = s_y[r * SLICES + x];
+        const float weight = from[D];
+        // (A slice of NaN parts alone has no maximum: its weight, NaN, stands for it.)
+        const float top = weight == 0.f ? -INFINITY : weight > 0.f ? from[D + 1] : weight;
+        add(top, weight, *reinterpret_cast<const f32x4*>(from + d0), m, l, y);
+      }
+      write(r, d0, m, l, y);
+    }
   }
 }
 
