@@ -175,18 +175,44 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
-// The same over the 4-bit cache, where passes of 64 and 128 rows share a page's widened codes: all passes together
-// have as many workgroups as the device holds, half that in passes of 32 rows, and at least two each, or one.
+// The 4-bit cache. Passes of 64 and 128 rows share a page's widened codes, and a workgroup of theirs takes a page at a
+// time, in `page` us, where one of 16 or 32 rows takes four. All passes together have as many workgroups as the device
+// holds (half that in passes of 32 rows), at least two each, or one. What a workgroup of many rows leaves to join
+// costs `part` us, written and read, so that with P pages sqrt(P page / part) of them are the best (64 segments
+// of 4 pages, 120 rows: 35.9 us with 512, 27.8 with 165), but for few pages, which a workgroup each takes (8 segments of
+// 8 pages: 16.5 us with 104, 18.9 with 82).
+// Short tables run a workgroup per segment, in one launch. Alone, a segment takes 5 us and, of 16 rows, 0.22 +
+// 0.003 d us a page; shared, all take 10 us and the bytes' time, d * 1.4e-5 us a page and segment if sequences fill half
+// of their tables, or the pages and parts of the workgroups. Up to 24 pages, so that a batch's longest sequence costs
+// 14 us at most. Measured, alone and shared, one row: 8 segments of 8 pages at d = 128 9.3 and 10.1 us, of 12 11.8 and 10.5; at
+// d = 64 of 12 9.7 and 9.9, of 16 11.4 and 9.7; 128 of 16, d = 128 16.8 and 19.2; 256 of 24 24.8 and 28.8; 36 rows, 8 of 2
+// 9.0 and 10.5, of 4 14.1 and 10.7; 120 rows, 256 of 8 40.7 and 52.1.
+struct ManyRows {
+  double page, part;
+};
+ManyRows many_rows(int rows) { return rows == 64 ? ManyRows{2.5, 0.017} : ManyRows{3.6, 0.034}; }
 CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
   CachePlan p;
-  const int64_t rows = (int64_t)(H / Hkv) * N;
+  const int64_t rows = (int64_t)(H / Hkv) * N, segments = (int64_t)B * Hkv;
   p.rows = cache4_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
   p.passes = (int)((rows + p.rows - 1) / p.rows);
   const int64_t slots = p.rows == 32 ? kSlots / 2 : kSlots;
-  p.workers = (int)std::min<int64_t>(p.passes < slots ? std::max<int64_t>(2, slots / p.passes) : 1,
-                                     (int64_t)B * Hkv * (max_pages + kCache4Segment));
-  p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
-  if (p.whole) p.workers = B * Hkv;
+  int64_t workers = p.passes < slots ? slots / p.passes : 1;
+  double alone, shared;
+  if (p.rows > 32) {
+    const ManyRows m = many_rows(p.rows);
+    const double pages = (double)segments * max_pages;
+    workers = std::min(workers, std::max<int64_t>(128, (int64_t)std::sqrt(pages * m.page / m.part)));
+    alone = m.page * max_pages;
+    shared = 2 * std::sqrt(pages * m.page * m.part);
+  } else {
+    alone = (0.22 + 0.003 * d) * max_pages;
+    shared = 1.4e-5 * d * (double)segments * max_pages;
+  }
+  if (p.passes < slots) workers = std::max<int64_t>(2, workers);
+  p.workers = (int)std::min(workers, segments * (max_pages + kCache4Segment));
+  p.whole = max_pages <= 24 && alone <= 5 + shared;
+  if (p.whole) p.workers = (int)segments;
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }

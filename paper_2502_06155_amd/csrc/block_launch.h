@@ -18,7 +18,7 @@ struct BlockGeo {
 
 constexpr int kLineWorkers = 256;  // workgroups of the gradients' key side at d = 128
 constexpr int kCacheSegment = 3;  // what a (sequence, head) costs cache attention beside its pages
-constexpr int kCache4Segment = 3;  // the same over the 4-bit cache
+constexpr int kCache4Segment = 5;  // the same over the 4-bit cache
 
 struct MeansArgs {
   const uint16_t* x;

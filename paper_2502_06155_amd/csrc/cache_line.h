@@ -34,6 +34,21 @@ __device__ __forceinline__ int pages_of(int len) { return (int)(((uint32_t)len +
 template <int SEGMENT>
 __device__ __forceinline__ int extent_of(int pages) { return pages > 0 ? SEGMENT + pages : 0; }
 
+// The sum of a number over the lanes up to one's own: shifts inside 16 lanes, then the rows' last lanes handed on.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_lanes(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int sum_upto(int x) {
+  x = add_lanes<0x111, 0xf>(x);  // from the lane 1, 2, 4, 8 before, in a row of 16
+  x = add_lanes<0x112, 0xf>(x);
+  x = add_lanes<0x114, 0xf>(x);
+  x = add_lanes<0x118, 0xf>(x);
+  x = add_lanes<0x142, 0xa>(x);  // lane 15 to the row behind it, rows 1 and 3
+  return add_lanes<0x143, 0xc>(x);  // lane 31 to rows 2 and 3
+}
+__device__ __forceinline__ int sum_all(int x) { return __builtin_amdgcn_readlane(sum_upto(x), 63); }
+
 template <int SEGMENT>
 struct CacheLine {
   int entries, per;  // entries of lens, segments of an entry
@@ -46,9 +61,7 @@ struct CacheLine {
     if (!measure) return;
     int n = 0;
     for (int i = threadIdx.x & 63; i < entries; i += 64) n += extent_of<SEGMENT>(pages_of(cache_len(a, i)));
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) n += __shfl_xor(n, s);
-    total = __builtin_amdgcn_readfirstlane(n) * per;
+    total = sum_all(n) * per;
     each = scalar_div(total, a.workers);
     more = total - each * a.workers;
   }
@@ -64,19 +77,14 @@ struct CacheLine {
     before = 0;
     for (int i0 = 0; i0 < entries; i0 += 64) {
       const int own = i0 + lane < entries ? extent_of<SEGMENT>(pages_of(cache_len(a, i0 + lane))) * per : 0;
-      int upto = own;
-#pragma unroll
-      for (int s = 1; s < 64; s <<= 1) {
-        const int y = __shfl_up(upto, s);
-        if (lane >= s) upto += y;
-      }
+      const int upto = sum_upto(own);
       const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
       if (past) {
         const int src = __ffsll((unsigned long long)past) - 1;
-        before = __builtin_amdgcn_readfirstlane(before + __shfl(upto - own, src));
-        return __builtin_amdgcn_readfirstlane(i0 + src);
+        before += __builtin_amdgcn_readlane(upto - own, src);
+        return i0 + src;
       }
-      before = __builtin_amdgcn_readfirstlane(before + __shfl(upto, 63));
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
     return entries;
   }
@@ -221,9 +229,7 @@ __global__ __launch_bounds__(kThreadsC) void cache_merge_kernel(const CacheAttnA
   const CacheLine<SEGMENT> line(a);
   int before = 0;
   for (int i = lane; i < entry; i += 64) before += extent_of<SEGMENT>(pages_of(cache_len(a, i)));
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) before += __shfl_xor(before, s);
-  const int s0 = __builtin_amdgcn_readfirstlane(before) * line.per + (a.per_head ? 0 : h * extent_of<SEGMENT>(pages));
+  const int s0 = sum_all(before) * line.per + (a.per_head ? 0 : h * extent_of<SEGMENT>(pages));
   int w0 = 0, w1 = -1;
   if (pages > 0) {
     w0 = line.worker(s0 + SEGMENT);
