@@ -504,7 +504,7 @@ int cache4_attn_write(const void* k, const void* v, void* k_pages, void* v_pages
                           static_cast<uint8_t*>(k_pages), static_cast<uint8_t*>(v_pages),
                           static_cast<uint8_t*>(k_scales), static_cast<uint8_t*>(v_scales), table, lens, n_new,
                           static_cast<uint16_t*>(k_held), static_cast<uint16_t*>(v_held), B, Hkv, N, d, max_pages,
-                          n_pages};
+                          n_pages, new_bytes * ((k_held != nullptr) + (v_held != nullptr)) > kStaysInCache};
   return launched(launch_cache4_write(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -533,7 +533,7 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
   const Cache4ReadArgs a{static_cast<const uint8_t*>(k_pages), static_cast<const uint8_t*>(v_pages),
                          static_cast<const uint8_t*>(k_scales), static_cast<const uint8_t*>(v_scales), table, lens,
                          static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), B, Hkv, N, d, max_pages,
-                         n_pages, first};
+                         n_pages, first, out * ((k_out != nullptr) + (v_out != nullptr)) > kStaysInCache};
   return launched(launch_cache4_read(a, static_cast<hipStream_t>(stream)));
 }
 

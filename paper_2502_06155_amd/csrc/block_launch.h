@@ -130,6 +130,7 @@ struct Cache4WriteArgs {
   uint16_t* k_held;      // or null
   uint16_t* v_held;      // or null
   int B, Hkv, N, d, max_pages, n_pages;
+  bool past;  // held values past the caches
 };
 
 struct Cache4ReadArgs {
@@ -142,6 +143,7 @@ struct Cache4ReadArgs {
   uint16_t* k_out;  // or null
   uint16_t* v_out;  // or null
   int B, Hkv, N, d, max_pages, n_pages, first;
+  bool past;  // results past the caches
 };
 
 // As over the 8-bit cache, with scales of its own (k_scales and v_scales are not looked at).

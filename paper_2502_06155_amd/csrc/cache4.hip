@@ -73,121 +73,121 @@ __device__ __forceinline__ int page_at(const int32_t* table, int max_pages, int 
   return page < n_pages ? page : -1;
 }
 
-constexpr int kTokensAhead = 4;  // tokens of a lane that are read together
+// Results go past the caches where all of them together would not stay there for whoever reads them (kStaysInCache): 245 MB of
+// read values 50 us so, 63 into the caches, and their reader 77 and 73 us; 31 MB 9.2 and 10.1, and 9.5 and 7.9. (A template: where
+// one kernel has both stores, the compiler makes one of them.)
+template <bool PAST>
+__device__ __forceinline__ void store16(uint16_t* p, u32x4 x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = x;
+}
 
-// Bound by the bytes. K and V of a token in the same lanes: a token that holds anything but finite numbers is
-// marked in K.
-template <int D>
+// Bound by the bytes: three prompts of 8191 tokens, 8 heads of 96, with the held values 31 us for 171 MB (5.5 TB/s; a large
+// copy 5.1); one token of 32 sequences 4.2 us, a chain of loads: length, table, then the stores. A token a lane:
+// two, four and eight, read together, took 33, 37 and 75 us.
+// K and V of a token in the same lanes: a token that holds anything but finite numbers is marked in K. Scales, bytes
+// that lie token by token, are gathered in LDS and leave for all tokens of the workgroup (38 us without).
+template <int D, bool PAST>
 __global__ __launch_bounds__(kThreadsC) void cache4_write_kernel(const Cache4WriteArgs a) {
   using Lanes = TokenLanes<D>;
+  constexpr int kTokens = Lanes::per_pass, kGroups = D / kGroup;
+  __shared__ uint8_t s_scale[2 * kGroups * kTokens];  // [K, V][group][token]
+  __shared__ int s_page[kTokens];
   const int b = blockIdx.y / a.Hkv, h = blockIdx.y - b * a.Hkv;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = lane / Lanes::lanes, l = lane - sub * Lanes::lanes;
-  if (sub >= Lanes::tokens) return;
   const int64_t len = max(a.lens[b], 0);
   const int n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
   const int32_t* table = a.table + (size_t)b * a.max_pages;
-  const int t0 = (int)blockIdx.x * kTokensAhead * Lanes::per_pass + wave * Lanes::tokens + sub;
-  const size_t row0 = ((size_t)b * a.Hkv + h) * a.N;
-
-  u32x4 k[kTokensAhead], v[kTokensAhead];
-  int page[kTokensAhead];
-#pragma unroll
-  for (int i = 0; i < kTokensAhead; ++i) {
-    const int t = t0 + i * Lanes::per_pass;
-    k[i] = v[i] = u32x4{0u, 0u, 0u, 0u};
-    page[i] = -1;
+  const int64_t first = (int64_t)blockIdx.x * kTokens;  // of the workgroup's tokens
+  if (sub < Lanes::tokens) {
+    const int in_wg = wave * Lanes::tokens + sub;
+    const int64_t t = first + in_wg;
+    const size_t at = (((size_t)b * a.Hkv + h) * a.N + t) * D + 8 * l;
+    u32x4 k = {0u, 0u, 0u, 0u}, v = k;
+    int page = -1;
     if (t < n) {
-      k[i] = load16(a.k + (row0 + t) * D + 8 * l);
-      v[i] = load16(a.v + (row0 + t) * D + 8 * l);
-      page[i] = page_at(table, a.max_pages, a.n_pages, len + t);
+      k = load16(a.k + at);
+      v = load16(a.v + at);
+      page = page_at(table, a.max_pages, a.n_pages, len + t);
     }
-  }
-#pragma unroll
-  for (int i = 0; i < kTokensAhead; ++i) {
-    const int t = t0 + i * Lanes::per_pass;
     uint32_t bad = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bad |= not_finite(k[i][e]) | not_finite(v[i][e]);
+    for (int e = 0; e < 4; ++e) bad |= not_finite(k[e]) | not_finite(v[e]);
     bool marked = false;
     if (const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0)) {
       marked = (any >> (sub * Lanes::lanes) & ((1ull << Lanes::lanes) - 1)) != 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        k[i][e] &= ~not_finite(k[i][e]);
-        v[i][e] &= ~not_finite(v[i][e]);
+        k[e] &= ~not_finite(k[e]);
+        v[e] &= ~not_finite(v[e]);
       }
     }
     uint32_t most_k = 0, most_v = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      most_k = max(most_k, max(k[i][e] & 0x7fffu, k[i][e] >> 16 & 0x7fffu));
-      most_v = max(most_v, max(v[i][e] & 0x7fffu, v[i][e] >> 16 & 0x7fffu));
+      most_k = max(most_k, max(k[e] & 0x7fffu, k[e] >> 16 & 0x7fffu));
+      most_v = max(most_v, max(v[e] & 0x7fffu, v[e] >> 16 & 0x7fffu));
     }
     most_k = max_from<0x4e>(max_from<0xb1>(most_k));  // of four lanes
     most_v = max_from<0x4e>(max_from<0xb1>(most_v));
-    uint32_t scale_k = scale_byte(most_k), scale_v = scale_byte(most_v);
-    const uint32_t code_k = encode8(k[i], scale_of(scale_k)), code_v = encode8(v[i], scale_of(scale_v));
+    uint32_t scale_k = scale_byte(most_k);
+    const uint32_t scale_v = scale_byte(most_v);
+    const uint32_t code_k = encode8(k, scale_of(scale_k)), code_v = encode8(v, scale_of(scale_v));
     if (marked) scale_k = kNanScale;
-    if (page[i] >= 0) {
-      const int at = (int)((len + t) % kBlock);
-      const size_t ph = (size_t)page[i] * a.Hkv + h;
-      const size_t code = (ph * kBlock + at) * (D / 2) + 4 * l, scale = (ph * (D / kGroup) + l / 4) * kBlock + at;
+    if (l % 4 == 0) {
+      s_scale[l / 4 * kTokens + in_wg] = (uint8_t)scale_k;
+      s_scale[(kGroups + l / 4) * kTokens + in_wg] = (uint8_t)scale_v;
+    }
+    if (l == 0) s_page[in_wg] = page;
+    if (page >= 0) {
+      const size_t code = (((size_t)page * a.Hkv + h) * kBlock + (int)((len + t) % kBlock)) * (D / 2) + 4 * l;
       *reinterpret_cast<uint32_t*>(a.k_pages + code) = code_k;
       *reinterpret_cast<uint32_t*>(a.v_pages + code) = code_v;
-      if (l % 4 == 0) {
-        a.k_scales[scale] = (uint8_t)scale_k;
-        a.v_scales[scale] = (uint8_t)scale_v;
-      }
     }
     if (t < a.N) {
-      const size_t to = (row0 + t) * D + 8 * l;
       const u32x4 none = {0u, 0u, 0u, 0u};
-      if (a.k_held) *reinterpret_cast<u32x4*>(a.k_held + to) = page[i] < 0 ? none : decode8(code_k, scale_of(scale_k));
-      if (a.v_held) *reinterpret_cast<u32x4*>(a.v_held + to) = page[i] < 0 ? none : decode8(code_v, scale_of(scale_v));
+      if (a.k_held) store16<PAST>(a.k_held + at, page < 0 ? none : decode8(code_k, scale_of(scale_k)));
+      if (a.v_held) store16<PAST>(a.v_held + at, page < 0 ? none : decode8(code_v, scale_of(scale_v)));
     }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * kGroups * kTokens; i += kThreadsC) {
+    const int in_wg = i % kTokens, row = i / kTokens, page = s_page[in_wg];
+    if (page < 0) continue;
+    uint8_t* scales = row < kGroups ? a.k_scales : a.v_scales;
+    scales[(((size_t)page * a.Hkv + h) * kGroups + row % kGroups) * kBlock + (int)((len + first + in_wg) % kBlock)] =
+        s_scale[i];
   }
 }
 
-// Bound by the bytes that it writes.
-template <int D>
+// Bound by the bytes that it writes: 2 sequences of 30001 tokens, 8 heads of 128, 45 us for 300 MB (6.6 TB/s); two and four
+// tokens a lane 46 and 49.
+template <int D, bool PAST>
 __global__ __launch_bounds__(kThreadsC) void cache4_read_kernel(const Cache4ReadArgs a) {
   using Lanes = TokenLanes<D>;
   const int b = blockIdx.y / a.Hkv, h = blockIdx.y - b * a.Hkv;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = lane / Lanes::lanes, l = lane - sub * Lanes::lanes;
-  if (sub >= Lanes::tokens) return;
-  const int len = a.lens[b];
-  const int32_t* table = a.table + (size_t)b * a.max_pages;
-  const int t0 = (int)blockIdx.x * kTokensAhead * Lanes::per_pass + wave * Lanes::tokens + sub;
-  const size_t row0 = ((size_t)b * a.Hkv + h) * a.N;
-
-  uint32_t k[kTokensAhead], v[kTokensAhead];
-  float ks[kTokensAhead], vs[kTokensAhead];
-#pragma unroll
-  for (int i = 0; i < kTokensAhead; ++i) {
-    const int t = t0 + i * Lanes::per_pass;
-    k[i] = v[i] = 0;
-    ks[i] = vs[i] = 1.f;
-    if (t >= a.N || a.first + t >= len) continue;
-    const int page = page_at(table, a.max_pages, a.n_pages, a.first + t);
-    if (page < 0) continue;
-    const int at = (a.first + t) % kBlock;
-    const size_t ph = (size_t)page * a.Hkv + h;
-    const size_t code = (ph * kBlock + at) * (D / 2) + 4 * l, scale = (ph * (D / kGroup) + l / 4) * kBlock + at;
-    k[i] = *reinterpret_cast<const uint32_t*>(a.k_pages + code);
-    v[i] = *reinterpret_cast<const uint32_t*>(a.v_pages + code);
-    ks[i] = scale_of(a.k_scales[scale]);
-    vs[i] = scale_of(a.v_scales[scale]);
+  const int64_t t = (int64_t)blockIdx.x * Lanes::per_pass + wave * Lanes::tokens + sub, pos = a.first + t;
+  if (sub >= Lanes::tokens || t >= a.N) return;
+  uint32_t k = 0, v = 0;
+  float ks = 1.f, vs = 1.f;
+  if (pos < a.lens[b]) {
+    const int page = page_at(a.table + (size_t)b * a.max_pages, a.max_pages, a.n_pages, pos);
+    if (page >= 0) {
+      const int at = (int)(pos % kBlock);
+      const size_t ph = (size_t)page * a.Hkv + h;
+      const size_t code = (ph * kBlock + at) * (D / 2) + 4 * l, scale = (ph * (D / kGroup) + l / 4) * kBlock + at;
+      k = *reinterpret_cast<const uint32_t*>(a.k_pages + code);
+      v = *reinterpret_cast<const uint32_t*>(a.v_pages + code);
+      ks = scale_of(a.k_scales[scale]);
+      vs = scale_of(a.v_scales[scale]);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < kTokensAhead; ++i) {
-    const int t = t0 + i * Lanes::per_pass;
-    if (t >= a.N) break;
-    const size_t to = (row0 + t) * D + 8 * l;
-    if (a.k_out) *reinterpret_cast<u32x4*>(a.k_out + to) = decode8(k[i], ks[i]);
-    if (a.v_out) *reinterpret_cast<u32x4*>(a.v_out + to) = decode8(v[i], vs[i]);
-  }
+  const size_t to = (((size_t)b * a.Hkv + h) * a.N + t) * D + 8 * l;
+  if (a.k_out) store16<PAST>(a.k_out + to, decode8(k, ks));
+  if (a.v_out) store16<PAST>(a.v_out + to, decode8(v, vs));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -700,8 +700,23 @@ hipError_t cache4_attn_for(const Cache4AttnArgs& a, hipStream_t s) {
 
 template <int D>
 dim3 token_grid(int N, int heads) {
-  constexpr int per = kTokensAhead * TokenLanes<D>::per_pass;
-  return dim3((unsigned)((N + per - 1) / per), (unsigned)heads);
+  constexpr int per = TokenLanes<D>::per_pass;
+  return dim3((unsigned)(((int64_t)N + per - 1) / per), (unsigned)heads);
+}
+
+template <int D>
+hipError_t write_tokens(const Cache4WriteArgs& a, hipStream_t s) {
+  const dim3 grid = token_grid<D>(a.N, a.B * a.Hkv);
+  if (a.past) cache4_write_kernel<D, true><<<grid, kThreadsC, 0, s>>>(a);
+  else cache4_write_kernel<D, false><<<grid, kThreadsC, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t read_tokens(const Cache4ReadArgs& a, hipStream_t s) {
+  const dim3 grid = token_grid<D>(a.N, a.B * a.Hkv);
+  if (a.past) cache4_read_kernel<D, true><<<grid, kThreadsC, 0, s>>>(a);
+  else cache4_read_kernel<D, false><<<grid, kThreadsC, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -709,17 +724,13 @@ dim3 token_grid(int N, int heads) {
 int cache4_rows_per_pass(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 hipError_t launch_cache4_write(const Cache4WriteArgs& a, hipStream_t s) {
-  if (a.d == 64) cache4_write_kernel<64><<<token_grid<64>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  else if (a.d == 96) cache4_write_kernel<96><<<token_grid<96>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  else cache4_write_kernel<128><<<token_grid<128>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.d == 64) return write_tokens<64>(a, s);
+  return a.d == 96 ? write_tokens<96>(a, s) : write_tokens<128>(a, s);
 }
 
 hipError_t launch_cache4_read(const Cache4ReadArgs& a, hipStream_t s) {
-  if (a.d == 64) cache4_read_kernel<64><<<token_grid<64>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  else if (a.d == 96) cache4_read_kernel<96><<<token_grid<96>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  else cache4_read_kernel<128><<<token_grid<128>(a.N, a.B * a.Hkv), kThreadsC, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.d == 64) return read_tokens<64>(a, s);
+  return a.d == 96 ? read_tokens<96>(a, s) : read_tokens<128>(a, s);
 }
 
 hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream) {

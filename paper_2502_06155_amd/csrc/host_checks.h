@@ -18,6 +18,9 @@ namespace host {
 constexpr int64_t kSlots = 512;
 constexpr int64_t kMaxGrid = (int64_t)UINT32_MAX / 256 - 8;
 
+// Results of more bytes than this leave past the caches: half of the last level.
+constexpr size_t kStaysInCache = (size_t)128 << 20;
+
 struct Span {
   const void* p;
   size_t bytes;
