@@ -67,13 +67,18 @@ def _check_cache(k_pages, v_pages, k_scales, v_scales):
     """(pages, key heads, d, device) of the cache's tensors."""
     if k_pages.dim() != 4 or not k_pages.is_cuda:
         raise ValueError("k_pages must be a [n_pages, Hkv, 128, d / 2] tensor on a GPU")
-    pages, Hkv, _, half = k_pages.shape
-    device = k_pages.device
+    pages, Hkv, _, half = shape = k_pages.shape
+    device, u8 = k_pages.device, torch.uint8
     codes, scales = (pages, Hkv, BLOCK_TOKENS, half), (pages, Hkv, half // (CACHE4_GROUP // 2), BLOCK_TOKENS)
-    _want(k_pages, "k_pages", codes, torch.uint8, device)
-    _want(v_pages, "v_pages", codes, torch.uint8, device)
-    _want(k_scales, "k_scales", scales, torch.uint8, device)
-    _want(v_scales, "v_scales", scales, torch.uint8, device)
+    # One comparison chain where all is well: four tensors a call.
+    if not (shape == codes == v_pages.shape and scales == k_scales.shape == v_scales.shape
+            and k_pages.dtype is u8 and v_pages.dtype is u8 and k_scales.dtype is u8 and v_scales.dtype is u8
+            and device == v_pages.device == k_scales.device == v_scales.device and k_pages.is_contiguous()
+            and v_pages.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+        _want(k_pages, "k_pages", codes, u8, device)
+        _want(v_pages, "v_pages", codes, u8, device)
+        _want(k_scales, "k_scales", scales, u8, device)
+        _want(v_scales, "v_scales", scales, u8, device)
     return pages, Hkv, 2 * half, device
 
 
@@ -103,8 +108,10 @@ def cache4_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new=
         _want(n_new, "n_new", (B,), torch.int32, device)
     with _on(device):
         held = (torch.empty_like(k), torch.empty_like(v)) if return_held else (None, None)
-        cache4_attn_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new, *held, B, Hkv, N, d, width,
-                          pages, _current(device))
+        _check(lib.cache4_attn_write(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                     k_scales.data_ptr(), v_scales.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                                     _ptr(n_new), *map(_ptr, held), B, Hkv, N, d, width, pages, _current(device)),
+               "cache4_attn_write")
     return held if return_held else None
 
 
@@ -117,9 +124,11 @@ def cache4_read(k_pages, v_pages, k_scales, v_scales, table, lens, N: int, first
     if N < 1:
         raise ValueError(f"N must be at least 1, got {N}")
     with _on(device):
-        out = tuple(torch.empty((B, Hkv, N, d), dtype=torch.bfloat16, device=device) for _ in range(2))
-        cache4_attn_read(k_pages, v_pages, k_scales, v_scales, table, lens, *out, B, Hkv, N, d, width, pages, first,
-                         _current(device))
+        k = torch.empty((B, Hkv, N, d), dtype=torch.bfloat16, device=device)
+        out = (k, torch.empty_like(k))
+        _check(lib.cache4_attn_read(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                    table.data_ptr(), lens.data_ptr(), k.data_ptr(), out[1].data_ptr(), B, Hkv, N, d,
+                                    width, pages, first, _current(device)), "cache4_attn_read")
     return out
 
 
@@ -147,8 +156,12 @@ def cache4_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: flo
             out = torch.empty_like(q)
         else:
             _want(out, "out", q.shape, torch.bfloat16, device)
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=device) if return_lse else None
+        lse = q.new_empty((B, H, N), dtype=torch.float32) if return_lse else None
         n = cache4_attn_fwd_workspace(B, H, Hkv, N, d, width)
-        cache4_attn_fwd(q, k_pages, v_pages, k_scales, v_scales, table, lens, per_head, out, lse, B, H, Hkv, N, d, width,
-                        pages, d ** -0.5 if scale is None else scale, _workspace(n, device), n, _current(device))
+        workspace = _workspace(n, device)
+        _check(lib.cache4_attn_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(),
+                                   v_scales.data_ptr(), table.data_ptr(), lens.data_ptr(), per_head, out.data_ptr(),
+                                   lse.data_ptr() if return_lse else None, B, H, Hkv, N, d, width, pages,
+                                   d ** -0.5 if scale is None else scale, workspace.data_ptr() if n else None, n,
+                                   _current(device)), "cache4_attn_fwd")
     return (out, lse) if return_lse else out

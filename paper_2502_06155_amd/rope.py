@@ -8,6 +8,7 @@ stream of the tensors' device. rope_freqs and grid_positions make what they take
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 from ._lib import lib
@@ -60,6 +61,12 @@ def head_rope_bwd_workspace(spec) -> int:
     return n.value
 
 
+@functools.lru_cache(maxsize=1024)
+def _grad_workspace(B: int, S: int, H: int, Hkv: int, d: int) -> int:
+    """head_rope_bwd_workspace of a spec of these sizes with a norm."""
+    return head_rope_bwd_workspace(HeadRopeSpec(B=B, S=S, H=H, Hkv=Hkv, d=d, norm=1, eps=1.0))
+
+
 def head_rope_bwd(spec, q, k, dq_out, dk_out, dv_out, dq, dk, dv, dq_weight=None, dk_weight=None, dq_bias=None,
                   dk_bias=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """head_rope_bwd of the C ABI: q, k, dq, dk, dv are Rows or None."""
@@ -89,25 +96,28 @@ def grid_positions(frames: int, height: int, width: int, text: int = 0, device="
 # The structs as bytes, which ctypes passes by address: a third of the time that building a Structure takes.
 _PACKED_ROWS = struct.Struct("Pqqq")
 _PACKED_SPEC = struct.Struct("6if4x4P2i4i2PqP")
+_WEIGHTS = ("q_weight", "k_weight", "q_bias", "k_bias")
 
 
-def _rows(t, name: str, shape, device) -> bytes:
-    """t is a bf16 tensor of this shape on this GPU whose values of a head lie together."""
-    if t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype is not torch.bfloat16:
-        raise ValueError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
-    if t.device != device:
+def _rows(t, name: str, B: int, S: int, heads: int, d: int, device) -> bytes:
+    """t is a bf16 [B, S, heads, d] tensor on this GPU whose values of a head lie together."""
+    if t.dtype is not torch.bfloat16 or t.shape != (B, S, heads, d) or t.device != device:
+        if t.shape != (B, S, heads, d):
+            raise ValueError(f"{name} must have the shape {(B, S, heads, d)}, got {tuple(t.shape)}")
+        if t.dtype is not torch.bfloat16:
+            raise ValueError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
         raise ValueError(f"{name} must be on the GPU {device}, got {t.device}")
     batch, token, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
     # (The stride of a dimension of one place says nothing.)
-    return _PACKED_ROWS.pack(t.data_ptr(), batch if shape[0] > 1 else 0, token if shape[1] > 1 else 0,
-                             head if shape[2] > 1 else 0)
+    return _PACKED_ROWS.pack(t.data_ptr(), batch if B > 1 else 0, token if S > 1 else 0, head if heads > 1 else 0)
 
 
-def _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias, norm, eps, lens):
+_STILL = (0,) * 9
+
+
+def _spec(q, k, v, positions, freqs, dims, layout, weights, norm, eps, lens):
     """(spec, device, B, S, H, Hkv, d) of the wrappers' arguments."""
     some = q if q is not None else k if k is not None else v
     if some is None:
@@ -125,16 +135,13 @@ def _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k
         raise ValueError(f"norm must be one of {list(NORMS)}, got {norm!r}")
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {list(ROPE_LAYOUTS)}, got {layout!r}")
-    w = [0, 0, 0, 0]
-    if norm is not None or q_weight is not None or k_weight is not None or q_bias is not None or k_bias is not None:
-        shape = (d,)
-        for i, t in enumerate((q_weight, k_weight, q_bias, k_bias)):
-            if t is not None:
-                _want(t, ("q_weight", "k_weight", "q_bias", "k_bias")[i], shape, torch.float32, device)
-                w[i] = t.data_ptr()
-    if positions is None:
-        turn = (0, 0, 0, 0, 0, 0, 0, 0, 0)
-    else:
+    at = [0, 0, 0, 0]
+    for i, t in enumerate(weights):
+        if t is not None:
+            _want(t, _WEIGHTS[i], (d,), torch.float32, device)
+            at[i] = t.data_ptr()
+    turn = _STILL
+    if positions is not None:
         dims = (d,) if dims is None else tuple(dims)
         n = len(dims)
         if not 1 <= n <= ROPE_AXES:
@@ -144,12 +151,12 @@ def _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k
         _want(freqs, "freqs", (sum(dims) // 2,), torch.float64, device)
         shared = positions.dim() == 2
         _want(positions, "positions", (S, n) if shared else (B, S, n), torch.int32, device)
-        turn = (ROPE_LAYOUTS[layout], n, *dims, *(0,) * (ROPE_AXES - n), freqs.data_ptr(), positions.data_ptr(),
+        turn = (ROPE_LAYOUTS[layout], n, *dims, *_STILL[n:ROPE_AXES], freqs.data_ptr(), positions.data_ptr(),
                 0 if shared else S * n)
     if lens is not None:
         _want(lens, "lens", (B,), torch.int32, device)
-    spec = _PACKED_SPEC.pack(B, S, H, Hkv, d, NORMS[norm], eps, *w, *turn, 0 if lens is None else lens.data_ptr())
-    return spec, device, B, S, H, Hkv, d
+        lens = lens.data_ptr()
+    return _PACKED_SPEC.pack(B, S, H, Hkv, d, NORMS[norm], eps, *at, *turn, lens or 0), device, B, S, H, Hkv, d
 
 
 def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleaved", norm=None, q_weight=None,
@@ -165,10 +172,10 @@ def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleave
     values). Without positions nothing is turned. lens (int32 [B]): tokens behind a sequence's end give zeros.
     out: the three results' tensors. Autograd does not record it (it warns where it would have): head_rope_grad
     gives the gradients."""
-    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias,
-                                          norm, eps, lens)
+    weights = (q_weight, k_weight, q_bias, k_bias)
+    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, weights, norm, eps, lens)
     if torch.is_grad_enabled():
-        for t in (q, k, v, q_weight, k_weight, q_bias, k_bias):
+        for t in (q, k, v, *weights):
             if t is not None and t.requires_grad:
                 _unrecorded("head_rope", "head_rope_grad gives the gradients")
                 break
@@ -177,7 +184,7 @@ def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleave
         if t is None:
             continue
         heads = Hkv if i else H
-        rows[i] = _rows(t, "qkv"[i], (B, S, heads, d), device)
+        rows[i] = _rows(t, "qkv"[i], B, S, heads, d, device)
         if out is None:
             y = t.new_empty((B, heads, S, d))
         else:
@@ -185,7 +192,7 @@ def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleave
             _want(y, "out", (B, heads, S, d), torch.bfloat16, device)
         outs[i], at[i] = y, y.data_ptr()
     with _on(device):
-        head_rope_fwd(spec, *rows, *at, _current(device))
+        _check(lib.head_rope_fwd(spec, *rows, *at, _current(device)), "head_rope_fwd")
     return tuple(outs)
 
 
@@ -196,26 +203,31 @@ def head_rope_grad(q, k, v, dq, dk, dv, positions=None, freqs=None, dims=None, l
     [B, S, heads, d], parts of one [B, S, H + 2 Hkv, d] tensor, the gradient of a projection of everything, or
     written to `out`, three tensors of any strides that keep a head's values together. What was None, or has
     no weight or bias, is None; v's own values are not read, only its shape."""
-    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, q_weight, k_weight, q_bias, k_bias,
+    spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, (q_weight, k_weight, q_bias, k_bias),
                                           norm, eps, lens)
-    given = ((q, dq, H), (k, dk, Hkv), (v, dv, Hkv))
     if out is None:
-        heads = [n if t is not None else 0 for t, _, n in given]
+        heads = [n if t is not None else 0 for t, n in ((q, H), (k, Hkv), (v, Hkv))]
         out = torch.empty((B, S, sum(heads), d), dtype=torch.bfloat16, device=device).split(heads, 2)
-    rows, grads, outs = [None, None, None], [None, None, None], [None, None, None]
-    for i, (t, g, n) in enumerate(given):
+    rows, grads, to, outs = [None, None, None], [None, None, None], [None, None, None], [None, None, None]
+    for i, (t, g) in enumerate(((q, dq), (k, dk), (v, dv))):
         if (t is None) != (g is None):
             raise ValueError(f"{'qkv'[i]} and d{'qkv'[i]} go together")
         if t is None:
             continue
-        shape = (B, S, n, d)
-        rows[i] = _rows(t, "qkv"[i], shape, device)
+        n = Hkv if i else H
+        rows[i] = _rows(t, "qkv"[i], B, S, n, d, device)
         _want(g, ("dq", "dk", "dv")[i], (B, n, S, d), torch.bfloat16, device)
         grads[i] = g.data_ptr()
-        outs[i] = _rows(out[i], "out", shape, device)
-    sums = [None if w is None or t is None else w.new_empty(d)
-            for t, w in ((q, q_weight), (k, k_weight), (q, q_bias), (k, k_bias))]
+        outs[i] = out[i]
+        to[i] = _rows(out[i], "out", B, S, n, d, device)
+    sums, at = [None, None, None, None], [None, None, None, None]
+    for i, w in enumerate((q_weight, k_weight, q_bias, k_bias)):
+        if w is not None and (k if i % 2 else q) is not None:
+            sums[i] = torch.empty_like(w)
+            at[i] = sums[i].data_ptr()
+    n = 0 if norm is None else _grad_workspace(B, S, H, Hkv, d)
     with _on(device):
-        n = head_rope_bwd_workspace(spec) if norm is not None else 0
-        head_rope_bwd(spec, rows[0], rows[1], *grads, *outs, *sums, _workspace(n, device), n, _current(device))
-    return (*(None if t is None else o for o, t in zip(out, (q, k, v))), *sums)
+        workspace = _workspace(n, device)
+        _check(lib.head_rope_bwd(spec, rows[0], rows[1], *grads, *to, *at, workspace.data_ptr() if n else None, n,
+                                 _current(device)), "head_rope_bwd")
+    return (*outs, *sums)
