@@ -216,20 +216,20 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
-int check_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
+int check_cache(int B, int H, int Hkv, int N, int d, int max_pages, int segment) {
   if (B < 1 || H < 1 || Hkv < 1 || N < 1 || max_pages < 1)
     return fail(TA_ERR_BAD_SHAPE, "B, H, Hkv, N and max_pages must be >= 1");
   if (H % Hkv) return fail(TA_ERR_BAD_SHAPE, "H must be a multiple of Hkv");
   if (max_pages > INT_MAX / TA_BLOCK) return fail(TA_ERR_BAD_SHAPE, "max_pages pages hold more than 2^31 - 1 tokens");
   // The sequences times heads are a grid dimension of their own.
-  if ((int64_t)B * Hkv * (max_pages + std::max(kCacheSegment, kCache4Segment)) > INT_MAX)
+  if ((int64_t)B * Hkv * (max_pages + segment) > INT_MAX)
     return fail(TA_ERR_BAD_SHAPE, "B * Hkv * max_pages exceeds 2^31 - 1");
   if ((int64_t)B * Hkv > 65535) return fail(TA_ERR_BAD_SHAPE, "B * Hkv exceeds the grid limit");
   return check_dim(d);
 }
 // Attention: so are the passes over its rows and the joins of 8 of them.
-int check_cache_attn(int B, int H, int Hkv, int N, int d, int max_pages) {
-  if (int st = check_cache(B, H, Hkv, N, d, max_pages)) return st;
+int check_cache_attn(int B, int H, int Hkv, int N, int d, int max_pages, int segment) {
+  if (int st = check_cache(B, H, Hkv, N, d, max_pages, segment)) return st;
   return (int64_t)(H / Hkv) * N <= 8 * 65535 ? TA_OK : fail(TA_ERR_BAD_SHAPE, "H / Hkv * N exceeds the grid limit");
 }
 
@@ -397,7 +397,7 @@ int cache_attn_write(const void* k, const void* v, void* k_pages, void* v_pages,
                      int max_pages, int n_pages, void* stream) {
   if (!k || !v || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens)
     return fail(TA_ERR_NULL_PTR, "k, v, the pages, the scales, table and lens must be non-NULL");
-  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages, kCacheSegment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (int st = check_aligned({k, v, k_pages, v_pages}, 16, "k, v and the pages must be 16-byte aligned")) return st;
   if (int st = check_aligned({k_scales, v_scales, table, lens, n_new}, 4,
@@ -420,7 +420,7 @@ int cache_attn_write(const void* k, const void* v, void* k_pages, void* v_pages,
 
 int cache_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes) {
   if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
-  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages, kCacheSegment)) return st;
   *bytes = plan_cache(B, H, Hkv, N, d, max_pages).bytes;
   clear_error();
   return TA_OK;
@@ -432,7 +432,7 @@ int cache_attn_fwd(const void* q, const void* k_pages, const void* v_pages, cons
                    void* workspace, size_t workspace_bytes, void* stream) {
   if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || !out)
     return fail(TA_ERR_NULL_PTR, "q, the pages, the scales, table, lens and out must be non-NULL");
-  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages, kCacheSegment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (!std::isfinite(scale)) return fail(TA_ERR_BAD_SCALE, "scale must be finite");
   if (int st = check_aligned({q, k_pages, v_pages, out}, 16, "q, out and the pages must be 16-byte aligned")) return st;
@@ -484,7 +484,7 @@ int cache4_attn_write(const void* k, const void* v, void* k_pages, void* v_pages
                       int B, int Hkv, int N, int d, int max_pages, int n_pages, void* stream) {
   if (!k || !v || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens)
     return fail(TA_ERR_NULL_PTR, "k, v, the pages, the scales, table and lens must be non-NULL");
-  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages, kCache4Segment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (int st = check_aligned({k, v, k_pages, v_pages, k_scales, v_scales, k_held, v_held}, 16,
                              "k, v, their held values, the pages and the scales must be 16-byte aligned"))
@@ -513,7 +513,7 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
                      int max_pages, int n_pages, int first, void* stream) {
   if (!k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || (!k_out && !v_out))
     return fail(TA_ERR_NULL_PTR, "the pages, the scales, table, lens and k_out or v_out must be non-NULL");
-  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages, kCache4Segment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (first < 0 || (int64_t)first + N > INT_MAX) return fail(TA_ERR_BAD_SHAPE, "first must be >= 0, first + N below 2^31");
   if (int st = check_aligned({k_pages, v_pages, k_scales, v_scales, k_out, v_out}, 16,
@@ -539,7 +539,7 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
 
 int cache4_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes) {
   if (!bytes) return fail(TA_ERR_NULL_PTR, "bytes must be non-NULL");
-  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages, kCache4Segment)) return st;
   *bytes = plan_cache4(B, H, Hkv, N, d, max_pages).bytes;
   clear_error();
   return TA_OK;
@@ -551,7 +551,7 @@ int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, con
                     void* workspace, size_t workspace_bytes, void* stream) {
   if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !table || !lens || !out)
     return fail(TA_ERR_NULL_PTR, "q, the pages, the scales, table, lens and out must be non-NULL");
-  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages)) return st;
+  if (int st = check_cache_attn(B, H, Hkv, N, d, max_pages, kCache4Segment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
   if (!std::isfinite(scale)) return fail(TA_ERR_BAD_SCALE, "scale must be finite");
   if (int st = check_aligned({q, k_pages, v_pages, k_scales, v_scales, out}, 16,

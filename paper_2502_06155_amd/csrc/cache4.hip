@@ -593,6 +593,16 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
             for (int rb = 0; rb < RB; ++rb)
               s[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i], 0, 0, 0);
           }
+        // Four K pieces are on their way from LDS while RB products use one (one sequence of 32768, 2048 rows: 315 us, 329
+        // as the compiler orders them).
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int x = 0; x < 4 * kSl - 4; ++x) {
+          __builtin_amdgcn_sched_group_barrier(0x008, RB, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4 * RB, 0);
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 pf[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {

@@ -3,7 +3,9 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <initializer_list>
 #include <string>
+#include <vector>
 
 #include "head_rope.h"
 #include "host_checks.h"
@@ -106,21 +108,25 @@ int check_rows(const RopeArgs& a, const ta_rows& r, int heads, const char* what,
   return TA_OK;
 }
 
-// No value of written rows stands for two rows: along each axis (of more than one place) a step is at least
-// as long as everything inside it.
-bool one_place_each(const RopeArgs& a, const ta_rows& r, int heads) {
-  struct Axis {
-    int64_t step;
-    int n;
-  } axes[3] = {{r.batch, a.B}, {r.token, a.S}, {r.head, heads}};
-  std::sort(axes, axes + 3, [](const Axis& x, const Axis& y) { return x.step < y.step; });
-  int64_t inside = a.d;
+// Whether places at these steps (of n each) hold pieces of `inside` values apart: in order of the steps, each is at
+// least as long as all that lies inside it.
+struct Axis {
+  int64_t step;
+  int n;
+};
+bool pieces_apart(std::initializer_list<Axis> in, int64_t inside) {
+  std::vector<Axis> axes(in);
+  std::sort(axes.begin(), axes.end(), [](const Axis& x, const Axis& y) { return x.step < y.step; });
   for (const Axis& x : axes) {
     if (x.n == 1) continue;
     if (x.step < inside) return false;
-    inside = (x.n - 1) * x.step + inside;
+    inside += (x.n - 1) * x.step;
   }
   return true;
+}
+// No value of written rows stands for two rows.
+bool one_place_each(const RopeArgs& a, const ta_rows& r, int heads) {
+  return pieces_apart({{r.batch, a.B}, {r.token, a.S}, {r.head, heads}}, a.d);
 }
 
 // Whether two written tensors share no value: their extents are apart, or they stand in one tensor, heads behind
@@ -130,16 +136,11 @@ bool apart(const RopeArgs& a, const ta_rows& p, int np, const ta_rows& q, int nq
   const bool first = reinterpret_cast<uintptr_t>(p.data) <= reinterpret_cast<uintptr_t>(q.data);
   const ta_rows& lo = first ? p : q;
   const ta_rows& hi = first ? q : p;
-  const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(hi.data) - reinterpret_cast<uintptr_t>(lo.data));
-  if (off % 2 || (a.B > 1 && lo.batch != hi.batch) || (a.S > 1 && lo.token != hi.token)) return false;
-  // Both as rows of `heads` pieces at the same steps: apart if lo's piece ends before hi's starts and hi's ends
-  // before lo's next one, of the next token or sequence, starts.
+  const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(hi.data) - reinterpret_cast<uintptr_t>(lo.data)) / 2;
+  if ((a.B > 1 && lo.batch != hi.batch) || (a.S > 1 && lo.token != hi.token)) return false;
+  // A token's heads of lo, then those of hi, are one piece, and pieces do not meet.
   const int64_t lo_piece = ((first ? np : nq) - 1) * lo.head + a.d, hi_piece = ((first ? nq : np) - 1) * hi.head + a.d;
-  const int64_t both = off / 2 + hi_piece;
-  if (off / 2 < lo_piece) return false;
-  if (a.S > 1 && lo.token < both) return false;
-  if (a.B > 1 && lo.batch < (a.S - 1) * lo.token + both) return false;
-  return true;
+  return off >= lo_piece && pieces_apart({{lo.batch, a.B}, {lo.token, a.S}}, off + hi_piece);
 }
 
 Rows to_rows(const ta_rows& r) {

@@ -442,6 +442,27 @@ def test_a_long_prompt_written_at_once():
         assert (off <= top * (2 / 7)).all()  # at most 2^e, and the largest is above 3.5 * 2^e
 
 
+def test_the_functions_of_the_c_abi():
+    rng = np.random.default_rng(4)
+    cache, table = held(rng, 2, 2, 96, [5000, 300], spare=3)
+    gpu, t, lens = to_gpu(cache), i32(table), i32([5000, 299])
+    k, v, q = (to_dev(bits(rng, 2, h, 1, 96)) for h in (2, 2, 6))
+    pages, width, stream = len(cache[0]), table.shape[1], torch.cuda.current_stream()
+    mine = [x.clone() for x in gpu]
+    want = ta.cache4_write(k, v, *mine, t, i32([-5, 299]), return_held=True)
+    got = [torch.empty_like(k), torch.empty_like(k)]
+    ta.cache4_attn_write(k, v, *gpu, t, i32([-5, 299]), None, *got, 2, 2, 1, 96, width, pages, stream)
+    assert all(torch.equal(a, b) for a, b in zip((*mine, *want), (*gpu, *got)))
+    ta.cache4_attn_read(*gpu, t, lens + 1, None, got[1], 2, 2, 1, 96, width, pages, 299, stream)
+    assert torch.equal(got[1], ta.cache4_read(*gpu, t, lens + 1, 1, first=299)[1])
+    out, lse = torch.empty_like(q), torch.empty(2, 6, 1, device="cuda")
+    n = ta.cache4_attn_fwd_workspace(2, 6, 2, 1, 96, width)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")  # (NaN)
+    ta.cache4_attn_fwd(q, *gpu, t, lens, False, out, lse, 2, 6, 2, 1, 96, width, pages, 0.1, ws, n, stream)
+    a, b = ta.cache4_attn(q, *gpu, t, lens, 0.1, return_lse=True)
+    assert n > 0 and torch.equal(a, out) and torch.equal(b, lse)
+
+
 def test_wrappers_refuse():
     rng = np.random.default_rng(1)
     cache, table = held(rng, 1, 2, 64, [200])

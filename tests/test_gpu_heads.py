@@ -218,6 +218,11 @@ def test_layouts_of_memory():
     for view in views:
         view.fill_(7.0)
     assert (wide == 7.0).all()
+    first = torch.empty(21, 3, 8, 96, dtype=torch.bfloat16, device="cuda").transpose(0, 1)  # tokens before sequences
+    first.copy_(x)
+    into = torch.zeros(21, 3, 8, 96, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    ta.head_rope_grad(*c.parts(first), *dy, out=c.parts(into), **c.args())
+    assert torch.equal(into, torch.cat(grads[:3], 2))
     one = x[:1, :, :1].expand(3, 21, 4, 96)
     a, b = (ta.head_rope(t, None, None, **{**c.args(), "k_weight": None})[0] for t in (one, one.contiguous()))
     assert torch.equal(a, b)
@@ -344,6 +349,28 @@ def test_on_another_stream_and_under_any_workspace_contents():
     s.synchronize()
     for a, b in zip(want, got):
         assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+
+
+def test_the_functions_of_the_c_abi():
+    c = Case(2, 30, 4, 2, 64, "layer", "split", (32, 16), lens=[30, 8])
+    x, dy, args = to_dev(c.x), [to_dev(g) for g in c.dy], c.args()
+    want = (*ta.head_rope(*c.parts(x), **args), *ta.head_rope_grad(*c.parts(x), *dy, **args))
+    w = {n: args[n].data_ptr() for n in WEIGHTS}
+    spec = ta.HeadRopeSpec(B=2, S=30, H=4, Hkv=2, d=64, norm=2, eps=1e-6, layout=3, axes=2, dims=(32, 16, 0, 0),
+                           freqs=args["freqs"].data_ptr(), positions=args["positions"].data_ptr(), positions_batch=0,
+                           lens=args["lens"].data_ptr(), **w)
+    row = lambda t, h: ta.Rows(t.data_ptr() + 2 * 64 * h, 30 * 8 * 64, 8 * 64, 64)  # noqa: E731
+    outs = [torch.empty_like(g) for g in dy]
+    stream = torch.cuda.current_stream()
+    ta.head_rope_fwd(spec, row(x, 0), row(x, 4), row(x, 6), *outs, stream)
+    dx, sums = torch.empty_like(x), [torch.empty(64, device="cuda") for _ in range(4)]
+    n = ta.head_rope_bwd_workspace(spec)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    ta.head_rope_bwd(spec, row(x, 0), row(x, 4), *dy, row(dx, 0), row(dx, 4), row(dx, 6), *sums, ws, n, stream)
+    for a, b in zip(want, (*outs, *c.parts(dx), *sums)):
+        assert torch.equal(a, b)
+    with pytest.raises(ta.TileAttnError, match="workspace"):
+        ta.head_rope_bwd(spec, row(x, 0), row(x, 4), *dy, row(dx, 0), row(dx, 4), row(dx, 6), *sums, ws, n - 1, stream)
 
 
 def test_wrappers_refuse():
