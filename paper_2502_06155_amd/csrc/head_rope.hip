@@ -21,6 +21,7 @@ constexpr int kNone = 0, kRms = 1, kLayer = 2;  // norms
 constexpr int kStill = 0, kNext = 1, kWhole = 2, kAny = 3;
 
 typedef float Floats8[8];
+constexpr double kTurn = 0.15915494309189533577;  // 1 / 2 pi
 
 template <int D>
 struct Shape {
@@ -56,36 +57,37 @@ __device__ __forceinline__ u32x4 narrow(const Floats8& x) {
   return __builtin_bit_cast(u32x4, __builtin_convertvector(y, bf16x8));
 }
 
-// What value e of a head is in the rotation: its partner, its pair (-1: it is not turned), the pair's axis,
-// and whether it is the pair's second value.
+// What value e of a head is in the rotation: its partner, its pair and the pair's axis, whether it is turned at all
+// and the pair's second value. Without branches (unused axes start behind every value): a lane asks for up to 8
+// values, and what it then loads should not wait for one another.
 struct Place {
   int partner, pair, axis;
-  bool second;
+  bool turned, second;
 };
 __device__ __forceinline__ Place place_of(const RopeArgs& a, int e) {
-  if (e >= a.turned) return {e, -1, 0, false};
-  int axis = 0;
-  if (a.layout == 3) {  // split
-    const int h = a.turned / 2;
-    const bool second = e >= h;
-    const int pair = second ? e - h : e;
+  const bool split = a.layout == 3, interleaved = a.layout == 1;
+  const int h = a.turned / 2;
+  const int at = split ? 2 * (e >= h ? e - h : e) : e;  // decides the axis
+  int axis = 0, start = 0, n = a.dims[0];
 #pragma unroll
-    for (int x = 1; x < kRopeAxes; ++x)
-      if (x < a.axes && 2 * pair >= a.start[x]) axis = x;
-    return {second ? e - h : e + h, pair, axis, second};
+  for (int x = 1; x < kRopeAxes; ++x) {
+    const bool past = at >= a.start[x];
+    axis = past ? x : axis;
+    start = past ? a.start[x] : start;
+    n = past ? a.dims[x] : n;
   }
-  int start = 0, n = a.dims[0];
-#pragma unroll
-  for (int x = 1; x < kRopeAxes; ++x)
-    if (x < a.axes && e >= a.start[x]) {
-      axis = x;
-      start = a.start[x];
-      n = a.dims[x];
-    }
-  if (a.layout == 1) return {e ^ 1, e / 2, axis, (e & 1) != 0};  // interleaved; axes start at even values
-  const int o = e - start;
-  const bool second = o >= n / 2;
-  return {second ? e - n / 2 : e + n / 2, start / 2 + (second ? o - n / 2 : o), axis, second};
+  const int half = split ? h : n / 2, o = split ? e : e - start;
+  Place p;
+  p.second = interleaved ? (e & 1) != 0 : o >= half;
+  p.partner = interleaved ? e ^ 1 : p.second ? e - half : e + half;  // (axes start at even values)
+  p.pair = interleaved ? e / 2 : (split ? 0 : start / 2) + (p.second ? o - half : o);
+  p.axis = axis;
+  p.turned = e < a.turned;
+  if (!p.turned) {
+    p.partner = e;
+    p.pair = 0;
+  }
+  return p;
 }
 
 // The lane's 8 values in the rotation. Angles: turns = position * (frequency / 2 pi) in fp64, right to 2^-53 of the
@@ -95,23 +97,36 @@ template <int D, int ROT>
 struct Turns {
   static constexpr int kAngles = ROT == kNext ? 4 : 8;
   double f[ROT == kStill ? 1 : kAngles];
-  int axis[ROT == kStill ? 1 : kAngles];
+  int axis[ROT == kStill ? 1 : ROT == kWhole ? 1 : kAngles];
   int from[ROT == kAny ? 8 : 1];  // byte of the partner in its row, or the lane that holds all eight
-  float sign[ROT == kStill || ROT == kNext ? 1 : 8];
+  float sign[ROT == kAny ? 8 : 1];
 
   __device__ __forceinline__ void place(const RopeArgs& a, int l) {
-    if constexpr (ROT != kStill) {
+    if constexpr (ROT == kWhole) {
+      // Eight values of one axis and half, their pairs one after the other. (A lane behind the row takes
+      // nothing from it: sums over the row's lanes add it too.)
+      const Place p = place_of(a, min(8 * l, D - 8));
+      from[0] = p.partner / 8;
+      axis[0] = p.axis;
+      sign[0] = 8 * l >= D ? 0.f : p.second ? 1.f : -1.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double x = a.freqs[p.turned ? p.pair + i : 0];
+        f[i] = p.turned ? x * kTurn : 0.;
+      }
+    } else if constexpr (ROT != kStill) {
+      Place p[kAngles];
+#pragma unroll
+      for (int i = 0; i < kAngles; ++i) p[i] = place_of(a, min(8 * l + (ROT == kNext ? 2 * i : i), D - 1));
 #pragma unroll
       for (int i = 0; i < kAngles; ++i) {
-        const Place p = place_of(a, min(8 * l + (ROT == kNext ? 2 * i : i), D - 1));
-        f[i] = p.pair >= 0 ? a.freqs[p.pair] * 0.15915494309189533577 : 0.;
-        axis[i] = p.axis;
-        if constexpr (ROT == kAny) from[i] = 2 * p.partner;
-        if constexpr (ROT == kWhole) {
-          if (i == 0) from[0] = p.partner / 8;
+        const double x = a.freqs[p[i].pair];
+        f[i] = p[i].turned ? x * kTurn : 0.;
+        axis[i] = p[i].axis;
+        if constexpr (ROT == kAny) {
+          from[i] = 2 * p[i].partner;
+          sign[i] = 8 * l >= D ? 0.f : p[i].second ? 1.f : -1.f;
         }
-        // (A lane behind the row takes nothing from it: sums over the row's lanes add it too.)
-        if constexpr (ROT != kNext) sign[i] = 8 * l >= D ? 0.f : p.second ? 1.f : -1.f;
       }
     }
   }
@@ -121,12 +136,13 @@ struct Turns {
       const int32_t* p = a.positions + b * a.positions_batch + (int64_t)t * a.axes;
       int pos[kRopeAxes];
 #pragma unroll
-      for (int x = 0; x < kRopeAxes; ++x) pos[x] = x < a.axes ? p[x] : 0;
+      for (int x = 0; x < kRopeAxes; ++x) pos[x] = p[min(x, a.axes - 1)];
 #pragma unroll
       for (int i = 0; i < kAngles; ++i) {
+        const int of = axis[ROT == kWhole ? 0 : i];
         int at = pos[0];
 #pragma unroll
-        for (int x = 1; x < kRopeAxes; ++x) at = axis[i] == x ? pos[x] : at;
+        for (int x = 1; x < kRopeAxes; ++x) at = of == x ? pos[x] : at;
         const double turns = (double)at * f[i];
         const float part = (float)(turns - __builtin_rint(turns));
         const float cs = __builtin_amdgcn_cosf(part), sn = __builtin_amdgcn_sinf(part);
@@ -136,7 +152,7 @@ struct Turns {
           s[2 * i + 1] = sn;
         } else {
           c[i] = cs;
-          s[i] = sign[i] * sn;
+          s[i] = sign[ROT == kWhole ? 0 : i] * sn;
         }
       }
     } else {
@@ -223,6 +239,7 @@ struct Token {
   int b, t;
   bool have;   // there is such a token
   bool valid;  // and it is no padding
+  bool any;    // so is that of some lane of the wave
   __device__ __forceinline__ Token(const RopeArgs& a, int64_t i) {
     const int64_t total = (int64_t)a.B * a.S;
     have = i < total;
@@ -230,6 +247,7 @@ struct Token {
     b = (int)(n / (uint32_t)a.S);
     t = (int)(n - (uint32_t)b * (uint32_t)a.S);
     valid = have && t < (a.lens ? a.lens[b] : a.S);
+    any = __builtin_amdgcn_ballot_w64(valid) != 0;
   }
 };
 
@@ -245,7 +263,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
   const int64_t token0 = ((int64_t)blockIdx.x * kRopeWaves + wave) * kTokens;
   if (token0 >= (int64_t)a.B * a.S) return;
   const Token tok(a, token0 + lane / L);
-  const bool reads = tok.valid && in_row, writes = tok.have && in_row;
+  const bool writes = tok.have && in_row;
+  const int at = in_row ? 8 * l : D - 8;  // lanes behind a row read its last values, as zeros
   u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * 64 : 0);
 
   // Heads of q, k and v in a line; this wave's are first .. last - 1. A step takes up to kAhead heads of one kind,
@@ -257,43 +276,53 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
   auto stop = [&](int f) { return min(min(f + kAhead, last), f < k0 ? k0 : f < v0 ? v0 : all); };
   auto load = [&](int f, u32x4 (&in)[kAhead]) {
     const int kind = kind_of(f), h = f - start_of(kind), n = stop(f) - f;
-    const Rows& x = a.x[kind];
-    const uint16_t* x0 = x.p + tok.b * x.batch + tok.t * x.token + 8 * l;
+    const Rows x = a.x[kind];
+    const uint16_t* x0 = x.p + tok.b * x.batch + tok.t * x.token + h * x.head + at;
+    if (tok.any) {  // (all of a step's loads without a branch between them: the last row again where there are fewer)
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      in[u] = u32x4{0u, 0u, 0u, 0u};
-      if (u < n && reads) in[u] = load16(x0 + (h + u) * x.head);
+      for (int u = 0; u < kAhead; ++u) in[u] = load16(x0 + min(u, n - 1) * x.head);
     }
+    const bool reads = tok.valid && in_row;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) in[u] = reads ? in[u] : u32x4{0u, 0u, 0u, 0u};
   };
   u32x4 in[kAhead], next[kAhead];
   load(first, in);
 
   Turns<D, ROT> turns;
   turns.place(a, l);
+  // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean; A, B and C of the kind `ready`, its weights and
+  // biases times the token's cosines and sines.
+  Floats8 A, Bp, C, w, wp, bs, bp;
+  auto weights = [&](int kind) {
+    const float* weight = NORM == kNone ? nullptr : a.weight[kind];
+    const float* bias = NORM == kLayer ? a.bias[kind] : nullptr;
+    load8<D>(weight, l, 1.f, w);
+    load_partners<D, ROT>(weight, l, 1.f, turns, wp);
+    load8<D>(bias, l, 0.f, bs);
+    load_partners<D, ROT>(bias, l, 0.f, turns, bp);
+  };
+  int ready = kind_of(first);
+  if (ready < 2) weights(ready);
   Floats8 c, s;
   turns.at(a, tok.b, tok.t, c, s);
-  // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean
-  Floats8 A, Bp, C;
-  int ready = -1;  // the kind whose factors these are
+  auto factors = [&]() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      A[e] = w[e] * c[e];
+      Bp[e] = wp[e] * s[e];
+      C[e] = NORM == kLayer ? fmaf(bs[e], c[e], bp[e] * s[e]) : 0.f;
+    }
+  };
+  if (ready < 2) factors();
   const int64_t plane = (int64_t)a.S * D;
   for (int f = first; f < last;) {
     const int f1 = stop(f), kind = kind_of(f);
     if (f1 < last) load(f1, next);
     if (kind < 2 && kind != ready) {
       ready = kind;
-      const float* weight = NORM == kNone ? nullptr : a.weight[kind];
-      const float* bias = NORM == kLayer ? a.bias[kind] : nullptr;
-      Floats8 w, wp, bs, bp;
-      load8<D>(weight, l, 1.f, w);
-      load_partners<D, ROT>(weight, l, 1.f, turns, wp);
-      load8<D>(bias, l, 0.f, bs);
-      load_partners<D, ROT>(bias, l, 0.f, turns, bp);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        A[e] = w[e] * c[e];
-        Bp[e] = wp[e] * s[e];
-        C[e] = NORM == kLayer ? fmaf(bs[e], c[e], bp[e] * s[e]) : 0.f;
-      }
+      weights(kind);
+      factors();
     }
     uint16_t* y0 = a.y[kind] + (((int64_t)tok.b * a.heads[kind] + (f - start_of(kind))) * a.S + tok.t) * D + 8 * l;
 #pragma unroll
@@ -346,6 +375,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
   const int64_t items = (int64_t)groups * parts, plane = (int64_t)a.S * D;
   const bool normed = NORM != kNone && kind < 2, turned = ROT != kStill && kind < 2;
   u32x4* rows = s_rows + (ROT >= kWhole ? wave * 64 : 0);
+  const int at = 8 * l;
+  const Rows x = a.x[kind], dx = a.dx[kind];
 
   Turns<D, ROT> turns;
   Floats8 w, dw, db;
@@ -360,14 +391,14 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
     const Token tok(a, (item - (int64_t)part * groups) * kTokens + lane / L);
     const bool reads = tok.valid && in_row, writes = tok.have && in_row;
     const int h0 = part * a.heads_per, h1 = min(h0 + a.heads_per, heads);
-    const uint16_t* g0 = a.y[kind] + ((int64_t)tok.b * heads * a.S + tok.t) * D + 8 * l;
-    const uint16_t* x0 = a.x[kind].p + tok.b * a.x[kind].batch + tok.t * a.x[kind].token + 8 * l;
-    uint16_t* d0 = a.dx[kind].p + tok.b * a.dx[kind].batch + tok.t * a.dx[kind].token + 8 * l;
+    const uint16_t* g0 = a.y[kind] + ((int64_t)tok.b * heads * a.S + tok.t) * D + at;
+    const uint16_t* x0 = x.p + tok.b * x.batch + tok.t * x.token + at;
+    uint16_t* d0 = dx.p + tok.b * dx.batch + tok.t * dx.token + at;
     u32x4 xin = {0u, 0u, 0u, 0u}, gin = {0u, 0u, 0u, 0u};
-    auto load = [&](int h, u32x4& x, u32x4& g) {
+    auto load = [&](int h, u32x4& xr, u32x4& g) {
       if (reads) {
         g = load16(g0 + h * plane);
-        if (normed) x = load16(x0 + h * a.x[kind].head);
+        if (normed) xr = load16(x0 + h * x.head);
       }
     };
     load(h0, xin, gin);
@@ -413,7 +444,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
         out = narrow(g);
         if (!tok.valid) out = u32x4{0u, 0u, 0u, 0u};
       }
-      if (writes) *reinterpret_cast<u32x4*>(d0 + h * a.dx[kind].head) = out;
+      if (writes) *reinterpret_cast<u32x4*>(d0 + h * dx.head) = out;
       if (h + 1 < h1) load(h + 1, xin, gin);
     }
   }

@@ -44,7 +44,10 @@ int from_spec(const head_rope_spec* spec, RopeArgs& a) {
   a.freqs = nullptr;
   a.positions = nullptr;
   a.positions_batch = 0;
-  for (int x = 0; x < kRopeAxes; ++x) a.dims[x] = a.start[x] = 0;
+  for (int x = 0; x < kRopeAxes; ++x) {
+    a.dims[x] = 0;
+    a.start[x] = INT32_MAX;  // behind every value
+  }
   if (s.layout != TA_ROPE_NONE) {
     if (s.axes < 1 || s.axes > TA_ROPE_AXES) return fail(TA_ERR_BAD_SHAPE, "axes must be in 1..TA_ROPE_AXES");
     a.axes = s.axes;

@@ -19,7 +19,7 @@ struct Rows {
 struct RopeArgs {
   int B, S, d, norm, layout, axes;
   int dims[kRopeAxes];
-  int start[kRopeAxes];  // first value of each axis
+  int start[kRopeAxes];  // first value of each axis; of those that are none, behind every value
   int turned;            // values that are turned: the sum of dims
   bool whole;            // partners of 8 values in a row, from a multiple of 8 on, are 8 such values again
   float eps;
