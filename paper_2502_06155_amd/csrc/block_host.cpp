@@ -158,7 +158,7 @@ bool whole_segments(int64_t segments, int d, int max_pages) {
 constexpr int64_t kPassSlots = 2 * kSlots;
 struct CachePlan {
   int workers, passes, rows;
-  bool whole;
+  bool whole, eight;
   size_t bytes;
 };
 CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
@@ -171,6 +171,7 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
                                       p.passes < kPassSlots ? std::max<int64_t>(2, kPassSlots / p.passes) : 1,
                                       (int64_t)B * Hkv * (max_pages + kCacheSegment)});
   p.whole = whole_segments((int64_t)B * Hkv, d, max_pages);
+  p.eight = false;
   if (p.whole) p.workers = B * Hkv;
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
@@ -181,12 +182,14 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
 // costs `part` us, written and read, so that with P pages sqrt(P page / part) of them are the best (64 segments
 // of 4 pages, 120 rows: 35.9 us with 512, 27.8 with 165), but for few pages, which a workgroup each takes (8 segments of
 // 8 pages: 16.5 us with 104, 18.9 with 82).
-// Short tables run a workgroup per segment, in one launch. Alone, a segment takes 5 us and, of 16 rows, 0.22 +
-// 0.003 d us a page; shared, all take 10 us and the bytes' time, d * 1.4e-5 us a page and segment if sequences fill half
-// of their tables, or the pages and parts of the workgroups. Up to 24 pages, so that a batch's longest sequence costs
-// 14 us at most. Measured, alone and shared, one row: 8 segments of 8 pages at d = 128 9.3 and 10.1 us, of 12 11.8 and 10.5; at
-// d = 64 of 12 9.7 and 9.9, of 16 11.4 and 9.7; 128 of 16, d = 128 16.8 and 19.2; 256 of 24 24.8 and 28.8; 36 rows, 8 of 2
-// 9.0 and 10.5, of 4 14.1 and 10.7; 120 rows, 256 of 8 40.7 and 52.1.
+// Short tables run a workgroup per segment, in one launch; of eight waves, in passes of 16 rows, where there are more than four
+// pages and no more segments than compute units. Alone, a segment takes 5 us and, of 16 rows, 0.22 + 0.002 d us a page
+// (0.003 d with four waves); shared, all take 10 us and the bytes' time, d * 1.4e-5 us a page and segment if sequences
+// fill half of their tables, or the pages and parts of the workgroups. Up to 24 pages, so that a batch's longest sequence
+// costs 14 us at most. Measured, eight waves alone, four alone, and shared, one row: 8 segments of 8 pages at d = 128 8.9, 9.3 and 10.3
+// us, of 16 12.7, 14.2 and 10.6; at d = 64 of 12 9.0, 9.7 and 9.7; 64 of 12, d = 128 10.9, 12.5 and 13.3; 128 of 16 14.5, 16.9 and
+// 19.7; 256 of 24 22.4, 24.7 and 28.6. Alone and shared, 36 rows: 8 of 2 9.0 and 10.5, of 4 14.1 and 10.7; 120 rows, 256 of 8 40.7
+// and 52.1.
 struct ManyRows {
   double page, part;
 };
@@ -198,6 +201,7 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.passes = (int)((rows + p.rows - 1) / p.rows);
   const int64_t slots = p.rows == 32 ? kSlots / 2 : kSlots;
   int64_t workers = p.passes < slots ? slots / p.passes : 1;
+  const bool eight = p.rows == 16 && max_pages > 4 && segments <= kSlots / 2;
   double alone, shared;
   if (p.rows > 32) {
     const ManyRows m = many_rows(p.rows);
@@ -206,12 +210,13 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
     alone = m.page * max_pages;
     shared = 2 * std::sqrt(pages * m.page * m.part);
   } else {
-    alone = (0.22 + 0.003 * d) * max_pages;
+    alone = (0.22 + (eight ? 0.002 : 0.003) * d) * max_pages;
     shared = 1.4e-5 * d * (double)segments * max_pages;
   }
   if (p.passes < slots) workers = std::max<int64_t>(2, workers);
   p.workers = (int)std::min(workers, segments * (max_pages + kCache4Segment));
   p.whole = max_pages <= 24 && alone <= 5 + shared;
+  p.eight = p.whole && eight;
   if (p.whole) p.workers = (int)segments;
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
@@ -594,6 +599,7 @@ int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, con
   a.n_pages = n_pages;
   fold_scale(scale, a.c, a.q_flip, a.q_keep);
   a.whole = p.whole;
+  a.eight = p.eight;
   a.workers = p.workers;
   a.row_blocks = p.passes;
   a.part = static_cast<float*>(workspace);

@@ -152,6 +152,7 @@ struct Cache4AttnArgs : CacheAttnArgs {
   const uint8_t* k_exps;
   const uint8_t* v_exps;
   uint32_t q_flip, q_keep;
+  bool eight;  // eight waves a workgroup, one workgroup a compute unit
 };
 
 hipError_t launch_block_means(const MeansArgs& a, hipStream_t stream);

@@ -263,12 +263,13 @@ struct Value4 {
 // Byte i of two words as a scale.
 __device__ __forceinline__ float scale_at(u32x2 w, int i) { return scale_of(w[i / 4] >> (8 * (i % 4)) & 0xffu); }
 
+// Waves a SIMD unit: at 16 rows 256 registers a lane are enough, at 32 rows it takes 512.
 template <int RB>
-constexpr int cache4_wgs() { return RB == 1 ? 2 : 1; }
+constexpr int cache4_waves() { return RB == 1 ? 2 : 1; }
 
-template <int D, int RB>
-__global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kernel(const Cache4AttnArgs a) {
-  constexpr int kRows = 16 * RB, kWaves = kThreadsC / 64, kSl = D / 32;
+template <int D, int RB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_kernel(const Cache4AttnArgs a) {
+  constexpr int kRows = 16 * RB, kWaves = WAVES, kSl = D / 32;
   constexpr int kCh = D == 64 ? 4 : 8;  // channels of a lane, and O^T instructions of a step
   __shared__ float s_o[kWaves][kRows][D + 4];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(kThreadsC, cache4_wgs<RB>()) void cache4_attn_kerne
       }
     }
     __syncthreads();
-    join_waves<D, kRows>(a, s_o, s_m, s_l, seg.q_row, row0, rows, seg.alone, seg.slot);
+    join_waves<D>(a, s_o, s_m, s_l, seg.q_row, row0, rows, seg.alone, seg.slot);
     __syncthreads();
   } while (walk.advance(a));
 }
@@ -687,8 +688,12 @@ constexpr int kMergeSlices = 8;
 template <int D, int ROWS>
 hipError_t cache4_attn_rows(const Cache4AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
-  if constexpr (ROWS <= 32) cache4_attn_kernel<D, ROWS / 16><<<grid, kThreadsC, 0, s>>>(a);
-  else cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsC, 0, s>>>(a);
+  if constexpr (ROWS > 32) {
+    cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsC, 0, s>>>(a);
+  } else {
+    if (ROWS == 16 && a.eight) cache4_attn_kernel<D, 1, 8><<<grid, 512, 0, s>>>(a);
+    else cache4_attn_kernel<D, ROWS / 16, 4><<<grid, kThreadsC, 0, s>>>(a);
+  }
   if (a.whole) return hipGetLastError();
   const int segments = a.B * a.Hkv, rows = a.G * a.N;
   auto segs = [&](int per) { return dim3((unsigned)segments, (unsigned)((rows + per - 1) / per)); };

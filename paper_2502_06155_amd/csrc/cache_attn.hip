@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kThreadsC, cache_wgs<RB>()) void cache_attn_kernel(
       for (int mb = 0; mb < kMb; ++mb) *reinterpret_cast<f32x4*>(&s_o[wave][16 * rb + n][16 * mb + 4 * g]) = o[rb][mb];
     }
     __syncthreads();
-    join_waves<D, kRows>(a, s_o, s_m, s_l, q_row, row0, rows, seg.alone, seg.slot);
+    join_waves<D>(a, s_o, s_m, s_l, q_row, row0, rows, seg.alone, seg.slot);
     __syncthreads();
   } while (walk.advance(a));
 }

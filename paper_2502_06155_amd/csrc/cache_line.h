@@ -173,25 +173,23 @@ struct CacheWalk {
   }
 };
 
-// The four waves' states (sums of weighted values, running maxima in base 2, sums of weights) become the
+// The waves' states (sums of weighted values, running maxima in base 2, sums of weights) become the
 // segment's results, or one of its partial results.
-template <int D, int ROWS>
-__device__ __forceinline__ void join_waves(const CacheAttnArgs& a, const float (&s_o)[kThreadsC / 64][ROWS][D + 4],
-                                           const float (&s_m)[kThreadsC / 64][ROWS],
-                                           const float (&s_l)[kThreadsC / 64][ROWS], size_t q_row, int row0, int rows,
-                                           bool alone, int slot) {
-  constexpr int kWaves = kThreadsC / 64;
+template <int D, int ROWS, int WAVES>
+__device__ __forceinline__ void join_waves(const CacheAttnArgs& a, const float (&s_o)[WAVES][ROWS][D + 4],
+                                           const float (&s_m)[WAVES][ROWS], const float (&s_l)[WAVES][ROWS],
+                                           size_t q_row, int row0, int rows, bool alone, int slot) {
   float* part = a.part + ((size_t)blockIdx.y * 2 * a.workers + slot) * ROWS * (D + 4);
-  for (int i = threadIdx.x; i < ROWS * (D / 4); i += kThreadsC) {
+  for (int i = threadIdx.x; i < ROWS * (D / 4); i += 64 * WAVES) {
     const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
     if (row0 + r >= rows) continue;
     float m = s_m[0][r];
 #pragma unroll
-    for (int x = 1; x < kWaves; ++x) m = fmaxf(m, s_m[x][r]);
+    for (int x = 1; x < WAVES; ++x) m = fmaxf(m, s_m[x][r]);
     float l = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
+    for (int x = 0; x < WAVES; ++x) {
       const float f = fast_exp2(s_m[x][r] - m);
       l += f * s_l[x][r];
       y += f * *reinterpret_cast<const f32x4*>(&s_o[x][r][d0]);

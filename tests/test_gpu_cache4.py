@@ -212,6 +212,28 @@ def test_many_short_sequences_and_one_long():
     check(out, lse, q, cache, table, lens)
 
 
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("B,pages,H,N", [(32, 12, 4, 2), (40, 7, 2, 1), (150, 9, 4, 1), (130, 24, 2, 1)])
+def test_short_tables_of_many_sequences(B, pages, H, N, d):
+    """Workgroups of eight and of four waves with a segment each; lengths of none to full tables, a marked token."""
+    rng = np.random.default_rng(B + d)
+    lens = [int(x) for x in rng.integers(0, 128 * pages + 1, B)]
+    lens[0], lens[1], lens[2] = 128 * pages, 0, 128 * pages - 1
+    cache, table = held(rng, B, 2, d, lens)
+    cache[2][table[2, pages - 1], 1, 0, 126] = 255
+    q = bits(rng, B, H, N, d)
+    assert ta.cache4_attn_fwd_workspace(B, H, 2, N, d, pages) == 0
+    out, lse = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), return_lse=True)
+    some = [0, 1, 2, 3, B // 2, B - 2, B - 1]  # (the reference is slow)
+    check(out[some], lse[some], q[some], cache, table[some], [lens[b] for b in some])
+    shared = np.concatenate([table, np.full((B, 60), -1, np.int32)], 1)
+    other, l2 = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(shared), i32(lens), return_lse=True)
+    assert ta.cache4_attn_fwd_workspace(B, H, 2, N, d, pages + 60) > 0
+    ok = ~torch.isnan(out)
+    assert torch.equal(ok, ~torch.isnan(other)) and torch.allclose(out[ok].float(), other[ok].float(), rtol=0.02, atol=0.02)
+    assert torch.allclose(lse.nan_to_num(7.0), l2.nan_to_num(7.0), rtol=0, atol=2 * ROOM)
+
+
 def test_lengths_past_the_table_and_pages_that_are_none():
     rng = np.random.default_rng(6)
     cache, table = held(rng, 2, 2, 96, [512, 512])
