@@ -170,20 +170,31 @@ int64_t groups_of(const RopeArgs& a) {
   return ((int64_t)a.B * a.S + tokens - 1) / tokens;
 }
 
-// Waves that a launch wants before it lets one take more heads of its tokens (eight a SIMD unit of the device).
-constexpr int64_t kWantedWaves = 8 * 1024;
+// Heads that a wave takes of its tokens: few, so that kFewWaves waves form (and two at least: one after the other
+// they wait for less); past that a wave's start, its angles and weights, should be worth `worth` heads, up to kManyWaves.
+// 2 sequences of 777, 10 heads, d = 64: 4.8 us with two heads a wave, 6.3 with four, 7.5 with eight. 4000 tokens, 72 heads, d = 96,
+// pairs anywhere in the row: 38.5 with 5 heads a wave, 29.4 with 9, 24.5 with 36; 17776 tokens, 144 heads, d = 64, neighbours:
+// 150 us with 144, 136 with 48, 132 with 21.
+constexpr int64_t kFewWaves = 2048, kManyWaves = 16 * 1024;
 int heads_per_wave(const RopeArgs& a, int heads) {
   const int64_t groups = groups_of(a);
-  const int64_t parts = std::max<int64_t>(1, (kWantedWaves + groups - 1) / groups);
-  return (int)std::max<int64_t>(std::min(heads, 4), (heads + parts - 1) / parts);
+  auto of = [&](int64_t waves) {
+    const int64_t parts = std::max<int64_t>(1, (waves + groups - 1) / groups);
+    return (heads + parts - 1) / parts;
+  };
+  const bool near = a.layout == TA_ROPE_NONE || a.layout == TA_ROPE_INTERLEAVED;
+  const int64_t worth = near ? 12 : a.whole ? 18 : 36;
+  return (int)std::max<int64_t>({std::min(heads, 2), of(kManyWaves), std::min(of(kFewWaves), worth)});
 }
 
 // Gradients: the heads that a wave takes at a time, and workgroups, four a compute unit at most, as many as are
-// resident at once, shared out by the bytes of a row of q, k (read twice, written) and v (read, written).
+// resident at once, shared out by the bytes of a row of q, k (read twice, written) and v (read, written). 28800 tokens, 72
+// heads, d = 96: 233 us so; 286 with 768 workgroups, 294 with 1280, 239 with 2048; 240 with 4 heads a wave, 234 with 24; shares by heads
+// alone 240. 512 tokens, 48 heads of 128: 13.9 us with 3 heads a wave, 17.5 with one.
 constexpr int64_t kGradWorkgroups = 1024;
 void plan_grad(RopeArgs& a) {
   const int64_t groups = groups_of(a), heads = (int64_t)a.heads[0] + a.heads[1] + a.heads[2];
-  a.heads_per = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * heads / (kGradWorkgroups * kRopeWaves)));
+  a.heads_per = (int)std::max<int64_t>(1, std::min<int64_t>(8, 2 * groups * heads / (kGradWorkgroups * kRopeWaves)));
   int64_t need[3], share[3], total = 0;
   for (int x = 0; x < 3; ++x) {
     need[x] = (groups * ((a.heads[x] + a.heads_per - 1) / a.heads_per) + kRopeWaves - 1) / kRopeWaves;
