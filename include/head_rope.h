@@ -11,7 +11,8 @@
  * the angle a = position * frequency:
  *   y_i = n_i cos(a) - n_j sin(a),    y_j = n_j cos(a) + n_i sin(a).
  * Rows of v are carried over as they are. Everything between the bf16 input and the bf16 result is fp32, but for
- * the angles: a product in fp64, as a number of turns, whose fraction alone goes on.
+ * the angles: a product in fp64, as a number of turns, whose fraction alone goes on. (A row's squares are summed in
+ * fp32: with a norm, magnitudes up to 2^60.)
  *
  * Axes: values 0 .. dims[0] - 1 of a head belong to axis 0 (time, say), the next dims[1] to axis 1, and so on;
  * dims are even, their sum R is at most d, and values from R on are not turned. Pair p (of R / 2, those of axis 0

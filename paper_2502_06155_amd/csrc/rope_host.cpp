@@ -1,11 +1,10 @@
 // Host side of the C ABI of head norms and rotations: argument checks and how work is cut. Nothing is allocated
 // and nothing is kept.
 #include <algorithm>
+#include <array>
 #include <cfloat>
 #include <cmath>
-#include <initializer_list>
 #include <string>
-#include <vector>
 
 #include "head_rope.h"
 #include "host_checks.h"
@@ -57,11 +56,11 @@ int from_spec(const head_rope_spec* spec, RopeArgs& a) {
       a.dims[x] = s.dims[x];
       a.start[x] = a.turned;
       a.turned += s.dims[x];
-      // (Halves that are multiples of 8 start at multiples of 16.)
+      // Halves that are multiples of 8 start at multiples of 16. Where all turned values have one half it takes all
+      // of them too: eight values belong to one axis only if each has a multiple of 8 pairs.
       if (s.dims[x] % 16) a.whole = false;
     }
     if (a.turned > s.d) return fail(TA_ERR_BAD_SHAPE, "the axes' dims must add up to d at most");
-    if (s.layout == TA_ROPE_SPLIT) a.whole = a.turned % 16 == 0;
     if (!s.freqs || !s.positions) return fail(TA_ERR_NULL_PTR, "freqs and positions must be non-NULL");
     if (s.positions_batch < 0) return fail(TA_ERR_BAD_SHAPE, "positions_batch must not be negative");
     if (int st = check_aligned({s.freqs}, 8, "freqs must be 8-byte aligned")) return st;
@@ -117,8 +116,7 @@ struct Axis {
   int64_t step;
   int n;
 };
-bool pieces_apart(std::initializer_list<Axis> in, int64_t inside) {
-  std::vector<Axis> axes(in);
+bool pieces_apart(std::array<Axis, 3> axes, int64_t inside) {
   std::sort(axes.begin(), axes.end(), [](const Axis& x, const Axis& y) { return x.step < y.step; });
   for (const Axis& x : axes) {
     if (x.n == 1) continue;
@@ -129,7 +127,7 @@ bool pieces_apart(std::initializer_list<Axis> in, int64_t inside) {
 }
 // No value of written rows stands for two rows.
 bool one_place_each(const RopeArgs& a, const ta_rows& r, int heads) {
-  return pieces_apart({{r.batch, a.B}, {r.token, a.S}, {r.head, heads}}, a.d);
+  return pieces_apart({{{r.batch, a.B}, {r.token, a.S}, {r.head, heads}}}, a.d);
 }
 
 // Whether two written tensors share no value: their extents are apart, or they stand in one tensor, heads behind
@@ -143,7 +141,7 @@ bool apart(const RopeArgs& a, const ta_rows& p, int np, const ta_rows& q, int nq
   if ((a.B > 1 && lo.batch != hi.batch) || (a.S > 1 && lo.token != hi.token)) return false;
   // A token's heads of lo, then those of hi, are one piece, and pieces do not meet.
   const int64_t lo_piece = ((first ? np : nq) - 1) * lo.head + a.d, hi_piece = ((first ? nq : np) - 1) * hi.head + a.d;
-  return off >= lo_piece && pieces_apart({{lo.batch, a.B}, {lo.token, a.S}}, off + hi_piece);
+  return off >= lo_piece && pieces_apart({{{lo.batch, a.B}, {lo.token, a.S}, {0, 1}}}, off + hi_piece);
 }
 
 Rows to_rows(const ta_rows& r) {

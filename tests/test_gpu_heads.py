@@ -162,6 +162,10 @@ CASES = [
     dict(B=2, S=50, H=2, Hkv=1, d=128, norm="rms", layout="halves", dims=(44, 42, 42)),
     dict(B=2, S=51, H=2, Hkv=2, d=128, norm="rms", layout="split", dims=(32, 48, 48), shared=False),
     dict(B=1, S=40, H=3, Hkv=1, d=96, norm="layer", layout="split", dims=(6, 10, 14, 20)),
+    # a multiple of 16 in all, but eight values that follow each other turn with two axes
+    dict(B=1, S=45, H=2, Hkv=1, d=128, norm="rms", layout="split", dims=(16, 56, 56)),
+    dict(B=2, S=13, H=3, Hkv=1, d=64, norm=None, layout="split", dims=(10, 22), lens=[13, 6]),
+    dict(B=1, S=30, H=2, Hkv=2, d=96, norm="layer", layout="split", dims=(8, 40), shared=False),
     dict(B=1, S=9, H=3, Hkv=1, d=64, norm="rms", layout="halves", dims=(2, 2)),
     dict(B=1, S=33, H=4, Hkv=2, d=128, norm="rms", layout="interleaved", dims=(32,)),
     dict(B=3, S=7, H=9, Hkv=1, d=96, norm="rms", layout="halves", dims=(16,), lens=[0, 9, -3]),
