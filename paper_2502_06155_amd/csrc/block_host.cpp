@@ -178,7 +178,8 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
 }
 // The 4-bit cache. Passes of 64 and 128 rows share a page's widened codes, and a workgroup of theirs takes a page at a
 // time, in `page` us, where one of 16 or 32 rows takes four. All passes together have as many workgroups as the device
-// holds (half that in passes of 32 rows), at least two each, or one. What a workgroup of many rows leaves to join
+// holds, at least two each, or one; with 17 to 32 rows half as many for up to four pages each (64 segments of 24 pages, d = 128:
+// 18.7 us with 256, 21.4 with 512; 128 of 24, d = 64 18.1 and 16.9; 192 of 157, d = 128 67.5 and 60.7). What a workgroup of many rows leaves to join
 // costs `part` us, written and read, so that with P pages sqrt(P page / part) of them are the best (64 segments
 // of 4 pages, 120 rows: 35.9 us with 512, 27.8 with 165), but for few pages, which a workgroup each takes (8 segments of
 // 8 pages: 16.5 us with 104, 18.9 with 82).
@@ -199,8 +200,7 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
   const int64_t rows = (int64_t)(H / Hkv) * N, segments = (int64_t)B * Hkv;
   p.rows = cache4_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
   p.passes = (int)((rows + p.rows - 1) / p.rows);
-  const int64_t slots = p.rows == 32 ? kSlots / 2 : kSlots;
-  int64_t workers = p.passes < slots ? slots / p.passes : 1;
+  int64_t workers = p.passes < kSlots ? kSlots / p.passes : 1;
   const bool eight = p.rows == 16 && max_pages > 4 && segments <= kSlots / 2;
   double alone, shared;
   if (p.rows > 32) {
@@ -210,10 +210,11 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
     alone = m.page * max_pages;
     shared = 2 * std::sqrt(pages * m.page * m.part);
   } else {
+    if (p.rows == 32 && segments * max_pages <= 4 * kSlots) workers = kSlots / 2;
     alone = (0.22 + (eight ? 0.002 : 0.003) * d) * max_pages;
     shared = 1.4e-5 * d * (double)segments * max_pages;
   }
-  if (p.passes < slots) workers = std::max<int64_t>(2, workers);
+  if (p.passes < kSlots) workers = std::max<int64_t>(2, workers);
   p.workers = (int)std::min(workers, segments * (max_pages + kCache4Segment));
   p.whole = max_pages <= 24 && alone <= 5 + shared;
   p.eight = p.whole && eight;

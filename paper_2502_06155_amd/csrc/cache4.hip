@@ -207,17 +207,23 @@ __global__ __launch_bounds__(kThreadsC) void cache4_read_kernel(const Cache4Read
 // So neither K nor V is kept transposed, no scale leaves its token, and nothing goes through LDS. K codes become bf16 exactly,
 // scales among it, and so do V's.
 
-// Words of K codes a lane holds of a token, and 8-value slices of them.
-template <int D>
+// T tokens, all of a page or half of it (above: T = 128; with 64 tokens, row n of instruction group i
+// is token 4 n + i, and a lane group has 16 tokens and two steps).
+template <int D, int T>
 struct Key4 {
-  static constexpr int kW = D / 32;
-  uint32_t k[8][kW];
-  u32x2 lo, hi;  // scales of the 8 tokens: of the lane's first group of 32 values, and of its last (d = 96)
+  static constexpr int kW = D / 32;  // words of K codes a lane holds of a token, and 8-value slices of them
+  static constexpr int kTokens = T / 16;
+  uint32_t k[kTokens][kW];
+  u32x2 lo, hi;  // scales of the tokens: of the lane's first group of 32 values, and of its last (d = 96)
+  __device__ __forceinline__ static u32x2 bytes(const uint8_t* p) {
+    if constexpr (kTokens == 8) return *reinterpret_cast<const u32x2*>(p);
+    else return u32x2{*reinterpret_cast<const uint32_t*>(p), 0u};
+  }
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int lane) {
-    const int n = lane & 15, g = lane >> 4;
+    const int n = lane & 15, g = lane >> 4, t0 = kTokens * n;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint8_t* p = codes + (uint32_t)((8 * n + i) * (D / 2) + g * (D / 8));
+    for (int i = 0; i < kTokens; ++i) {
+      const uint8_t* p = codes + (uint32_t)((t0 + i) * (D / 2) + g * (D / 8));
       if constexpr (D == 128) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
@@ -231,8 +237,8 @@ struct Key4 {
         for (int e = 0; e < 3; ++e) k[i][e] = reinterpret_cast<const uint32_t*>(p)[e];
       }
     }
-    lo = *reinterpret_cast<const u32x2*>(scales + (uint32_t)(g * kW / 4 * kBlock + 8 * n));
-    if constexpr (D == 96) hi = *reinterpret_cast<const u32x2*>(scales + (uint32_t)((g * kW + kW - 1) / 4 * kBlock + 8 * n));
+    lo = bytes(scales + (uint32_t)(g * kW / 4 * kBlock + t0));
+    if constexpr (D == 96) hi = bytes(scales + (uint32_t)((g * kW + kW - 1) / 4 * kBlock + t0));
   }
   // Scales of slice m (of kW).
   __device__ __forceinline__ u32x2 scales_of(int m, int g) const {
@@ -241,35 +247,37 @@ struct Key4 {
     return last ? hi : lo;
   }
 };
-template <int D>
+template <int D, int T>
 struct Value4 {
-  uint32_t v[4][8];  // token 32 g + 8 c + i
-  u32x4 scales[2];   // of tokens 32 g .. + 31
+  static constexpr int kSteps = T / 32;
+  uint32_t v[kSteps][8];      // token T / 4 g + 8 c + i
+  u32x4 scales[kSteps / 2];   // of the lane group's T / 4 tokens
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* group_scales, int lane) {
-    const int n = lane & 15, g = lane >> 4;
+    const int n = lane & 15, g = lane >> 4, t0 = T / 4 * g;
     // d = 96: lanes 12 to 15 of a group have no channels and read those of lane 11.
     const int word = D == 128 ? n : D == 96 ? min(n, 11) : n / 2, group = D == 64 ? n / 8 : word / 4;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < kSteps; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        v[c][i] = *reinterpret_cast<const uint32_t*>(codes + (uint32_t)((32 * g + 8 * c + i) * (D / 2) + 4 * word));
+        v[c][i] = *reinterpret_cast<const uint32_t*>(codes + (uint32_t)((t0 + 8 * c + i) * (D / 2) + 4 * word));
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-      scales[x] = *reinterpret_cast<const u32x4*>(group_scales + (uint32_t)(group * kBlock + 32 * g + 16 * x));
+    for (int x = 0; x < kSteps / 2; ++x)
+      scales[x] = *reinterpret_cast<const u32x4*>(group_scales + (uint32_t)(group * kBlock + t0 + 16 * x));
   }
 };
 
 // Byte i of two words as a scale.
 __device__ __forceinline__ float scale_at(u32x2 w, int i) { return scale_of(w[i / 4] >> (8 * (i % 4)) & 0xffu); }
 
-// Waves a SIMD unit: at 16 rows 256 registers a lane are enough, at 32 rows it takes 512.
-template <int RB>
-constexpr int cache4_waves() { return RB == 1 ? 2 : 1; }
-
+// Two waves a SIMD unit, of 256 registers a lane: enough for a page at 16 rows and for half of one at 32. 24 sequences of up to
+// 100000 tokens, 8 key heads of 128: 117 us with 16 rows (5.1 TB/s), 145 with 32 (174 with a whole page, 350
+// registers and one wave a unit); of 96, up to 80000, 32 rows: 107 us, 148 so.
 template <int D, int RB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_kernel(const Cache4AttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4AttnArgs a) {
   constexpr int kRows = 16 * RB, kWaves = WAVES, kSl = D / 32;
+  constexpr int kT = RB == 1 ? kBlock : kBlock / 2, kParts = kBlock / kT;  // tokens at a time
+  constexpr int kGroups = kT / 16, kSteps = kT / 32;
   constexpr int kCh = D == 64 ? 4 : 8;  // channels of a lane, and O^T instructions of a step
   __shared__ float s_o[kWaves][kRows][D + 4];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
@@ -292,21 +300,21 @@ __global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_ke
       const int x = table[p];
       return x < a.n_pages ? x : -1;
     };
-    auto load_k = [&](Key4<D>& t, int page) {
+    auto load_k = [&](Key4<D, kT>& t, int page, int from) {
       const size_t ph = (size_t)page * a.Hkv + seg.h;
-      t.load(a.k_pages + ph * kBlock * (D / 2), a.k_exps + ph * kBlock * (D / kGroup), lane);
+      t.load(a.k_pages + (ph * kBlock + from) * (D / 2), a.k_exps + ph * kBlock * (D / kGroup) + from, lane);
     };
-    auto load_v = [&](Value4<D>& t, int page) {
+    auto load_v = [&](Value4<D, kT>& t, int page, int from) {
       const size_t ph = (size_t)page * a.Hkv + seg.h;
-      t.load(a.v_pages + ph * kBlock * (D / 2), a.v_exps + ph * kBlock * (D / kGroup), lane);
+      t.load(a.v_pages + (ph * kBlock + from) * (D / 2), a.v_exps + ph * kBlock * (D / kGroup) + from, lane);
     };
     int p = p0 + wave;
     int page = page_of(p);
-    Key4<D> kt;
-    Value4<D> vt;
+    Key4<D, kT> kt;
+    Value4<D, kT> vt;
     if (page >= 0) {
-      load_k(kt, page);
-      load_v(vt, page);
+      load_k(kt, page, 0);
+      load_v(vt, page, 0);
     }
 
     int end[RB];  // tokens this lane's row attends to
@@ -329,14 +337,16 @@ __global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_ke
       for (int t = 0; t < kCh; ++t) o[rb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // The next page's K loads go out as soon as this one's K is used, its V loads when V is.
-    for (; p < p1; p += kWaves) {
-      const int next = page_of(p + kWaves);
-      const int tok0 = p * kBlock;
-      f32x4 s[RB][8];
+    // The next tokens' K loads go out as soon as these ones' K is used, their V loads when V is.
+    int part = 0, next = page;  // (the page of the next tokens, the same for the page's second half)
+    while (p < p1) {
+      const int tok0 = p * kBlock + part * kT;
+      if (part == kParts - 1) next = page_of(p + kWaves);
+      const int next_from = part == kParts - 1 ? 0 : kT;
+      f32x4 s[RB][kGroups];
       if (page >= 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kGroups; ++i) {
 #pragma unroll
           for (int m = 0; m < kSl; ++m) {
             const bf16x8 kf = as_bf16x8(decode8(kt.k[i][m], scale_at(kt.scales_of(m, g), i)));
@@ -348,22 +358,22 @@ __global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_ke
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) load_k(kt, next);
+      if (next >= 0) load_k(kt, next, next_from);
       __builtin_amdgcn_sched_barrier(0);
       if (page >= 0) {
-        bf16x8 pf[RB][4];
+        bf16x8 pf[RB][kSteps];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          if (tok0 + kBlock > len - (a.N - 1)) {
+          if (tok0 + kT > len - (a.N - 1)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < kGroups; ++i)
 #pragma unroll
               for (int j = 0; j < 4; ++j)
-                if (tok0 + 32 * g + 8 * j + i >= end[rb]) s[rb][i][j] = -INFINITY;
+                if (tok0 + kT / 4 * g + kGroups * j + i >= end[rb]) s[rb][i][j] = -INFINITY;
           }
           float mx = s[rb][0][0];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
           const float m_new = fmaxf(m_ref[rb], group_max(mx) * a.c);
@@ -376,23 +386,23 @@ __global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_ke
           }
           float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
               sum += x;
-              pf[rb][j][i] = (__bf16)x;
+              pf[rb][(kGroups * j + i) / 8][(kGroups * j + i) % 8] = (__bf16)x;
             }
           l_run[rb] += sum;
         }
-        if (tok0 + kBlock > len) {  // scales behind the last token may be anything: those of V become 2^-127
+        if (tok0 + kT > len) {  // scales behind the last token may be anything: those of V become 2^-127
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < kSteps / 2; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vt.scales[x][e] &= bytes_before(len - (tok0 + 32 * g + 16 * x + 4 * e));
+            for (int e = 0; e < 4; ++e) vt.scales[x][e] &= bytes_before(len - (tok0 + kT / 4 * g + 16 * x + 4 * e));
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kSteps; ++c) {
           // vf[t]: of channel t of the lane, the step's 8 tokens.
           u32x4 vf[kCh];
 #pragma unroll
@@ -420,8 +430,14 @@ __global__ __launch_bounds__(64 * WAVES, cache4_waves<RB>()) void cache4_attn_ke
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) load_v(vt, next);
+      if (next >= 0) load_v(vt, next, next_from);
       page = next;
+      if (part == kParts - 1) {
+        p += kWaves;
+        part = 0;
+      } else {
+        ++part;
+      }
     }
 
     // The waves' states join in LDS.
