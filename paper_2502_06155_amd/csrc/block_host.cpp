@@ -176,31 +176,31 @@ CachePlan plan_cache(int B, int H, int Hkv, int N, int d, int max_pages) {
   p.bytes = p.whole || p.workers == 1 ? 0 : (size_t)p.passes * 2 * p.workers * p.rows * (d + 4) * sizeof(float);
   return p;
 }
-// The 4-bit cache. Passes of 64 and 128 rows share a page's widened codes, and a workgroup of theirs takes a page at a
-// time, in `page` us, where one of 16 or 32 rows takes four. All passes together have as many workgroups as the device
-// holds, at least two each, or one; with 17 to 32 rows half as many for up to four pages each (64 segments of 24 pages, d = 128:
-// 18.7 us with 256, 21.4 with 512; 128 of 24, d = 64 18.1 and 16.9; 192 of 157, d = 128 67.5 and 60.7). What a workgroup of many rows leaves to join
-// costs `part` us, written and read, so that with P pages sqrt(P page / part) of them are the best (64 segments
-// of 4 pages, 120 rows: 35.9 us with 512, 27.8 with 165), but for few pages, which a workgroup each takes (8 segments of
-// 8 pages: 16.5 us with 104, 18.9 with 82).
+// The 4-bit cache. Passes of 64 and 128 rows share a page's widened codes, and a workgroup of theirs, one a compute unit, takes
+// a page at a time, in `page` us, where one of 16 or 32 rows takes four. All passes together have as many workgroups as
+// the device holds, at least two each, or one; with 17 to 32 rows half as many for up to four pages each (64 segments of 24 pages, d = 128:
+// 18.7 us with 256, 21.4 with 512; 128 of 24, d = 64 18.1 and 16.9; 192 of 157, d = 128 67.5 and 60.7). What a workgroup of
+// many rows leaves to join costs `part` us, written and read, so that with P pages sqrt(P page / part) of them are the
+// best (64 segments of 16 pages, d = 64, 72 rows: 17.0 us, 18.6 with a fifth fewer), but for few pages, which a workgroup each takes.
 // Short tables run a workgroup per segment, in one launch; of eight waves, in passes of 16 rows, where there are more than four
 // pages and no more segments than compute units. Alone, a segment takes 5 us and, of 16 rows, 0.22 + 0.002 d us a page
 // (0.003 d with four waves); shared, all take 10 us and the bytes' time, d * 1.4e-5 us a page and segment if sequences
 // fill half of their tables, or the pages and parts of the workgroups. Up to 24 pages, so that a batch's longest sequence
 // costs 14 us at most. Measured, eight waves alone, four alone, and shared, one row: 8 segments of 8 pages at d = 128 8.9, 9.3 and 10.3
 // us, of 16 12.7, 14.2 and 10.6; at d = 64 of 12 9.0, 9.7 and 9.7; 64 of 12, d = 128 10.9, 12.5 and 13.3; 128 of 16 14.5, 16.9 and
-// 19.7; 256 of 24 22.4, 24.7 and 28.6. Alone and shared, 36 rows: 8 of 2 9.0 and 10.5, of 4 14.1 and 10.7; 120 rows, 256 of 8 40.7
-// and 52.1.
+// 19.7; 256 of 24 22.4, 24.7 and 28.6. Alone and shared, 36 rows: 8 of 2 7.6 and 10.3, of 8 16.7 and 10.9, 64 of 4 11.0 and 15.1, of 16
+// 29.6 and 20.9; 120 rows, 8 of 4 16.5 and 15.5, 64 of 4 17.3 and 23.9, 256 of 8 33.1 and 38.8.
 struct ManyRows {
   double page, part;
 };
-ManyRows many_rows(int rows) { return rows == 64 ? ManyRows{2.5, 0.017} : ManyRows{3.6, 0.034}; }
+ManyRows many_rows(int rows) { return rows == 64 ? ManyRows{1.3, 0.0125} : ManyRows{1.9, 0.025}; }
 CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
   CachePlan p;
   const int64_t rows = (int64_t)(H / Hkv) * N, segments = (int64_t)B * Hkv;
   p.rows = cache4_rows_per_pass((int)std::min<int64_t>(rows, INT_MAX));
   p.passes = (int)((rows + p.rows - 1) / p.rows);
-  int64_t workers = p.passes < kSlots ? kSlots / p.passes : 1;
+  const int64_t slots = p.rows > 32 ? kSlots / 2 : kSlots;
+  int64_t workers = p.passes < slots ? slots / p.passes : 1;
   const bool eight = p.rows == 16 && max_pages > 4 && segments <= kSlots / 2;
   double alone, shared;
   if (p.rows > 32) {
@@ -214,7 +214,7 @@ CachePlan plan_cache4(int B, int H, int Hkv, int N, int d, int max_pages) {
     alone = (0.22 + (eight ? 0.002 : 0.003) * d) * max_pages;
     shared = 1.4e-5 * d * (double)segments * max_pages;
   }
-  if (p.passes < kSlots) workers = std::max<int64_t>(2, workers);
+  if (p.passes < slots) workers = std::max<int64_t>(2, workers);
   p.workers = (int)std::min(workers, segments * (max_pages + kCache4Segment));
   p.whole = max_pages <= 24 && alone <= 5 + shared;
   p.eight = p.whole && eight;

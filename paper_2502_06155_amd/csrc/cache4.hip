@@ -464,32 +464,48 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
   } while (walk.advance(a));
 }
 
-// Many rows. Above, every 32 rows of a key head widen every page again. Here the four waves of a workgroup have 16 RB
-// rows each and go through the pages together: a page's codes are widened once, by all of them, into LDS, where the
-// matrix operands of all rows come from; the next page's codes arrive in registers meanwhile.
+// Many rows. Above, every 32 rows of a key head widen every page again. Here a workgroup of eight waves has four sets of
+// 16 RB rows, each with a wave for the first half of a page's tokens and one for the second, which join at the end: a page's codes are
+// widened once, K by four waves and V by the other four, into LDS, where the matrix operands of all rows come from.
+// While a page is multiplied the next one is widened into the other half of the LDS, and the one behind it is on its way.
+// Bound by the vector work beside the products (exponentials, widening): one sequence of 32768, 32 heads on 8 of 128, 2048 rows
+// 1121 us (981 TFLOP/s), 512 workgroups of four waves that had a page's tokens to themselves 1166. A step's 128 rows take 2.3 us a
+// page at d = 128, 2.7 at 96. Waves of K widening before their products and waves of V behind them: 1261; two sets of 48 rows, four
+// waves each, for 96 rows: 36.3 us for 32.5, the joins of four waves cost more than the even rows give.
 //   K: row 16 i + n of the tile is the token that row n of instruction group i computes, 32 (i / 2) + 8 (n / 4) + 4 (i % 2) + n % 4,
 //   so that the scores of groups 2 c and 2 c + 1 are, in lane group g, tokens 32 c + 8 g .. + 7: P^T of step c. Rows are 16
 //   bytes longer than their d values, which puts 16 rows' pieces on different banks.
 //   V^T: a row of 128 tokens for each channel, its 16-byte pieces of 8 tokens at places exchanged by the channel's
 //   number (key): both the writes (16 channels' words of the same 8 tokens) and the reads (row n of instruction t: channel 8 n + t,
 //   4 n + t at d = 64) fall on different banks.
+constexpr int kThreadsMany = 512;
 template <int D, int RB>
-__global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4AttnArgs a) {
-  constexpr int kWaves = kThreadsC / 64, kRows = 16 * RB * kWaves, kSl = D / 32;
+__global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cache4AttnArgs a) {
+  constexpr int kSets = 4, kRows = 16 * RB * kSets, kSl = D / 32;
+  constexpr int kParts = 2, kT = kBlock / kParts;  // of a page, and their tokens
+  constexpr int kGroups = kT / 16, kSteps = kT / 32;
   constexpr int kCh = D == 64 ? 4 : 8;
   constexpr int kPitch = D + 8;                       // of a K row, in values
+  constexpr int kHalf = kThreadsMany / 2;             // threads that widen K, and V
   constexpr int kKUnits = kBlock * (D / kGroup);      // 32 values of a token
-  constexpr int kKPer = (kKUnits + kThreadsC - 1) / kThreadsC;
+  constexpr int kKPer = (kKUnits + kHalf - 1) / kHalf;
   constexpr int kWords = D / 8;                       // of a token's codes
   constexpr int kVUnits = kBlock / 8 * kWords;        // a word of 8 tokens
-  __shared__ __attribute__((aligned(16))) uint16_t s_k[kBlock * kPitch];
-  __shared__ __attribute__((aligned(16))) uint16_t s_v[D * kBlock];
+  static_assert(kKPer <= 2 && kVUnits <= kHalf, "codes a thread widens");
+  constexpr int kPage = kBlock * kPitch + D * kBlock;  // a widened page, in values
+  constexpr int kLanes = D == 96 ? 48 : 64;            // that hold channels
+  constexpr int kState = kLanes * RB * (kCh + 1);      // 16-byte pieces of a wave's state
+  static_assert(kSets * kState * 16 <= 2 * kPage * 2, "states take the pages' place");
+  __shared__ __attribute__((aligned(16))) uint16_t s_page[2 * kPage];
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 15, g = lane >> 4;
-  const int rows = a.G * a.N, row0 = blockIdx.y * kRows + 16 * RB * wave;
+  const int set = wave % kSets, part = wave / kSets;  // rows, and tokens kT part .. of a page
+  const int rows = a.G * a.N, row0 = blockIdx.y * kRows + 16 * RB * set;
   const bool works = row0 < rows;
-  const int v_word = tid % kWords, v_part = tid / kWords;  // tokens 8 v_part .. + 7
+  const bool for_k = wave < 4;  // what it widens
+  const int unit = tid % kHalf;
+  const int v_word = unit % kWords, v_part = unit / kWords;  // tokens 8 v_part .. + 7
 
   CacheWalk<kCache4Segment> walk(a, blockIdx.x);
   if (walk.none()) return;
@@ -508,51 +524,55 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
       }
       return p;
     };
-    u32x4 kw[kKPer];
-    uint32_t ks[kKPer], vw[8];
-    u32x2 vs;
-    auto load = [&](int p) {
+    u32x4 cw[2];     // K: 16 bytes of codes; V: words of 8 tokens
+    uint32_t sc[2];  // their scales
+    auto load = [&]() {
       const size_t ph = (size_t)page * a.Hkv + seg.h;
-      const uint8_t* k = a.k_pages + ph * kBlock * (D / 2);
-      const uint8_t* ke = a.k_exps + ph * kBlock * (D / kGroup);
-      const uint8_t* v = a.v_pages + ph * kBlock * (D / 2);
-      const uint8_t* ve = a.v_exps + ph * kBlock * (D / kGroup);
+      if (for_k) {
+        const uint8_t* k = a.k_pages + ph * kBlock * (D / 2);
+        const uint8_t* ke = a.k_exps + ph * kBlock * (D / kGroup);
 #pragma unroll
-      for (int i = 0; i < kKPer; ++i) {
-        const int u = tid + kThreadsC * i, t = u / (D / kGroup), grp = u % (D / kGroup);
-        if (u < kKUnits) {
-          kw[i] = *reinterpret_cast<const u32x4*>(k + (uint32_t)(t * (D / 2) + 16 * grp));
-          ks[i] = ke[(uint32_t)(grp * kBlock + t)];
+        for (int i = 0; i < kKPer; ++i) {
+          const int u = unit + kHalf * i, t = u / (D / kGroup), grp = u % (D / kGroup);
+          if (u < kKUnits) {
+            cw[i] = *reinterpret_cast<const u32x4*>(k + (uint32_t)(t * (D / 2) + 16 * grp));
+            sc[i] = ke[(uint32_t)(grp * kBlock + t)];
+          }
         }
-      }
-      if (tid < kVUnits) {
+      } else if (unit < kVUnits) {
+        const uint8_t* v = a.v_pages + ph * kBlock * (D / 2);
+        const uint8_t* ve = a.v_exps + ph * kBlock * (D / kGroup);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          vw[i] = *reinterpret_cast<const uint32_t*>(v + (uint32_t)((8 * v_part + i) * (D / 2) + 4 * v_word));
-        vs = *reinterpret_cast<const u32x2*>(ve + (uint32_t)(v_word / 4 * kBlock + 8 * v_part));
+          cw[i / 4][i % 4] = *reinterpret_cast<const uint32_t*>(v + (uint32_t)((8 * v_part + i) * (D / 2) + 4 * v_word));
+        const u32x2 vs = *reinterpret_cast<const u32x2*>(ve + (uint32_t)(v_word / 4 * kBlock + 8 * v_part));
+        sc[0] = vs[0];
+        sc[1] = vs[1];
       }
     };
-    auto to_lds = [&](int p) {
+    auto widen = [&](uint16_t* s_k, int p) {
+      if (for_k) {
 #pragma unroll
-      for (int i = 0; i < kKPer; ++i) {
-        const int u = tid + kThreadsC * i, t = u / (D / kGroup), grp = u % (D / kGroup);
-        if (u < kKUnits) {
-          const int row = (t & ~31) + 16 * (t >> 2 & 1) + 4 * (t >> 3 & 3) + (t & 3);
-          const float f = scale_of(ks[i]);
+        for (int i = 0; i < kKPer; ++i) {
+          const int u = unit + kHalf * i, t = u / (D / kGroup), grp = u % (D / kGroup);
+          if (u < kKUnits) {
+            const int row = (t & ~31) + 16 * (t >> 2 & 1) + 4 * (t >> 3 & 3) + (t & 3);
+            const float f = scale_of(sc[i]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<u32x4*>(s_k + row * kPitch + 32 * grp + 8 * e) = decode8(kw[i][e], f);
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<u32x4*>(s_k + row * kPitch + 32 * grp + 8 * e) = decode8(cw[i][e], f);
+          }
         }
-      }
-      if (tid < kVUnits) {
+      } else if (unit < kVUnits) {
+        uint16_t* s_v = s_k + kBlock * kPitch;
         // Scales behind the last token may be anything: theirs become 2^-127.
         const int left = len - (p * kBlock + 8 * v_part);
-        vs[0] &= bytes_before(left);
-        vs[1] &= bytes_before(left - 4);
+        const u32x2 vs = {sc[0] & bytes_before(left), sc[1] & bytes_before(left - 4)};
         u32x4 x[8];  // of the word's 8 channels
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-          const u32x4 x0 = decode8(vw[i], scale_at(vs, i)), x1 = decode8(vw[i + 1], scale_at(vs, i + 1));
+          const u32x4 x0 = decode8(cw[i / 4][i % 4], scale_at(vs, i));
+          const u32x4 x1 = decode8(cw[i / 4][i % 4 + 1], scale_at(vs, i + 1));
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             x[2 * y][i / 2] = __builtin_amdgcn_perm(x1[y], x0[y], 0x05040100u);
@@ -568,7 +588,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
     };
 
     int p = seek(p0);
-    if (p < p1) load(p);
+    if (p < p1) load();
     int end[RB];  // tokens this lane's row attends to
     bf16x8 qf[RB][kSl];
     f32x4 o[RB][kCh];
@@ -589,50 +609,59 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
       for (int t = 0; t < kCh; ++t) o[rb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    while (p < p1) {
-      __syncthreads();  // the page before is done with
-      to_lds(p);
+    int now = p;  // the page that is multiplied, the next one being widened and p the one on its way
+    uint16_t* s_now = s_page;
+    uint16_t* s_next = s_page + kPage;
+    if (now < p1) {
+      widen(s_now, now);
+      p = seek(now + 1);
+      if (p < p1) load();
       __syncthreads();
-      const int tok0 = p * kBlock;
-      p = seek(p + 1);
-      if (p < p1) load(p);
-      if (!works) continue;
-      // 64 tokens at a time: their scores and weights fit the registers beside sums, queries and the next page.
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        f32x4 s[RB][4];
+    }
+    while (now < p1) {
+      const int tok0 = now * kBlock + kT * part;
+      now = p;
+      if (now < p1) {
+        widen(s_next, now);
+        p = seek(now + 1);
+        if (p < p1) load();
+      }
+      if (works) {
+        const uint16_t* s_k = s_now + kT * part * kPitch;
+        const uint16_t* s_v = s_now + kBlock * kPitch;
+        f32x4 s[RB][kGroups];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kGroups; ++i)
 #pragma unroll
           for (int m = 0; m < kSl; ++m) {
-            const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_k + (64 * half + 16 * i + n) * kPitch + 32 * m + 8 * g));
+            const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_k + (16 * i + n) * kPitch + 32 * m + 8 * g));
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
               s[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i], 0, 0, 0);
           }
-        // Four K pieces are on their way from LDS while RB products use one (one sequence of 32768, 2048 rows: 315 us, 329
-        // as the compiler orders them).
+        // Four K pieces are on their way from LDS while RB products use one (one sequence of 32768, 8 heads, 512 rows each: 315 us,
+        // 329 as the compiler orders them, with four waves).
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-        for (int x = 0; x < 4 * kSl - 4; ++x) {
+        for (int x = 0; x < kGroups * kSl - 4; ++x) {
           __builtin_amdgcn_sched_group_barrier(0x008, RB, 0);
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4 * RB, 0);
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pf[RB][2];
+        bf16x8 pf[RB][kSteps];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          if (tok0 + kBlock > len - (a.N - 1)) {
+          if (tok0 + kT > len - (a.N - 1)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < kGroups; ++i)
 #pragma unroll
               for (int j = 0; j < 4; ++j)
-                if (tok0 + 64 * half + 32 * (i / 2) + 8 * g + 4 * (i % 2) + j >= end[rb]) s[rb][i][j] = -INFINITY;
+                if (tok0 + 32 * (i / 2) + 8 * g + 4 * (i % 2) + j >= end[rb]) s[rb][i][j] = -INFINITY;
           }
           float mx = s[rb][0][0];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[rb][i][j]);
           const float m_new = fmaxf(m_ref[rb], group_max(mx) * a.c);
@@ -645,7 +674,7 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
           }
           float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
@@ -655,48 +684,78 @@ __global__ __launch_bounds__(kThreadsC, 2) void cache4_rows_kernel(const Cache4A
           l_run[rb] += sum;
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < kSteps; ++c)
 #pragma unroll
           for (int t = 0; t < kCh; ++t) {
             // (d = 96: rows 12 to 15 of an instruction are no channels and read those of row 11.)
             const int key = D == 96 ? min(n, 11) : n;
-            const bf16x8 vf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_v + (kCh * key + t) * kBlock + 8 * ((8 * half + 4 * c + g) ^ key)));
+            const bf16x8 vf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_v + (kCh * key + t) * kBlock + 8 * ((kT / 8 * part + 4 * c + g) ^ key)));
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
               o[rb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][c], o[rb][t], 0, 0, 0);
           }
       }
+      __syncthreads();  // this page is done with, the next one is there
+      uint16_t* x = s_now;
+      s_now = s_next;
+      s_next = x;
     }
 
-    // A wave's rows are its own: results or partial results straight from its registers.
+    // The states of a set's two waves join, through the pages' place, each lane its own.
+    f32x4* state = reinterpret_cast<f32x4*>(s_page) + set * kState;
+    if (works && part == 1) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = row0 + 16 * rb + n;
-      const float l = group_sum(l_run[rb]);
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      // (A row of NaN stays one: its sums are NaN, and so is its quotient's product.)
-      const float lse2 = l == 0.f ? -INFINITY : m_ref[rb] + __builtin_amdgcn_logf(l);
-      if (r >= rows) continue;
-      float* pr = a.part + (((size_t)blockIdx.y * 2 * a.workers + seg.slot) * kRows + (r - blockIdx.y * kRows)) * (D + 4);
+      for (int rb = 0; rb < RB; ++rb) {
+        const float l = group_sum(l_run[rb]);
+        f32x4* to = state + kLanes * rb * (kCh + 1);
+        if (g == 0) to[kLanes * kCh + n] = f32x4{m_ref[rb], l, 0.f, 0.f};
+        if (lane < kLanes) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ch = kCh * (4 * g + j);
-        if (ch >= D) continue;
-#pragma unroll
-        for (int t = 0; t < kCh; t += 4) {
-          const f32x4 y = f32x4{o[rb][t][j], o[rb][t + 1][j], o[rb][t + 2][j], o[rb][t + 3][j]} * inv;
-          if (seg.alone)
-            *reinterpret_cast<u32x2*>(a.out + (seg.q_row + r) * D + ch + t) =
-                __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
-          else
-            *reinterpret_cast<f32x4*>(pr + ch + t) = y;
+          for (int t = 0; t < kCh; ++t) to[kLanes * t + lane] = o[rb][t];
         }
       }
-      if (g == 0) {
-        if (!seg.alone) pr[D] = lse2;
-        else if (a.lse) a.lse[seg.q_row + r] = lse2 * 0.69314718055994531f;
+    }
+    __syncthreads();
+    // A wave's rows are its own: results or partial results straight from its registers.
+    if (part == 0 && works) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const f32x4* from = state + kLanes * rb * (kCh + 1);
+        const f32x4 other = from[kLanes * kCh + n];
+        const float m = fmaxf(m_ref[rb], other[0]);
+        float f0 = fast_exp2(m_ref[rb] - m), f1 = fast_exp2(other[0] - m);
+        const float l = group_sum(l_run[rb]) * f0 + other[1] * f1;
+        const int r = row0 + 16 * rb + n;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        f0 *= inv;
+        f1 *= inv;
+#pragma unroll
+        for (int t = 0; t < kCh; ++t) o[rb][t] = o[rb][t] * f0 + from[kLanes * t + min(lane, kLanes - 1)] * f1;
+        // (A row of NaN stays one: its sums are NaN, and so is its quotient's product.)
+        const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+        if (r >= rows) continue;
+        float* pr = a.part + (((size_t)blockIdx.y * 2 * a.workers + seg.slot) * kRows + 16 * (RB * set + rb) + n) * (D + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int ch = kCh * (4 * g + j);
+          if (ch >= D) continue;
+#pragma unroll
+          for (int t = 0; t < kCh; t += 4) {
+            const f32x4 y = f32x4{o[rb][t][j], o[rb][t + 1][j], o[rb][t + 2][j], o[rb][t + 3][j]};
+            if (seg.alone)
+              *reinterpret_cast<u32x2*>(a.out + (seg.q_row + r) * D + ch + t) =
+                  __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+            else
+              *reinterpret_cast<f32x4*>(pr + ch + t) = y;
+          }
+        }
+        if (g == 0) {
+          if (!seg.alone) pr[D] = lse2;
+          else if (a.lse) a.lse[seg.q_row + r] = lse2 * 0.69314718055994531f;
+        }
       }
     }
+    __syncthreads();
   } while (walk.advance(a));
 }
 
@@ -705,7 +764,7 @@ template <int D, int ROWS>
 hipError_t cache4_attn_rows(const Cache4AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.workers, (unsigned)a.row_blocks);
   if constexpr (ROWS > 32) {
-    cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsC, 0, s>>>(a);
+    cache4_rows_kernel<D, ROWS / 64><<<grid, kThreadsMany, 0, s>>>(a);
   } else {
     if (ROWS == 16 && a.eight) cache4_attn_kernel<D, 1, 8><<<grid, 512, 0, s>>>(a);
     else cache4_attn_kernel<D, ROWS / 16, 4><<<grid, kThreadsC, 0, s>>>(a);

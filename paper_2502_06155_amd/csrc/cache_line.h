@@ -92,8 +92,8 @@ struct CacheLine {
 
 // max and sum over the four lane groups that hold one query row's tokens.
 __device__ __forceinline__ float group_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);  // groups 0 0 2 2, 1 1 3 3
+  return pair_max(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
 }
 __device__ __forceinline__ float group_sum(float x) {
   x += __shfl_xor(x, 16);
