@@ -205,10 +205,15 @@ def head_rope_grad(q, k, v, dq, dk, dv, positions=None, freqs=None, dims=None, l
     no weight or bias, is None; v's own values are not read, only its shape."""
     spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, (q_weight, k_weight, q_bias, k_bias),
                                           norm, eps, lens)
+    rows, grads, to, outs = [None, None, None], [None, None, None], [None, None, None], out
     if out is None:
+        # Rows of one new tensor: their places are known.
         heads = [n if t is not None else 0 for t, n in ((q, H), (k, Hkv), (v, Hkv))]
-        out = torch.empty((B, S, sum(heads), d), dtype=torch.bfloat16, device=device).split(heads, 2)
-    rows, grads, to, outs = [None, None, None], [None, None, None], [None, None, None], [None, None, None]
+        n = sum(heads)
+        one = torch.empty((B, S, n, d), dtype=torch.bfloat16, device=device)
+        outs = one.split_with_sizes(heads, 2)
+        place, token = one.data_ptr(), n * d
+    outs = [y if t is not None else None for t, y in zip((q, k, v), outs)]
     for i, (t, g) in enumerate(((q, dq), (k, dk), (v, dv))):
         if (t is None) != (g is None):
             raise ValueError(f"{'qkv'[i]} and d{'qkv'[i]} go together")
@@ -218,13 +223,17 @@ def head_rope_grad(q, k, v, dq, dk, dv, positions=None, freqs=None, dims=None, l
         rows[i] = _rows(t, "qkv"[i], B, S, n, d, device)
         _want(g, ("dq", "dk", "dv")[i], (B, n, S, d), torch.bfloat16, device)
         grads[i] = g.data_ptr()
-        outs[i] = out[i]
-        to[i] = _rows(out[i], "out", B, S, n, d, device)
+        if out is None:
+            to[i] = _PACKED_ROWS.pack(place, S * token, token, d)
+            place += 2 * n * d
+        else:
+            to[i] = _rows(out[i], "out", B, S, n, d, device)
     sums, at = [None, None, None, None], [None, None, None, None]
-    for i, w in enumerate((q_weight, k_weight, q_bias, k_bias)):
-        if w is not None and (k if i % 2 else q) is not None:
-            sums[i] = torch.empty_like(w)
-            at[i] = sums[i].data_ptr()
+    wanted = [i for i, w in enumerate((q_weight, k_weight, q_bias, k_bias))
+              if w is not None and (k if i % 2 else q) is not None]
+    if wanted:
+        for i, w in zip(wanted, torch.empty((len(wanted), d), dtype=torch.float32, device=device).unbind()):
+            sums[i], at[i] = w, w.data_ptr()
     n = 0 if norm is None else _grad_workspace(B, S, H, Hkv, d)
     with _on(device):
         workspace = _workspace(n, device)
