@@ -184,7 +184,9 @@ def check(out, lse, q, cache, table, lens, scale=None):
     (2, 3, 3, 4, 96, [2, 700]),       # fewer tokens than rows: some rows see none
     (2, 16, 2, 2, 128, [193, 3000]),
     (2, 20, 1, 1, 64, [500, 77]),     # more than 16 rows
-    (1, 16, 1, 5, 96, [900]),         # 80 rows: three passes
+    (1, 9, 1, 3, 96, [2900]),         # 27 rows
+    (2, 8, 1, 4, 128, [1500, 66]),    # 32 rows, a last page of which the second half is empty
+    (1, 16, 1, 5, 96, [900]),         # 80 rows: one pass of 128
     (2, 34, 2, 3, 128, [130, 257]),
     (20, 6, 3, 1, 64, [0, 5, 0, 0, 300, 128, 0, 1, 640, 2, 0, 256, 7, 0, 90, 0, 0, 1280, 3, 0]),
 ])
@@ -277,8 +279,22 @@ def test_marked_tokens_reach_the_rows_that_see_them_alone(d, width):
     assert got[:, :3, 3:].isnan().all() and lse[:, :3, 3:].isnan().all()
 
 
+@pytest.mark.parametrize("width", [4, 40])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("N", [7, 20, 40])  # 21 rows a key head: half a page at a time; 60 and 120: a page's tokens shared by two waves
+def test_marked_tokens_among_many_rows(N, d, width):
+    rng = np.random.default_rng(N + d + width)
+    cache, table = held(rng, 1, 3, d, [400], width)
+    cache[2][table[0, 3], 0, :, 398 - 384] = 255  # the last but one: two rows see it
+    cache[2][table[0, 0], 2, :, 100] = 255        # in the second half of the first page: every row
+    q = bits(rng, 1, 9, N, d)
+    got, lse = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32([400]), return_lse=True)
+    check(got, lse, q, cache, table, [400])
+    assert got[:, :3, N - 2:].isnan().all() and not got[:, :6, :N - 2].isnan().any() and got[:, 6:].isnan().all()
+
+
 @pytest.mark.parametrize("B,H,Hkv,N,d,lens,width", [
-    (1, 8, 2, 40, 128, [3000], 40),             # five passes of 32 rows, each a share of the workgroups
+    (1, 8, 2, 40, 128, [3000], 40),             # 160 rows: two passes, each a share of the workgroups
     (2, 8, 2, 300, 64, [900, 333], 40),         # as many tokens as one sequence holds, fewer than the other's
     (1, 4, 4, 257, 96, [257], None),            # short tables: a workgroup a segment and pass
     (3, 8, 1, 129, 128, [128, 0, 2100], 40),    # rows before a sequence's start, and none at all
@@ -299,9 +315,9 @@ def test_chunks_of_a_prompt(B, H, Hkv, N, d, lens, width):
     (1, 4, 4, 1, 64, 40, 40),
     (3, 8, 2, 1, 128, 40, 23),
     (2, 12, 3, 4, 96, 33, 33),
-    (2, 40, 2, 2, 128, 20, 20),    # 40 rows a key head: two passes
+    (2, 40, 2, 2, 128, 20, 20),    # 40 rows a key head
     (40, 6, 3, 1, 64, 20, 20),     # more segments than a wave scans at once
-    (1, 8, 2, 70, 64, 40, 30),     # nine passes that share the workgroups
+    (1, 8, 2, 70, 64, 40, 30),     # three passes that share the workgroups
     (2, 8, 2, 1, 96, 5, 5),        # short tables
 ])
 def test_a_page_table_for_each_key_head(B, H, Hkv, N, d, width, most):
