@@ -91,6 +91,14 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int e) {
   return p;
 }
 
+// A value's place where pairs are anywhere in the row: formed once a workgroup, by a thread a value, and kept in LDS.
+struct __attribute__((aligned(16))) PlaceEntry {
+  double f;         // turns per position
+  uint16_t from;    // byte of the partner in its row
+  uint16_t axis;
+  float sign;       // of the partner's sine
+};
+
 // The lane's 8 values in the rotation. Angles: turns = position * (frequency / 2 pi) in fp64, right to 2^-53 of the
 // angle however far the position, then the fraction alone, in fp32, for v_sin_f32 and v_cos_f32 (which take
 // turns; off by at most 1.3e-7 in [-0.5, 0.5]).
@@ -102,8 +110,24 @@ struct Turns {
   int from[ROT == kAny ? 8 : 1];  // byte of the partner in its row, or the lane that holds all eight
   float sign[ROT == kAny ? 8 : 1];
 
-  __device__ __forceinline__ void place(const RopeArgs& a, int l) {
-    if constexpr (ROT == kWhole) {
+  // (With kAny all threads of a workgroup call it together.)
+  __device__ __forceinline__ void place(const RopeArgs& a, int l, PlaceEntry* entries) {
+    if constexpr (ROT == kAny) {
+      if (threadIdx.x < D) {
+        const Place p = place_of(a, threadIdx.x);
+        const double x = a.freqs[p.pair];
+        entries[threadIdx.x] = PlaceEntry{p.turned ? x * kTurn : 0., (uint16_t)(2 * p.partner), (uint16_t)p.axis, p.second ? 1.f : -1.f};
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const PlaceEntry p = entries[min(8 * l + i, D - 1)];
+        f[i] = p.f;
+        axis[i] = p.axis;
+        from[i] = p.from;
+        sign[i] = 8 * l >= D ? 0.f : p.sign;
+      }
+    } else if constexpr (ROT == kWhole) {
       // Eight values of one axis and half, their pairs one after the other. (A lane behind the row takes
       // nothing from it: sums over the row's lanes add it too.)
       const Place p = place_of(a, min(8 * l, D - 8));
@@ -115,19 +139,15 @@ struct Turns {
         const double x = a.freqs[p.turned ? p.pair + i : 0];
         f[i] = p.turned ? x * kTurn : 0.;
       }
-    } else if constexpr (ROT != kStill) {
+    } else if constexpr (ROT == kNext) {
       Place p[kAngles];
 #pragma unroll
-      for (int i = 0; i < kAngles; ++i) p[i] = place_of(a, min(8 * l + (ROT == kNext ? 2 * i : i), D - 1));
+      for (int i = 0; i < kAngles; ++i) p[i] = place_of(a, min(8 * l + 2 * i, D - 1));
 #pragma unroll
       for (int i = 0; i < kAngles; ++i) {
         const double x = a.freqs[p[i].pair];
         f[i] = p[i].turned ? x * kTurn : 0.;
         axis[i] = p[i].axis;
-        if constexpr (ROT == kAny) {
-          from[i] = 2 * p[i].partner;
-          sign[i] = 8 * l >= D ? 0.f : p[i].second ? 1.f : -1.f;
-        }
       }
     }
   }
@@ -197,7 +217,7 @@ __device__ __forceinline__ void load8(const float* w, int l, float none, Floats8
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = w ? w[e0 + e] : none;
 }
-// The same of the values' partners.
+// The same of the values' partners. (kAny: only where there is no array; with one they come from LDS.)
 template <int D, int ROT>
 __device__ __forceinline__ void load_partners(const float* w, int l, float none, const Turns<D, ROT>& t, Floats8& x) {
   if constexpr (ROT == kNext) {
@@ -207,12 +227,9 @@ __device__ __forceinline__ void load_partners(const float* w, int l, float none,
     for (int e = 0; e < 8; ++e) x[e] = own[e ^ 1];
   } else if constexpr (ROT == kWhole) {
     load8<D>(w, t.from[0], none, x);
-  } else if constexpr (ROT == kAny) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = w ? w[t.from[e] / 2] : none;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = ROT == kAny ? none : 0.f;
   }
 }
 
@@ -256,17 +273,22 @@ struct Token {
 // TB/s (a large copy 4.9 to 5.1); 17776 tokens, 144 heads of 64, layer norms, 132 us, 4.95 TB/s. Single tokens by their chain of
 // loads: 32 of them, 48 heads of 128, 4.8 us. Four rows of a lane are read together, the next four meanwhile; without
 // the next ones two together took 504 us and one 556. Results past the caches: 480, not worth a second kernel.
+// With pairs anywhere in the row a workgroup forms the places, and puts the weights, into LDS first: 62982 tokens, 9 heads of 96
+// 56 us (places by every lane for its 8 values 70, weights from memory 60); 8 tokens, 10 heads of 64 4.4 us (5.3).
 constexpr int kAhead = 4;
 
 template <int D, int NORM, int ROT>
 __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeArgs a) {
   constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
   __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAhead * 64 : 1];
+  __shared__ PlaceEntry s_place[ROT == kAny ? D : 1];
+  __shared__ float s_weights[2][ROT == kAny && NORM != kNone ? 2 * D : 1];  // of q and k, weights and biases
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l = lane % L;
   const bool in_row = 8 * l < D;
   const int64_t token0 = ((int64_t)blockIdx.x * kRopeWaves + wave) * kTokens;
-  if (token0 >= (int64_t)a.B * a.S) return;
+  const bool none = token0 >= (int64_t)a.B * a.S;
+  if (ROT != kAny && none) return;
   const Token tok(a, token0 + lane / L);
   const bool writes = tok.have && in_row;
   const int at = in_row ? 8 * l : D - 8;  // lanes behind a row read its last values, as zeros
@@ -295,11 +317,31 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
   load(first, in);
 
   Turns<D, ROT> turns;
-  turns.place(a, l);
+  if constexpr (ROT == kAny && NORM != kNone) {
+    for (int i = threadIdx.x; i < 2 * D; i += 64 * kRopeWaves) {
+      const int kind = i / D, e = i % D;
+      s_weights[kind][e] = a.weight[kind] ? a.weight[kind][e] : 1.f;
+      if (NORM == kLayer) s_weights[kind][D + e] = a.bias[kind] ? a.bias[kind][e] : 0.f;
+    }
+  }
+  turns.place(a, l, s_place);
+  if (none) return;
   // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean; A, B and C of the kind `ready`, its weights and
   // biases times the token's cosines and sines.
   Floats8 A, Bp, C, w, wp, bs, bp;
   auto weights = [&](int kind) {
+    if constexpr (ROT == kAny && NORM != kNone) {  // (lanes behind the row: signs of 0)
+      const float* of = s_weights[kind];
+      const int e0 = min(8 * l, D - 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = of[e0 + e];
+        wp[e] = of[turns.from[e] / 2];
+        bs[e] = NORM == kLayer ? of[D + e0 + e] : 0.f;
+        bp[e] = NORM == kLayer ? of[D + turns.from[e] / 2] : 0.f;
+      }
+      return;
+    }
     const float* weight = NORM == kNone ? nullptr : a.weight[kind];
     const float* bias = NORM == kLayer ? a.bias[kind] : nullptr;
     load8<D>(weight, l, 1.f, w);
@@ -371,6 +413,7 @@ template <int D, int NORM, int ROT>
 __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const RopeArgs a) {
   constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
   __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * 64 : 1];
+  __shared__ PlaceEntry s_place[ROT == kAny ? D : 1];
   __shared__ float s_sum[kRopeWaves][2][D];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l = lane % L;
@@ -388,7 +431,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
   Turns<D, ROT> turns;
   Floats8 w, dw, db;
   if (kind < 2) {
-    turns.place(a, l);
+    turns.place(a, l, s_place);
     load8<D>(NORM == kNone ? nullptr : a.weight[kind], l, 1.f, w);
   }
 #pragma unroll

@@ -171,8 +171,8 @@ int64_t groups_of(const RopeArgs& a) {
 // Heads that a wave takes of its tokens: few, so that kFewWaves waves form (and two at least: one after the other
 // they wait for less); past that a wave's start, its angles and weights, should be worth `worth` heads, up to kManyWaves.
 // 2 sequences of 777, 10 heads, d = 64: 4.8 us with two heads a wave, 6.3 with four, 7.5 with eight. 4000 tokens, 72 heads, d = 96,
-// pairs anywhere in the row: 38.5 with 5 heads a wave, 29.4 with 9, 24.5 with 36; 17776 tokens, 144 heads, d = 64, neighbours:
-// 150 us with 144, 136 with 48, 132 with 21.
+// pairs anywhere in the row: 23.6 with 18 heads a wave, 24.9 with 36; 17776 tokens, 144 heads, d = 64, neighbours: 150 us with 144, 136
+// with 48, 132 with 21.
 constexpr int64_t kFewWaves = 2048, kManyWaves = 16 * 1024;
 int heads_per_wave(const RopeArgs& a, int heads) {
   const int64_t groups = groups_of(a);
@@ -181,7 +181,7 @@ int heads_per_wave(const RopeArgs& a, int heads) {
     return (heads + parts - 1) / parts;
   };
   const bool near = a.layout == TA_ROPE_NONE || a.layout == TA_ROPE_INTERLEAVED;
-  const int64_t worth = near ? 12 : a.whole ? 18 : 36;
+  const int64_t worth = near ? 12 : 18;
   return (int)std::max<int64_t>({std::min(heads, 2), of(kManyWaves), std::min(of(kFewWaves), worth)});
 }
 
