@@ -355,6 +355,29 @@ def test_on_another_stream_and_under_any_workspace_contents():
         assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
 
 
+@pytest.mark.parametrize("layout,dims", [("halves", (128,)), ("split", (10, 36, 36))])
+def test_offsets_past_32_bits(layout, dims):
+    """A projection of more than 2^32 bytes, and results of as many: its last tokens as in a call of their own."""
+    S, H, Hkv, d, last = 165000, 96, 4, 128, 77
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(1, S, H + 2 * Hkv, d, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() * 2 > 2 ** 32
+    x.normal_(generator=gen)
+    p = torch.randint(0, 1000, (S, len(dims)), generator=gen, device="cuda").to(torch.int32)
+    how = dict(freqs=ta.rope_freqs(dims), dims=dims, layout=layout, norm="rms",
+               q_weight=1 + 0.2 * torch.randn(d, generator=gen, device="cuda"))
+    cut = lambda t: (t[:, :, :H], t[:, :, H:H + Hkv], t[:, :, H + Hkv:])  # noqa: E731
+    got = ta.head_rope(*cut(x), positions=p, **how)
+    tail = cut(x[:, S - last:])
+    want = ta.head_rope(*tail, positions=p[S - last:].contiguous(), **how)
+    for a, b in zip(got, want):
+        assert torch.equal(a[:, :, S - last:], b)
+    dx = ta.head_rope_grad(*cut(x), *got, positions=p, **how)
+    part = ta.head_rope_grad(*tail, *want, positions=p[S - last:].contiguous(), **how)
+    for a, b in zip(dx[:3], part[:3]):
+        assert torch.equal(a[:, S - last:], b)
+
+
 def test_the_functions_of_the_c_abi():
     c = Case(2, 30, 4, 2, 64, "layer", "split", (32, 16), lens=[30, 8])
     x, dy, args = to_dev(c.x), [to_dev(g) for g in c.dy], c.args()
