@@ -469,12 +469,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
 // widened once, K by four waves and V by the other four, into LDS, where the matrix operands of all rows come from.
 // While a page is multiplied the next one is widened into the other half of the LDS, and the one behind it is on its way.
 // Bound by the vector work beside the products (exponentials, widening): one sequence of 32768, 32 heads on 8 of 128, 2048 rows
-// 1121 us (981 TFLOP/s), 512 workgroups of four waves that had a page's tokens to themselves 1166. A step's 128 rows take 2.3 us a
-// page at d = 128, 2.7 at 96. Waves of K widening before their products and waves of V behind them: 1261; two sets of 48 rows, four
+// 1107 us (993 TFLOP/s), 512 workgroups of four waves that had a page's tokens to themselves 1166. 128 rows take 2.3 us a
+// page at d = 128, 2.6 at 96 (of which 2.0 for scores, exponentials and products, 0.5 for widening). Waves of K widening before their products and waves of V behind them: 1261; two sets of 48 rows, four
 // waves each, for 96 rows: 36.3 us for 32.5, the joins of four waves cost more than the even rows give.
 //   K: row 16 i + n of the tile is the token that row n of instruction group i computes, 32 (i / 2) + 8 (n / 4) + 4 (i % 2) + n % 4,
-//   so that the scores of groups 2 c and 2 c + 1 are, in lane group g, tokens 32 c + 8 g .. + 7: P^T of step c. Rows are 16
-//   bytes longer than their d values, which puts 16 rows' pieces on different banks.
+//   so that the scores of groups 2 c and 2 c + 1 are, in lane group g, tokens 32 c + 8 g .. + 7: P^T of step c. The 16-byte pieces
+//   of a row lie at places exchanged by the row's number (d = 64: in order, rows 16 bytes longer than their values), which puts
+//   16 rows' pieces on different banks (2048 rows over 32768: 1107 us, 1124 with longer rows).
 //   V^T: a row of 128 tokens for each channel, its 16-byte pieces of 8 tokens at places exchanged by the channel's
 //   number (key): both the writes (16 channels' words of the same 8 tokens) and the reads (row n of instruction t: channel 8 n + t,
 //   4 n + t at d = 64) fall on different banks.
@@ -485,7 +486,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
   constexpr int kParts = 2, kT = kBlock / kParts;  // of a page, and their tokens
   constexpr int kGroups = kT / 16, kSteps = kT / 32;
   constexpr int kCh = D == 64 ? 4 : 8;
-  constexpr int kPitch = D + 8;                       // of a K row, in values
+  constexpr int kPitch = D == 64 ? 72 : 128;          // of a K row, in values
   constexpr int kHalf = kThreadsMany / 2;             // threads that widen K, and V
   constexpr int kKUnits = kBlock * (D / kGroup);      // 32 values of a token
   constexpr int kKPer = (kKUnits + kHalf - 1) / kHalf;
@@ -504,6 +505,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
   const int rows = a.G * a.N, row0 = blockIdx.y * kRows + 16 * RB * set;
   const bool works = row0 < rows;
   const bool for_k = wave < 4;  // what it widens
+  auto k_key = [](int row) { return D == 64 ? 0 : row & 15; };  // places of a K row's pieces
   const int unit = tid % kHalf;
   const int v_word = unit % kWords, v_part = unit / kWords;  // tokens 8 v_part .. + 7
 
@@ -526,6 +528,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
     };
     u32x4 cw[2];     // K: 16 bytes of codes; V: words of 8 tokens
     uint32_t sc[2];  // their scales
+    // (Every thread loads, the last unit again where there are fewer: without a branch the loads stay on their way.)
     auto load = [&]() {
       const size_t ph = (size_t)page * a.Hkv + seg.h;
       if (for_k) {
@@ -533,19 +536,18 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
         const uint8_t* ke = a.k_exps + ph * kBlock * (D / kGroup);
 #pragma unroll
         for (int i = 0; i < kKPer; ++i) {
-          const int u = unit + kHalf * i, t = u / (D / kGroup), grp = u % (D / kGroup);
-          if (u < kKUnits) {
-            cw[i] = *reinterpret_cast<const u32x4*>(k + (uint32_t)(t * (D / 2) + 16 * grp));
-            sc[i] = ke[(uint32_t)(grp * kBlock + t)];
-          }
+          const int u = min(unit + kHalf * i, kKUnits - 1), t = u / (D / kGroup), grp = u % (D / kGroup);
+          cw[i] = *reinterpret_cast<const u32x4*>(k + (uint32_t)(t * (D / 2) + 16 * grp));
+          sc[i] = ke[(uint32_t)(grp * kBlock + t)];
         }
-      } else if (unit < kVUnits) {
+      } else {
         const uint8_t* v = a.v_pages + ph * kBlock * (D / 2);
         const uint8_t* ve = a.v_exps + ph * kBlock * (D / kGroup);
+        const int u = min(unit, kVUnits - 1), word = u % kWords, part = u / kWords;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          cw[i / 4][i % 4] = *reinterpret_cast<const uint32_t*>(v + (uint32_t)((8 * v_part + i) * (D / 2) + 4 * v_word));
-        const u32x2 vs = *reinterpret_cast<const u32x2*>(ve + (uint32_t)(v_word / 4 * kBlock + 8 * v_part));
+          cw[i / 4][i % 4] = *reinterpret_cast<const uint32_t*>(v + (uint32_t)((8 * part + i) * (D / 2) + 4 * word));
+        const u32x2 vs = *reinterpret_cast<const u32x2*>(ve + (uint32_t)(word / 4 * kBlock + 8 * part));
         sc[0] = vs[0];
         sc[1] = vs[1];
       }
@@ -560,7 +562,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
             const float f = scale_of(sc[i]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<u32x4*>(s_k + row * kPitch + 32 * grp + 8 * e) = decode8(cw[i][e], f);
+              *reinterpret_cast<u32x4*>(s_k + row * kPitch + 8 * ((4 * grp + e) ^ k_key(row))) = decode8(cw[i][e], f);
           }
         }
       } else if (unit < kVUnits) {
@@ -634,7 +636,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
         for (int i = 0; i < kGroups; ++i)
 #pragma unroll
           for (int m = 0; m < kSl; ++m) {
-            const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_k + (16 * i + n) * kPitch + 32 * m + 8 * g));
+            const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_k + (16 * i + n) * kPitch + 8 * ((4 * m + g) ^ k_key(n))));
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
               s[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][m], m == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][i], 0, 0, 0);
@@ -687,8 +689,8 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
         for (int c = 0; c < kSteps; ++c)
 #pragma unroll
           for (int t = 0; t < kCh; ++t) {
-            // (d = 96: rows 12 to 15 of an instruction are no channels and read those of row 11.)
-            const int key = D == 96 ? min(n, 11) : n;
+            // (d = 96: rows 12 to 15 of an instruction are no channels and read those of rows 0 to 3.)
+            const int key = D == 96 && n > 11 ? n - 12 : n;
             const bf16x8 vf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_v + (kCh * key + t) * kBlock + 8 * ((kT / 8 * part + 4 * c + g) ^ key)));
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
