@@ -29,6 +29,8 @@ struct Shape {
   static constexpr int lanes = D == 64 ? 8 : 16;  // of a row
   static constexpr int tokens = 64 / lanes;
   static_assert(tokens == rope_tokens(D), "tokens of a wave");
+  // A row in LDS: its 16-byte pieces and one of zeros (d = 96: lanes behind the row write it).
+  static constexpr int none = D / 8, pitch = D == 96 ? lanes : none + 1, pieces = tokens * pitch;
 };
 
 // The sum over a row's lanes, in all of them: neighbours, pairs, then mirrored halves (of 8 and of 16 lanes).
@@ -94,7 +96,7 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int e) {
 // A value's place where pairs are anywhere in the row: formed once a workgroup, by a thread a value, and kept in LDS.
 struct __attribute__((aligned(16))) PlaceEntry {
   double f;         // turns per position
-  uint16_t from;    // byte of the partner in its row
+  uint16_t from;    // byte of the partner in its row, of the zeros for a value that is not turned
   uint16_t axis;
   float sign;       // of the partner's sine
 };
@@ -107,8 +109,10 @@ struct Turns {
   static constexpr int kAngles = ROT == kNext ? 4 : 8;
   double f[ROT == kStill ? 1 : kAngles];
   int axis[ROT == kStill ? 1 : ROT == kWhole ? 1 : kAngles];
-  int from[ROT == kAny ? 8 : 1];  // byte of the partner in its row, or the lane that holds all eight
+  int from[ROT == kAny ? 8 : 1];  // byte of the partner in its row, or the piece with all eight
   float sign[ROT == kAny ? 8 : 1];
+  bool every;  // kNext: all values of a head are turned
+  int left;    // kNext: how many of the lane's are
 
   // (With kAny all threads of a workgroup call it together.)
   __device__ __forceinline__ void place(const RopeArgs& a, int l, PlaceEntry* entries) {
@@ -116,7 +120,8 @@ struct Turns {
       if (threadIdx.x < D) {
         const Place p = place_of(a, threadIdx.x);
         const double x = a.freqs[p.pair];
-        entries[threadIdx.x] = PlaceEntry{p.turned ? x * kTurn : 0., (uint16_t)(2 * p.partner), (uint16_t)p.axis, p.second ? 1.f : -1.f};
+        entries[threadIdx.x] = PlaceEntry{p.turned ? x * kTurn : 0., (uint16_t)(p.turned ? 2 * p.partner : 16 * Shape<D>::none),
+                                          (uint16_t)p.axis, p.second ? 1.f : -1.f};
       }
       __syncthreads();
 #pragma unroll
@@ -131,7 +136,7 @@ struct Turns {
       // Eight values of one axis and half, their pairs one after the other. (A lane behind the row takes
       // nothing from it: sums over the row's lanes add it too.)
       const Place p = place_of(a, min(8 * l, D - 8));
-      from[0] = p.partner / 8;
+      from[0] = p.turned ? p.partner / 8 : Shape<D>::none;
       axis[0] = p.axis;
       sign[0] = 8 * l >= D ? 0.f : p.second ? 1.f : -1.f;
 #pragma unroll
@@ -140,6 +145,8 @@ struct Turns {
         f[i] = p.turned ? x * kTurn : 0.;
       }
     } else if constexpr (ROT == kNext) {
+      every = a.turned >= D;
+      left = a.turned - 8 * l;
       Place p[kAngles];
 #pragma unroll
       for (int i = 0; i < kAngles; ++i) p[i] = place_of(a, min(8 * l + 2 * i, D - 1));
@@ -184,18 +191,25 @@ struct Turns {
       }
     }
   }
-  // The partners of the lane's 8 values of a row. `row`: the 16-byte pieces of the wave's rows in LDS; only
-  // this wave writes and reads them.
+  // The zeros behind the pieces of the wave's rows.
+  __device__ __forceinline__ static void clear(u32x4* rows, int n, int lane) {
+    if (D != 96 && lane < n * Shape<D>::tokens) rows[lane * Shape<D>::pitch + Shape<D>::none] = u32x4{0u, 0u, 0u, 0u};
+  }
+  // The partners of the lane's 8 values of a row, 0 for those that are not turned: their sine is 0, but an infinity times
+  // it is not. `row`: the 16-byte pieces of the wave's rows in LDS; only this wave writes and reads them.
   __device__ __forceinline__ void partners(const u32x4& w, const Floats8& x, u32x4* row, int lane, Floats8& xp) const {
     constexpr int L = Shape<D>::lanes;
     if constexpr (ROT == kNext) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) xp[e] = x[e ^ 1];
+      if (every) return;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xp[e] = e < left ? xp[e] : 0.f;
     } else if constexpr (ROT == kWhole || ROT == kAny) {
-      row[lane] = w;
+      u32x4* mine = row + lane / L * Shape<D>::pitch;
+      mine[lane % L] = w;
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const u32x4* mine = row + lane / L * L;
       if constexpr (ROT == kWhole) {
         widen(mine[from[0]], xp);
       } else {
@@ -217,16 +231,19 @@ __device__ __forceinline__ void load8(const float* w, int l, float none, Floats8
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = w ? w[e0 + e] : none;
 }
-// The same of the values' partners. (kAny: only where there is no array; with one they come from LDS.)
+// The same of the values' partners, 0 for values that are not turned. (kAny: only where there is no array; with one they come
+// from LDS.)
 template <int D, int ROT>
 __device__ __forceinline__ void load_partners(const float* w, int l, float none, const Turns<D, ROT>& t, Floats8& x) {
   if constexpr (ROT == kNext) {
     Floats8 own;
     load8<D>(w, l, none, own);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = own[e ^ 1];
+    for (int e = 0; e < 8; ++e) x[e] = e < t.left ? own[e ^ 1] : 0.f;
   } else if constexpr (ROT == kWhole) {
     load8<D>(w, t.from[0], none, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = t.from[0] < Shape<D>::none ? x[e] : 0.f;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = ROT == kAny ? none : 0.f;
@@ -279,10 +296,12 @@ constexpr int kAhead = 4;
 
 template <int D, int NORM, int ROT>
 __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeArgs a) {
-  constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
-  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAhead * 64 : 1];
+  constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens, kPieces = Shape<D>::pieces;
+  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * kAhead * kPieces : 1];
   __shared__ PlaceEntry s_place[ROT == kAny ? D : 1];
-  __shared__ float s_weights[2][ROT == kAny && NORM != kNone ? 2 * D : 1];  // of q and k, weights and biases
+  // Of q and k: weights, biases, each with the partner's of a value that is not turned, 0, behind it.
+  constexpr int kPitch = D + 1;
+  __shared__ float s_weights[2][ROT == kAny && NORM != kNone ? 2 * kPitch : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l = lane % L;
   const bool in_row = 8 * l < D;
@@ -292,7 +311,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
   const Token tok(a, token0 + lane / L);
   const bool writes = tok.have && in_row;
   const int at = in_row ? 8 * l : D - 8;  // lanes behind a row read its last values, as zeros
-  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * 64 : 0);
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * kAhead * kPieces : 0);
 
   // Heads of q, k and v in a line; this wave's are first .. last - 1. A step takes up to kAhead heads of one kind,
   // and the next step's rows are on their way meanwhile (the first one's while the angles are formed).
@@ -318,14 +337,15 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
 
   Turns<D, ROT> turns;
   if constexpr (ROT == kAny && NORM != kNone) {
-    for (int i = threadIdx.x; i < 2 * D; i += 64 * kRopeWaves) {
-      const int kind = i / D, e = i % D;
-      s_weights[kind][e] = a.weight[kind] ? a.weight[kind][e] : 1.f;
-      if (NORM == kLayer) s_weights[kind][D + e] = a.bias[kind] ? a.bias[kind][e] : 0.f;
+    for (int i = threadIdx.x; i < 2 * kPitch; i += 64 * kRopeWaves) {
+      const int kind = i / kPitch, e = i % kPitch;
+      s_weights[kind][e] = e == D ? 0.f : a.weight[kind] ? a.weight[kind][e] : 1.f;
+      if (NORM == kLayer) s_weights[kind][kPitch + e] = e == D || !a.bias[kind] ? 0.f : a.bias[kind][e];
     }
   }
   turns.place(a, l, s_place);
   if (none) return;
+  if constexpr (ROT >= kWhole) turns.clear(rows, kAhead, lane);
   // y_e = r (x_e A_e + x_partner B_e) + C_e with x less its mean; A, B and C of the kind `ready`, its weights and
   // biases times the token's cosines and sines.
   Floats8 A, Bp, C, w, wp, bs, bp;
@@ -337,8 +357,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
       for (int e = 0; e < 8; ++e) {
         w[e] = of[e0 + e];
         wp[e] = of[turns.from[e] / 2];
-        bs[e] = NORM == kLayer ? of[D + e0 + e] : 0.f;
-        bp[e] = NORM == kLayer ? of[D + turns.from[e] / 2] : 0.f;
+        bs[e] = NORM == kLayer ? of[kPitch + e0 + e] : 0.f;
+        bp[e] = NORM == kLayer ? of[kPitch + turns.from[e] / 2] : 0.f;
       }
       return;
     }
@@ -379,7 +399,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
       if (kind < 2 && (NORM != kNone || ROT != kStill)) {
         Floats8 x, xp, y;
         widen(in[u], x);
-        turns.partners(in[u], x, rows + (ROT >= kWhole ? 64 * u : 0), lane, xp);
+        turns.partners(in[u], x, rows + (ROT >= kWhole ? kPieces * u : 0), lane, xp);
         float mean;
         const float r = norm_factor<D, NORM>(a.eps, in_row, x, mean);
 #pragma unroll
@@ -412,7 +432,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
 template <int D, int NORM, int ROT>
 __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const RopeArgs a) {
   constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
-  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * 64 : 1];
+  __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * Shape<D>::pieces : 1];
   __shared__ PlaceEntry s_place[ROT == kAny ? D : 1];
   __shared__ float s_sum[kRopeWaves][2][D];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -424,7 +444,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
   const int heads = a.heads[kind], parts = (heads + a.heads_per - 1) / a.heads_per;
   const int64_t items = (int64_t)groups * parts, plane = (int64_t)a.S * D;
   const bool normed = NORM != kNone && kind < 2, turned = ROT != kStill && kind < 2;
-  u32x4* rows = s_rows + (ROT >= kWhole ? wave * 64 : 0);
+  u32x4* rows = s_rows + (ROT >= kWhole ? wave * Shape<D>::pieces : 0);
   const int at = 8 * l;
   const Rows x = a.x[kind], dx = a.dx[kind];
 
@@ -432,6 +452,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
   Floats8 w, dw, db;
   if (kind < 2) {
     turns.place(a, l, s_place);
+    if constexpr (ROT >= kWhole) turns.clear(rows, 1, lane);
     load8<D>(NORM == kNone ? nullptr : a.weight[kind], l, 1.f, w);
   }
 #pragma unroll

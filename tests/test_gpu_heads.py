@@ -280,6 +280,49 @@ def test_a_row_that_is_no_number_stays_alone():
         assert torch.equal(a[~bad], b[~bad])
 
 
+@pytest.mark.parametrize("norm", [None, "rms"])
+@pytest.mark.parametrize("layout,dims,d", [
+    ("interleaved", (32,), 64), ("interleaved", (6, 12, 12), 96), ("halves", (32,), 64), ("halves", (16, 32), 96),
+    ("halves", (20,), 128), ("split", (32, 32), 128), ("split", (10, 24), 96), ("split", (8,), 64)])
+def test_values_that_are_not_turned_take_nothing_from_others(layout, dims, d, norm):
+    """Infinities and NaN behind the turned values: each stays at its place, or (with a norm) reaches what the
+    formula says, and no neighbour; forward and gradients, in rows and in weights."""
+    R = sum(dims)
+    c = Case(1, 12, 2, 1, d, norm, layout, dims)
+    places = (R, R + 1, d - 8, d - 1)
+    for t, (bad, e) in enumerate((b, e) for b in (0x7F80, 0xFF80, 0x7FC0) for e in places):  # inf, -inf, NaN
+        c.x[0, t, :2, e] = bad
+    x = widen(c.x)
+    got = ta.head_rope(*c.parts(to_dev(c.x)), **c.args())
+    for name, part, y in zip("qk", c.parts(x), got):
+        with np.errstate(invalid="ignore"):
+            ref = oh.forward(part, weight=c.p[name + "_weight"], **c.how())
+        y = widen(from_dev(y))
+        assert np.array_equal(np.isnan(y), np.isnan(ref)) and np.array_equal(y[np.isinf(ref)], ref[np.isinf(ref)])
+        some = np.isfinite(ref)
+        mag = c.magnitudes(np.where(np.isfinite(part), part, 0), name).transpose(0, 2, 1, 3)
+        room = HALF * np.abs(ref) + 2.0 ** -16 * mag
+        assert (np.abs(y[some] - ref[some]) <= room[some]).all()
+        if norm is None:
+            assert np.array_equal(y[..., R:], ref[..., R:], equal_nan=True) and not np.isnan(y[..., :R]).any()
+    # gradients: of the rows without a norm; with one, of a weight for each value
+    c = Case(1, 12, 2, 1, d, norm, layout, dims, seed=1)
+    for t, e in enumerate(places):
+        c.dy[0][0, 1, t, e] = (0x7F80, 0x7FC0)[t % 2]
+    dx, _, _, dw, _, _, _ = ta.head_rope_grad(*c.parts(to_dev(c.x)), *(to_dev(g) for g in c.dy), **c.args())
+    if norm is None:
+        ref, _, _ = oh.backward(c.parts(widen(c.x))[0], widen(c.dy[0]), **c.how())
+        dx = widen(from_dev(dx))
+        assert np.array_equal(dx[..., R:], ref[..., R:], equal_nan=True) and np.isfinite(dx[..., :R]).all()
+    else:
+        bad = ~torch.isfinite(dw).cpu().numpy()
+        assert set(np.flatnonzero(bad)) == set(places)
+        c = Case(1, 5, 2, 1, d, norm, layout, dims)
+        c.p["q_weight"][R], c.p["q_weight"][d - 1] = np.inf, np.nan
+        y = widen(from_dev(ta.head_rope(*c.parts(to_dev(c.x)), **c.args())[0]))
+        assert set(np.flatnonzero(~np.isfinite(y).all((0, 1, 2)))) == {R, d - 1}
+
+
 def test_rows_of_zeros_and_of_large_values():
     c = Case(1, 8, 2, 1, 64, "layer", "interleaved", (64,))
     x = to_dev(c.x)
