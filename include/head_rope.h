@@ -96,7 +96,8 @@ int head_rope_fwd(const head_rope_spec* spec, const ta_rows* q, const ta_rows* k
  * and token strides) but share no value. q and k are the forward's inputs (only looked at with a norm; v is
  * not asked for). What was left out of the forward is NULL throughout.
  * dq_weight, dk_weight, dq_bias, dk_bias: fp32 [d], summed over all tokens and heads, or NULL where not wanted (biases
- * only with TA_NORM_LAYER, weights only with a norm). A sum's terms are added in an order that the sizes alone set.
+ * only with TA_NORM_LAYER, weights only with a norm). A sum's terms are added in an order that the sizes alone set, each
+ * through fewer than 512 additions in fp32, however many rows there are.
  */
 int head_rope_bwd_workspace(const head_rope_spec* spec, size_t* bytes);
 int head_rope_bwd(const head_rope_spec* spec, const ta_rows* q, const ta_rows* k, const void* dq_out,

@@ -428,13 +428,18 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_kernel(const RopeAr
 // before it: reading it earlier, beside that one's work, took 261 us, two rows at a time 357.
 // Workgroups first[kind] .. first[kind + 1] - 1 have the rows of q, k or v and deal out (tokens, heads) items among
 // their waves, so that the sums of weights and biases, kept in a lane's registers, leave few rows of partial
-// sums; they are added in an order that the sizes set.
+// sums; they are added in an order that the sizes set. After kChain rows a lane's sums go to LDS and start again, so that no
+// chain of additions grows with the call: 86400 tokens, 24 + 24 heads, have 344 rows a lane. (Four waves a SIMD unit, the workgroups
+// that are resident at once: without that bound layer norms with pairs anywhere take 130 registers, and 62982 tokens, 9 heads of 96,
+// 107 us for 75.)
+constexpr int kChain = 256;
 template <int D, int NORM, int ROT>
-__global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const RopeArgs a) {
+__global__ __launch_bounds__(64 * kRopeWaves, 4) void head_rope_grad_kernel(const RopeArgs a) {
   constexpr int L = Shape<D>::lanes, kTokens = Shape<D>::tokens;
   __shared__ u32x4 s_rows[ROT >= kWhole ? kRopeWaves * Shape<D>::pieces : 1];
   __shared__ PlaceEntry s_place[ROT == kAny ? D : 1];
   __shared__ float s_sum[kRopeWaves][2][D];
+  __shared__ float s_run[NORM == kLayer ? 16 : NORM != kNone ? 8 : 1][64 * kRopeWaves];  // a lane's sums of earlier chains
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l = lane % L;
   const bool in_row = 8 * l < D;
@@ -457,6 +462,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.f;
+  int chain = 0;  // rows in dw and db
+  bool runs = false;
   for (int64_t item = (int64_t)((int)blockIdx.x - a.first[kind]) * kRopeWaves + wave; item < items; item += waves) {
     const int part = (int)(item / groups);
     const Token tok(a, (item - (int64_t)part * groups) * kTokens + lane / L);
@@ -518,9 +525,30 @@ __global__ __launch_bounds__(64 * kRopeWaves) void head_rope_grad_kernel(const R
       if (writes) *reinterpret_cast<u32x4*>(d0 + h * dx.head) = out;
       if (h + 1 < h1) load(h + 1, xin, gin);
     }
+    chain += h1 - h0;
+    if (normed && chain + a.heads_per > kChain) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s_run[e][threadIdx.x] = runs ? s_run[e][threadIdx.x] + dw[e] : dw[e];
+        dw[e] = 0.f;
+        if constexpr (NORM == kLayer) {
+          s_run[8 + e][threadIdx.x] = runs ? s_run[8 + e][threadIdx.x] + db[e] : db[e];
+          db[e] = 0.f;
+        }
+      }
+      chain = 0;
+      runs = true;
+    }
   }
   if constexpr (NORM != kNone) {
     if (kind < 2 && a.part) {
+      if (runs) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          dw[e] += s_run[e][threadIdx.x];
+          if constexpr (NORM == kLayer) db[e] += s_run[8 + e][threadIdx.x];
+        }
+      }
       // Tokens of the wave, then waves, then (the second kernel) workgroups.
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

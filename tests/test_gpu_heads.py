@@ -398,6 +398,23 @@ def test_on_another_stream_and_under_any_workspace_contents():
         assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
 
 
+def test_long_sums_keep_their_small_terms():
+    """Sums over 26 million rows: a large term first in every lane's part, ones behind it. With rows of 1 and -1 normed rows
+    are the rows themselves, and all terms are exact. Chains: 256 rows a lane, its 4 parts, 3 additions of lanes, 4 of
+    waves, 64 and 16 of workgroups: 347 additions of 2^-24."""
+    S, H, d, first = 131072, 200, 64, 32768
+    one = torch.tensor([1.0, -1.0] * (d // 2), dtype=torch.bfloat16, device="cuda")
+    g = torch.ones(1, H, S, d, dtype=torch.bfloat16, device="cuda")
+    g[0, 0, :first] = 2.0 ** 24
+    w = torch.ones(d, device="cuda")
+    _, _, _, dw, _, db, _ = ta.head_rope_grad(one.expand(1, S, H, d), None, None, g, None, None, norm="layer", q_weight=w,
+                                              q_bias=torch.zeros_like(w), eps=1e-30)
+    want = first * 2.0 ** 24 + (S * H - first)
+    for got, sign in ((dw, one.double()), (db, 1.0)):
+        off = (got.double() * sign - want).abs().max().item()
+        assert off <= 347 * 2.0 ** -24 * want, off / want
+
+
 @pytest.mark.parametrize("layout,dims", [("halves", (128,)), ("split", (10, 36, 36))])
 def test_offsets_past_32_bits(layout, dims):
     """A projection of more than 2^32 bytes, and results of as many: its last tokens as in a call of their own."""
