@@ -48,7 +48,8 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
 
 /*
  * Attention of the last N tokens of each sequence over its pages, as cache_attn_fwd (per_head among it). V scales
- * above 252 in a page that is attended to may make all its rows NaN.
+ * above 252 in a page that is attended to may make all its rows NaN. Logits scale * <q, k> may be up to 2^126 in magnitude; a
+ * logit is a number of fp32, and weights are off by up to 2^-23 of its magnitude, as the log-sum-exp is.
  */
 int cache4_attn_fwd_workspace(int B, int H, int Hkv, int N, int d, int max_pages, size_t* bytes);
 int cache4_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const void* k_scales,

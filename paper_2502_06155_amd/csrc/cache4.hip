@@ -384,12 +384,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
             for (int t = 0; t < kCh; ++t) o[rb][t] *= alpha;
             m_ref[rb] = m_new;
           }
+          float c = a.c;
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(is_far(m_ref[rb])) != 0, 0)) {
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) s[rb][i] *= c;
+            c = 1.f;
+          }
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
+              const float x = fast_exp2(fmaf(s[rb][i][j], c, -m_ref[rb]));
               sum += x;
               pf[rb][(kGroups * j + i) / 8][(kGroups * j + i) % 8] = (__bf16)x;
             }
@@ -674,12 +680,26 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
             for (int t = 0; t < kCh; ++t) o[rb][t] *= alpha;
             m_ref[rb] = m_new;
           }
+        }
+        // (One question for all rows: 2048 rows over 32768 take 2% more with one for each 16 and 3% with rounded products everywhere.)
+        float c = a.c;
+        bool far = is_far(m_ref[0]);
+        if (RB == 2) far = far || is_far(m_ref[RB - 1]);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) s[rb][i] *= c;
+          c = 1.f;
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(fmaf(s[rb][i][j], a.c, -m_ref[rb]));
+              const float x = fast_exp2(fmaf(s[rb][i][j], c, -m_ref[rb]));
               sum += x;
               pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)x;
             }

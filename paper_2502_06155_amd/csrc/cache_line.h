@@ -3,6 +3,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <stdint.h>
 
 #include "block_launch.h"
@@ -108,7 +109,10 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-constexpr float kNoRef = -1e30f;  // a running maximum before the first token (base-2 logits)
+constexpr float kNoRef = -FLT_MAX;  // a running maximum before the first token (base-2 logits)
+// A row's logits are so far from 0 that their products with c have to be rounded as their maximum's was: in the exact difference
+// of fma(s, c, -m) the rounding of m, up to 2^-24 of it, would leave the exponent's range from 2^31 on.
+__device__ __forceinline__ bool is_far(float m) { return fabsf(m) > 0x1p24f && m > kNoRef; }
 
 // A part of a segment: pages p0 .. p1 - 1 of key head h of an entry of lens, the group's first query row, whether
 // that is the whole segment, and the slot of the partial result if it is not.

@@ -264,6 +264,40 @@ def test_scales_of_any_magnitude(d):
     check(out, lse, q, cache, table, [200])
 
 
+@pytest.mark.parametrize("e", [31, 60, 122])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("B,H,Hkv,N,d,pages,width", [
+    (1, 4, 2, 2, 64, 6, 6), (2, 8, 2, 1, 128, 30, 40),    # up to 16 rows: a workgroup a segment, and shared
+    (1, 8, 1, 3, 96, 9, 40),                              # 24 rows: half a page at a time
+    (1, 6, 1, 8, 96, 6, 6), (1, 4, 2, 45, 128, 20, 40)])  # 48 rows a workgroup a segment, 90 shared
+def test_logits_far_from_zero(B, H, Hkv, N, d, pages, width, sign, e):
+    """Keys of one value, times 2^e, and queries that take it as it is: every row has one largest logit (all of them may
+    be far below zero), and its weight is exactly 1. The log-sum-exp is the logit in base 2 (two roundings) in base e
+    (one of the factor, one of the product): 2^-22 of it."""
+    rng = np.random.default_rng(e + d)
+    n = 128 * pages - 3
+    cache, table = held(rng, B, Hkv, d, [n] * B, width)
+    cache[0][...] = 0
+    cache[0][..., 0] = rng.choice([2, 3, 4, 5] if sign > 0 else [12, 13, 14, 15], cache[0].shape[:3])  # 1 to 3; -2 to -6
+    cache[2][:, :, 0] = e + 127
+    top = rng.integers(0, n - N, (B, Hkv))
+    for b in range(B):
+        for h in range(Hkv):
+            page, at = table[b, top[b, h] // 128], top[b, h] % 128
+            cache[0][page, h, at, 0] = 6 if sign > 0 else 10  # 4; -1
+    q = np.zeros((B, H, N, d), np.uint16)
+    q[..., 0] = 0x3F80
+    out, lse = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32([n] * B), 1.0, return_lse=True)
+    logit = (4.0 if sign > 0 else -1.0) * 2.0 ** e
+    assert (np.abs(lse.cpu().numpy().astype(np.float64) - logit) <= 2.0 ** -22 * abs(logit)).all()
+    for b in range(B):
+        for h in range(H):
+            g = h * Hkv // H
+            page, at = table[b, top[b, g] // 128], top[b, g] % 128
+            v = o4.values(cache[1][page, g, at:at + 1], cache[3][page, g, :, at:at + 1])[0]
+            assert np.array_equal(widen(from_dev(out[b, h])), np.broadcast_to(v, (N, d)))
+
+
 @pytest.mark.parametrize("width", [3, 40])
 @pytest.mark.parametrize("d", [64, 96, 128])
 def test_marked_tokens_reach_the_rows_that_see_them_alone(d, width):

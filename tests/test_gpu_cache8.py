@@ -124,6 +124,34 @@ def check(out, lse, q, cache, table, lens, scale=None):
     assert np.abs(l[some] - rlse[some]).max(initial=0) <= 2e-4
 
 
+@pytest.mark.parametrize("e", [40, 110])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("H,N,d,pages,width", [(4, 2, 64, 4, 4), (8, 1, 128, 30, 40), (8, 5, 96, 12, 40)])
+def test_logits_far_from_zero(H, N, d, pages, width, sign, e):
+    """Keys of one value and a scale of 2^e, with one largest logit a row, below zero too: its weight is exactly 1. The
+    log-sum-exp: the logit times two factors, rounded each (and their product), in base 2 and back: 2^-21 of it."""
+    rng = np.random.default_rng(e + d)
+    n = 128 * pages - 3
+    k, v, k_scales, v_scales = new_pages(rng, pages, 1, d)
+    v[(v & 127) == 127] = 0
+    k[...] = 0
+    k[..., 0] = rng.choice([0x38, 0x3C, 0x40] if sign > 0 else [0xC0, 0xC8], k.shape[:3])  # 1, 1.5, 2; -2, -4
+    k_scales[...] = 2.0 ** e
+    table = np.full((1, width), -1, np.int32)
+    table[0, :pages] = rng.permutation(pages)
+    top = int(rng.integers(0, n - N))
+    page, at = table[0, top // 128], top % 128
+    k[page, 0, at, 0] = 0x44 if sign > 0 else 0xB8  # 3; -1
+    q = np.zeros((1, H, N, d), np.uint16)
+    q[..., 0] = 0x3F80
+    cache = [k, v, k_scales, v_scales]
+    out, lse = ta.cache_attn(to_dev(q), *to_gpu(cache), i32(table), i32([n]), 1.0, return_lse=True)
+    logit = (3.0 if sign > 0 else -1.0) * 2.0 ** e
+    assert (np.abs(lse.cpu().numpy().astype(np.float64) - logit) <= 2.0 ** -21 * abs(logit)).all()
+    row = torch.from_numpy(v[page, 0, :, at].copy()).view(torch.float8_e4m3fn).double().numpy() * float(v_scales[page, 0])
+    assert np.array_equal(widen(from_dev(out)), np.broadcast_to(row, (1, H, N, d)))
+
+
 def held(rng, B, Hkv, d, lens, width=None, spare=2):
     """A cache whose sequences hold lens tokens; everything behind them is any code."""
     need = [-(-x // 128) for x in lens]
