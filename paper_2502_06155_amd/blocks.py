@@ -18,6 +18,7 @@ from .api import _check, _ptr, _stream
 
 try:
     import torch
+    import torch.autograd.forward_ad as _forward_ad
 except ImportError:  # the functions of the C ABI take addresses and do without
     torch = None
 
@@ -113,11 +114,21 @@ def _want(t, name: str, shape, dtype, device) -> None:
     raise ValueError(f"{name} must be contiguous")
 
 
-def _unrecorded(name: str, instead: str) -> None:
-    """Called where an input requires a gradient: says that the outputs carry no graph, if autograd
-    would have recorded the call."""
+def _unrecorded(name: str, instead: str, tensors, tangents=()) -> None:
+    """Says that the outputs carry neither a graph nor a tangent, if autograd would have recorded the call: where
+    one of `tensors` requires a gradient, or one of them or of `tangents` has a tangent of forward mode."""
+    lost = False
     if torch.is_grad_enabled():
-        warnings.warn(f"{name} is not recorded by autograd, its inputs get no gradient from it: {instead}", stacklevel=3)
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                lost = True
+    if getattr(_forward_ad, "_current_level", 0) >= 0:  # (a level is open; without the name all tensors are asked)
+        for t in (*tensors, *tangents):
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                lost = True
+    if lost:
+        warnings.warn(f"{name} is not recorded by autograd, its inputs get no gradient and its outputs no tangent from "
+                      f"it: {instead}", stacklevel=3)
 
 
 def _out(out, shape, dtype, device):
@@ -215,8 +226,7 @@ def block_attn(q, k, v, lists, causal=False, scale: float | None = None, lens=No
     takes a call for each (cache_attn takes them together). Autograd does not record it (it warns where
     it would have): block_attn_grad gives the gradients. Returns out, or (out, lse)."""
     sizes = _check_qkv(q, k, v, lists)
-    if q.requires_grad or k.requires_grad or v.requires_grad:
-        _unrecorded("block_attn", "block_attn_grad gives the gradients")
+    _unrecorded("block_attn", "block_attn_grad gives the gradients", (q, k, v))
     B, H, _, Sq, _, d, _ = sizes
     with _on(q.device):
         if out is None:
@@ -290,8 +300,7 @@ def cache_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: floa
     or (out, lse)."""
     if q.dim() != 4 or not q.is_cuda:
         raise ValueError("q must be a [B, H, N, d] tensor on a GPU")
-    if q.requires_grad:
-        _unrecorded("cache_attn", "it has no gradient")
+    _unrecorded("cache_attn", "it has no gradient", (q,))
     pages, Hkv, d = _check_cache(k_pages, v_pages, k_scales, v_scales, q.device)
     B, H, N, _ = q.shape
     _want(q, "q", (B, H, N, d), torch.bfloat16, q.device)

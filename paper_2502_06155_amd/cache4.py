@@ -96,7 +96,8 @@ def cache4_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new=
     uint8 [n_pages, Hkv, 128, d / 2] and k_scales, v_scales uint8 [n_pages, Hkv, d / 32, 128] (cache4_new), table int32
     [B, max_pages], lens int32 [B] (left as it is). n_new (int32 [B]): how many of the N tokens each sequence takes.
     With return_held it returns (k, v) as the cache holds them, zeros for tokens that were not written: what later
-    tokens will attend to, for the attention of the tokens themselves."""
+    tokens will attend to, for the attention of the tokens themselves, without a gradient (it warns where autograd
+    would have recorded one)."""
     pages, Hkv, d, device = _check_cache(k_pages, v_pages, k_scales, v_scales)
     if k.dim() != 4:
         raise ValueError("k must be a [B, Hkv, N, d] tensor on a GPU")
@@ -106,6 +107,8 @@ def cache4_write(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, n_new=
     width = _check_table(table, lens, B, device)
     if n_new is not None:
         _want(n_new, "n_new", (B,), torch.int32, device)
+    if return_held:
+        _unrecorded("cache4_write", "what it returns is rounded to the cache's numbers", (k, v))
     with _on(device):
         held = (torch.empty_like(k), torch.empty_like(v)) if return_held else (None, None)
         _check(lib.cache4_attn_write(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
@@ -140,8 +143,7 @@ def cache4_attn(q, k_pages, v_pages, k_scales, v_scales, table, lens, scale: flo
     pages, Hkv, d, device = _check_cache(k_pages, v_pages, k_scales, v_scales)
     if q.dim() != 4:
         raise ValueError("q must be a [B, H, N, d] tensor on a GPU")
-    if q.requires_grad:
-        _unrecorded("cache4_attn", "it has no gradient")
+    _unrecorded("cache4_attn", "it has no gradient", (q,))
     B, H, N, _ = q.shape
     _want(q, "q", (B, H, N, d), torch.bfloat16, device)
     per_head = table.dim() == 3

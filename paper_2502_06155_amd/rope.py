@@ -174,11 +174,7 @@ def head_rope(q, k, v, positions=None, freqs=None, dims=None, layout="interleave
     gives the gradients."""
     weights = (q_weight, k_weight, q_bias, k_bias)
     spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, weights, norm, eps, lens)
-    if torch.is_grad_enabled():
-        for t in (q, k, v, *weights):
-            if t is not None and t.requires_grad:
-                _unrecorded("head_rope", "head_rope_grad gives the gradients")
-                break
+    _unrecorded("head_rope", "head_rope_grad gives the gradients", (q, k, v, *weights))
     rows, outs, at = [None, None, None], [None, None, None], [None, None, None]
     for i, t in enumerate((q, k, v)):
         if t is None:
@@ -202,9 +198,11 @@ def head_rope_grad(q, k, v, dq, dk, dv, positions=None, freqs=None, dims=None, l
     results. Returns (of q, of k, of v, of q_weight, of k_weight, of q_bias, of k_bias); the first three as
     [B, S, heads, d], parts of one [B, S, H + 2 Hkv, d] tensor, the gradient of a projection of everything, or
     written to `out`, three tensors of any strides that keep a head's values together. What was None, or has
-    no weight or bias, is None; v's own values are not read, only its shape."""
+    no weight or bias, is None; v's own values are not read, only its shape. It has no second derivative (and warns where
+    autograd would have recorded one)."""
     spec, device, B, S, H, Hkv, d = _spec(q, k, v, positions, freqs, dims, layout, (q_weight, k_weight, q_bias, k_bias),
                                           norm, eps, lens)
+    _unrecorded("head_rope_grad", "it has no second derivative", (dq, dk, dv), (q, k, v, q_weight, k_weight))
     rows, grads, to, outs = [None, None, None], [None, None, None], [None, None, None], out
     if out is None:
         # Rows of one new tensor: their places are known.

@@ -495,6 +495,54 @@ def test_wrappers_refuse():
         ta.head_rope(q.detach().clone().requires_grad_(), k, v, **args)
 
 
+def test_what_autograd_would_have_recorded_is_said():
+    """Inputs that require a gradient, gradients that do, and tangents of forward mode: a warning each, and none where
+    nothing would have been recorded."""
+    import warnings
+
+    import torch.autograd.forward_ad as fw
+
+    c = Case(1, 6, 2, 1, 64, "rms", "halves", (64,))
+    q, k, v = (x.contiguous() for x in c.parts(to_dev(c.x)))
+    dy, args = [to_dev(g) for g in c.dy], c.args()
+    at = dict(dtype=torch.int32, device="cuda")
+    held = (*ta.cache4_new(1, 1, 64), torch.zeros(1, 1, **at), torch.zeros(1, **at))
+    kt, qt = (torch.zeros(1, h, 3, 64, dtype=torch.bfloat16, device="cuda") for h in (1, 2))
+    lists = torch.zeros(1, 1, 1, 1, **at)
+
+    def calls(f):
+        return [
+            ("head_rope ", lambda: ta.head_rope(f(q), k, v, **args)), ("head_rope ", lambda: ta.head_rope(q, k, f(v), **args)),
+            ("head_rope ", lambda: ta.head_rope(q, k, v, **{**args, "k_weight": f(args["k_weight"])})),
+            ("head_rope_grad ", lambda: ta.head_rope_grad(q, k, v, dy[0], f(dy[1]), dy[2], **args)),
+            ("cache4_write ", lambda: ta.cache4_write(f(kt), kt, *held, return_held=True)),
+            ("cache4_write ", lambda: ta.cache4_write(kt, f(kt), *held, return_held=True)),
+            ("cache4_attn ", lambda: ta.cache4_attn(f(qt), *held)),
+            ("block_attn ", lambda: ta.block_attn(qt, f(kt), kt, lists))]
+
+    for name, call in calls(lambda t: t.clone().requires_grad_()):
+        with pytest.warns(UserWarning, match=name + "is not recorded"):
+            call()
+    with fw.dual_level():
+        dual = calls(lambda t: fw.make_dual(t.clone(), torch.ones_like(t)))
+        dual.append(("head_rope_grad ", lambda: ta.head_rope_grad(fw.make_dual(q, q.clone()), k, v, *dy, **args)))
+        for name, call in dual:
+            with pytest.warns(UserWarning, match=name + "is not recorded"):
+                call()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        for _, call in calls(lambda t: t):
+            call()
+        with fw.dual_level():
+            for _, call in calls(lambda t: t):
+                call()
+        with torch.no_grad():
+            for _, call in calls(lambda t: t.clone().requires_grad_()):
+                call()
+        ta.head_rope_grad(q.clone().requires_grad_(), k, v, *dy, **args)  # a program that goes back by itself
+        ta.cache4_write(kt.clone().requires_grad_(), kt, *held)           # nothing comes back
+
+
 @pytest.mark.parametrize("causal", [False, True])
 def test_between_a_projection_and_attention(causal):
     """A layer's attention and its gradients: from the projection's output through norms, rotation, lists and
