@@ -126,6 +126,8 @@ def cache4_read(k_pages, v_pages, k_scales, v_scales, table, lens, N: int, first
     width = _check_table(table, lens, B, device)
     if N < 1:
         raise ValueError(f"N must be at least 1, got {N}")
+    if not -(1 << 31) <= first < 1 << 31:  # (a C int would take what is left of it)
+        raise ValueError(f"first must be a token below 2^31, got {first}")
     with _on(device):
         k = torch.empty((B, Hkv, N, d), dtype=torch.bfloat16, device=device)
         out = (k, torch.empty_like(k))

@@ -493,6 +493,13 @@ def test_offsets_past_32_bits():
     check(out, lse, q, small, near, [300])
 
 
+@pytest.mark.parametrize("first", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 64, -2 ** 32])
+def test_a_first_token_past_a_c_int_is_refused(first):
+    cache, table = held(np.random.default_rng(1), 1, 1, 64, [200])
+    with pytest.raises(ValueError, match="first"):
+        ta.cache4_read(*to_gpu(cache), i32(table), i32([200]), 3, first=first)
+
+
 def test_a_long_prompt_written_at_once():
     """Into a table a little too short for it: the same bytes as in two calls, and back."""
     N, d, pages = 540000, 64, 4200
