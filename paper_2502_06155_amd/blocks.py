@@ -141,7 +141,7 @@ def _out(out, shape, dtype, device):
 
 def _on(device):
     """The context in which `device` is the current one."""
-    return _HERE if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
 def _current(device) -> int:
