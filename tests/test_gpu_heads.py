@@ -177,6 +177,10 @@ CASES = [
     dict(B=2, S=19, H=4, Hkv=2, d=128, norm=None, layout=None, dims=None, lens=[19, 1]),
     # enough tokens that waves take many heads and items
     dict(B=1, S=9001, H=3, Hkv=1, d=64, norm="layer", layout="halves", dims=(64,)),
+    # nine heads a wave forward, for each pairing; three items a wave in the gradients
+    dict(B=1, S=8197, H=5, Hkv=2, d=96, norm="layer", layout="interleaved", dims=(32, 32, 32)),
+    dict(B=2, S=8200, H=5, Hkv=2, d=64, norm="rms", layout="split", dims=(16, 48), lens=[8200, 5001]),
+    dict(B=1, S=30001, H=3, Hkv=1, d=96, norm="layer", layout="halves", dims=(28, 34, 34)),
 ]
 
 
@@ -398,6 +402,77 @@ def test_on_another_stream_and_under_any_workspace_contents():
         assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
 
 
+@pytest.mark.parametrize("B,S,H,Hkv,d,norm,layout,dims,lens", [
+    (1, 86400, 24, 24, 96, "rms", "halves", (32, 32, 32), None),         # pieces of 8: 72 heads, 18 a wave
+    (1, 33001, 31, 8, 64, "layer", "interleaved", (16, 24, 24), None),   # neighbours: 47 heads, 12 a wave
+    (2, 20003, 13, 3, 96, "layer", "split", (28, 34, 34), [20003, 9999]),  # anywhere: 19 heads, 18 and 1
+    (1, 20001, 40, 8, 128, "rms", "halves", (44, 42, 42), None),         # anywhere: 56 heads
+    (2, 9000, 9, 9, 128, "rms", "interleaved", (64,), [8999, 9000]),     # half of a head turned
+    (1, 60000, 14, 2, 64, "layer", "halves", (20, 10), None)])
+def test_whole_layers(B, S, H, Hkv, d, norm, layout, dims, lens):
+    """Calls whose waves go through many heads, several steps of each kind and several items: every result and
+    gradient against the formulas in 64 bits, a head at a time."""
+    gen = torch.Generator(device="cuda").manual_seed(S + d)
+    rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda")  # noqa: E731
+    heads = H + 2 * Hkv
+    x = torch.empty(B, S, heads, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    dy = [torch.empty(B, h, S, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for h in (H, Hkv, Hkv)]
+    w = {n: 1 + 0.3 * rand(d) if n.endswith("weight") else 0.2 * rand(d) if norm == "layer" else None for n in WEIGHTS}
+    p = torch.randint(0, 400, (S, len(dims)), generator=gen, device="cuda").to(torch.int32)
+    how = dict(positions=p, freqs=ta.rope_freqs(dims), dims=dims, layout=layout, norm=norm, lens=gpu(lens, torch.int32), **w)
+    parts = x.split_with_sizes([H, Hkv, Hkv], 2)
+    got, grads = ta.head_rope(*parts, **how), ta.head_rope_grad(*parts, *dy, **how)
+
+    # every value's partner, cosine and signed sine; 1 and 0 where it is not turned
+    angle = torch.cat([p[:, a:a + 1].double() * f for a, f in enumerate(how["freqs"].split_with_sizes([n // 2 for n in dims]))], 1)
+    partner = torch.arange(d, device="cuda")
+    cos, sin = torch.ones(S, d, dtype=torch.float64, device="cuda"), torch.zeros(S, d, dtype=torch.float64, device="cuda")
+    for i, (e0, e1, _) in enumerate(oh.pairs(dims, layout)):
+        partner[e0], partner[e1] = e1, e0
+        cos[:, e0] = cos[:, e1] = angle[:, i].cos()
+        sin[:, e1] = angle[:, i].sin()
+        sin[:, e0] = -sin[:, e1]
+    turned = (sin != 0).any(0)
+    with_partner = lambda m: m + torch.where(turned, m[..., partner], 0)  # noqa: E731
+    valid = torch.ones(B, S, 1, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens or ()):
+        valid[b, n:] = False
+
+    def near(a, ref, room, what):
+        off = (a.double() - ref).abs() - room
+        assert off.max().item() <= 0, (what, off.max().item())
+
+    for i, name in enumerate("qk"):
+        weight, bias = (None if t is None else t.double() for t in (w[name + "_weight"], w[name + "_bias"]))
+        sums = [0.0, 0.0, 0.0, 0.0]  # dw, db, and their terms' magnitudes
+        for h in range(parts[i].shape[2]):
+            row = torch.where(valid, parts[i][:, :, h].double(), 0)
+            mean = row.mean(-1, keepdim=True) if norm == "layer" else 0.0
+            r = ((row - mean).square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+            hat = (row - mean) * r
+            wide = (row.abs() + row.abs().mean(-1, keepdim=True)) * r if norm == "layer" else hat.abs()
+            n, mag = hat * weight, wide * weight.abs()
+            if bias is not None:
+                n, mag = n + bias, mag + bias.abs()
+            y = torch.where(valid, n * cos + n[..., partner] * sin, 0)
+            near(got[i][:, h], y, HALF * y.abs() + 2.0 ** -16 * with_partner(mag), name)
+            g = torch.where(valid, dy[i][:, h].double(), 0)
+            gm = with_partner(g.abs())
+            g = g * cos + (g * sin)[..., partner]
+            for j, term in enumerate((g * hat, g, gm * wide, gm)):
+                sums[j] = sums[j] + term.sum((0, 1))
+            u, um = g * weight, gm * weight.abs()
+            dx = u - hat * (u * hat).mean(-1, keepdim=True) - (u.mean(-1, keepdim=True) if norm == "layer" else 0)
+            room = r * (um + um.mean(-1, keepdim=True) + wide * (um * wide).mean(-1, keepdim=True))
+            near(grads[i][:, :, h], dx * r, HALF * (dx * r).abs() + 2.0 ** -14 * room, "d" + name)
+        near(grads[3 + i], sums[0], 2.0 ** -14 * sums[2], "dw")
+        if bias is not None:
+            near(grads[5 + i], sums[1], 2.0 ** -14 * sums[3], "db")
+    keep = valid[:, None]
+    assert torch.equal(got[2], torch.where(keep, parts[2].transpose(1, 2), 0))
+    assert torch.equal(grads[2], torch.where(keep, dy[2], 0).transpose(1, 2))
+
+
 def test_long_sums_keep_their_small_terms():
     """Sums over 26 million rows: a large term first in every lane's part, ones behind it. With rows of 1 and -1 normed rows
     are the rows themselves, and all terms are exact. Chains: 256 rows a lane, its 4 parts, 3 additions of lanes, 4 of
@@ -562,3 +637,30 @@ def test_between_a_projection_and_attention(causal):
     dout = to_dev(bits(np.random.default_rng(1), B, H, S, d))
     c.dy = [from_dev(g) for g in ta.block_attn_grad(q, k, v, lists, out, dout, lse, causal=causal)]
     check_gradients(c, ta.head_rope_grad(*parts, *(to_dev(g) for g in c.dy), **args))
+
+
+@pytest.mark.parametrize("P", [0, 37])
+def test_between_a_projection_and_tile_attention(P):
+    """The same with the fixed frame mask, with and without text before the video (at position 0, not turned): one
+    projection and norm for both, the layout that the attention takes, and back."""
+    from oracle import mmdit as om
+    from tests.gpu_helpers import assert_parity
+
+    B, H, d, F, h, w = 1, 3, 96, 4, 6, 11
+    T, S = h * w, P + F * h * w
+    c = Case(B, S, H, H, d, "rms", "halves", (32, 32, 32))
+    c.positions = ta.grid_positions(F, h, w, P).cpu().numpy()
+    x, args = to_dev(c.x), c.args()
+    q, k, v = ta.head_rope(*c.parts(x), **args)
+    check_forward(c, (q, k, v))
+    mask, scale, stream = ta.tile_attn_make_mask(F, 1, "col"), d ** -0.5, torch.cuda.current_stream()
+    out, lse = torch.empty_like(q), torch.empty(B, H, S, device="cuda")
+    ta.tile_attn_fwd_mmdit(q, k, v, out, B, H, F, T, P, d, mask, scale, lse, stream)
+    assert_parity(from_dev(out), om.attention_mmdit(from_dev(q), from_dev(k), from_dev(v), mask, T, P, scale), f"P = {P}")
+    if P == 0:
+        assert torch.equal(out, ta.tile_attn(q, k, v, mask, T))
+    dout = to_dev(bits(np.random.default_rng(2), B, H, S, d))
+    back = [torch.empty_like(q) for _ in range(3)]
+    ta.tile_attn_bwd_mmdit(q, k, v, out, dout, lse, *back, B, H, F, T, P, d, mask, scale, stream)
+    c.dy = [from_dev(g) for g in back]
+    check_gradients(c, ta.head_rope_grad(*c.parts(x), *back, **args))
