@@ -345,6 +345,53 @@ def test_chunks_of_a_prompt(B, H, Hkv, N, d, lens, width):
     assert torch.equal(got, ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens)))
 
 
+def stretch(B, H, Hkv, N, d, width):
+    """Pages on the line of all sequences (each segment with the five that its start counts as) for a workgroup, if all
+    tables were full: workspaces hold two partial results of every workgroup's rows."""
+    rows = H // Hkv * N
+    per = 16 if rows <= 16 else 32 if rows <= 32 else 64 if rows <= 64 else 128
+    workers = ta.cache4_attn_fwd_workspace(B, H, Hkv, N, d, width) // (2 * per * (d + 4) * 4 * -(-rows // per))
+    return B * Hkv * (width + 5) / workers
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("N", [1, 3, 6, 12])  # 8, 24, 48 and 96 rows a key head: each of the kernels' ways through a page
+def test_long_stretches_of_pages(N, d):
+    """Workgroups that go through many pages of a sequence: 16 sequences of 40 to 130 pages, the last ones in part, pages that
+    are none among them, and tokens that are marked in a late page, for all rows and for the last ones."""
+    B, H, Hkv, width = 16, 32, 4, 130
+    rng = np.random.default_rng(N + d)
+    lens = [int(x) for x in rng.integers(40 * 128, width * 128, B)]
+    lens[0], lens[5], lens[9] = 128 * 47 + 1, 128 * 61 - 1, 128 * 44 + 70
+    cache, table = held(rng, B, Hkv, d, lens, width)
+    assert stretch(B, H, Hkv, N, d, width) > 12
+    cache[2][table[5, 57], 1, :, 3] = 255                # (key head 1)
+    cache[2][table[9, 44], 2, :, 70 - min(N, 2)] = 255   # the last tokens'
+    table[0, 9], table[0, 10], table[0, 33], table[5, 20], table[9, 0] = -1, -1, len(cache[0]), -2 ** 31, -1
+    q = bits(rng, B, H, N, d)
+    out, lse = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32(lens), return_lse=True)
+    some = [0, 5, 9]  # (the reference is slow)
+    check(out[some], lse[some], q[some], cache, table[some], [lens[b] for b in some])
+    bad = torch.isnan(lse)
+    assert bad[5, 8:16].all() and bad[9, 16:24, -1].all() and bad.sum() == 8 * N + 8 * min(N, 2)
+
+
+@pytest.mark.parametrize("H,Hkv,N,d", [(16, 2, 640, 128), (16, 2, 640, 96), (12, 1, 300, 64), (24, 4, 200, 128)])
+def test_long_stretches_under_many_passes(H, Hkv, N, d):
+    """Prompts of thousands of rows a key head, so that few workgroups share a pass and each goes through many pages, with pages
+    that are none in between and a marked token that the last rows see."""
+    width, n = 70, 128 * 55 + 77
+    rng = np.random.default_rng(N + d)
+    cache, table = held(rng, 1, Hkv, d, [n], width)
+    assert stretch(1, H, Hkv, N, d, width) > 8
+    table[0, 3], table[0, 17], table[0, 18], table[0, 40] = -1, len(cache[0]), -1, -2 ** 31
+    cache[2][table[0, 55], 0, :, 77 - 5] = 255
+    q = bits(rng, 1, H, N, d)
+    out, lse = ta.cache4_attn(to_dev(q), *to_gpu(cache), i32(table), i32([n]), return_lse=True)
+    check(out, lse, q, cache, table, [n])
+    assert torch.isnan(lse).sum() == 5 * H // Hkv
+
+
 @pytest.mark.parametrize("B,H,Hkv,N,d,width,most", [
     (1, 4, 4, 1, 64, 40, 40),
     (3, 8, 2, 1, 128, 40, 23),
