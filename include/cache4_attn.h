@@ -30,7 +30,7 @@ extern "C" {
  * largest magnitude is at most 7 (6 is the largest code, and 7 is as far from it as rounding takes any number
  * between 4 and 6); codes are the nearest, ties to the even one. Infinities and NaN are left out of a group's
  * magnitude and stored as 0, and the token is marked: all its K scales are 255, so that its key reads back as NaN
- * and a row that attends to it comes out as NaN. (A V scale is never 255.)
+ * and a row that attends to it comes out as NaN. (A V scale is never 255.) N is at most 2^28 - 256, here and in reading.
  * k, v: bf16 [B, Hkv, N, d]. k_held, v_held: bf16 of the same shape, or NULL: the numbers that the cache now holds
  * for these tokens (zeros for those that were not written), for a prompt's own attention.
  */

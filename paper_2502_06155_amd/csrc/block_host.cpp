@@ -492,6 +492,7 @@ int cache4_attn_write(const void* k, const void* v, void* k_pages, void* v_pages
     return fail(TA_ERR_NULL_PTR, "k, v, the pages, the scales, table and lens must be non-NULL");
   if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages, kCache4Segment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
+  if (int st = check_grid((double)N / cache4_tokens(d) + 1)) return st;
   if (int st = check_aligned({k, v, k_pages, v_pages, k_scales, v_scales, k_held, v_held}, 16,
                              "k, v, their held values, the pages and the scales must be 16-byte aligned"))
     return st;
@@ -521,6 +522,7 @@ int cache4_attn_read(const void* k_pages, const void* v_pages, const void* k_sca
     return fail(TA_ERR_NULL_PTR, "the pages, the scales, table, lens and k_out or v_out must be non-NULL");
   if (int st = check_cache(B, Hkv, Hkv, N, d, max_pages, kCache4Segment)) return st;
   if (n_pages < 1) return fail(TA_ERR_BAD_SHAPE, "n_pages must be >= 1");
+  if (int st = check_grid((double)N / cache4_tokens(d) + 1)) return st;
   if (first < 0 || (int64_t)first + N > INT_MAX) return fail(TA_ERR_BAD_SHAPE, "first must be >= 0, first + N below 2^31");
   if (int st = check_aligned({k_pages, v_pages, k_scales, v_scales, k_out, v_out}, 16,
                              "the pages, the scales and the outputs must be 16-byte aligned"))

@@ -19,6 +19,8 @@ struct BlockGeo {
 constexpr int kLineWorkers = 256;  // workgroups of the gradients' key side at d = 128
 constexpr int kCacheSegment = 3;  // what a (sequence, head) costs cache attention beside its pages
 constexpr int kCache4Segment = 5;  // the same over the 4-bit cache
+// Tokens of a head that a workgroup writes to it or reads back: a wave's 64 lanes hold 8 values each.
+constexpr int cache4_tokens(int d) { return 4 * (64 / (d / 8)); }
 
 struct MeansArgs {
   const uint16_t* x;

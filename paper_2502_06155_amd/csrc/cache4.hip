@@ -28,6 +28,7 @@ template <int D>
 struct TokenLanes {
   static constexpr int lanes = D / 8, tokens = 64 / lanes;  // (d = 96: 5 tokens in 60 lanes)
   static constexpr int per_pass = kThreadsC / 64 * tokens;
+  static_assert(per_pass == cache4_tokens(D), "tokens of a workgroup");
 };
 
 template <int CTRL>

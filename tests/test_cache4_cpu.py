@@ -73,6 +73,18 @@ def test_write_errors():
         assert _write(**kw) == OVERLAP, kw
 
 
+@pytest.mark.parametrize("d,most", [(64, 32), (96, 20), (128, 16)])
+def test_more_tokens_than_the_grid_holds(d, most):
+    """256 threads a workgroup and 2^32 in a grid; `most` tokens a workgroup. What fits goes on to the next check."""
+    far = dict(k=1 << 50, v=1 << 51, kh=1 << 52, vh=1 << 53, B=1, Hkv=1, d=d, max_pages=1 << 23)
+    limit = ((1 << 32) // 256 - 9) * most
+    assert limit >= 2 ** 28 - 256
+    for call, kw in ((_write, far), (_read, {**far, "k": 1 << 50, "v": 1 << 51})):
+        kw = {n: x for n, x in kw.items() if call is _write or n not in ("kh", "vh")}
+        assert call(**kw, N=limit + 2 * most) == SHAPE
+        assert call(**kw, N=limit - most, lens=8 * M + 1) == ALIGN
+
+
 def test_read_errors():
     assert _read(first=-1) == SHAPE and _read(first=2 ** 31 - 3) == SHAPE
     for p in ("kp", "vp", "ks", "vs", "k", "v"):
