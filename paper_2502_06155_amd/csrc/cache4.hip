@@ -205,6 +205,9 @@ __global__ __launch_bounds__(kThreadsC) void cache4_read_kernel(const Cache4Read
 //   each of those tokens 4 bytes (2 at d = 64), 8 channels beside each other (4), widens them with the token's scale and
 //   swaps halves of words so that words hold two tokens of one channel: the operands of 8 (4) instructions, row n
 //   of instruction t being channel 8 n + t (4 n + t).
+// P is rounded to bf16 for its product, its sum is not: off by up to 2^-8 of p |v|, below the result's own rounding, and all that the
+// results have beside that. In two bf16 parts, with twice the instructions, they come within 1e-6 of fp32 weights' (4e-4 so, of their mean
+// magnitude), but 24 sequences of up to 100000 tokens take 125 us for 118, 512 tokens over 32768 (below) 377 for 292.
 // So neither K nor V is kept transposed, no scale leaves its token, and nothing goes through LDS. K codes become bf16 exactly,
 // scales among it, and so do V's.
 
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
     const int p0 = seg.p0, p1 = seg.p1;
     if (p1 <= p0 && !a.whole) continue;  // (alone, a segment without tokens gets its zeros)
     const ScalarInts table = (ScalarInts)(a.table + (size_t)seg.entry * a.max_pages);
-    // Pages p0 + wave, + 4, ... up to p1. A page that is none is passed over: its tokens are not read.
+    // Pages p0 + wave, + WAVES, ... up to p1. A page that is none is passed over: its tokens are not read.
     auto page_of = [&](int p) {
       if (p >= p1) return -1;
       const int x = table[p];
@@ -475,14 +478,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
 // 16 RB rows, each with a wave for the first half of a page's tokens and one for the second, which join at the end: a page's codes are
 // widened once, K by four waves and V by the other four, into LDS, where the matrix operands of all rows come from.
 // While a page is multiplied the next one is widened into the other half of the LDS, and the one behind it is on its way.
-// Bound by the vector work beside the products (exponentials, widening): one sequence of 32768, 32 heads on 8 of 128, 2048 rows
+// Bound by the vector work beside the products (exponentials, widening): one sequence of 32768, 32 heads on 8 of 128, the last 2048 tokens
 // 1107 us (993 TFLOP/s), 512 workgroups of four waves that had a page's tokens to themselves 1166. 128 rows take 2.3 us a
 // page at d = 128, 2.6 at 96 (of which 2.0 for scores, exponentials and products, 0.5 for widening). Waves of K widening before their products and waves of V behind them: 1261; two sets of 48 rows, four
 // waves each, for 96 rows: 36.3 us for 32.5, the joins of four waves cost more than the even rows give.
 //   K: row 16 i + n of the tile is the token that row n of instruction group i computes, 32 (i / 2) + 8 (n / 4) + 4 (i % 2) + n % 4,
 //   so that the scores of groups 2 c and 2 c + 1 are, in lane group g, tokens 32 c + 8 g .. + 7: P^T of step c. The 16-byte pieces
 //   of a row lie at places exchanged by the row's number (d = 64: in order, rows 16 bytes longer than their values), which puts
-//   16 rows' pieces on different banks (2048 rows over 32768: 1107 us, 1124 with longer rows).
+//   16 rows' pieces on different banks (2048 tokens over 32768: 1107 us, 1124 with longer rows).
 //   V^T: a row of 128 tokens for each channel, its 16-byte pieces of 8 tokens at places exchanged by the channel's
 //   number (key): both the writes (16 channels' words of the same 8 tokens) and the reads (row n of instruction t: channel 8 n + t,
 //   4 n + t at d = 64) fall on different banks.
@@ -682,7 +685,8 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
             m_ref[rb] = m_new;
           }
         }
-        // (One question for all rows: 2048 rows over 32768 take 2% more with one for each 16 and 3% with rounded products everywhere.)
+        // (One question for all rows: 512 tokens over 32768, 32 heads on 8, take 2% more with one for each 16 rows, and 3% with
+        // rounded products everywhere.)
         float c = a.c;
         bool far = is_far(m_ref[0]);
         if (RB == 2) far = far || is_far(m_ref[RB - 1]);

@@ -101,9 +101,9 @@ struct __attribute__((aligned(16))) PlaceEntry {
   float sign;       // of the partner's sine
 };
 
-// The lane's 8 values in the rotation. Angles: turns = position * (frequency / 2 pi) in fp64, right to 2^-53 of the
-// angle however far the position, then the fraction alone, in fp32, for v_sin_f32 and v_cos_f32 (which take
-// turns; off by at most 1.3e-7 in [-0.5, 0.5]).
+// The lane's 8 values in the rotation. Angles: turns = position * (frequency / 2 pi) in fp64, three roundings (1 / 2 pi's, two
+// products') of at most 2^-53 of the angle however far the position, then the fraction alone, in fp32, for v_sin_f32 and v_cos_f32
+// (which take turns; off by at most 1.3e-7 in [-0.5, 0.5]: nothing beside a result's rounding to bf16).
 template <int D, int ROT>
 struct Turns {
   static constexpr int kAngles = ROT == kNext ? 4 : 8;
@@ -291,7 +291,8 @@ struct Token {
 // loads: 32 of them, 48 heads of 128, 4.8 us. Four rows of a lane are read together, the next four meanwhile; without
 // the next ones two together took 504 us and one 556. Results past the caches: 480, not worth a second kernel.
 // With pairs anywhere in the row a workgroup forms the places, and puts the weights, into LDS first: 62982 tokens, 9 heads of 96
-// 56 us (places by every lane for its 8 values 70, weights from memory 60); 8 tokens, 10 heads of 64 4.4 us (5.3).
+// 56 us (places by every lane for its 8 values 70, weights from memory 60); 8 tokens, 10 heads of 64 4.4 us (5.3). Few heads pay for
+// a token's angles and a workgroup's places: 60000 tokens, 3 heads of 64 20.9 us for 9.2 us of bytes (19.0 with pieces of 8).
 constexpr int kAhead = 4;
 
 template <int D, int NORM, int ROT>

@@ -403,7 +403,7 @@ def test_on_another_stream_and_under_any_workspace_contents():
 
 
 @pytest.mark.parametrize("B,S,H,Hkv,d,norm,layout,dims,lens", [
-    (1, 86400, 24, 24, 96, "rms", "halves", (32, 32, 32), None),         # pieces of 8: 72 heads, 18 a wave
+    (1, 86400, 24, 24, 96, "rms", "halves", (32, 32, 32), None),         # pieces of 8: 72 heads a wave
     (1, 33001, 31, 8, 64, "layer", "interleaved", (16, 24, 24), None),   # neighbours: 47 heads, 12 a wave
     (2, 20003, 13, 3, 96, "layer", "split", (28, 34, 34), [20003, 9999]),  # anywhere: 19 heads, 18 and 1
     (1, 20001, 40, 8, 128, "rms", "halves", (44, 42, 42), None),         # anywhere: 56 heads
