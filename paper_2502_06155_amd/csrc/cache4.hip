@@ -389,10 +389,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache4_attn_kernel(const Cache4
             m_ref[rb] = m_new;
           }
           float c = a.c;
-          if (__builtin_expect(__builtin_amdgcn_ballot_w64(is_far(m_ref[rb])) != 0, 0)) {
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(is_far(m_ref[rb])) != 0, 0)) {  // (rows that are not keep theirs)
+            const bool far = is_far(m_ref[rb]);
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i) s[rb][i] *= c;
-            c = 1.f;
+            for (int i = 0; i < kGroups; ++i) s[rb][i] *= far ? c : 1.f;
+            c = far ? 1.f : c;
           }
           float sum = 0.f;
 #pragma unroll
@@ -687,15 +688,17 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
         }
         // (One question for all rows: 512 tokens over 32768, 32 heads on 8, take 2% more with one for each 16 rows, and 3% with
         // rounded products everywhere.)
-        float c = a.c;
-        bool far = is_far(m_ref[0]);
-        if (RB == 2) far = far || is_far(m_ref[RB - 1]);
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+        float c[RB];
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
+        for (int rb = 0; rb < RB; ++rb) c[rb] = a.c;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(is_far(m_ref[0]) || is_far(m_ref[RB - 1])) != 0, 0)) {
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i) s[rb][i] *= c;
-          c = 1.f;
+          for (int rb = 0; rb < RB; ++rb) {
+            const bool far = is_far(m_ref[rb]);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) s[rb][i] *= far ? a.c : 1.f;
+            c[rb] = far ? 1.f : a.c;
+          }
         }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -704,7 +707,7 @@ __global__ __launch_bounds__(kThreadsMany, 2) void cache4_rows_kernel(const Cach
           for (int i = 0; i < kGroups; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = fast_exp2(fmaf(s[rb][i][j], c, -m_ref[rb]));
+              const float x = fast_exp2(fmaf(s[rb][i][j], c[rb], -m_ref[rb]));
               sum += x;
               pf[rb][i / 2][4 * (i % 2) + j] = (__bf16)x;
             }

@@ -298,6 +298,29 @@ def test_logits_far_from_zero(B, H, Hkv, N, d, pages, width, sign, e):
             assert np.array_equal(widen(from_dev(out[b, h])), np.broadcast_to(v, (N, d)))
 
 
+@pytest.mark.parametrize("H,Hkv,N,d,pages,width", [(4, 1, 2, 64, 6, 6), (8, 1, 3, 96, 20, 40), (4, 1, 30, 128, 20, 40)])
+def test_rows_far_from_zero_leave_others_as_they_were(H, Hkv, N, d, pages, width):
+    """A query of large numbers, and one of infinities, beside others in the same wave: theirs keep every bit, with logits of
+    some 3e5, whose products' rounding would show."""
+    rng = np.random.default_rng(d)
+    n = 128 * pages - 9
+    cache, table = held(rng, 1, Hkv, d, [n], width)
+    cache[0][..., :16] = 0
+    cache[0][..., 0], cache[2][:, :, 0] = 2, 20 + 127  # every key's first value is 2^20
+    q = bits(rng, 1, H, N, d)
+    q[..., 0] = 0x3F80
+    gpu = to_gpu(cache)
+    want, l0 = ta.cache4_attn(to_dev(q), *gpu, i32(table), i32([n]), 0.3, return_lse=True)
+    far = q.copy()
+    far[0, 1, 0] = workloads.f32_to_bf16_bits((widen(q[0, 1, 0]) * 2.0 ** 90).astype(np.float32))
+    far[0, 2, N - 1, ::2] = 0x7F80
+    got, l1 = ta.cache4_attn(to_dev(far), *gpu, i32(table), i32([n]), 0.3, return_lse=True)
+    same_rows = torch.ones(1, H, N, dtype=torch.bool, device="cuda")
+    same_rows[0, 1, 0] = same_rows[0, 2, N - 1] = False
+    assert torch.equal(got[same_rows], want[same_rows]) and torch.equal(l1[same_rows], l0[same_rows])
+    assert torch.isfinite(got[0, 1, 0]).all() and not torch.equal(got[0, 1, 0], want[0, 1, 0])
+
+
 @pytest.mark.parametrize("width", [3, 40])
 @pytest.mark.parametrize("d", [64, 96, 128])
 def test_marked_tokens_reach_the_rows_that_see_them_alone(d, width):
